@@ -1,6 +1,7 @@
 /*
  * fa.h -- C ABI of the attention forward for AMD Instinct MI355X (gfx950): the fused kernel, its
- * split mode, and the unfused layer-by-layer operators it is measured against.
+ * split mode, the unfused layer-by-layer operators it is measured against, and a paged key/value cache: appending to
+ * it and attention over it.
  *
  * Operation (the paper's scaled dot-product attention, Eq. (1), Sec. 2.1, replicated over heads):
  *
@@ -270,6 +271,114 @@ size_t fa_lbl_workspace_bytes(int B, int Hq, int Sq, int Sk);
 fa_status_t fa_fwd_unfused(const void* Q, const void* K, const void* V, void* O, float* LSE, int B, int Hq,
                            int Hkv, int Sq, int Sk, int d_qk, int d_v, float scale, int causal,
                            void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Paged key/value cache. A serving program keeps the keys and values of its sequences in pages of page_size
+ * tokens that lie anywhere in two buffers; a block table names the pages of every sequence in order: key j of
+ * sequence b is slot j % page_size of page block_table[b][j / page_size]. The T new tokens of a call are packed, those
+ * of sequence b being tokens q_starts[b] .. q_starts[b + 1] - 1, and are the last of its kv_lens[b] keys: token i of
+ * n new ones is at position kv_lens[b] - n + i. fa_kv_append writes the keys and values of new tokens to the cache (and
+ * turns keys and queries by their positions); fa_fwd_paged is their attention over it.
+ *
+ * Block table, kv_lens, q_starts and scales are device arrays that the host does not read. The kernels read and
+ * write inside the buffers whatever is in them:
+ *   - kv_lens[b] counts as clamped to [0, max_blocks * page_size], q_starts[b] to [0, T]; q_starts must not
+ *     decrease (else the results of the call are undefined); q_starts[b] == q_starts[b + 1] is a sequence without
+ *     new tokens; tokens before q_starts[0] or from q_starts[B] on belong to no sequence, and their rows of every
+ *     output are left as they were;
+ *   - entries of the table behind a sequence's last key are not used; a page number outside [0, n_pages) is a page
+ *     that is not there: nothing is written to it, and its keys are not visible;
+ *   - slots behind a sequence's last key are not read into any result (whatever bits they hold).
+ * Pages may be shared for reading; a page that the new tokens of two sequences are written to (or the same table
+ * entry twice in one sequence's written range) gets one of the two tokens in each 16 bytes, whichever comes last.
+ */
+typedef enum {
+  FA_CACHE_BF16 = 0, /* bf16 */
+  FA_CACHE_E4M3 = 1  /* 8-bit floats (OCP e4m3), times a scale per key/value head */
+} fa_cache_type_t;
+
+/* The cache: K is [n_pages][Hkv][page_size][d_qk] and V the same with d_v, in any order of the first three
+ * dimensions: element (page, head, slot, 0) lies at page * k_page + head * k_head + slot * k_slot, its d elements one
+ * after the other. Strides are in elements, not negative, a multiple of 16 bytes; k_slot >= d_qk, v_slot >= d_v, and a
+ * slot stride times 16 is below 2^31 bytes. page_size is a power of two from 16 to 2^20. An element of an e4m3 cache
+ * stands for its value times k_scale[head] (v_scale[head]); NULL stands for ones, and bf16 caches take NULL. */
+typedef struct {
+  void* K;
+  void* V;
+  const float* k_scale;
+  const float* v_scale;
+  long long k_page, k_head, k_slot, v_page, v_head, v_slot;
+  int n_pages, page_size, Hkv, d_qk, d_v;
+  int type; /* fa_cache_type_t */
+} fa_paged_cache_t;
+
+/* The batch: int32 arrays block_table [B][max_blocks] (rows table_stride elements apart), kv_lens [B] and q_starts
+ * [B + 1], and the number of packed tokens T. */
+typedef struct {
+  const int* block_table;
+  long long table_stride;
+  const int* kv_lens;
+  const int* q_starts;
+  int B, max_blocks, T;
+} fa_paged_batch_t;
+
+/*
+ * fa_kv_append -- write the keys and values of the new tokens to the cache, turning keys (and queries) by the
+ * position rotation on the way.
+ *   cache, batch     as above; kv_lens counts the new tokens already
+ *   K, V             bf16 [T][Hkv][d_qk], [T][Hkv][d_v]; element (t, h, 0) at t * k_token + h * k_head
+ *   Q, Q_out, Hq     bf16 [T][Hq][d_qk] likewise, or Hq = 0 for none; Q_out is Q itself (same strides) or does not
+ *                    overlap it
+ *   strides          {q_token, q_head, qo_token, qo_head, k_token, k_head, v_token, v_head}, in elements, multiples of 8
+ *   cos_sin          float32 [n_pos][rot_dim], 16-byte aligned: the cosines of a position's rot_dim / 2 angles, then
+ *                    their sines; NULL with rot_dim = 0 for no rotation
+ *   rot_begin, rot_dim  the dims that turn. interleaved == 0: dim rot_begin + c pairs with rot_begin + rot_dim / 2 + c
+ *                    (rot_dim a multiple of 16); else 2c with 2c + 1 (a multiple of 8). rot_begin is a multiple of 8.
+ * A pair (x, y) becomes (x cos - y sin, y cos + x sin), computed in fp32 and rounded once, to bf16 or, for an
+ * e4m3 cache, after division by the head's scale to e4m3 (nearest even; what passes +-448 becomes +-448, NaN
+ * stays NaN). V, and dims that do not turn, are copied (or divided and rounded). n_pos >= max_blocks * page_size, so that
+ * every position has its row. A token before position 0 (more new tokens than keys) is left out, and nothing is
+ * written for it. Inputs must not overlap the cache. Enqueues one kernel.
+ *
+ * Errors, in this order: cache, batch, strides or cos_sin description NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE: negative
+ * (table_stride too), Hkv <= 0 with T > 0, Hq not a multiple of Hkv, max_blocks * page_size or T * Hq >= 2^31, n_pos too small, the rotated dims
+ * outside [0, d_qk)); head dimensions, page size, type or rotation not supported (FA_ERR_UNSUPPORTED); a NULL buffer that
+ * has elements (FA_ERR_NULL_POINTER); alignment (FA_ERR_UNSUPPORTED: 16 bytes for buffers and strides, 4 for the int
+ * and scale arrays); cache strides negative, too large, or letting two elements of the cache overlap (FA_ERR_BAD_SHAPE).
+ * T == 0 or B == 0 returns FA_OK without a launch.
+ */
+fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* K, const void* V,
+                         const void* Q, void* Q_out, int Hq, const long long* strides, const float* cos_sin, int n_pos,
+                         int rot_begin, int rot_dim, int interleaved, hipStream_t stream);
+
+/*
+ * fa_fwd_paged -- attention of the new tokens over the paged cache: for token t of sequence b at position p,
+ *     O[t,h] = softmax over visible j of (scale * q[t,h] . K[b,g,j]) * V[b,g,j],   g = h / (Hq / Hkv),
+ * j <= p when causal, j < kv_lens[b] else. Arithmetic as for fa_fwd_ex (e4m3 caches: K and V are widened exactly, P is
+ * rounded to fp16). A row with no visible key gets O = 0, LSE = -inf.
+ *   Q, O        bf16 [T][Hq][d_qk], [T][Hq][d_v]; element (t, h, 0) at t * q_token + h * q_head
+ *   LSE         float32 [T][Hq] (contiguous), or NULL
+ *   strides     {q_token, q_head, o_token, o_head}, in elements, multiples of 8
+ *   max_q       the most new tokens of one sequence, as far as the host knows: it chooses the kernels, the results
+ *               are right for any
+ *   workspace   16-byte aligned, at least fa_fwd_paged_workspace_bytes(...) bytes, overwritten; nothing needs to be in
+ *               it before, and it must not be used elsewhere until the call's work has completed
+ * The work is cut on the device by the lengths found there, so one captured call serves whatever lengths the arrays
+ * hold at a replay.
+ *
+ * Errors, in this order: cache, batch or strides NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE: as for fa_kv_append, max_q < 0,
+ * Hkv * (T * Hq / Hkv / 32 + B) * (max_blocks * page_size / 128 + 2) >= 2^31); head dimensions, page size, type
+ * (FA_ERR_UNSUPPORTED); NULL buffers (FA_ERR_NULL_POINTER); scale (FA_ERR_BAD_SCALE); alignment (FA_ERR_UNSUPPORTED); cache
+ * strides (FA_ERR_BAD_SHAPE); workspace NULL or too small (FA_ERR_WORKSPACE), not aligned (FA_ERR_UNSUPPORTED). T == 0, B == 0 or
+ * Hq == 0 returns FA_OK without a launch.
+ */
+fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* Q, void* O, float* LSE,
+                         int Hq, const long long* strides, int max_q, float scale, int causal, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of fa_fwd_paged: it does not depend on the lengths. Host arithmetic only; 0 for sizes <= 0, Hq not a
+ * multiple of Hkv, or an unsupported type or head dimension. */
+size_t fa_fwd_paged_workspace_bytes(int T, int Hq, int Hkv, int d_qk, int d_v, int type);
 
 /* Static, human-readable name of a status code ("FA_OK", ...); "unknown status" otherwise. */
 const char* fa_status_str(fa_status_t s);

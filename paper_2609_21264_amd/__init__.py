@@ -16,16 +16,21 @@ kernel. The functions below marshal arguments and translate status codes, nothin
 * :func:`forward` -- convenience wrapper over torch tensors (``n_split`` > 1 selects split mode and
   takes the workspace from torch's allocator; ``decode=True`` the decode-shaped path).
 * :func:`forward_unfused` -- the same over the unfused path (``fa_fwd_unfused``).
+* :func:`kv_append`, :func:`forward_paged` -- a paged key/value cache: appending new tokens to it with their
+  position rotation, and their attention over it (C: ``fa_kv_append``, ``fa_fwd_paged``, whose descriptions are the
+  ctypes structures :class:`PagedCache` and :class:`PagedBatch`).
 """
 
 from __future__ import annotations
 
 import contextlib
+import ctypes
 import math
 from typing import Optional
 
 from . import _lib
-from ._lib import (FA_ERR_BAD_SCALE, FA_ERR_BAD_SHAPE, FA_ERR_HIP, FA_ERR_NULL_POINTER,  # noqa: F401
+from ._lib import (AppendStrides, PagedBatch, PagedCache, PagedStrides, FA_CACHE_BF16, FA_CACHE_E4M3,  # noqa: F401
+                   FA_ERR_BAD_SCALE, FA_ERR_BAD_SHAPE, FA_ERR_HIP, FA_ERR_NULL_POINTER,
                    FA_ERR_UNSUPPORTED, FA_ERR_WORKSPACE, FA_INSTANCE_HALVES, FA_INSTANCE_LONG, FA_INSTANCE_NONE,
                    FA_INSTANCE_QUARTERS, FA_INSTANCE_SHORT, FA_INSTANCE_SHORT_WIDE, FA_NOALLOC_SCRATCH_BYTES, FA_OK,
                    LIB_PATH)
@@ -33,7 +38,9 @@ from ._lib import (FA_ERR_BAD_SCALE, FA_ERR_BAD_SHAPE, FA_ERR_HIP, FA_ERR_NULL_P
 __all__ = ["fa_fwd", "fa_fwd_ex", "fa_fwd_split", "fa_fwd_split_workspace_bytes", "fa_fwd_split_parts",
            "fa_status_str", "fa_block_rows", "fa_fwd_rows", "fa_lbl_scores", "fa_lbl_softmax", "fa_lbl_pv", "fa_lbl_ld",
            "fa_lbl_workspace_bytes", "fa_fwd_unfused", "fa_fwd_decode", "fa_fwd_decode_parts",
-           "fa_fwd_decode_noalloc", "fa_fwd_instance", "forward", "forward_unfused", "FaError", "LIB_PATH", "FA_NOALLOC_SCRATCH_BYTES"]
+           "fa_fwd_decode_noalloc", "fa_fwd_instance", "forward", "forward_unfused", "FaError", "LIB_PATH", "FA_NOALLOC_SCRATCH_BYTES",
+           "fa_kv_append", "fa_fwd_paged", "fa_fwd_paged_workspace_bytes", "PagedCache", "PagedBatch", "AppendStrides",
+           "PagedStrides", "FA_CACHE_BF16", "FA_CACHE_E4M3", "kv_append", "forward_paged"]
 
 
 class FaError(RuntimeError):
@@ -150,6 +157,31 @@ def fa_fwd_unfused(Q: int, K: int, V: int, O: int, LSE: Optional[int], B: int, H
     """C ``fa_fwd_unfused``: raw device addresses and sizes; returns the status code."""
     return int(_lib.load().fa_fwd_unfused(Q, K, V, O, LSE, B, Hq, Hkv, Sq, Sk, d_qk, d_v, float(scale),
                                           int(bool(causal)), workspace, int(workspace_bytes), stream))
+
+
+def fa_kv_append(cache: PagedCache, batch: PagedBatch, K: int, V: int, Q: Optional[int], Q_out: Optional[int], Hq: int,
+                 strides: AppendStrides, cos_sin: Optional[int], n_pos: int, rot_begin: int, rot_dim: int,
+                 interleaved: bool, stream: int) -> int:
+    """C ``fa_kv_append``: descriptions, raw device addresses and sizes; returns the status code."""
+    return int(_lib.load().fa_kv_append(_ref(cache), _ref(batch), K, V, Q, Q_out, Hq, strides, cos_sin, n_pos, rot_begin,
+                                        rot_dim, int(bool(interleaved)), stream))
+
+
+def fa_fwd_paged(cache: PagedCache, batch: PagedBatch, Q: int, O: int, LSE: Optional[int], Hq: int,
+                 strides: PagedStrides, max_q: int, scale: float, causal: bool, workspace: Optional[int],
+                 workspace_bytes: int, stream: int) -> int:
+    """C ``fa_fwd_paged``: descriptions, raw device addresses and sizes; returns the status code."""
+    return int(_lib.load().fa_fwd_paged(_ref(cache), _ref(batch), Q, O, LSE, Hq, strides, max_q, float(scale),
+                                        int(bool(causal)), workspace, int(workspace_bytes), stream))
+
+
+def fa_fwd_paged_workspace_bytes(T: int, Hq: int, Hkv: int, d_qk: int, d_v: int, type: int = FA_CACHE_BF16) -> int:
+    """C ``fa_fwd_paged_workspace_bytes``."""
+    return int(_lib.load().fa_fwd_paged_workspace_bytes(int(T), int(Hq), int(Hkv), int(d_qk), int(d_v), int(type)))
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
 
 
 # What a call costs on the host bounds the smallest problems (one head S256 d64: a 4.7 us kernel in a call
@@ -318,4 +350,197 @@ def forward(q, k, v, causal: bool = False, scale: Optional[float] = None, return
         if st in (FA_ERR_NULL_POINTER, FA_ERR_BAD_SHAPE, FA_ERR_UNSUPPORTED, FA_ERR_BAD_SCALE, FA_ERR_WORKSPACE):
             raise ValueError(f"{name} rejected the arguments: {fa_status_str(st)}")
         raise FaError(st)
+    return (out, lse) if return_lse else out
+
+
+def _own_stream(stream):
+    """Context for allocating what kernels on ``stream`` use: the memory belongs to that stream, so that nothing
+    still running elsewhere uses it."""
+    import torch
+
+    return _NO_SWITCH if stream is None else torch.cuda.stream(stream)
+
+
+def _check_rows(name, t, shape, device, writes=False):
+    """A packed [T, H, d] bf16 tensor with any strides of T and H: returns them, 0 for a dimension of one."""
+    import torch
+
+    if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be a 3-d bfloat16 torch tensor [tokens, heads, d]")
+    if t.device != device:
+        raise ValueError(f"{name} must be on the cache's device {device}, not {t.device}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}, not {list(t.shape)}")
+    T, H, d = shape
+    st, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError(f"the elements of a head of {name} must lie one after the other")
+    st, sh = st if T > 1 else 0, sh if H > 1 else 0
+    if writes and not ((sh >= d or H <= 1) and (st >= (H - 1) * sh + d or T <= 1)
+                       or (st >= d or T <= 1) and (sh >= (T - 1) * st + d or H <= 1)):
+        raise ValueError(f"rows of {name} overlap")
+    return st, sh
+
+
+def _check_paged(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale, v_scale, T):
+    """Checks of the cache and the batch; their C descriptions."""
+    import torch
+
+    tensor = torch.Tensor
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        if not isinstance(t, tensor) or t.dim() != 4 or t.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise ValueError(f"{name} must be a 4-d torch tensor [pages, heads, page_size, d], bfloat16 or float8_e4m3fn")
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be on a GPU")
+        if t.stride(3) != 1:
+            raise ValueError(f"the elements of a head of {name} must lie one after the other")
+    device = k_cache.device
+    if k_cache.dtype != v_cache.dtype or k_cache.shape[:3] != v_cache.shape[:3] or v_cache.device != device:
+        raise ValueError("k_cache and v_cache must agree in type, device, pages, heads and page size")
+    pages, hkv, page, dqk = k_cache.shape
+    for name, t, dim in (("block_table", block_table, 2), ("kv_lens", kv_lens, 1), ("q_starts", q_starts, 1)):
+        if not isinstance(t, tensor) or t.dim() != dim or t.dtype != torch.int32:
+            raise ValueError(f"{name} must be a {dim}-d int32 torch tensor")
+        if t.device != device:
+            raise ValueError(f"{name} must be on the cache's device {device}, not {t.device}")
+        if t.numel() > 1 and t.stride(dim - 1) != 1 and t.shape[dim - 1] > 1:
+            raise ValueError(f"the entries of {name} must lie one after the other")
+    B = kv_lens.shape[0]
+    if block_table.shape[0] != B or q_starts.shape[0] != B + 1:
+        raise ValueError(f"block_table [B, blocks], kv_lens [B] and q_starts [B + 1] do not agree: "
+                         f"{list(block_table.shape)}, {list(kv_lens.shape)}, {list(q_starts.shape)}")
+    fp8 = k_cache.dtype == torch.float8_e4m3fn
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if t is None:
+            continue
+        if not fp8:
+            raise ValueError(f"{name} goes with a float8_e4m3fn cache")
+        if not isinstance(t, tensor) or t.dtype != torch.float32 or tuple(t.shape) != (hkv,) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous float32 tensor [heads]")
+        if t.device != device:
+            raise ValueError(f"{name} must be on the cache's device {device}, not {t.device}")
+    ks, vs = k_cache.stride(), v_cache.stride()
+    if pages <= 1 or hkv <= 1:  # the stride of a dimension of one means nothing
+        ks, vs = ([x if n > 1 else 0 for x, n in zip(st[:2], (pages, hkv))] + [st[2]] for st in (ks, vs))
+    cache = PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+                       None if v_scale is None else v_scale.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], pages,
+                       page, hkv, dqk, v_cache.shape[3], FA_CACHE_E4M3 if fp8 else FA_CACHE_BF16)
+    batch = PagedBatch(block_table.data_ptr(), block_table.stride(0) if B > 1 else 0, kv_lens.data_ptr(),
+                       q_starts.data_ptr(), B, block_table.shape[1], T)
+    return device, cache, batch
+
+
+def _raise(name, st):
+    if st in (FA_ERR_NULL_POINTER, FA_ERR_BAD_SHAPE, FA_ERR_UNSUPPORTED, FA_ERR_BAD_SCALE, FA_ERR_WORKSPACE):
+        raise ValueError(f"{name} rejected the arguments: {fa_status_str(st)}")
+    raise FaError(st)
+
+
+def kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q=None, q_out=None, cos_sin=None,
+              rot_begin: int = 0, interleaved: bool = False, k_scale=None, v_scale=None, stream=None):
+    """Write the keys and values of new tokens to a paged cache, turning keys and queries by their positions.
+
+    k [T, Hkv, d_qk] and v [T, Hkv, d_v] (bf16) hold the packed new tokens; those of sequence b are
+    ``q_starts[b]`` to ``q_starts[b + 1] - 1``, the last of its ``kv_lens[b]`` keys. k_cache and v_cache are
+    [pages, Hkv, page_size, d] in bf16 or float8_e4m3fn (an element then stands for itself times ``k_scale[h]``,
+    ``v_scale[h]``); ``block_table`` [B, blocks] names every sequence's pages in order (int32, like the lengths). Any strides
+    of the outer dimensions. ``cos_sin`` float32 [positions, rot_dim] holds the cosines and then the sines of a
+    position's angles; dims ``rot_begin`` to ``rot_begin + rot_dim - 1`` of k and q turn, in pairs (c, c + rot_dim / 2) or,
+    ``interleaved``, (2c, 2c + 1). With ``q`` [T, Hq, d_qk] returns the turned queries, in ``q_out`` (which may be ``q``) or a
+    new tensor; rows of tokens that belong to no sequence are left as they were, so a new tensor's hold anything.
+
+    The kernel is enqueued on ``stream`` (default: torch's current stream; a new tensor belongs to that
+    stream); the call does not synchronise, and reads no array on the host."""
+    import torch
+
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("k must be a 3-d bfloat16 torch tensor [tokens, heads, d]")
+    T = k.shape[0]
+    device, cache, batch = _check_paged(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale, v_scale, T)
+    hkv, dqk, dv = cache.Hkv, cache.d_qk, cache.d_v
+    kt, kh = _check_rows("k", k, (T, hkv, dqk), device)
+    vt, vh = _check_rows("v", v, (T, hkv, dv), device)
+    n_pos = rot = 0
+    if cos_sin is not None:
+        if not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2 or cos_sin.dtype != torch.float32 or not cos_sin.is_contiguous():
+            raise ValueError("cos_sin must be a contiguous float32 tensor [positions, rotated dims]")
+        if cos_sin.device != device:
+            raise ValueError(f"cos_sin must be on the cache's device {device}, not {cos_sin.device}")
+        n_pos, rot = cos_sin.shape
+    stream, handle = _stream(stream, device)
+    with _on_device(device):
+        hq = qt = qh = ot = oh = 0
+        if q is not None:
+            if not isinstance(q, torch.Tensor) or q.dim() != 3:
+                raise ValueError("q must be a 3-d bfloat16 torch tensor [tokens, heads, d]")
+            hq = q.shape[1]
+            qt, qh = _check_rows("q", q, (T, hq, dqk), device, writes=q_out is q)
+            if q_out is None:
+                with _own_stream(stream):
+                    q_out = torch.empty((T, hq, dqk), dtype=torch.bfloat16, device=device)
+            elif q_out is not q and isinstance(q_out, torch.Tensor) and q_out.numel() > 0 and \
+                    q_out.untyped_storage().data_ptr() == q.untyped_storage().data_ptr():
+                raise ValueError("q_out must be q itself or lie in a storage of its own")
+            ot, oh = (qt, qh) if q_out is q else _check_rows("q_out", q_out, (T, hq, dqk), device, writes=True)
+        elif q_out is not None:
+            raise ValueError("q_out goes with q")
+        st = fa_kv_append(cache, batch, k.data_ptr(), v.data_ptr(), None if q is None else q.data_ptr(),
+                          None if q is None else q_out.data_ptr(), hq, AppendStrides(qt, qh, ot, oh, kt, kh, vt, vh),
+                          None if cos_sin is None else cos_sin.data_ptr(), n_pos, int(rot_begin), rot, interleaved, handle)
+    if st != FA_OK:
+        _raise("fa_kv_append", st)
+    return q_out
+
+
+def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Optional[int] = None, causal: bool = True,
+                  scale: Optional[float] = None, k_scale=None, v_scale=None, return_lse: bool = False, out=None, lse=None,
+                  workspace=None, stream=None):
+    """Attention of the new tokens q [T, Hq, d_qk] over a paged cache (see :func:`kv_append` for the cache and the
+    batch, whose new tokens are in the cache already): returns O [T, Hq, d_v] (bf16) and, with ``return_lse``, LSE
+    [T, Hq] (float32, natural log). Token i of the n new ones of sequence b sees the keys up to its position
+    ``kv_lens[b] - n + i`` (all ``kv_lens[b]`` where not ``causal``). ``max_q``, the most new tokens of one sequence, chooses
+    the kernels (default: the mean, rounded up); the results are right for any. Rows of tokens that belong to no
+    sequence are left as they were, so a new tensor's hold anything.
+
+    ``scale`` defaults to 1/sqrt(d_qk). ``workspace`` is a uint8 CUDA tensor of ``fa_fwd_paged_workspace_bytes`` (default: from
+    torch's allocator). The kernels are enqueued on ``stream`` (default: torch's current stream; new tensors belong to that
+    stream); the call does not synchronise, and reads no array on the host: captured into a graph, it serves
+    whatever lengths the arrays hold at a replay."""
+    import torch
+
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a 3-d bfloat16 torch tensor [tokens, heads, d]")
+    T, hq = q.shape[0], q.shape[1]
+    device, cache, batch = _check_paged(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale, v_scale, T)
+    dqk, dv = cache.d_qk, cache.d_v
+    qt, qh = _check_rows("q", q, (T, hq, dqk), device)
+    if scale is None:
+        scale = 1.0 / math.sqrt(dqk) if dqk else 1.0
+    if max_q is None:
+        max_q = -(-T // batch.B) if batch.B else 0
+    if workspace is not None and (not isinstance(workspace, torch.Tensor) or workspace.device != device
+                                  or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    stream, handle = _stream(stream, device)
+    with _on_device(device):
+        with _own_stream(stream):
+            if out is None:
+                out = torch.empty((T, hq, dv), dtype=torch.bfloat16, device=device)
+            if return_lse and lse is None:
+                lse = torch.empty((T, hq), dtype=torch.float32, device=device)
+            if workspace is None:
+                nbytes = fa_fwd_paged_workspace_bytes(T, hq, cache.Hkv, dqk, dv, cache.type)
+                workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        ot, oh = _check_rows("out", out, (T, hq, dv), device, writes=True)
+        if lse is not None:
+            if (not isinstance(lse, torch.Tensor) or tuple(lse.shape) != (T, hq) or lse.dtype != torch.float32
+                    or not lse.is_contiguous()):
+                raise ValueError("lse must be a contiguous float32 tensor [T, Hq]")
+            if lse.device != device:
+                raise ValueError(f"lse must be on the cache's device {device}, not {lse.device}")
+        st = fa_fwd_paged(cache, batch, q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, hq,
+                          PagedStrides(qt, qh, ot, oh), int(max_q), scale, causal, workspace.data_ptr(),
+                          workspace.numel() * workspace.element_size(), handle)
+    if st != FA_OK:
+        _raise("fa_fwd_paged", st)
     return (out, lse) if return_lse else out

@@ -36,7 +36,31 @@ FA_NOALLOC_SCRATCH_BYTES = 32 << 20
 EXPORTED = ("fa_fwd", "fa_fwd_ex", "fa_fwd_split", "fa_fwd_split_workspace_bytes", "fa_fwd_split_parts",
             "fa_status_str", "fa_block_rows", "fa_fwd_rows", "fa_lbl_scores", "fa_lbl_softmax", "fa_lbl_pv", "fa_lbl_ld",
             "fa_lbl_workspace_bytes", "fa_fwd_unfused", "fa_fwd_decode", "fa_fwd_decode_parts",
-            "fa_fwd_decode_noalloc", "fa_fwd_instance")
+            "fa_fwd_decode_noalloc", "fa_fwd_instance", "fa_kv_append", "fa_fwd_paged", "fa_fwd_paged_workspace_bytes")
+
+# Values of fa_cache_type_t.
+FA_CACHE_BF16 = 0
+FA_CACHE_E4M3 = 1
+
+
+class PagedCache(ctypes.Structure):
+    """fa_paged_cache_t."""
+
+    _fields_ = [*((n, ctypes.c_void_p) for n in ("K", "V", "k_scale", "v_scale")),
+                *((n, ctypes.c_longlong) for n in ("k_page", "k_head", "k_slot", "v_page", "v_head", "v_slot")),
+                *((n, ctypes.c_int) for n in ("n_pages", "page_size", "Hkv", "d_qk", "d_v", "type"))]
+
+
+class PagedBatch(ctypes.Structure):
+    """fa_paged_batch_t."""
+
+    _fields_ = [("block_table", ctypes.c_void_p), ("table_stride", ctypes.c_longlong), ("kv_lens", ctypes.c_void_p),
+                ("q_starts", ctypes.c_void_p), *((n, ctypes.c_int) for n in ("B", "max_blocks", "T"))]
+
+
+#: Element strides of fa_kv_append and of fa_fwd_paged.
+AppendStrides = ctypes.c_longlong * 8
+PagedStrides = ctypes.c_longlong * 4
 
 _lib = None
 
@@ -89,5 +113,11 @@ def load() -> ctypes.CDLL:
     lib.fa_fwd_decode_noalloc.restype = i
     lib.fa_fwd_decode_parts.argtypes = [i, i, i, i, i, i]
     lib.fa_fwd_decode_parts.restype = i
+    lib.fa_kv_append.argtypes = [vp, vp, vp, vp, vp, vp, i, vp, vp, i, i, i, i, vp]
+    lib.fa_kv_append.restype = i
+    lib.fa_fwd_paged.argtypes = [vp, vp, vp, vp, vp, i, vp, i, f, i, vp, ctypes.c_size_t, vp]
+    lib.fa_fwd_paged.restype = i
+    lib.fa_fwd_paged_workspace_bytes.argtypes = [i, i, i, i, i, i]
+    lib.fa_fwd_paged_workspace_bytes.restype = ctypes.c_size_t
     _lib = lib
     return lib

@@ -224,9 +224,195 @@ fa::LblParams lbl_params(int B, int Hq, int Hkv, int Sq, int Sk, float scale, in
   return p;
 }
 
+// ---- paged cache ---------------------------------------------------------------------------------
+
+bool dims_supported(int d_qk, int d_v) { return fa::block_rows(d_qk, d_v, true) != 0; }
+
+// Checks that both paged entry points begin with, in the order fa.h documents: sizes, then what is supported. Hq may be
+// 0 (no queries). On FA_OK fills the kernels' view of the cache and the batch.
+fa_status_t check_paged_shape(const fa_paged_cache_t* c, const fa_paged_batch_t* bt, int Hq) {
+  if (bt->B < 0 || bt->T < 0 || bt->max_blocks < 0 || c->n_pages < 0 || c->Hkv < 0 || Hq < 0) return FA_ERR_BAD_SHAPE;
+  if ((bt->T > 0 || Hq > 0) && (c->Hkv <= 0 || Hq % c->Hkv != 0)) return FA_ERR_BAD_SHAPE;
+  if (bt->table_stride < 0 || static_cast<int64_t>(bt->max_blocks) * c->page_size > INT_MAX) return FA_ERR_BAD_SHAPE;
+  const int64_t heads = Hq > c->Hkv ? Hq : c->Hkv;
+  if (static_cast<int64_t>(bt->T) * heads > INT_MAX || bt->B == INT_MAX) return FA_ERR_BAD_SHAPE;
+  return FA_OK;
+}
+fa_status_t check_paged_support(const fa_paged_cache_t* c) {
+  if (!dims_supported(c->d_qk, c->d_v)) return FA_ERR_UNSUPPORTED;
+  if (c->page_size < 16 || c->page_size > (1 << 20) || (c->page_size & (c->page_size - 1)) != 0) return FA_ERR_UNSUPPORTED;
+  if (c->type != FA_CACHE_BF16 && c->type != FA_CACHE_E4M3) return FA_ERR_UNSUPPORTED;
+  if (c->type == FA_CACHE_BF16 && (c->k_scale != nullptr || c->v_scale != nullptr)) return FA_ERR_UNSUPPORTED;
+  return FA_OK;
+}
+bool paged_pointers(const fa_paged_cache_t* c, const fa_paged_batch_t* bt) {
+  if (bt->kv_lens == nullptr || bt->q_starts == nullptr) return false;
+  if (bt->max_blocks > 0 && bt->block_table == nullptr) return false;
+  return c->n_pages == 0 || c->Hkv == 0 || (c->K != nullptr && c->V != nullptr);
+}
+bool paged_aligned(const fa_paged_cache_t* c, const fa_paged_batch_t* bt) {
+  const long long m = c->type == FA_CACHE_E4M3 ? 15 : 7;  // elements of 16 bytes, less one
+  return aligned(c->K, 16) && aligned(c->V, 16) && aligned(c->k_scale, 4) && aligned(c->v_scale, 4) &&
+         aligned(bt->block_table, 4) && aligned(bt->kv_lens, 4) && aligned(bt->q_starts, 4) &&
+         ((c->k_page | c->k_head | c->k_slot | c->v_page | c->v_head | c->v_slot) & m) == 0;
+}
+// Strides of K or V: not negative, slots apart by a row at least and close enough for the kernels' 32-bit offsets,
+// the whole buffer addressable; `writes`: no element has two places in the index space.
+bool paged_strides(long long page, long long head, long long slot, const fa_paged_cache_t* c, int d, bool writes) {
+  const int64_t size = c->type == FA_CACHE_E4M3 ? 1 : 2;
+  if (page < 0 || head < 0 || slot < d || slot > INT_MAX / (16 * size)) return false;
+  const long long st[3] = {page, head, slot};
+  const int64_t n[3] = {c->n_pages, c->Hkv, c->page_size};
+  double last = d;
+  for (int i = 0; i < 3; ++i)
+    if (n[i] > 1) last += static_cast<double>(n[i] - 1) * static_cast<double>(st[i]);
+  if (last * static_cast<double>(size) >= 1e15) return false;
+  if (!writes) return true;
+  // Innermost first: every dimension has to step over all that the smaller strides reach.
+  bool done[3] = {false, false, false};
+  int64_t reach = d;
+  for (int k = 0; k < 3; ++k) {
+    int at = -1;
+    for (int i = 0; i < 3; ++i)
+      if (!done[i] && n[i] > 1 && (at < 0 || st[i] < st[at])) at = i;
+    if (at < 0) break;
+    if (st[at] < reach) return false;
+    reach += (n[at] - 1) * st[at];
+    done[at] = true;
+  }
+  return true;
+}
+fa_status_t check_paged_strides(const fa_paged_cache_t* c, bool writes) {
+  return paged_strides(c->k_page, c->k_head, c->k_slot, c, c->d_qk, writes) &&
+                 paged_strides(c->v_page, c->v_head, c->v_slot, c, c->d_v, writes)
+             ? FA_OK
+             : FA_ERR_BAD_SHAPE;
+}
+void paged_view(const fa_paged_cache_t* c, const fa_paged_batch_t* bt, fa::PagedCache* v, fa::PagedBatch* w) {
+  int shift = 0;
+  while ((1 << shift) < c->page_size) ++shift;
+  *v = fa::PagedCache{c->K,      c->V,      c->k_scale, c->v_scale, c->k_page, c->k_head, c->k_slot, c->v_page,
+                      c->v_head, c->v_slot, c->n_pages, shift,      c->Hkv,    c->d_qk,   c->d_v};
+  *w = fa::PagedBatch{bt->block_table, bt->kv_lens, bt->q_starts, bt->table_stride,
+                      bt->B,           bt->T,       bt->max_blocks * c->page_size};
+}
+// Element strides of a packed input or output: multiples of 16 bytes that double-checked offsets can hold.
+bool token_strides(const long long* s, int n) {
+  for (int i = 0; i < n; ++i)
+    if (s[i] < 0 || (s[i] & 7) != 0 || s[i] > (1ll << 40)) return false;
+  return true;
+}
+// Columns and bytes of the workspace of fa_fwd_paged (sizes checked); the three arrays in it are 16-byte aligned.
+struct PagedWorkspace {
+  int n_wg, cols;
+  int64_t o, lse, bytes;
+};
+PagedWorkspace paged_workspace(int T, int group, int d_qk, int d_v, int type) {
+  PagedWorkspace w;
+  w.n_wg = fa::paged_workgroups(d_qk, type == FA_CACHE_E4M3);
+  const int64_t rows = static_cast<int64_t>(T) * group;
+  w.cols = rows < 32 ? static_cast<int>(rows) : 32;
+  const int64_t places = 2ll * w.n_wg * w.cols;
+  w.o = 0;
+  w.lse = places * d_v * 4;
+  w.bytes = w.lse + (places * 4 + 15) / 16 * 16;
+  w.bytes += static_cast<int64_t>(w.n_wg) * sizeof(fa::PagedItem);
+  return w;
+}
+
 }  // namespace
 
 extern "C" {
+
+fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* K, const void* V,
+                         const void* Q, void* Q_out, int Hq, const long long* strides, const float* cos_sin, int n_pos,
+                         int rot_begin, int rot_dim, int interleaved, hipStream_t stream) {
+  if (cache == nullptr || batch == nullptr || strides == nullptr) return FA_ERR_NULL_POINTER;
+  fa_status_t st = check_paged_shape(cache, batch, Hq);
+  if (st != FA_OK) return st;
+  if (rot_dim < 0 || rot_begin < 0 || static_cast<int64_t>(rot_begin) + rot_dim > cache->d_qk || n_pos < 0) return FA_ERR_BAD_SHAPE;
+  if (rot_dim > 0 && n_pos < static_cast<int64_t>(batch->max_blocks) * cache->page_size) return FA_ERR_BAD_SHAPE;
+  st = check_paged_support(cache);
+  if (st != FA_OK) return st;
+  if (rot_dim > 0 && (rot_begin % 8 != 0 || rot_dim % (interleaved != 0 ? 8 : 16) != 0)) return FA_ERR_UNSUPPORTED;
+  if (batch->T == 0 || batch->B == 0) return FA_OK;
+  if (!paged_pointers(cache, batch) || K == nullptr || V == nullptr || (Hq > 0 && (Q == nullptr || Q_out == nullptr)) ||
+      (rot_dim > 0 && cos_sin == nullptr))
+    return FA_ERR_NULL_POINTER;
+  if (!paged_aligned(cache, batch) || !aligned(K, 16) || !aligned(V, 16) || !aligned(Q, 16) || !aligned(Q_out, 16) ||
+      !aligned(cos_sin, 16) || !token_strides(strides, 8))
+    return FA_ERR_UNSUPPORTED;
+  st = check_paged_strides(cache, true);
+  if (st != FA_OK) return st;
+  fa::AppendParams p{};
+  paged_view(cache, batch, &p.c, &p.bt);
+  p.q = static_cast<const uint16_t*>(Q);
+  p.q_out = static_cast<uint16_t*>(Q_out);
+  p.k = static_cast<const uint16_t*>(K);
+  p.v = static_cast<const uint16_t*>(V);
+  p.cos_sin = cos_sin;
+  p.q_token = strides[0], p.q_head = strides[1], p.qo_token = strides[2], p.qo_head = strides[3];
+  p.k_token = strides[4], p.k_head = strides[5], p.v_token = strides[6], p.v_head = strides[7];
+  p.hq = Hq;
+  p.rot = rot_dim;
+  p.begin = rot_dim > 0 ? rot_begin : 0;
+  p.inter = rot_dim > 0 && interleaved != 0;
+  return fa::launch_append(p, cache->type == FA_CACHE_E4M3, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
+
+size_t fa_fwd_paged_workspace_bytes(int T, int Hq, int Hkv, int d_qk, int d_v, int type) {
+  if (T <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || !dims_supported(d_qk, d_v) ||
+      (type != FA_CACHE_BF16 && type != FA_CACHE_E4M3))
+    return 0;
+  return static_cast<size_t>(paged_workspace(T, Hq / Hkv, d_qk, d_v, type).bytes);
+}
+
+fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* Q, void* O, float* LSE,
+                         int Hq, const long long* strides, int max_q, float scale, int causal, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream) {
+  if (cache == nullptr || batch == nullptr || strides == nullptr) return FA_ERR_NULL_POINTER;
+  fa_status_t st = check_paged_shape(cache, batch, Hq);
+  if (st != FA_OK) return st;
+  if (max_q < 0) return FA_ERR_BAD_SHAPE;
+  if (Hq > 0) {
+    // The kernel's line of work is counted in 32 bits.
+    const int64_t blocks = (static_cast<int64_t>(batch->T) * (Hq / cache->Hkv) / 32 + batch->B) * cache->Hkv;  // < 2^58
+    const int64_t tiles = static_cast<int64_t>(batch->max_blocks) * cache->page_size / 128 + 2;
+    if (blocks > INT_MAX / tiles) return FA_ERR_BAD_SHAPE;
+  }
+  st = check_paged_support(cache);
+  if (st != FA_OK) return st;
+  if (batch->T == 0 || batch->B == 0 || Hq == 0) return FA_OK;
+  if (!paged_pointers(cache, batch) || Q == nullptr || O == nullptr) return FA_ERR_NULL_POINTER;
+  if (!isfinite(scale)) return FA_ERR_BAD_SCALE;
+  const double c = static_cast<double>(scale) * 1.4426950408889634074;
+  if (fabs(c) > FLT_MAX) return FA_ERR_BAD_SCALE;
+  if (!paged_aligned(cache, batch) || !aligned(Q, 16) || !aligned(O, 16) || !aligned(LSE, 4) || !token_strides(strides, 4))
+    return FA_ERR_UNSUPPORTED;
+  st = check_paged_strides(cache, false);
+  if (st != FA_OK) return st;
+  const PagedWorkspace w = paged_workspace(batch->T, Hq / cache->Hkv, cache->d_qk, cache->d_v, cache->type);
+  if (workspace == nullptr || workspace_bytes < static_cast<size_t>(w.bytes)) return FA_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return FA_ERR_UNSUPPORTED;
+
+  fa::PagedParams p{};
+  paged_view(cache, batch, &p.c, &p.bt);
+  p.q = static_cast<const uint16_t*>(Q);
+  p.o = static_cast<uint16_t*>(O);
+  p.lse = LSE;
+  p.q_token = strides[0], p.q_head = strides[1], p.o_token = strides[2], p.o_head = strides[3];
+  p.hq = Hq;
+  p.group = Hq / cache->Hkv;
+  p.causal = causal != 0;
+  p.cs = static_cast<float>(c);
+  p.n_wg = w.n_wg;
+  p.part_cols = w.cols;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  p.o_part = reinterpret_cast<float*>(ws + w.o);
+  p.lse_part = reinterpret_cast<float*>(ws + w.lse);
+  p.desc = reinterpret_cast<fa::PagedItem*>(ws + w.bytes - static_cast<int64_t>(w.n_wg) * sizeof(fa::PagedItem));
+  return fa::launch_paged_few(p, cache->d_qk, cache->type == FA_CACHE_E4M3, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
 
 fa_status_t fa_fwd_ex(const void* Q, const void* K, const void* V, void* O, float* LSE, int B, int Hq, int Hkv,
                       int Sq, int Sk, int d_qk, int d_v, float scale, int causal, hipStream_t stream) {

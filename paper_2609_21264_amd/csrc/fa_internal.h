@@ -137,4 +137,69 @@ hipError_t launch_lbl_scores(const LblParams& p, int d_qk, hipStream_t stream);
 hipError_t launch_lbl_softmax(const LblParams& p, hipStream_t stream);
 hipError_t launch_lbl_pv(const LblParams& p, int d_v, hipStream_t stream);
 
+// ---- paged key/value cache (fa_paged_kernel.hip) -------------------------------------------------
+
+// The cache: strides in elements (2 bytes each, or 1 for e4m3); a page holds 1 << page_shift slots.
+struct PagedCache {
+  void* k;
+  void* v;
+  const float* k_scale;  // fp32 [Hkv] or nullptr (1): an e4m3 element stands for itself times the scale
+  const float* v_scale;
+  int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
+  int n_pages, page_shift, hkv, d_qk, d_v;
+};
+
+// The batch; all arrays are device data.
+struct PagedBatch {
+  const int* block_table;  // [n_seq], rows table_stride apart: page numbers
+  const int* kv_lens;      // [n_seq]
+  const int* q_starts;     // [n_seq + 1]
+  int64_t table_stride;
+  int n_seq, n_tokens;
+  int max_keys;            // keys that a row of the table has pages for
+};
+
+struct AppendParams {
+  PagedCache c;
+  PagedBatch bt;
+  const uint16_t* q;
+  uint16_t* q_out;
+  const uint16_t* k;
+  const uint16_t* v;
+  const float* cos_sin;  // fp32 [positions][rot]: cosines, then sines
+  int64_t q_token, q_head, qo_token, qo_head, k_token, k_head, v_token, v_head;
+  int hq;                // 0: no queries
+  int rot, begin, inter; // rotated dims (0: none), the first of them, neighbouring pairs
+};
+
+// An item of the attention that several workgroups share, written by the first of them for the join kernel.
+struct PagedItem {
+  int n_parts;  // 0 or 1: nothing to join
+  int q0;       // first packed token of the sequence
+  int n_cols, c0, g;
+  int pad[3];
+};
+
+struct PagedParams {
+  PagedCache c;
+  PagedBatch bt;
+  const uint16_t* q;
+  uint16_t* o;
+  float* lse;            // fp32 [n_tokens][Hq] or nullptr
+  int64_t q_token, q_head, o_token, o_head;
+  int hq, group, causal;
+  float cs;              // scale * log2(e)
+  int n_wg, min_units;   // workgroups, fewest units of work of one
+  int part_cols;         // columns of a place in the workspace
+  float* o_part;         // fp32 [2 * n_wg][part_cols][d_v]
+  float* lse_part;       // fp32 [2 * n_wg][part_cols]
+  PagedItem* desc;       // [n_wg]
+};
+
+hipError_t launch_append(AppendParams p, bool fp8, hipStream_t stream);
+// Workgroups of the attention kernel (as many as the chip holds at once).
+int paged_workgroups(int d_qk, bool fp8);
+// Attention and join, on `stream`; (d_qk, d_v) as for the other paths.
+hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, hipStream_t stream);
+
 }  // namespace fa

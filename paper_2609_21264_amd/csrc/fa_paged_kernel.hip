@@ -1,0 +1,662 @@
+// Paged key/value cache for gfx950: appending new tokens with their position rotation, and the attention
+// of few new tokens per sequence over the cache, split over its length and joined.
+//
+// The cache holds keys and values in pages of `page_size` tokens; a block table names the pages of a
+// sequence in order. What a sequence holds (kv_lens), which of the packed tokens are its new ones
+// (q_starts) and its pages (block_table) are device arrays, so the host never sees them: every index
+// that comes from them is checked or clamped here before it reaches an address.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "fa_device.h"
+#include "fa_internal.h"
+#include "fa_paged_device.h"
+
+namespace fa {
+namespace {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// ---- append ------------------------------------------------------------------------------------------
+//
+// One workgroup per packed token. A thread owns 16 bytes of a head, and with them the 16 bytes of their
+// partners where dim c turns with dim c + rot / 2, so that a pair is read, turned in fp32 and written by one
+// thread (Q may be rotated in place), and takes every kHeads-th head: the cos and sin of its dims stay in
+// registers. What bounds it: the bytes of Q, K and V and the latency of the chain token -> sequence ->
+// page -> store, over which the loads of Q, K and V are in flight.
+
+// Sequence of packed token t: the last b with q_starts[b] <= t, by 64 probes at a time (one step up to 63
+// sequences, two up to 4 095). -1 if t comes before the first sequence; n_seq if behind the last.
+__device__ __forceinline__ int sequence_of(const int* q_starts, int n_seq, int t, int lane) {
+  int lo = 0, len = n_seq + 1;
+  while (true) {
+    const int step = (len + 63) / 64, at = lane * step;
+    const bool below = at < len && q_starts[lo + at] <= t;
+    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(below));
+    if (n == 0) return lo - 1;
+    lo += (n - 1) * step;
+    if (step == 1) return lo;
+    len = min(step, len - (n - 1) * step);
+  }
+}
+
+// Eight bf16 as fp32 and back (RNE).
+struct F8 {
+  float x[8];
+};
+__device__ __forceinline__ F8 unpack8(const u32x4& w) {
+  F8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r.x[2 * i] = __uint_as_float(w[i] << 16);
+    r.x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+  return r;
+}
+__device__ __forceinline__ u32x4 pack8(const F8& f) {
+  return u32x4{pack_bf16x2(f.x[0], f.x[1]), pack_bf16x2(f.x[2], f.x[3]), pack_bf16x2(f.x[4], f.x[5]),
+               pack_bf16x2(f.x[6], f.x[7])};
+}
+// x / scale in e4m3, rounded to nearest even; what passes the largest finite value (448) becomes it, NaN
+// stays NaN.
+__device__ __forceinline__ u32x2 pack8_e4m3(const F8& f, float scale) {
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = f.x[i] / scale;
+    y[i] = x > 448.f ? 448.f : x < -448.f ? -448.f : x;
+  }
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
+  return u32x2{(uint32_t)lo, (uint32_t)hi};
+}
+
+constexpr int kAppendThreads = 256;
+
+template <bool FP8>
+__global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams p) {
+  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int b = __builtin_amdgcn_readfirstlane(sequence_of(p.bt.q_starts, p.bt.n_seq, t, lane));
+  if (b < 0 || b >= p.bt.n_seq) return;
+  const PagedSeq s = load_seq(p.bt, b);
+  const int64_t pos = (int64_t)s.kv - s.q_end + t;
+  if (t >= s.q_end || pos < 0) return;
+  // A token whose page number is none of the cache's leaves the cache alone; its query is rotated.
+  const int page = scalar_load(p.bt.block_table + b * p.bt.table_stride + (pos >> p.c.page_shift));
+  const bool held = page >= 0 && page < p.c.n_pages;
+  const int64_t slot = pos & ((1 << p.c.page_shift) - 1);
+
+  const int half = p.inter ? 0 : p.rot / 16;  // chunks between the partners of a pair
+  const int first = p.begin / 8, turned = p.inter ? p.rot / 8 : half;
+  // Q and K: thread (h0, j) takes chunk j of every kHeads-th head; the first `turned` chunks are those that
+  // turn (each with its partner `half` chunks on), the others are copied.
+  const int tasks = p.c.d_qk / 8 - half, lanes = kAppendThreads / tasks;
+  const int j = tid % tasks, h0 = tid / tasks;
+  if (h0 < lanes) {
+    const bool turn = j < turned;
+    int ch = first + j;
+    if (!turn) {
+      const int o = j - turned;  // o-th of the chunks outside [first, first + turned + half)
+      ch = o < first ? o : o + turned + half;
+    }
+    F8 cs{}, sn{};
+    if (turn) {
+      // Half-split: cos and sin of 8 pairs; neighbouring pairs: of the chunk's 4.
+      const float* row = p.cos_sin + pos * p.rot + (p.inter ? 4 * j : 8 * j);
+      const float* srow = row + p.rot / 2;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (i > 0 && p.inter) break;
+        const f32x4 c4 = *reinterpret_cast<const f32x4*>(row + 4 * i), s4 = *reinterpret_cast<const f32x4*>(srow + 4 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) cs.x[4 * i + e] = c4[e], sn.x[4 * i + e] = s4[e];
+      }
+    }
+    const bool pair = turn && !p.inter;
+    const int heads = p.hq + (held ? p.c.hkv : 0);
+    for (int h = h0; h < heads; h += lanes) {
+      const bool is_q = h < p.hq;
+      const int g = h - p.hq;
+      const uint16_t* src =
+          (is_q ? p.q + t * p.q_token + h * p.q_head : p.k + t * p.k_token + g * p.k_head) + 8 * ch;
+      F8 x = unpack8(*reinterpret_cast<const u32x4*>(src)), y;
+      if (pair) {
+        y = unpack8(*reinterpret_cast<const u32x4*>(src + 8 * half));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float a = x.x[e], c = y.x[e];
+          x.x[e] = a * cs.x[e] - c * sn.x[e];
+          y.x[e] = c * cs.x[e] + a * sn.x[e];
+        }
+      } else if (turn) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float a = x.x[2 * e], c = x.x[2 * e + 1];
+          x.x[2 * e] = a * cs.x[e] - c * sn.x[e];
+          x.x[2 * e + 1] = c * cs.x[e] + a * sn.x[e];
+        }
+      }
+      if (is_q) {
+        uint16_t* dst = p.q_out + t * p.qo_token + h * p.qo_head + 8 * ch;
+        *reinterpret_cast<u32x4*>(dst) = pack8(x);
+        if (pair) *reinterpret_cast<u32x4*>(dst + 8 * half) = pack8(y);
+      } else {
+        const int64_t at = page * p.c.k_page + g * p.c.k_head + slot * p.c.k_slot + 8 * ch;
+        if constexpr (FP8) {
+          const float sc = p.c.k_scale != nullptr ? p.c.k_scale[g] : 1.f;
+          uint8_t* dst = static_cast<uint8_t*>(p.c.k) + at;
+          *reinterpret_cast<u32x2*>(dst) = pack8_e4m3(x, sc);
+          if (pair) *reinterpret_cast<u32x2*>(dst + 8 * half) = pack8_e4m3(y, sc);
+        } else {
+          uint16_t* dst = static_cast<uint16_t*>(p.c.k) + at;
+          *reinterpret_cast<u32x4*>(dst) = pack8(x);
+          if (pair) *reinterpret_cast<u32x4*>(dst + 8 * half) = pack8(y);
+        }
+      }
+    }
+  }
+  if (!held) return;
+  const int vch = p.c.d_v / 8;
+  for (int i = tid; i < p.c.hkv * vch; i += kAppendThreads) {
+    const int g = i / vch, ch = i % vch;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p.v + t * p.v_token + g * p.v_head + 8 * ch);
+    const int64_t at = page * p.c.v_page + g * p.c.v_head + slot * p.c.v_slot + 8 * ch;
+    if constexpr (FP8)
+      *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(p.c.v) + at) =
+          pack8_e4m3(unpack8(w), p.c.v_scale != nullptr ? p.c.v_scale[g] : 1.f);
+    else
+      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.c.v) + at) = w;
+  }
+}
+
+// ---- attention of few rows per sequence -------------------------------------------------------------
+//
+// An item is one column block of one (sequence, key/value head): up to 32 of its group * n_q row-heads
+// (column c = row * group + member) as the columns of 32x32 MFMAs, against the key tiles visible to them.
+// The lengths are on the device, so the host cannot cut the work: all items lie on one line, kItemCost +
+// tiles units each, and workgroup i takes units [i * per, (i + 1) * per) of it, `per` from the line's length.
+// Every workgroup so has the same work whatever the lengths are, a long sequence is split over as many
+// workgroups as it is long, and at most one item per boundary is split. An item that lies in one workgroup is
+// finished there; of a split one every workgroup leaves its part (O normalised by the part's own sum, and
+// the part's LSE) in its own two places of the workspace, and the join kernel adds the parts with
+// their log-sum-exp weights.
+//
+// Inside an item: the waves take 32 keys each of a tile and stream them HBM -> LDS into a ring of their
+// own (no barrier), two 16-key halves per K and V block, each half inside one page. S^T = K Q^T, exact
+// running maximum per tile, O^T += V^T P^T as in the decode kernel. An e4m3 cache stays 8-bit in LDS and is
+// widened (exactly) as fragments are read: K to bf16, V to fp16, so that P keeps 11 bits there; the scales
+// of K and V enter with the scores' scale and with the final division.
+
+constexpr int kItemCost = 1;  // fixed cost of an item in tiles
+
+template <int DQK_, int DV_, bool FP8_, int NW_, int SLOTS_>
+struct FewCfg {
+  static constexpr int DQK = DQK_, DV = DV_, NW = NW_, SLOTS = SLOTS_;
+  static constexpr bool FP8 = FP8_;
+  static constexpr int E = FP8 ? 1 : 2;                         // bytes per element
+  static constexpr int KS = DQK / 16, DB = DV / 32;
+  static constexpr int KROW = DQK * E, VROW = DV * E;           // bytes per LDS row
+  static constexpr int KCH = KROW / 16, VCH = VROW / 16;        // 16-byte chunks per row
+  static constexpr int KL = KCH / 4, VL = VCH / 4;              // loads per 16-key half (16 rows / 64 lanes)
+  static constexpr int K_BYTES = 32 * KROW, V_BYTES = 32 * VROW, WSLOT = K_BYTES + V_BYTES;
+  static constexpr int RING = NW * SLOTS * WSLOT;
+  static constexpr int TILE = 32 * NW;                          // keys per tile
+  static constexpr int OROW = DV + 4;
+  static constexpr int O_BYTES = NW * 32 * OROW * 4;
+  static constexpr int JOIN_BYTES = O_BYTES + 2 * NW * 32 * 4;
+  static constexpr int LDS_BYTES = RING > JOIN_BYTES ? RING : JOIN_BYTES;
+  static constexpr int D = SLOTS - 1;                           // tiles loaded ahead
+  static constexpr int L = 2 * (KL + VL);                       // loads per tile
+  static_assert(LDS_BYTES <= 163840 && KCH % 4 == 0 && VCH % 4 == 0, "LDS budget, whole loads");
+  static_assert(2 * VL + D * L < 64, "vmcnt range");
+};
+
+// XOR swizzles of the 16-byte chunks of an 8-bit row, so that lanes served together hit different 16-byte
+// bank slots: K rows are read whole chunks at a time by 16 rows at once; V by 8 keys x two chunks.
+template <int CH>
+__device__ __forceinline__ int k8_swizzle(int row) { return CH % 8 == 0 ? (row >> 1) & 7 : (row >> 2) & 3; }
+template <int CH>
+__device__ __forceinline__ int v8_swizzle(int row) { return CH % 8 == 0 ? 2 * ((row >> 1) & 3) : 2 * ((row >> 2) & 1); }
+
+// Eight e4m3 (two registers) as bf16 or fp16, exactly.
+__device__ __forceinline__ bf16x8 widen_bf16(uint32_t a, uint32_t b) {
+  return bit_cast<bf16x8>(u32x4{bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false)),
+                                bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true)),
+                                bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false)),
+                                bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true))});
+}
+__device__ __forceinline__ f16x8 widen_f16(uint32_t a, uint32_t b) {
+  return bit_cast<f16x8>(u32x4{bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false)),
+                               bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true)),
+                               bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false)),
+                               bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true))});
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  f32x2 f = {lo, hi};
+  return bit_cast<uint32_t>(__builtin_convertvector(f, f16x2));  // RNE
+}
+
+__device__ __forceinline__ void load_q16(bf16x8& r, const void* ptr) {
+  asm volatile("global_load_dwordx4 %0, %1, off" : "=v"(r) : "v"(ptr) : "memory");
+}
+__device__ __forceinline__ void q_settled(bf16x8& r) { asm volatile("" : "+v"(r)); }
+
+// Units of sequence b on the line of work, and what they are made of.
+template <int TILE>
+struct SeqWork {
+  int tiles, n_cb;
+  int64_t units;
+  __device__ __forceinline__ SeqWork(const PagedSeq& s, int group, int hkv) {
+    tiles = (s.kv + TILE - 1) / TILE;
+    n_cb = (int)(((int64_t)s.n_q * group + 31) / 32);
+    units = (int64_t)n_cb * hkv * (tiles + kItemCost);
+  }
+};
+
+template <class C>
+__global__ __attribute__((amdgpu_flat_work_group_size(C::NW * 64, C::NW * 64)))
+void fa_paged_few_kernel(PagedParams p) {
+  constexpr int DQK = C::DQK, DV = C::DV, KS = C::KS, DB = C::DB, NW = C::NW, TILE = C::TILE, D = C::D;
+  constexpr bool FP8 = C::FP8;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS_BYTES];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i32 = lane & 31, h = lane >> 5;
+  const int me = blockIdx.x;
+
+  // The line's length, and the sequence that holds this workgroup's first unit (every wave for itself).
+  int64_t mine = 0;
+  for (int b = lane; b < p.bt.n_seq; b += 64)
+    mine += SeqWork<TILE>(load_seq_lane(p.bt, b), p.group, p.c.hkv).units;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o);
+  const int total = __builtin_amdgcn_readfirstlane((int)min(mine, (int64_t)INT32_MAX));
+  const int per = max(p.min_units, (int)(((int64_t)total + p.n_wg - 1) / p.n_wg));
+  if (tid == 0) p.desc[me].n_parts = 0;
+  const int64_t r0w = (int64_t)me * per;
+  if (r0w >= total) return;
+  const int r0 = (int)r0w, r1 = (int)min((int64_t)total, r0w + per);
+  int b = 0, start = 0;
+  for (int c = 0;; c += 64) {
+    const int bl = c + lane;
+    const int64_t u =
+        bl < p.bt.n_seq ? SeqWork<TILE>(load_seq_lane(p.bt, bl), p.group, p.c.hkv).units : 0;
+    int64_t incl = u;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t x = __shfl_up(incl, o);
+      if (lane >= o) incl += x;
+    }
+    const uint64_t above = __builtin_amdgcn_ballot_w64(start + incl > r0);
+    if (above != 0) {
+      const int l = __builtin_ctzll(above);
+      b = c + l;
+      start += __builtin_amdgcn_readlane((int)(incl - u), l);
+      break;
+    }
+    if (c + 64 >= p.bt.n_seq) return;  // not reached: r0 < total
+    start += __builtin_amdgcn_readlane((int)incl, 63);
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  start = __builtin_amdgcn_readfirstlane(start);
+
+  unsigned char* const ring = smem + wave * C::SLOTS * C::WSLOT;
+  const uint32_t ring_lds = __builtin_amdgcn_readfirstlane(lds_offset(ring));
+  // Source offsets of this lane in a 16-key half: load i brings 16-byte chunks 64 i .. 64 i + 63, chunk x of
+  // the half being chunk x % CH of its row x / CH, whose place holds logical chunk (x % CH) ^ swizzle(row).
+  // The swizzles repeat every 16 rows, so both halves have the same offsets.
+  uint32_t koff[C::KL], voff[C::VL];
+#pragma unroll
+  for (int i = 0; i < C::KL; ++i) {
+    const int x = i * 64 + lane, row = x / C::KCH;
+    const int sw = FP8 ? k8_swizzle<C::KCH>(row) : k_swizzle<DQK>(row);
+    koff[i] = (uint32_t)row * (uint32_t)(p.c.k_slot * C::E) + (uint32_t)((x % C::KCH) ^ sw) * 16u;
+  }
+#pragma unroll
+  for (int i = 0; i < C::VL; ++i) {
+    const int x = i * 64 + lane, row = x / C::VCH;
+    const int sw = FP8 ? v8_swizzle<C::VCH>(row) : v_swizzle<DV>(row);
+    voff[i] = (uint32_t)row * (uint32_t)(p.c.v_slot * C::E) + (uint32_t)((x % C::VCH) ^ sw) * 16u;
+  }
+  // Lane constants of the V transpose reads: the key of a 16-key step and the chunk this lane points at.
+  const int v_key = FP8 ? 8 * h + ((lane & 15) >> 1) : 8 * h + ((lane & 15) >> 2);
+  const int v_t = FP8 ? (((lane >> 4) & 1) ^ v8_swizzle<C::VCH>(v_key))
+                      : ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<DV>(v_key));
+  const int v_half = (lane & 1) * 8;
+
+  int r = r0;
+  while (r < r1) {
+    PagedSeq s = load_seq(p.bt, b);
+    SeqWork<TILE> sw(s, p.group, p.c.hkv);
+    while (sw.units == 0 || r >= start + sw.units) {
+      start += (int)sw.units;
+      if (++b >= p.bt.n_seq) return;  // not reached: r < total
+      s = load_seq(p.bt, b);
+      sw = SeqWork<TILE>(s, p.group, p.c.hkv);
+    }
+    const int cost = sw.tiles + kItemCost;
+    const int item = (r - start) / cost, item0 = start + item * cost;
+    const int g = item / sw.n_cb, cb = item % sw.n_cb;
+    const int end = min(r1, item0 + cost);
+    // Tiles of the item in this workgroup; the item belongs to the workgroups that have tiles of it (one without
+    // a tile to that of its first unit).
+    const int t0 = max(0, r - item0 - kItemCost), t1 = end - item0 - kItemCost;
+    const bool single = sw.tiles == 0;
+    r = end;
+    if (single ? item0 < r0 : t1 <= t0) continue;
+    const int first_wg = single ? me : (item0 + kItemCost) / per;
+    const int n_parts = single ? 1 : (item0 + cost - 1) / per - first_wg + 1;
+
+    // Column of this lane. Columns past the item's rows repeat the last and are never stored.
+    const int cols = s.n_q * p.group, c0 = cb * 32;
+    const int c = min(c0 + i32, cols - 1);
+    const int qi = c / p.group, member = c - qi * p.group;
+    const int last_key = p.causal ? s.kv - s.n_q + qi : s.kv - 1;
+    // Keys visible to the block's last row; tiles behind them are left out.
+    const int last_row = min(c0 + 31, cols - 1) / p.group;
+    const int k_end = p.causal ? max(0, s.kv - s.n_q + last_row + 1) : s.kv;
+    const int nt = max(0, min(t1, (k_end + TILE - 1) / TILE) - t0);
+
+    bf16x8 qf[KS];
+    {
+      const uint16_t* qp = p.q + (int64_t)(s.q0 + qi) * p.q_token + (int64_t)(g * p.group + member) * p.q_head;
+      // bf16: k-step ks holds dims 16 ks + 8 h .. + 7. e4m3: a lane reads 16 bytes of K at once, dims 32 m +
+      // 16 h .. + 15, which serve k-steps 2 m and 2 m + 1; Q takes the same order.
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        load_q16(qf[ks], qp + (FP8 ? 32 * (ks / 2) + 16 * h + 8 * (ks & 1) : 16 * ks + 8 * h));
+    }
+
+    const unsigned char* kbase = static_cast<const unsigned char*>(p.c.k) + (int64_t)g * p.c.k_head * C::E;
+    const unsigned char* vbase = static_cast<const unsigned char*>(p.c.v) + (int64_t)g * p.c.v_head * C::E;
+    const int* table = p.bt.block_table + (int64_t)b * p.bt.table_stride;
+    const int smask = (1 << p.c.page_shift) - 1;
+    // The pages of this wave's two halves of tile t (an index past the sequence's last page repeats that).
+    auto page_of = [&](int t, int u) {
+      const int key = min(t * TILE + 32 * wave + 16 * u, s.kv - 1);
+      return key < 0 ? -1 : scalar_load(table + (key >> p.c.page_shift));
+    };
+    // Buffer over the slots of a half that hold keys below k_end: none where the page is none of the cache's.
+    auto half_rsrc = [&](const unsigned char* base, int64_t page_str, int64_t slot_str, int page, int key0) {
+      const bool ok = page >= 0 && page < p.c.n_pages;
+      const int64_t at = ((int64_t)(ok ? page : 0) * page_str + (int64_t)(key0 & smask) * slot_str) * C::E;
+      const int rows = ok ? max(0, min(16, k_end - key0)) : 0;
+      const uint64_t a = reinterpret_cast<uint64_t>(base) + (uint64_t)at;
+      return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+                   (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu)),
+                   (uint32_t)__builtin_amdgcn_readfirstlane(rows * (int)(slot_str * C::E)), 0x00020000u};
+    };
+    auto issue = [&](int t, int pg0, int pg1) {
+      const uint32_t l = ring_lds + (uint32_t)((unsigned)t % C::SLOTS) * C::WSLOT;
+      const int key0 = t * TILE + 32 * wave;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const u32x4 rs = half_rsrc(kbase, p.c.k_page, p.c.k_slot, u ? pg1 : pg0, key0 + 16 * u);
+#pragma unroll
+        for (int i = 0; i < C::KL; ++i) dma16_buffer(rs, koff[i], l + (u * C::KL + i) * 1024);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const u32x4 rs = half_rsrc(vbase, p.c.v_page, p.c.v_slot, u ? pg1 : pg0, key0 + 16 * u);
+#pragma unroll
+        for (int i = 0; i < C::VL; ++i) dma16_buffer(rs, voff[i], l + C::K_BYTES + (u * C::VL + i) * 1024);
+      }
+    };
+    // Bits 2 k, 2 k + 1: whether the two halves of the k-th tile from the current one on have a page.
+    uint32_t valid = 0;
+    auto page_bits = [&](int pg0, int pg1) {
+      return (uint32_t)(pg0 >= 0 && pg0 < p.c.n_pages) | (uint32_t)(pg1 >= 0 && pg1 < p.c.n_pages) << 1;
+    };
+
+    const float cs = p.cs * (FP8 && p.c.k_scale != nullptr ? scalar_load(p.c.k_scale + g) : 1.f);
+    f32x16 oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
+    float m_run = -INFINITY, l_run = 0.f;
+    const int n0t = t0, n1t = t0 + nt;
+    // (Also without a tile: behind k_end nothing is read, and every path waits for Q the same way.)
+#pragma unroll
+    for (int k = 0; k < D; ++k) {
+      const int a = page_of(n0t + k, 0), z = page_of(n0t + k, 1);
+      issue(n0t + k, a, z);
+      valid |= page_bits(a, z) << (2 * k);
+    }
+    int pgn0 = page_of(n0t + D, 0), pgn1 = page_of(n0t + D, 1);
+    wait_vmcnt<D * C::L>();  // Q
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) q_settled(qf[ks]);
+
+    for (int t = n0t; t < n1t; ++t) {
+      compiler_fence();
+      issue(t + D, pgn0, pgn1);
+      valid |= page_bits(pgn0, pgn1) << (2 * D);
+      pgn0 = page_of(t + D + 1, 0), pgn1 = page_of(t + D + 1, 1);
+      compiler_fence();
+      wait_vmcnt<2 * C::VL + D * C::L>();  // K(t)
+      compiler_fence();
+      const unsigned char* sK = ring + ((unsigned)t % C::SLOTS) * C::WSLOT;
+      const unsigned char* sV = sK + C::K_BYTES;
+      const int n0 = t * TILE + 32 * wave;
+
+      // Scores: register r holds key n0 + 16 (r / 8) + 8 h + r % 8 of column i32.
+      f32x16 sc;
+      const unsigned char* krow = sK + perm32(i32) * C::KROW;
+      if constexpr (FP8) {
+        const int ksw = k8_swizzle<C::KCH>(perm32(i32) & 15);
+#pragma unroll
+        for (int m = 0; m < KS / 2; ++m) {
+          const u32x4 a = *reinterpret_cast<const u32x4*>(krow + (((2 * m + h) ^ ksw) << 4));
+          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen_bf16(a[0], a[1]), qf[2 * m], m == 0 ? f32x16{} : sc, 0, 0, 0);
+          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen_bf16(a[2], a[3]), qf[2 * m + 1], sc, 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 a = *reinterpret_cast<const u32x4*>(krow + (((2 * ks + h) ^ k_lane_swizzle<DQK>(i32)) << 4));
+          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bit_cast<bf16x8>(a), qf[ks], ks == 0 ? f32x16{} : sc, 0, 0, 0);
+        }
+      }
+      // Mask keys past the column's last visible key and those of halves without a page.
+      const int lim = last_key - n0 - 8 * h;
+      const int lim0 = (valid & 1u) ? lim : -1, lim1 = (valid & 2u) ? lim : -1;
+      valid >>= 2;
+      float mt = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = (16 * (e >> 3) + (e & 7)) > (e < 8 ? lim0 : lim1) ? -INFINITY : sc[e] * cs;
+        sc[e] = x;
+        mt = fmaxf(mt, x);
+      }
+      mt = half_swap_max(mt);
+      const float m_new = fmaxf(m_run, mt);
+      const float mref = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m_run - mref);  // 0 while nothing was visible
+      m_run = m_new;
+      float rs = 0.f;
+      uint32_t pk[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float e0 = __builtin_amdgcn_exp2f(sc[2 * e] - mref), e1 = __builtin_amdgcn_exp2f(sc[2 * e + 1] - mref);
+        rs += e0 + e1;
+        pk[e] = FP8 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
+      }
+      l_run = l_run * alpha + rs;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+      compiler_fence();
+      wait_vmcnt<D * C::L>();  // V(t)
+      compiler_fence();
+#pragma unroll
+      for (int ps = 0; ps < 2; ++ps) {
+        const u32x4 pw = {pk[4 * ps], pk[4 * ps + 1], pk[4 * ps + 2], pk[4 * ps + 3]};
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          if constexpr (FP8) {
+            const unsigned char* vb = sV + (16 * ps + v_key) * C::VROW + (((2 * db) ^ v_t) << 4) + v_half;
+            const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vb));
+            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen_f16(w.x, w.y), bit_cast<f16x8>(pw), oacc[db], 0, 0, 0);
+          } else {
+            const unsigned char* vb = sV + (16 * ps + v_key) * C::VROW + (((4 * db) ^ v_t) << 4) + v_half;
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vb));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vb + 4 * C::VROW));
+            const bf16x8 va = bit_cast<bf16x8>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, bit_cast<bf16x8>(pw), oacc[db], 0, 0, 0);
+          }
+        }
+      }
+    }
+
+    // Join the waves through LDS: no load may still be writing the ring, and every wave must be done with its
+    // last tile.
+    compiler_fence();
+    wait_vmcnt<0>();
+    compiler_fence();
+    __syncthreads();
+    float* ob = reinterpret_cast<float*>(smem);               // [wave][column][OROW]
+    float* mb = reinterpret_cast<float*>(smem + C::O_BYTES);  // [wave][column]
+    float* lb = mb + NW * 32;                                 // [wave][column]
+    const float l_tot = half_swap_sum(l_run);
+    if (h == 0) {
+      mb[wave * 32 + i32] = m_run;
+      lb[wave * 32 + i32] = l_tot;
+    }
+    float* orow = ob + (wave * 32 + i32) * C::OROW + 4 * h;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4)
+        *reinterpret_cast<f32x4*>(orow + 32 * db + 8 * g4) =
+            f32x4{oacc[db][4 * g4], oacc[db][4 * g4 + 1], oacc[db][4 * g4 + 2], oacc[db][4 * g4 + 3]};
+    __syncthreads();
+
+    constexpr int TPC = NW * 64 / 32;  // threads per column
+    static_assert(DV % (8 * TPC) == 0, "a thread finishes whole 16-byte chunks of the output");
+    const int col = tid / TPC, d0 = (tid % TPC) * (DV / TPC);
+    if (c0 + col < cols) {
+      float mw[NW], M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        mw[w] = mb[w * 32 + col];
+        M = fmaxf(M, mw[w]);
+      }
+      float wt[NW], Lsum = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        wt[w] = mw[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[w] - M);
+        Lsum += wt[w] * lb[w * 32 + col];
+      }
+      const bool some = Lsum > 0.f;  // else no visible key, or a score that is no number: O = 0, LSE = -inf
+      const float vs = FP8 && p.c.v_scale != nullptr ? scalar_load(p.c.v_scale + g) : 1.f;
+      const float inv = some ? vs / Lsum : 0.f;
+      const float lse = some ? (M + log2f(Lsum)) * kLn2 : -INFINITY;
+      f32x4 o[DV / TPC / 4];
+#pragma unroll
+      for (int d = 0; d < DV / TPC; d += 4) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+          acc += wt[w] * *reinterpret_cast<const f32x4*>(ob + (w * 32 + col) * C::OROW + d0 + d);
+        o[d / 4] = some ? acc * inv : f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      if (n_parts == 1) {
+        const int row = (c0 + col) / p.group, mem = (c0 + col) - row * p.group;
+        const int head = g * p.group + mem;
+        const int64_t tok = s.q0 + row;
+        uint16_t* dst = p.o + tok * p.o_token + (int64_t)head * p.o_head + d0;
+#pragma unroll
+        for (int d = 0; d < DV / TPC; d += 8) {
+          const f32x4 x = o[d / 4], y = o[d / 4 + 1];
+          *reinterpret_cast<u32x4*>(dst + d) =
+              u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+        }
+        if (tid % TPC == 0 && p.lse != nullptr) p.lse[tok * p.hq + head] = lse;
+      } else {
+        // Place 2 me: a part of an item that begins before; 2 me + 1: the first part of one.
+        const int64_t place = 2 * (int64_t)me + (me == first_wg ? 1 : 0);
+        float* dst = p.o_part + (place * p.part_cols + col) * DV + d0;
+#pragma unroll
+        for (int d = 0; d < DV / TPC; d += 4) *reinterpret_cast<f32x4*>(dst + d) = o[d / 4];
+        if (tid % TPC == 0) p.lse_part[place * p.part_cols + col] = lse;
+      }
+    }
+    if (n_parts > 1 && me == first_wg && tid == 0)
+      p.desc[me] = PagedItem{n_parts, s.q0, min(32, cols - c0), c0, g};
+    __syncthreads();  // the next item's loads overwrite the buffers above
+  }
+}
+
+// Join of the parts of the item that begins in workgroup `me` of the kernel above and goes on in the next ones
+// (none: n_parts 0): O = sum_k w_k O_k / sum_k w_k with w_k = exp(LSE_k - max LSE), added in the order of
+// the parts. DV / 4 threads per column, each with 4 output dims.
+template <int DV>
+__global__ __launch_bounds__(256) void fa_paged_join_kernel(PagedParams p) {
+  const PagedItem it = p.desc[blockIdx.x];
+  if (it.n_parts <= 1) return;
+  constexpr int TD = DV / 4, NG = 256 / TD;  // threads per column, columns at once
+  const int q = threadIdx.x % TD;
+  const int64_t first = 2 * (int64_t)blockIdx.x + 1;
+  for (int col = blockIdx.y * NG + threadIdx.x / TD; col < it.n_cols; col += gridDim.y * NG) {
+    auto place = [&](int k) { return (k == 0 ? first : first + 2 * k - 1) * p.part_cols + col; };
+    float M = -INFINITY;
+    for (int k = 0; k < it.n_parts; ++k) M = fmaxf(M, p.lse_part[place(k)]);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float den = 0.f;
+    if (M != -INFINITY)
+      for (int k = 0; k < it.n_parts; ++k) {
+        const float w = expf(p.lse_part[place(k)] - M);
+        den += w;
+        acc += w * *reinterpret_cast<const f32x4*>(p.o_part + place(k) * DV + 4 * q);
+      }
+    acc *= den > 0.f ? 1.f / den : 0.f;
+    const int c = it.c0 + col, row = c / p.group, head = it.g * p.group + c - row * p.group;
+    const int64_t tok = it.q0 + row;
+    *reinterpret_cast<u32x2*>(p.o + tok * p.o_token + (int64_t)head * p.o_head + 4 * q) =
+        u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
+    if (q == 0 && p.lse != nullptr) p.lse[tok * p.hq + head] = den > 0.f ? M + logf(den) : -INFINITY;
+  }
+}
+
+template <class C>
+hipError_t launch_few(PagedParams p, hipStream_t stream) {
+  void* args[] = {&p};
+  return hipLaunchKernel(reinterpret_cast<const void*>(&fa_paged_few_kernel<C>), dim3(p.n_wg), dim3(C::NW * 64), args, 0,
+                         stream);
+}
+
+}  // namespace
+
+hipError_t launch_append(AppendParams p, bool fp8, hipStream_t stream) {
+  void* args[] = {&p};
+  return hipLaunchKernel(fp8 ? reinterpret_cast<const void*>(&fa_append_kernel<true>)
+                             : reinterpret_cast<const void*>(&fa_append_kernel<false>),
+                         dim3(p.bt.n_tokens), dim3(kAppendThreads), args, 0, stream);
+}
+
+int paged_workgroups(int d_qk, bool fp8) { return d_qk == 64 || fp8 ? 512 : 256; }
+
+hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, hipStream_t stream) {
+  p.min_units = 4;
+  hipError_t e;
+  if (d_qk == 64)
+    e = fp8 ? launch_few<FewCfg<64, 64, true, 4, 4>>(p, stream) : launch_few<FewCfg<64, 64, false, 4, 2>>(p, stream);
+  else if (d_qk == 128)
+    e = fp8 ? launch_few<FewCfg<128, 128, true, 4, 2>>(p, stream) : launch_few<FewCfg<128, 128, false, 4, 2>>(p, stream);
+  else
+    e = fp8 ? launch_few<FewCfg<192, 128, true, 4, 2>>(p, stream) : launch_few<FewCfg<192, 128, false, 4, 2>>(p, stream);
+  if (e != hipSuccess) return e;
+  void* args[] = {&p};
+  return hipLaunchKernel(d_qk == 64 ? reinterpret_cast<const void*>(&fa_paged_join_kernel<64>)
+                                    : reinterpret_cast<const void*>(&fa_paged_join_kernel<128>),
+                         dim3(p.n_wg, 4), dim3(256), args, 0, stream);
+}
+
+}  // namespace fa

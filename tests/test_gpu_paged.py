@@ -1,0 +1,198 @@
+"""GPU tests of the attention over a paged cache (fa_fwd_paged) against float64, at the sizes and contents where it
+can go wrong. Unused slots of every cache hold NaN."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_21264_amd as fa
+from paged import Batch, f64
+
+pytestmark = pytest.mark.gpu
+
+DIMS = [(64, 64), (128, 128), (192, 128)]
+TYPES = [False, True]
+
+
+def run(bt, causal=True, scale=None, what="", **kw):
+    scale = 1.0 / math.sqrt(bt.dqk) if scale is None else scale
+    o, lse = bt.attend(causal=causal, scale=scale, return_lse=True, **kw)
+    bt.check(o, lse, scale, causal, what)
+    return o, lse
+
+
+@pytest.mark.parametrize("fp8", TYPES)
+@pytest.mark.parametrize("dqk,dv", DIMS)
+@pytest.mark.parametrize("keys", [[1], [15], [16], [17], [31, 32, 33], [127, 128, 129, 255], [640, 1, 1000]], ids=str)
+def test_one_token(keys, dqk, dv, fp8):
+    run(Batch([1] * len(keys), keys, 8, 2, dqk, dv, 16, fp8, seed=len(keys)))
+
+
+@pytest.mark.parametrize("fp8", TYPES)
+@pytest.mark.parametrize("dqk,dv", DIMS)
+@pytest.mark.parametrize("page", [16, 32, 64, 256])
+def test_long_sequences_are_split(page, dqk, dv, fp8):
+    # One sequence, one key/value head: its keys are split over many workgroups and joined.
+    run(Batch([1], [9001], 4, 1, dqk, dv, page, fp8, seed=page))
+    run(Batch([1, 2], [5003, 2049], 3, 3, dqk, dv, page, fp8, seed=page + 1))
+
+
+@pytest.mark.parametrize("fp8", TYPES)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dqk,dv", DIMS)
+def test_ragged_new_tokens(dqk, dv, causal, fp8):
+    # No new token, no key, more new tokens than keys (rows without a visible key), several column blocks.
+    run(Batch([3, 0, 1, 5, 2, 40, 0, 7], [700, 50, 0, 3, 2, 333, 0, 129], 14, 2, dqk, dv, 16, fp8, seed=5), causal=causal)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (5, 5), (48, 1), (33, 11), (64, 8)])
+def test_heads(Hq, Hkv):
+    run(Batch([1, 4, 9], [77, 300, 515], Hq, Hkv, 128, 128, 32, seed=Hq))
+
+
+@pytest.mark.parametrize("B", [63, 64, 65, 300])
+def test_many_sequences(B):
+    rng = np.random.RandomState(B)
+    new = rng.randint(0, 3, B).tolist()
+    keys = [n + int(x) for n, x in zip(new, rng.choice([0, 1, 40, 200, 600], B))]
+    run(Batch(new, keys, 4, 2, 64, 64, 16, seed=B))
+
+
+@pytest.mark.parametrize("max_q", [0, 1, 5, 1000])
+def test_max_q_is_a_hint(max_q):
+    run(Batch([5, 70, 1], [50, 333, 200], 8, 2, 128, 128, 16, seed=9), max_q=max_q)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-30, 2.0])
+def test_scales(scale):
+    run(Batch([1, 3], [200, 1500], 4, 2, 64, 64, 16, seed=3), scale=scale)
+
+
+@pytest.mark.parametrize("fp8", TYPES)
+def test_nhd_cache_and_strided_tensors(fp8):
+    bt = Batch([2, 1, 6], [300, 40, 1027], 8, 2, 128, 128, 16, fp8, seed=21, order="nhd")
+    qkv = torch.zeros(bt.T, bt.Hq + 2 * bt.Hkv, 128, dtype=torch.bfloat16, device="cuda")
+    qkv[:, : bt.Hq] = bt.d_q
+    bt.d_q = qkv[:, : bt.Hq]
+    out = torch.full((bt.Hq, bt.T, 136), 7.0, dtype=torch.bfloat16, device="cuda")
+    o, _ = run(bt, out=out[:, :, :128].transpose(0, 1))
+    assert o.data_ptr() == out.data_ptr() and torch.all(out[:, :, 128:] == 7)
+
+
+@pytest.mark.parametrize("fp8", TYPES)
+@pytest.mark.parametrize("causal", [True, False])
+def test_pages_that_are_not_there(causal, fp8):
+    bt = Batch([1, 3, 2], [200, 333, 40], 4, 2, 128, 128, 16, fp8, seed=31)
+    bt.table[0, 3], bt.table[0, 12] = -1, bt.n_pages        # the second holds the last keys
+    bt.table[1, 0:4], bt.table[1, 20] = 2 ** 31 - 1, -2 ** 31
+    bt.table[2, :] = -1                                     # no key at all
+    bt.d_table = bt.table.cuda()
+    run(bt, causal=causal)
+
+
+def test_lengths_are_clamped_to_the_table():
+    bt = Batch([1, 2], [64, 32], 4, 2, 64, 64, 16, seed=33)
+    bt.d_kv_lens = torch.tensor([2 ** 31 - 1, -5], dtype=torch.int32, device="cuda")
+    bt.kv_lens = torch.tensor([64, 0], dtype=torch.int32)
+    run(bt)
+
+
+@pytest.mark.parametrize("max_q", [1, 300])
+def test_rows_of_no_sequence_are_left(max_q):
+    bt = Batch([2, 3], [40, 600], 4, 2, 128, 128, 16, seed=35, extra=4)
+    bt.q_starts = torch.tensor([1, 2, 5], dtype=torch.int32)   # the first token belongs to none either
+    bt.d_q_starts = bt.q_starts.cuda()
+    bt.new = [1, 3]
+    out = torch.full((bt.T, 4, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((bt.T, 4), 5.0, device="cuda")
+    run(bt, out=out, lse=lse, max_q=max_q)
+    rest = [0, *range(5, bt.T)]
+    assert torch.all(out[rest] == 3) and torch.all(lse[rest] == 5)
+
+
+def test_no_tokens_and_no_sequences():
+    bt = Batch([0, 0], [5, 0], 4, 2, 64, 64, 16, seed=37)
+    o, lse = bt.attend(return_lse=True)
+    assert o.shape == (0, 4, 64) and lse.shape == (0, 4)
+
+
+def test_results_do_not_change_between_runs():
+    bt = Batch([1] * 20, [37 * i + 1 for i in range(20)], 8, 2, 128, 128, 16, seed=39)
+    first = bt.attend(return_lse=True)
+    for _ in range(3):
+        again = bt.attend(return_lse=True)
+        assert torch.equal(first[0].view(torch.int16), again[0].view(torch.int16)) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("max_q", [1, 64])
+def test_captured_call_serves_other_lengths(max_q):
+    bt = Batch([1, 1, 1], [900, 40, 300], 8, 2, 128, 128, 16, seed=41)
+    ws = torch.empty(fa.fa_fwd_paged_workspace_bytes(3, 8, 2, 128, 128), dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty(3, 8, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(3, 8, device="cuda")
+    bt.attend(out=out, lse=lse, return_lse=True, workspace=ws, max_q=max_q)  # first call outside the capture
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bt.attend(out=out, lse=lse, return_lse=True, workspace=ws, max_q=max_q)
+    for keys, starts in (([900, 40, 300], [0, 1, 2, 3]), ([17, 1, 299], [0, 1, 2, 3]), ([900, 40, 300], [0, 2, 2, 3]),
+                         ([0, 0, 1], [0, 1, 1, 1])):
+        bt.kv_lens, bt.q_starts = torch.tensor(keys, dtype=torch.int32), torch.tensor(starts, dtype=torch.int32)
+        bt.d_kv_lens.copy_(bt.kv_lens)
+        bt.d_q_starts.copy_(bt.q_starts)
+        out.fill_(float("nan"))
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        n = starts[-1]
+        eager = bt.attend(return_lse=True, max_q=max_q)
+        assert torch.equal(out[:n].view(torch.int16), eager[0][:n].view(torch.int16)), keys
+        assert torch.equal(lse[:n], eager[1][:n])
+        bt.check(out, lse, 128 ** -0.5, True, str(keys))
+
+
+def test_two_streams():
+    a = Batch([1, 1], [4000, 700], 8, 2, 128, 128, 16, seed=43)
+    b = Batch([2], [3000], 8, 2, 64, 64, 16, seed=44)
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        got.append((a, a.attend(return_lse=True, stream=sa)))
+        got.append((b, b.attend(return_lse=True, stream=sb.cuda_stream)))
+    torch.cuda.synchronize()
+    for bt, (o, lse) in got:
+        bt.check(o, lse, bt.dqk ** -0.5, True)
+
+
+def test_not_finite_values_stay_in_their_rows():
+    """A NaN in a key, or an infinity, reaches the rows that see it and no others; a row whose sum is no number has
+    O = 0 and LSE = -inf."""
+    bt = Batch([1, 1, 1], [100, 100, 3000], 4, 2, 128, 128, 16, seed=45)
+    clean, _ = run(bt)
+    kc = bt.d_k_cache
+    kc[int(bt.table[0, 1]), 0, 3, 5] = float("nan")
+    kc[int(bt.table[2, 100]), 1, 0, 0] = float("inf")
+    o, lse = bt.attend(return_lse=True)
+    torch.cuda.synchronize()
+    assert torch.equal(o[0, 2:], clean[0, 2:]) and torch.equal(o[1], clean[1]) and torch.equal(o[2, :2], clean[2, :2])
+    assert torch.all(o[0, :2] == 0) and torch.all(torch.isneginf(lse[0, :2]))
+
+
+def test_offsets_past_32_bits():
+    """A cache of 4.5 GiB per buffer, its last pages in use."""
+    pages, page = 73728, 64
+    kc = torch.zeros(pages, 4, page, 128, dtype=torch.bfloat16, device="cuda")
+    vc = torch.zeros_like(kc)
+    assert kc.numel() * 2 > 2 ** 32
+    bt = Batch([1, 2], [300, 130], 8, 4, 128, 128, page, seed=47)
+    where = torch.arange(pages - bt.n_pages, pages, device="cuda")
+    kc[where], vc[where] = bt.d_k_cache, bt.d_v_cache
+    bt.d_k_cache, bt.d_v_cache = kc, vc
+    bt.d_table = torch.where(bt.d_table >= 0, bt.d_table + (pages - bt.n_pages), bt.d_table)
+    run(bt)
+    k, v = torch.randn(3, 4, 128, device="cuda").bfloat16(), torch.randn(3, 4, 128, device="cuda").bfloat16()
+    fa.kv_append(k, v, kc, vc, bt.d_table, bt.d_kv_lens, bt.d_q_starts)
+    got = kc[int(bt.d_table[0, 299 // page]), :, 299 % page]
+    assert torch.equal(got, k[0]) and np.isfinite(f64(vc[where[-1]])).any()
