@@ -362,7 +362,8 @@ fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
  *   max_q       the most new tokens of one sequence, as far as the host knows: it chooses the kernels, the results
  *               are right for any
  *   workspace   16-byte aligned, at least fa_fwd_paged_workspace_bytes(...) bytes, overwritten; nothing needs to be in
- *               it before, and it must not be used elsewhere until the call's work has completed
+ *               it before, and it must not be used elsewhere until the call's work has completed. NULL only when no
+ *               byte is needed.
  * The work is cut on the device by the lengths found there, so one captured call serves whatever lengths the arrays
  * hold at a replay.
  *
@@ -376,9 +377,9 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
                          int Hq, const long long* strides, int max_q, float scale, int causal, void* workspace,
                          size_t workspace_bytes, hipStream_t stream);
 
-/* Workspace bytes of fa_fwd_paged: it does not depend on the lengths. Host arithmetic only; 0 for sizes <= 0, Hq not a
- * multiple of Hkv, or an unsupported type or head dimension. */
-size_t fa_fwd_paged_workspace_bytes(int T, int Hq, int Hkv, int d_qk, int d_v, int type);
+/* Workspace bytes of a fa_fwd_paged call with these sizes and this max_q (it does not depend on the lengths; 0 is possible).
+ * Host arithmetic only; 0 for sizes <= 0, max_q < 0, Hq not a multiple of Hkv, or an unsupported type or head dimension. */
+size_t fa_fwd_paged_workspace_bytes(int B, int T, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q);
 
 /* Static, human-readable name of a status code ("FA_OK", ...); "unknown status" otherwise. */
 const char* fa_status_str(fa_status_t s);

@@ -302,21 +302,44 @@ bool token_strides(const long long* s, int n) {
     if (s[i] < 0 || (s[i] & 7) != 0 || s[i] > (1ll << 40)) return false;
   return true;
 }
-// Columns and bytes of the workspace of fa_fwd_paged (sizes checked); the three arrays in it are 16-byte aligned.
-struct PagedWorkspace {
-  int n_wg, cols;
-  int64_t o, lse, bytes;
+// What a call of fa_fwd_paged runs, and its workspace (sizes checked). Sequences with more than kFewCols row-heads per
+// key/value head go to the kernel for many rows, if the host expects any; where it expects no others, all do.
+constexpr int kFewCols = 64;
+struct PagedPlan {
+  bool few, many, split;  // kernels to launch; whether that for many rows splits blocks
+  int few_cols, n_wg, cols, many_wg;
+  int64_t lse, desc, many_o, many_lse, many_desc, bytes;  // 16-byte aligned offsets
 };
-PagedWorkspace paged_workspace(int T, int group, int d_qk, int d_v, int type) {
-  PagedWorkspace w;
-  w.n_wg = fa::paged_workgroups(d_qk, type == FA_CACHE_E4M3);
+PagedPlan paged_plan(int B, int T, int Hkv, int group, int d_qk, int d_v, int type, int max_q) {
+  PagedPlan w{};
   const int64_t rows = static_cast<int64_t>(T) * group;
-  w.cols = rows < 32 ? static_cast<int>(rows) : 32;
-  const int64_t places = 2ll * w.n_wg * w.cols;
-  w.o = 0;
-  w.lse = places * d_v * 4;
-  w.bytes = w.lse + (places * 4 + 15) / 16 * 16;
-  w.bytes += static_cast<int64_t>(w.n_wg) * sizeof(fa::PagedItem);
+  w.many = type == FA_CACHE_BF16 && static_cast<int64_t>(max_q) * group > kFewCols && rows > kFewCols;
+  w.few = !w.many || static_cast<int64_t>(max_q) * B != T;
+  w.few_cols = !w.many ? INT_MAX : w.few ? kFewCols : 0;
+  if (w.many) {
+    int64_t blocks = 0;
+    w.split = fa::paged_many_split(B, T, Hkv, group, w.few_cols, d_qk, &blocks);
+  }
+  auto place = [&](int64_t n) {
+    const int64_t at = w.bytes;
+    w.bytes += (n + 15) / 16 * 16;
+    return at;
+  };
+  if (w.few) {
+    w.n_wg = fa::paged_workgroups(d_qk, type == FA_CACHE_E4M3);
+    w.cols = rows < 32 ? static_cast<int>(rows) : 32;
+    const int64_t places = 2ll * w.n_wg * w.cols;
+    place(places * d_v * 4);
+    w.lse = place(places * 4);
+    w.desc = place(w.n_wg * static_cast<int64_t>(sizeof(fa::PagedItem)));
+  }
+  if (w.split) {
+    w.many_wg = fa::paged_many_workgroups(d_qk);
+    const int64_t places = 2ll * w.many_wg * fa::paged_block_cols();
+    w.many_o = place(places * d_v * 4);
+    w.many_lse = place(places * 4);
+    w.many_desc = place(w.many_wg * static_cast<int64_t>(sizeof(fa::PagedItem)));
+  }
   return w;
 }
 
@@ -360,11 +383,11 @@ fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   return fa::launch_append(p, cache->type == FA_CACHE_E4M3, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 
-size_t fa_fwd_paged_workspace_bytes(int T, int Hq, int Hkv, int d_qk, int d_v, int type) {
-  if (T <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || !dims_supported(d_qk, d_v) ||
+size_t fa_fwd_paged_workspace_bytes(int B, int T, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q) {
+  if (B <= 0 || T <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_q < 0 || !dims_supported(d_qk, d_v) ||
       (type != FA_CACHE_BF16 && type != FA_CACHE_E4M3))
     return 0;
-  return static_cast<size_t>(paged_workspace(T, Hq / Hkv, d_qk, d_v, type).bytes);
+  return static_cast<size_t>(paged_plan(B, T, Hkv, Hq / Hkv, d_qk, d_v, type, max_q).bytes);
 }
 
 fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* Q, void* O, float* LSE,
@@ -391,8 +414,8 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
     return FA_ERR_UNSUPPORTED;
   st = check_paged_strides(cache, false);
   if (st != FA_OK) return st;
-  const PagedWorkspace w = paged_workspace(batch->T, Hq / cache->Hkv, cache->d_qk, cache->d_v, cache->type);
-  if (workspace == nullptr || workspace_bytes < static_cast<size_t>(w.bytes)) return FA_ERR_WORKSPACE;
+  const PagedPlan w = paged_plan(batch->B, batch->T, cache->Hkv, Hq / cache->Hkv, cache->d_qk, cache->d_v, cache->type, max_q);
+  if (w.bytes > 0 && (workspace == nullptr || workspace_bytes < static_cast<size_t>(w.bytes))) return FA_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return FA_ERR_UNSUPPORTED;
 
   fa::PagedParams p{};
@@ -404,14 +427,25 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   p.hq = Hq;
   p.group = Hq / cache->Hkv;
   p.causal = causal != 0;
-  p.cs = static_cast<float>(c);
+  const float cmag = fabs(c) < FLT_MIN ? FLT_MIN : static_cast<float>(fabs(c));  // a masked score stays infinite
+  p.cs = c < 0 ? -cmag : cmag;
+  p.few_cols = w.few_cols;
   p.n_wg = w.n_wg;
   p.part_cols = w.cols;
+  p.many_wg = w.many_wg;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
-  p.o_part = reinterpret_cast<float*>(ws + w.o);
+  p.o_part = reinterpret_cast<float*>(ws);
   p.lse_part = reinterpret_cast<float*>(ws + w.lse);
-  p.desc = reinterpret_cast<fa::PagedItem*>(ws + w.bytes - static_cast<int64_t>(w.n_wg) * sizeof(fa::PagedItem));
-  return fa::launch_paged_few(p, cache->d_qk, cache->type == FA_CACHE_E4M3, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
+  p.desc = reinterpret_cast<fa::PagedItem*>(ws + w.desc);
+  p.many_o = reinterpret_cast<float*>(ws + w.many_o);
+  p.many_lse = reinterpret_cast<float*>(ws + w.many_lse);
+  p.many_desc = reinterpret_cast<fa::PagedItem*>(ws + w.many_desc);
+  hipError_t e = hipSuccess;
+  if (w.many) e = fa::launch_paged_many(p, cache->d_qk, stream);
+  if (e == hipSuccess && w.few) e = fa::launch_paged_few(p, cache->d_qk, cache->type == FA_CACHE_E4M3, stream);
+  if (e == hipSuccess && w.few) e = fa::launch_paged_join(p, cache->d_v, false, stream);
+  if (e == hipSuccess && w.split) e = fa::launch_paged_join(p, cache->d_v, true, stream);
+  return e == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 
 fa_status_t fa_fwd_ex(const void* Q, const void* K, const void* V, void* O, float* LSE, int B, int Hq, int Hkv,

@@ -113,7 +113,7 @@ struct Ring {
 // K and V fragments read ahead from LDS (KPF, VPF), K and V ring slots in LDS (NKR, NVR), and the
 // parts each key tile is split into between the waves (KSPLIT).
 template <int DQK_, int DV_, int BN_, int NWAVES_, int QB_, bool CAUSAL_, bool SPLIT_, int OCC_, int KPF_, int VPF_,
-          int NKR_, int NVR_, int KSPLIT_ = 1>
+          int NKR_, int NVR_, int KSPLIT_ = 1, bool PAGED_ = false>
 struct Cfg {
   static constexpr int DQK = DQK_, DV = DV_, BN = BN_, NWAVES = NWAVES_, QB = QB_;
   // KSPLIT = 2: the waves form two sets of NWAVES / 2 (RWAVES) that own the same query rows; set k
@@ -126,6 +126,9 @@ struct Cfg {
   // SPLIT: each workgroup takes one of n_split contiguous parts of its query block's key tiles and
   // writes a partial result (O normalised by its own row sum, fp32, and its LSE) for a merge pass.
   static constexpr bool SPLIT = SPLIT_;
+  // PAGED: the keys lie in pages (PagedKeys below), the columns of a wave are any rows of any of the group's heads,
+  // and the last key each of them sees is in a register.
+  static constexpr bool PAGED = PAGED_;
   static constexpr bool CHUNKED = QB > 1;  // long instance: key/value heads in chunks (launch_cfg)
   static constexpr int NT = NWAVES * 64;
   // Waves per SIMD the registers are budgeted for: the workgroup's own (4 SIMDs per CU) times the
@@ -183,6 +186,22 @@ __device__ __forceinline__ uint32_t fast_div(uint32_t n, uint32_t m, uint32_t sh
   return (t + ((n - t) >> (sh & 1u))) >> (sh >> 1);
 }
 
+// What the step needs to know of a paged sequence (nothing otherwise): the last key that each of the lane's
+// columns sees, the pages, and whether some page that it visits is not there (its keys are masked then).
+template <bool PAGED, int QB>
+struct PagedKeys {};
+template <int QB>
+struct PagedKeys<true, QB> {
+  int last_key[QB];
+  const int* table;
+  int64_t page_stride, slot_stride;
+  int page_shift, n_pages;
+  bool holes;
+  __device__ __forceinline__ int page_of(int key) const {
+    return *(const __attribute__((address_space(4))) int*)(uintptr_t)(table + (key >> page_shift));
+  }
+};
+
 // Per-wave state and the math of the pipelined step.
 //
 // Reference maximum (the lazy form of Alg. 1's running maximum): the first tile sets m_run to the
@@ -193,7 +212,7 @@ __device__ __forceinline__ uint32_t fast_div(uint32_t n, uint32_t m, uint32_t sh
 // O / l is invariant under the choice of reference, and l >= 1 since the reference is always a
 // score that has been seen.
 template <class C>
-struct Attn {
+struct Attn : PagedKeys<C::PAGED, C::QB> {
   static constexpr int DQK = C::DQK, DV = C::DV, BN = C::WBN, QB = C::QB;  // BN: this wave's keys of a tile
   static constexpr int KS = DQK / 16;  // k-steps of the score product
   static constexpr int KB = BN / 32;   // 32-key blocks per tile
@@ -264,8 +283,13 @@ struct Attn {
     const uint32_t mv = __float_as_uint(mask_val);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      const int row = qw + qb * 32 + i32;
-      const int last_key = C::CAUSAL ? min(row + diag, sk - 1) : sk - 1;
+      int last_key;
+      if constexpr (C::PAGED) {
+        last_key = this->last_key[qb];
+      } else {
+        const int row = qw + qb * 32 + i32;
+        last_key = C::CAUSAL ? min(row + diag, sk - 1) : sk - 1;
+      }
       const int lim = last_key - n0 - 8 * h;  // key offset kb*32 + 16*(r/8) + r%8 is masked iff > lim
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -273,6 +297,23 @@ struct Attn {
         for (int r = 0; r < 16; ++r) {
           const uint32_t m = (uint32_t)((lim - (kb * 32 + 16 * (r >> 3) + (r & 7))) >> 31);  // all ones if masked
           s[kb][qb][r] = __uint_as_float((__float_as_uint(s[kb][qb][r]) & ~m) | (mv & m));
+        }
+    }
+    if constexpr (C::PAGED) {
+      if (!this->holes) return;
+      // Registers 8 u .. 8 u + 7 of block kb hold keys of one page.
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int key = n0 + kb * 32 + 16 * u;
+          const int page = key < sk ? this->page_of(key) : 0;
+          const uint32_t m = page < 0 || page >= this->n_pages ? ~0u : 0u;
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int r = 8 * u; r < 8 * u + 8; ++r)
+              s[kb][qb][r] = __uint_as_float((__float_as_uint(s[kb][qb][r]) & ~m) | (mv & m));
         }
     }
   }
@@ -362,10 +403,19 @@ struct Attn {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       const int row = min(n0 + kb * 32 + perm32(i32), sk - 1);
-      const uint16_t* krow = kg + (size_t)row * DQK + 8 * h;
+      const uint16_t* krow;
+      bool there = true;
+      if constexpr (C::PAGED) {
+        const int page = this->table[row >> this->page_shift];
+        there = page >= 0 && page < this->n_pages;
+        krow = kg + page * this->page_stride + (row & ((1 << this->page_shift) - 1)) * this->slot_stride + 8 * h;
+      } else {
+        krow = kg + (size_t)row * DQK + 8 * h;
+      }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(krow + 16 * ks);
+        u32x4 a = {0u, 0u, 0u, 0u};
+        if (!C::PAGED || there) a = *reinterpret_cast<const u32x4*>(krow + 16 * ks);
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
           cur[kb][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bit_cast<bf16x8>(a), qf[qb][ks],
@@ -450,6 +500,12 @@ struct Attn {
     bool over = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) over = over || !(rs[qb] <= kOverflowSum);
+    // Without pages that are not there a row that sees any key of its range sees the first, so it has a reference from
+    // tile 0 on; with them it takes one as soon as a tile has a key for it.
+    if constexpr (C::PAGED) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) over = over || (this->holes && m_run[qb] == -INFINITY);
+    }
     if (__builtin_amdgcn_ballot_w64(over) != 0) rebase(pk_new, rs, n0, masked);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) l_run[qb] += rs[qb];

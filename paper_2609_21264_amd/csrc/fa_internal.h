@@ -194,12 +194,29 @@ struct PagedParams {
   float* o_part;         // fp32 [2 * n_wg][part_cols][d_v]
   float* lse_part;       // fp32 [2 * n_wg][part_cols]
   PagedItem* desc;       // [n_wg]
+  // Sequences with more than few_cols row-heads per key/value head run in the kernel for many rows, which has work
+  // units, places and items of its own (the latter three only where it splits blocks).
+  int few_cols;
+  int many_wg, many_min_units;
+  float* many_o;         // fp32 [2 * many_wg][paged_block_cols()][d_v]
+  float* many_lse;       // fp32 [2 * many_wg][paged_block_cols()]
+  PagedItem* many_desc;  // [many_wg]
+  uint32_t m_group, sh_group;  // division by group, filled by launch_paged_many
 };
 
 hipError_t launch_append(AppendParams p, bool fp8, hipStream_t stream);
 // Workgroups of the attention kernel (as many as the chip holds at once).
 int paged_workgroups(int d_qk, bool fp8);
-// Attention and join, on `stream`; (d_qk, d_v) as for the other paths.
+// The kernels below run on `stream`; (d_qk, d_v) as for the other paths. Few rows: every sequence with at most few_cols
+// row-heads per key/value head.
 hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, hipStream_t stream);
+// Joins of split items: of the kernel for few rows, or for many.
+hipError_t launch_paged_join(PagedParams p, int d_v, bool many, hipStream_t stream);
+// Many rows (fa_paged_fwd_kernel.hip; bf16 caches): all other sequences. paged_many_split: whether it splits blocks (and
+// needs a join), and the most blocks per key/value head that there can be.
+int paged_many_workgroups(int d_qk);
+int paged_block_cols();
+bool paged_many_split(int n_seq, int n_tokens, int hkv, int group, int few_cols, int d_qk, int64_t* blocks);
+hipError_t launch_paged_many(PagedParams p, int d_qk, hipStream_t stream);
 
 }  // namespace fa

@@ -1,0 +1,540 @@
+// Attention of many new tokens per sequence over a paged key/value cache (gfx950): prompts and chunks of them.
+// The pipelined step of the fused forward (fa_fwd_attn.h) with another source of keys and another arrangement of
+// rows and work:
+//  * A block is 256 consecutive row-heads of one (sequence, key/value head): column c of the block's item is
+//    token c / group of the sequence's new ones and query head c % group of the group, so all heads of a group share
+//    every K/V tile whatever the group's size, and a short chunk pads at most once. Each lane keeps the
+//    last key its columns see; the mask is the same with and without causal masking.
+//  * A wave brings BN / 4 (16 or 8) consecutive keys of a tile, which lie in one page (pages have 16 slots at
+//    least): the page's number makes the buffer descriptor, one per wave and tile. A register holds the page numbers
+//    of the wave's next 64 tiles, one per lane; a step reads its own with a lane read, so no step waits for the table.
+//  * Pages that are not there are rare: each item looks for one first, and only then masks every tile by pages.
+//  * Where there are blocks enough, a workgroup takes one block, a sequence's last (longest) blocks first.
+//    Otherwise (SPLIT) the blocks lie on one line of work, kBlockCost + tiles units each, that the workgroups share
+//    evenly; parts of a block that several share are joined as those of the kernel for few rows are.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "fa_device.h"
+#include "fa_fwd_attn.h"
+#include "fa_internal.h"
+#include "fa_paged_device.h"
+
+namespace fa {
+namespace {
+
+constexpr int kBlockCols = 256;  // row-heads per block: 4 waves x 64
+constexpr int kBlockCost = 4;    // fixed cost of a block in tiles
+
+// This wave's share of the loads of one K or V tile: BN / NWAVES rows, all in one page.
+template <int NWAVES, int BN, int CH>
+struct PagedLoader {
+  static constexpr int R = BN / NWAVES, NI = BN * CH / 64 / NWAVES;
+  static_assert(R * CH == NI * 64 && R <= 16 && 16 % R == 0, "a wave's rows are whole loads inside one page");
+  uint64_t base;        // head, in page 0
+  int64_t page_bytes;
+  uint32_t slot_bytes;
+  uint32_t voff[NI];    // bytes from the wave's first row
+  template <class Swz>
+  __device__ __forceinline__ void init(const uint16_t* head, int64_t page_stride, int64_t slot_stride, int wave, int lane,
+                                       Swz swz) {
+    base = reinterpret_cast<uint64_t>(head);
+    page_bytes = page_stride * 2;
+    slot_bytes = (uint32_t)(slot_stride * 2);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int x = i * 64 + lane, row = x / CH;
+      voff[i] = (uint32_t)row * slot_bytes + (uint32_t)((x % CH) ^ swz(wave * R + row)) * 16u;
+    }
+  }
+  // Buffer of the rows from key `key` on that lie before `lim`, in page `page`: none if that is none of the cache's.
+  __device__ __forceinline__ u32x4 rsrc(int page, int n_pages, int key, int smask, int lim) const {
+    const bool ok = page >= 0 && page < n_pages;
+    const uint64_t a = base + (uint64_t)((int64_t)(ok ? page : 0) * page_bytes + (int64_t)(key & smask) * slot_bytes);
+    const int rows = ok ? max(0, min(R, lim - key)) : 0;
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu)),
+                 (uint32_t)__builtin_amdgcn_readfirstlane(rows * (int)slot_bytes), 0x00020000u};
+  }
+  __device__ __forceinline__ void issue_one(const u32x4& r, uint32_t l, int i) const {
+    dma16_buffer(r, voff[i], l + i * 1024);
+  }
+  __device__ __forceinline__ void issue(const u32x4& r, uint32_t l) const {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) issue_one(r, l, i);
+  }
+};
+
+// A block's place: which keys its columns see.
+template <int BN>
+struct Block {
+  int cols, c0, row0, row1;  // row-heads of the item, the block's first, its first and last row
+  int kv_end, plain;         // keys visible to its last row; leading tiles that need no mask for any row
+  __device__ __forceinline__ Block(const PagedSeq& s, int cb, const PagedParams& p) {
+    cols = s.n_q * p.group;
+    c0 = cb * kBlockCols;
+    row0 = (int)fast_div((uint32_t)c0, p.m_group, p.sh_group);
+    row1 = (int)fast_div((uint32_t)min(c0 + kBlockCols, cols) - 1u, p.m_group, p.sh_group);
+    kv_end = p.causal ? max(0, s.kv - s.n_q + row1 + 1) : s.kv;
+    plain = (p.causal ? max(0, s.kv - s.n_q + row0 + 1) : s.kv) / BN;
+  }
+  __device__ __forceinline__ int tiles() const { return (kv_end + BN - 1) / BN; }
+};
+__device__ __forceinline__ int n_blocks(const PagedSeq& s, const PagedParams& p) {
+  const int64_t cols = (int64_t)s.n_q * p.group;
+  return cols > p.few_cols ? (int)((cols + kBlockCols - 1) / kBlockCols) : 0;
+}
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+  return __builtin_amdgcn_readfirstlane(x);
+}
+// Inclusive prefix sum over the wave.
+__device__ __forceinline__ int wave_scan(int x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+template <int BN>
+__device__ __forceinline__ int head_units(const PagedSeq& s, int n_cb, const PagedParams& p, int lane) {
+  int sum = 0;
+  for (int c = lane; c < n_cb; c += 64) sum += kBlockCost + Block<BN>(s, c, p).tiles();
+  return wave_sum(sum);
+}
+__device__ __forceinline__ PagedSeq seq_of_lane(const PagedSeq& s, int l) {
+  return PagedSeq{__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.q_end, l),
+                  __builtin_amdgcn_readlane(s.n_q, l), __builtin_amdgcn_readlane(s.kv, l)};
+}
+
+template <class C>
+__global__ __attribute__((amdgpu_flat_work_group_size(C::NT, C::NT), amdgpu_waves_per_eu(C::WPE, C::WPE)))
+void fa_paged_fwd_kernel(PagedParams p) {
+  using A = Attn<C>;
+  constexpr int DQK = C::DQK, DV = C::DV, BN = C::BN, QB = C::QB;
+  static_assert(C::KA == C::VA && C::KSPLIT == 1 && C::NWAVES == 4 && 32 * QB * 4 == kBlockCols, "one page lookup per tile");
+  constexpr int R = BN / C::NWAVES;  // keys that a wave brings of a tile
+
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS_BYTES];
+  const int tid = threadIdx.x;
+  int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  A st;
+  st.qw = st.diag = 0;
+  st.cs = p.cs;
+  st.mask_val = p.cs < 0.f ? INFINITY : -INFINITY;
+  st.page_stride = p.c.k_page;
+  st.slot_stride = p.c.k_slot;
+  st.page_shift = p.c.page_shift;
+  st.n_pages = p.c.n_pages;
+  const int smask = (1 << p.c.page_shift) - 1;
+
+  // ---- this workgroup's work ----
+  // SPLIT: units [r, r1) of the line; consecutive workgroups run on different XCDs, so the line is dealt to the XCDs
+  // in eighths, and what shares a key/value head mostly shares an L2.
+  const int me = C::SPLIT ? (int)(blockIdx.x % kNumXcd) * (p.many_wg / kNumXcd) + (int)(blockIdx.x / kNumXcd) : 0;
+  int b = 0, g = 0, cb = 0, n_cb = 0, start = 0, r = 0, r1 = 0, per = 1;
+  PagedSeq s{};
+  if constexpr (C::SPLIT) {
+    int64_t sum = 0;
+    for (int c = 0; c < p.bt.n_seq; c += 64) {
+      PagedSeq sl{};
+      if (c + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, c + lane);
+      uint64_t left = __builtin_amdgcn_ballot_w64(n_blocks(sl, p) > 0);
+      while (left != 0) {
+        const PagedSeq x = seq_of_lane(sl, __builtin_ctzll(left));
+        left &= left - 1;
+        sum += (int64_t)head_units<BN>(x, n_blocks(x, p), p, lane) * p.c.hkv;
+      }
+    }
+    const int total = (int)min(sum, (int64_t)INT32_MAX);
+    per = max(p.many_min_units, (int)(((int64_t)total + p.many_wg - 1) / p.many_wg));
+    if (tid == 0) p.many_desc[me].n_parts = 0;
+    if ((int64_t)me * per >= total) return;
+    r = me * per;
+    r1 = (int)min((int64_t)total, (int64_t)r + per);
+    // The sequence, head and block that hold unit r.
+    bool found = false;
+    for (int c = 0; c < p.bt.n_seq && !found; c += 64) {
+      PagedSeq sl{};
+      if (c + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, c + lane);
+      uint64_t left = __builtin_amdgcn_ballot_w64(n_blocks(sl, p) > 0);
+      while (left != 0 && !found) {
+        const int l = __builtin_ctzll(left);
+        left &= left - 1;
+        s = seq_of_lane(sl, l);
+        n_cb = n_blocks(s, p);
+        const int units = head_units<BN>(s, n_cb, p, lane);
+        if ((int64_t)r < start + (int64_t)units * p.c.hkv) {
+          b = c + l;
+          g = (r - start) / units;
+          start += g * units;
+          found = true;
+        } else {
+          start += units * p.c.hkv;
+        }
+      }
+    }
+    if (!found) return;  // not reached: r < total
+    for (int c = 0; c < n_cb; c += 64) {
+      const int u = c + lane < n_cb ? kBlockCost + Block<BN>(s, c + lane, p).tiles() : 0;
+      const int incl = wave_scan(u, lane);
+      const uint64_t above = __builtin_amdgcn_ballot_w64(start + incl > r);
+      if (above != 0) {
+        const int l = __builtin_ctzll(above);
+        cb = c + l;
+        start += __builtin_amdgcn_readlane(incl - u, l);
+        break;
+      }
+      start += __builtin_amdgcn_readlane(incl, 63);
+    }
+  } else {
+    g = (int)(blockIdx.x % (uint32_t)p.c.hkv);
+    int idx = (int)(blockIdx.x / (uint32_t)p.c.hkv);
+    bool found = false;
+    for (int c = 0; c < p.bt.n_seq && !found; c += 64) {
+      PagedSeq sl{};
+      if (c + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, c + lane);
+      const int n = n_blocks(sl, p), incl = wave_scan(n, lane);
+      const uint64_t above = __builtin_amdgcn_ballot_w64(incl > idx);
+      if (above != 0) {
+        const int l = __builtin_ctzll(above);
+        b = c + l;
+        s = seq_of_lane(sl, l);
+        n_cb = __builtin_amdgcn_readlane(n, l);
+        cb = __builtin_amdgcn_readlane(incl, l) - 1 - idx;  // the last block, with the most keys, first
+        found = true;
+      } else {
+        idx -= __builtin_amdgcn_readlane(incl, 63);
+      }
+    }
+    if (!found) return;  // the grid is sized for the most blocks there can be
+  }
+
+  while (true) {
+    const Block<BN> blk(s, cb, p);
+    const int tiles = blk.tiles();
+    int t0 = 0, nt = tiles, n_parts = 1, first_wg = me;
+    bool skip = false;
+    if constexpr (C::SPLIT) {
+      const int cost = kBlockCost + tiles, end = min(r1, start + cost);
+      t0 = max(0, r - start - kBlockCost);
+      nt = max(0, end - start - kBlockCost - t0);
+      // The block belongs to the workgroups that have tiles of it (one without a tile: to that of its first unit).
+      skip = tiles == 0 ? start < r : nt == 0;
+      if (tiles != 0) {
+        first_wg = (start + kBlockCost) / per;
+        n_parts = (start + cost - 1) / per - first_wg + 1;
+      }
+      r = end;
+    }
+    if (!skip) {
+      // What follows from the lane is computed for each block anew (and again for its output): kept over the loop,
+      // the addresses would not fit in the registers beside the step.
+      if constexpr (C::SPLIT) asm volatile("" : "+v"(lane));
+      st.i32 = lane & 31;
+      st.h = lane >> 5;
+      st.v_key = 8 * (lane >> 5) + ((lane & 15) >> 2);
+      st.v_t = (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<DV>(st.v_key);
+      st.v_half = (lane & 1) * 8;
+      const int kb0 = t0 * BN, t1 = t0 + nt;
+      const int kv_lim = min(blk.kv_end, t1 * BN);  // keys loaded; behind it the tile loads read zeros
+      st.sk = s.kv;
+      st.table = p.bt.block_table + (int64_t)b * p.bt.table_stride;
+
+      // Q of this wave's columns, straight into registers; columns behind the last repeat it and are not stored.
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        const uint32_t c = (uint32_t)min(blk.c0 + wave * 32 * QB + qb * 32 + st.i32, blk.cols - 1);
+        const int qi = (int)fast_div(c, p.m_group, p.sh_group), member = (int)c - qi * p.group;
+        st.last_key[qb] = p.causal ? s.kv - s.n_q + qi : s.kv - 1;
+        const uint16_t* qp = p.q + (int64_t)(s.q0 + qi) * p.q_token + (int64_t)(g * p.group + member) * p.q_head + st.h * 8;
+#pragma unroll
+        for (int ks = 0; ks < A::KS; ++ks) load_q<A::AG>(st.qf[qb][ks], qp + ks * 16);
+      }
+
+      // The pages of this wave's keys of tiles w0 .. w0 + 63, one per lane (behind the last key: the last one's).
+      int entries = 0;
+      auto window = [&](int w0) {
+        const int key = min((w0 + lane) * BN + wave * R, kv_lim - 1);
+        entries = key >= 0 ? st.table[key >> p.c.page_shift] : -1;
+        asm volatile("" : "+v"(entries));  // waited for here, not at every use
+      };
+      window(t0);
+      bool hole = false;
+      for (int e = (kb0 >> p.c.page_shift) + lane; e < (kv_lim + smask) >> p.c.page_shift; e += 64) {
+        const int page = st.table[e];
+        hole = hole || page < 0 || page >= p.c.n_pages;
+      }
+      st.holes = __builtin_amdgcn_ballot_w64(hole) != 0;
+      int n_plain = st.holes ? 0 : min(max(blk.plain - t0, 0), nt);
+
+      const uint16_t* kh = static_cast<const uint16_t*>(p.c.k) + (int64_t)g * p.c.k_head;
+      const uint16_t* vh = static_cast<const uint16_t*>(p.c.v) + (int64_t)g * p.c.v_head;
+      st.kg = kh;
+      PagedLoader<C::NWAVES, BN, C::KCH> kload;
+      PagedLoader<C::NWAVES, BN, C::VCH> vload;
+      kload.init(kh, p.c.k_page, p.c.k_slot, wave, lane, [](int row) { return k_swizzle<DQK>(row); });
+      vload.init(vh, p.c.v_page, p.c.v_slot, wave, lane, [](int row) { return v_swizzle<DV>(row); });
+      auto kslot = [&](int t) { return smem + ((unsigned)t % C::NKR) * C::K_BYTES; };
+      auto vslot = [&](int t) { return smem + C::NKR * C::K_BYTES + ((unsigned)t % C::NVR) * C::V_BYTES; };
+      auto lds_of = [&](const unsigned char* slot, int ni) {
+        return (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds_offset(slot) + wave * ni * 1024));
+      };
+      u32x4 gk, gv;
+      uint32_t gkl, gvl;
+      auto aim = [&](int j) {  // descriptors and LDS places of tile j of the item's part
+        const int page = __builtin_amdgcn_readlane(entries, j & 63), key = kb0 + j * BN + wave * R;
+        gk = kload.rsrc(page, p.c.n_pages, key, smask, kv_lim);
+        gv = vload.rsrc(page, p.c.n_pages, key, smask, kv_lim);
+        gkl = lds_of(kslot(j), C::K_LOADS);
+        gvl = lds_of(vslot(j), C::V_LOADS);
+      };
+      // The prologue's groups -KA .. -1, as in the fused forward: tiles 0 .. KA - 1, and zeros in the slot of the V
+      // tile before the first, which step 0 multiplies by P = 0.
+#pragma unroll
+      for (int t = 0; t < C::KA; ++t) {
+        if (t == 1) vload.issue(u32x4{0u, 0u, 0u, 0x00020000u}, lds_of(vslot(C::NVR - 1), C::V_LOADS));
+        aim(t);
+        kload.issue(gk, gkl);
+        vload.issue(gv, gvl);
+      }
+      // Q and K0: behind K0 are V0, the zeros and the groups after.
+      wait_vmcnt<2 * C::V_LOADS + (C::KA - 1) * (C::K_LOADS + C::V_LOADS)>();
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int ks = 0; ks < A::KS; ++ks) q_ready<A::AG>(st.qf[qb][ks]);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        st.m_run[qb] = -INFINITY;
+        st.l_run[qb] = 0.f;
+#pragma unroll
+        for (int db = 0; db < A::DB; ++db) {
+          st.oacc[db][qb] = f32x16{};
+          agpr_fence<A::AG>(st.oacc[db][qb]);
+        }
+      }
+
+      typename A::Scores sA, sB;
+      typename A::Probs pA, pB;
+      if (nt > 0) {
+        compiler_fence();
+        __builtin_amdgcn_s_barrier();
+        compiler_fence();
+        st.scores(sA, kslot(0));
+        if (n_plain == 0) st.mask_tile(sA, kb0);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) st.m_run[qb] = st.row_max(sA, qb);
+#pragma unroll
+        for (int kb = 0; kb < A::KB; ++kb)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pB[kb][qb][e] = 0u;
+      }
+      // Before step j: K(j+1) and V(j-1) have landed; see the fused forward.
+      auto sync_step = [&](int j) {
+        wait_vmcnt<C::V_LOADS + (C::KA - 2) * (C::K_LOADS + C::V_LOADS)>();
+        compiler_fence();
+        __builtin_amdgcn_s_barrier();
+        compiler_fence();
+        if (((j + C::KA) & 63) == 0) window(t0 + j + C::KA);
+        aim(j + C::KA);
+      };
+      auto issue = [&](int k) {
+        if (k < C::K_LOADS)
+          kload.issue_one(gk, gkl, k);
+        else
+          vload.issue_one(gv, gvl, k - C::K_LOADS);
+      };
+      unsigned char* const vzero = vslot(C::NVR - 1);
+      int j = 0;
+      for (; j + 1 < nt; j += 2) {
+        sync_step(j);
+        st.step(sA, sB, pA, pB, kslot(j + 1), j > 0 ? vslot(j - 1) : vzero, j >= n_plain, kb0 + j * BN, issue);
+        sync_step(j + 1);
+        st.step(sB, sA, pB, pA, kslot(j + 2), vslot(j), j + 1 >= n_plain, kb0 + (j + 1) * BN, issue);
+      }
+      if (j < nt) {
+        sync_step(j);
+        st.step(sA, sB, pA, pB, kslot(j + 1), j > 0 ? vslot(j - 1) : vzero, j >= n_plain, kb0 + j * BN, issue);
+      }
+      if (nt > 0) {
+        // P V of the last tile, on a selected copy of P (see the fused forward).
+        wait_vmcnt<C::VA * (C::K_LOADS + C::V_LOADS)>();
+        compiler_fence();
+        __builtin_amdgcn_s_barrier();
+        compiler_fence();
+        typename A::Probs pl;
+        const uint32_t take_a = (nt & 1) ? 0xffffffffu : 0u;
+#pragma unroll
+        for (int kb = 0; kb < A::KB; ++kb)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pl[kb][qb][e] = (pA[kb][qb][e] & take_a) | (pB[kb][qb][e] & ~take_a);
+        st.pv_tile(pl, vslot(nt - 1));
+      }
+      // Every load has landed and every wave is done with the last V tile: the output is staged in the rings.
+      wait_vmcnt<0>();
+      compiler_fence();
+      __builtin_amdgcn_s_barrier();
+      compiler_fence();
+
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int db = 0; db < A::DB; ++db) agpr_fence<A::AG>(st.oacc[db][qb]);
+      if constexpr (C::SPLIT) asm volatile("" : "+v"(lane));
+      st.i32 = lane & 31;
+      st.h = lane >> 5;
+      constexpr int WROWS = 32 * QB, RB = DV * 2;
+      const int col0 = wave * WROWS;  // this wave's first column of the block
+      if (C::SPLIT && n_parts > 1) {
+        // A part: O normalised by its own sum (fp32), and its LSE. Place 2 me: of a block that begins before.
+        const int64_t place = (2 * (int64_t)me + (me == first_wg ? 1 : 0)) * kBlockCols;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const float l_tot = half_swap_sum(st.l_run[qb]);
+          const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+          const int col = col0 + qb * 32 + st.i32;
+          if (blk.c0 + col < blk.cols) {
+            float* orow = p.many_o + (place + col) * DV;
+#pragma unroll
+            for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+              for (int g4 = 0; g4 < 4; ++g4)
+                *reinterpret_cast<f32x4*>(orow + db * 32 + 8 * g4 + 4 * st.h) =
+                    f32x4{st.oacc[db][qb][4 * g4] * inv, st.oacc[db][qb][4 * g4 + 1] * inv,
+                          st.oacc[db][qb][4 * g4 + 2] * inv, st.oacc[db][qb][4 * g4 + 3] * inv};
+            if (st.h == 0) p.many_lse[place + col] = l_tot > 0.f ? (st.m_run[qb] + log2f(l_tot)) * kLn2 : -INFINITY;
+          }
+        }
+        if (me == first_wg && tid == 0)
+          p.many_desc[me] = PagedItem{n_parts, s.q0, min(kBlockCols, blk.cols - blk.c0), blk.c0, g};
+      } else {
+        // O through LDS, so that each store instruction writes whole rows (layout: see the fused forward).
+        unsigned char* stage = smem + wave * WROWS * RB;
+        const int osw = o_swizzle<DV>(st.i32) << 4, ohalf = (st.h ^ o_half<DV>(st.i32)) << 3;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const float l_tot = half_swap_sum(st.l_run[qb]);
+          const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+          const bool some = l_tot > 0.f;  // else no visible key, or a score that is no number
+          unsigned char* srow = stage + (qb * 32 + st.i32) * RB + ohalf;
+#pragma unroll
+          for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+              const uint32_t w0 = pack_bf16x2(st.oacc[db][qb][4 * g4] * inv, st.oacc[db][qb][4 * g4 + 1] * inv);
+              const uint32_t w1 = pack_bf16x2(st.oacc[db][qb][4 * g4 + 2] * inv, st.oacc[db][qb][4 * g4 + 3] * inv);
+              *reinterpret_cast<uint2*>(srow + (((4 * db + g4) << 4) ^ osw)) = some ? make_uint2(w0, w1) : make_uint2(0u, 0u);
+            }
+          const uint32_t c = (uint32_t)(blk.c0 + col0 + qb * 32 + st.i32);
+          if (p.lse != nullptr && st.h == 0 && (int)c < blk.cols) {
+            const int qi = (int)fast_div(c, p.m_group, p.sh_group);
+            p.lse[(int64_t)(s.q0 + qi) * p.hq + g * p.group + ((int)c - qi * p.group)] =
+                some ? (st.m_run[qb] + log2f(l_tot)) * kLn2 : -INFINITY;
+          }
+        }
+        // Each wave reads back only its own rows, so no barrier.
+        constexpr int CPR = RB / 16, RPI = 64 / CPR, NIT = WROWS / RPI;
+        const int ch = lane % CPR;
+        u32x4 ov[NIT];
+#pragma unroll
+        for (int it = 0; it < NIT; ++it) {
+          const int row = it * RPI + lane / CPR;
+          const unsigned char* chunk = stage + row * RB + ((ch ^ o_swizzle<DV>(row)) << 4);
+          const int hl = o_half<DV>(row) << 3;
+          const uint2 x = *reinterpret_cast<const uint2*>(chunk + hl);
+          const uint2 y = *reinterpret_cast<const uint2*>(chunk + (hl ^ 8));
+          ov[it] = u32x4{x.x, x.y, y.x, y.y};
+        }
+#pragma unroll
+        for (int it = 0; it < NIT; ++it) asm volatile("" : "+v"(ov[it]));
+#pragma unroll
+        for (int it = 0; it < NIT; ++it) {
+          const uint32_t c = (uint32_t)(blk.c0 + col0 + it * RPI + lane / CPR);
+          if ((int)c < blk.cols) {
+            const int qi = (int)fast_div(c, p.m_group, p.sh_group);
+            uint16_t* dst = p.o + (int64_t)(s.q0 + qi) * p.o_token + (int64_t)(g * p.group + ((int)c - qi * p.group)) * p.o_head;
+            *reinterpret_cast<u32x4*>(dst + ch * 8) = ov[it];
+          }
+        }
+      }
+    }
+    if constexpr (!C::SPLIT) {
+      break;
+    } else {
+      if (r >= r1) break;
+      // The next block: of this head, of the next, of the next sequence with any.
+      start += kBlockCost + tiles;
+      if (++cb == n_cb) {
+        cb = 0;
+        if (++g == p.c.hkv) {
+          g = 0;
+          do {
+            if (++b >= p.bt.n_seq) return;  // not reached: r < total
+            s = load_seq(p.bt, b);
+            n_cb = n_blocks(s, p);
+          } while (n_cb == 0);
+        }
+      }
+      __syncthreads();  // the next block's loads overwrite what the stores above were read from
+    }
+  }
+}
+
+// The long instances of the fused forward. (d = 64: 32-key tiles, two workgroups per CU.)
+template <int DQK, int DV, bool SPLIT>
+struct PagedInstance {
+  using C = Cfg<DQK, DV, 64, 4, 2, true, SPLIT, 1, 2, 6, 2, 4, 1, true>;
+};
+template <bool SPLIT>
+struct PagedInstance<64, 64, SPLIT> {
+  using C = Cfg<64, 64, 32, 4, 2, true, SPLIT, 2, 2, 4, 2, 4, 1, true>;
+};
+
+template <class C>
+hipError_t launch_many(PagedParams p, int64_t blocks, hipStream_t stream) {
+  void* args[] = {&p};
+  const dim3 grid((unsigned)(C::SPLIT ? p.many_wg : blocks * p.c.hkv));
+  return hipLaunchKernel(reinterpret_cast<const void*>(&fa_paged_fwd_kernel<C>), grid, dim3(C::NT), args, 0, stream);
+}
+
+}  // namespace
+
+int paged_many_workgroups(int d_qk) { return d_qk == 64 ? 512 : 256; }
+int paged_block_cols() { return kBlockCols; }
+
+bool paged_many_split(int n_seq, int n_tokens, int hkv, int group, int few_cols, int d_qk, int64_t* blocks) {
+  // The most blocks that the packed tokens can make: whole ones, and a last one for each sequence of this kernel.
+  const int64_t rows = (int64_t)n_tokens * group;
+  int64_t seqs = rows / (few_cols + 1);
+  if (seqs > n_seq) seqs = n_seq;
+  *blocks = rows / kBlockCols + seqs;
+  return *blocks * hkv < 2 * paged_many_workgroups(d_qk);
+}
+
+hipError_t launch_paged_many(PagedParams p, int d_qk, hipStream_t stream) {
+  const FastDiv fg = make_fastdiv(p.group);
+  p.m_group = fg.m;
+  p.sh_group = fg.sh;
+  p.many_min_units = kBlockCost + 4;
+  int64_t blocks = 0;
+  const bool split = paged_many_split(p.bt.n_seq, p.bt.n_tokens, p.c.hkv, p.group, p.few_cols, d_qk, &blocks);
+  if (d_qk == 64)
+    return split ? launch_many<PagedInstance<64, 64, true>::C>(p, blocks, stream)
+                 : launch_many<PagedInstance<64, 64, false>::C>(p, blocks, stream);
+  if (d_qk == 128)
+    return split ? launch_many<PagedInstance<128, 128, true>::C>(p, blocks, stream)
+                 : launch_many<PagedInstance<128, 128, false>::C>(p, blocks, stream);
+  return split ? launch_many<PagedInstance<192, 128, true>::C>(p, blocks, stream)
+               : launch_many<PagedInstance<192, 128, false>::C>(p, blocks, stream);
+}
+
+}  // namespace fa

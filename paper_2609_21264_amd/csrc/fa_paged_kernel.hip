@@ -255,10 +255,11 @@ template <int TILE>
 struct SeqWork {
   int tiles, n_cb;
   int64_t units;
-  __device__ __forceinline__ SeqWork(const PagedSeq& s, int group, int hkv) {
+  __device__ __forceinline__ SeqWork(const PagedSeq& s, const PagedParams& p) {
+    const int64_t cols = (int64_t)s.n_q * p.group;
     tiles = (s.kv + TILE - 1) / TILE;
-    n_cb = (int)(((int64_t)s.n_q * group + 31) / 32);
-    units = (int64_t)n_cb * hkv * (tiles + kItemCost);
+    n_cb = cols > p.few_cols ? 0 : (int)((cols + 31) / 32);
+    units = (int64_t)n_cb * p.c.hkv * (tiles + kItemCost);
   }
 };
 
@@ -276,7 +277,7 @@ void fa_paged_few_kernel(PagedParams p) {
   // The line's length, and the sequence that holds this workgroup's first unit (every wave for itself).
   int64_t mine = 0;
   for (int b = lane; b < p.bt.n_seq; b += 64)
-    mine += SeqWork<TILE>(load_seq_lane(p.bt, b), p.group, p.c.hkv).units;
+    mine += SeqWork<TILE>(load_seq_lane(p.bt, b), p).units;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o);
   const int total = __builtin_amdgcn_readfirstlane((int)min(mine, (int64_t)INT32_MAX));
@@ -289,7 +290,7 @@ void fa_paged_few_kernel(PagedParams p) {
   for (int c = 0;; c += 64) {
     const int bl = c + lane;
     const int64_t u =
-        bl < p.bt.n_seq ? SeqWork<TILE>(load_seq_lane(p.bt, bl), p.group, p.c.hkv).units : 0;
+        bl < p.bt.n_seq ? SeqWork<TILE>(load_seq_lane(p.bt, bl), p).units : 0;
     int64_t incl = u;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -336,12 +337,12 @@ void fa_paged_few_kernel(PagedParams p) {
   int r = r0;
   while (r < r1) {
     PagedSeq s = load_seq(p.bt, b);
-    SeqWork<TILE> sw(s, p.group, p.c.hkv);
+    SeqWork<TILE> sw(s, p);
     while (sw.units == 0 || r >= start + sw.units) {
       start += (int)sw.units;
       if (++b >= p.bt.n_seq) return;  // not reached: r < total
       s = load_seq(p.bt, b);
-      sw = SeqWork<TILE>(s, p.group, p.c.hkv);
+      sw = SeqWork<TILE>(s, p);
     }
     const int cost = sw.tiles + kItemCost;
     const int item = (r - start) / cost, item0 = start + item * cost;
@@ -594,27 +595,28 @@ void fa_paged_few_kernel(PagedParams p) {
   }
 }
 
-// Join of the parts of the item that begins in workgroup `me` of the kernel above and goes on in the next ones
+// Join of the parts of the item that begins in workgroup blockIdx.x of an attention kernel and goes on in the next ones
 // (none: n_parts 0): O = sum_k w_k O_k / sum_k w_k with w_k = exp(LSE_k - max LSE), added in the order of
 // the parts. DV / 4 threads per column, each with 4 output dims.
 template <int DV>
-__global__ __launch_bounds__(256) void fa_paged_join_kernel(PagedParams p) {
-  const PagedItem it = p.desc[blockIdx.x];
+__global__ __launch_bounds__(256) void fa_paged_join_kernel(PagedParams p, const PagedItem* desc, const float* o_part,
+                                                            const float* lse_part, int part_cols) {
+  const PagedItem it = desc[blockIdx.x];
   if (it.n_parts <= 1) return;
   constexpr int TD = DV / 4, NG = 256 / TD;  // threads per column, columns at once
   const int q = threadIdx.x % TD;
   const int64_t first = 2 * (int64_t)blockIdx.x + 1;
   for (int col = blockIdx.y * NG + threadIdx.x / TD; col < it.n_cols; col += gridDim.y * NG) {
-    auto place = [&](int k) { return (k == 0 ? first : first + 2 * k - 1) * p.part_cols + col; };
+    auto place = [&](int k) { return (k == 0 ? first : first + 2 * k - 1) * part_cols + col; };
     float M = -INFINITY;
-    for (int k = 0; k < it.n_parts; ++k) M = fmaxf(M, p.lse_part[place(k)]);
+    for (int k = 0; k < it.n_parts; ++k) M = fmaxf(M, lse_part[place(k)]);
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float den = 0.f;
     if (M != -INFINITY)
       for (int k = 0; k < it.n_parts; ++k) {
-        const float w = expf(p.lse_part[place(k)] - M);
+        const float w = expf(lse_part[place(k)] - M);
         den += w;
-        acc += w * *reinterpret_cast<const f32x4*>(p.o_part + place(k) * DV + 4 * q);
+        acc += w * *reinterpret_cast<const f32x4*>(o_part + place(k) * DV + 4 * q);
       }
     acc *= den > 0.f ? 1.f / den : 0.f;
     const int c = it.c0 + col, row = c / p.group, head = it.g * p.group + c - row * p.group;
@@ -652,11 +654,17 @@ hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, hipStream_t strea
     e = fp8 ? launch_few<FewCfg<128, 128, true, 4, 2>>(p, stream) : launch_few<FewCfg<128, 128, false, 4, 2>>(p, stream);
   else
     e = fp8 ? launch_few<FewCfg<192, 128, true, 4, 2>>(p, stream) : launch_few<FewCfg<192, 128, false, 4, 2>>(p, stream);
-  if (e != hipSuccess) return e;
-  void* args[] = {&p};
-  return hipLaunchKernel(d_qk == 64 ? reinterpret_cast<const void*>(&fa_paged_join_kernel<64>)
-                                    : reinterpret_cast<const void*>(&fa_paged_join_kernel<128>),
-                         dim3(p.n_wg, 4), dim3(256), args, 0, stream);
+  return e;
+}
+
+hipError_t launch_paged_join(PagedParams p, int d_v, bool many, hipStream_t stream) {
+  const PagedItem* desc = many ? p.many_desc : p.desc;
+  const float *o = many ? p.many_o : p.o_part, *lse = many ? p.many_lse : p.lse_part;
+  int cols = many ? paged_block_cols() : p.part_cols;
+  void* args[] = {&p, &desc, &o, &lse, &cols};
+  return hipLaunchKernel(d_v == 64 ? reinterpret_cast<const void*>(&fa_paged_join_kernel<64>)
+                                   : reinterpret_cast<const void*>(&fa_paged_join_kernel<128>),
+                         dim3(many ? p.many_wg : p.n_wg, many ? 32 : 4), dim3(256), args, 0, stream);
 }
 
 }  // namespace fa

@@ -129,7 +129,7 @@ def test_results_do_not_change_between_runs():
 @pytest.mark.parametrize("max_q", [1, 64])
 def test_captured_call_serves_other_lengths(max_q):
     bt = Batch([1, 1, 1], [900, 40, 300], 8, 2, 128, 128, 16, seed=41)
-    ws = torch.empty(fa.fa_fwd_paged_workspace_bytes(3, 8, 2, 128, 128), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(fa.fa_fwd_paged_workspace_bytes(3, 3, 8, 2, 128, 128, fa.FA_CACHE_BF16, max_q), dtype=torch.uint8, device="cuda")
     out, lse = torch.empty(3, 8, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(3, 8, device="cuda")
     bt.attend(out=out, lse=lse, return_lse=True, workspace=ws, max_q=max_q)  # first call outside the capture
     torch.cuda.synchronize()

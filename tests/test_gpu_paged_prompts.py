@@ -1,0 +1,123 @@
+"""GPU tests of the attention over a paged cache with many new tokens per sequence (prompts and chunks), against float64."""
+
+import pytest
+import torch
+
+import paper_2609_21264_amd as fa
+from paged import Batch
+from test_gpu_paged import DIMS, run
+
+pytestmark = pytest.mark.gpu
+
+
+def splits(bt):
+    """Whether the call needs a workspace: blocks are split where they would not fill the chip."""
+    return fa.fa_fwd_paged_workspace_bytes(len(bt.new), bt.T, bt.Hq, bt.Hkv, bt.dqk, bt.dv, fa.FA_CACHE_BF16, max(bt.new)) > 0
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("dqk,dv", DIMS)
+@pytest.mark.parametrize("n,extra", [(65, 0), (256, 0), (257, 1), (300, 1000), (100, 5000)])
+def test_prompt_and_chunk(n, extra, dqk, dv, page, causal):
+    bt = Batch([n], [n + extra], 4, 2, dqk, dv, page, seed=n)
+    assert splits(bt)
+    run(bt, causal=causal)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (7, 1), (14, 2), (5, 5), (96, 2)])
+def test_groups(Hq, Hkv):
+    # 256 row-heads of a block end anywhere inside a token's group.
+    run(Batch([129, 70], [129, 400], Hq, Hkv, 64, 64, 16, seed=Hq))
+    run(Batch([129, 70], [129, 400], Hq, Hkv, 128, 128, 32, seed=Hq + 1))
+
+
+@pytest.mark.parametrize("dqk,dv", DIMS)
+@pytest.mark.parametrize("causal", [True, False])
+def test_mixed_lengths(dqk, dv, causal):
+    # Single tokens, none, prompts, a chunk, more tokens than keys (a prompt's first rows see nothing).
+    run(Batch([1, 300, 0, 5, 131, 1, 200], [1000, 300, 40, 77, 2000, 1, 90], 8, 2, dqk, dv, 16, seed=7), causal=causal)
+
+
+@pytest.mark.parametrize("dqk,dv,hkv", [(64, 64, 112), (128, 128, 64), (192, 128, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_whole_blocks(dqk, dv, hkv, causal):
+    """Enough blocks to fill the chip: none is split."""
+    new = [1111, 1111]
+    bt = Batch(new, [1111, 1500], hkv, hkv, dqk, dv, 32, seed=3)
+    assert not splits(bt)
+    run(bt, causal=causal)
+
+
+def test_whole_blocks_beside_tokens():
+    bt = Batch([1, 900, 0, 1, 1033, 2, 77], [300, 900, 9, 5, 1300, 2, 400], 64, 64, 128, 128, 16, seed=5, extra=2)
+    run(bt)
+
+
+@pytest.mark.parametrize("B", [63, 65, 130])
+def test_many_sequences(B):
+    new = [1 + (37 * i) % 90 for i in range(B)]
+    run(Batch(new, [n + (i % 3) * 100 for i, n in enumerate(new)], 4, 2, 64, 64, 16, seed=B))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_pages_that_are_not_there(causal):
+    bt = Batch([150, 90, 200], [700, 333, 200], 8, 2, 128, 128, 16, seed=31)
+    bt.table[0, 3], bt.table[0, 43] = -1, bt.n_pages
+    bt.table[1, 0:4], bt.table[1, 20] = 2 ** 31 - 1, -2 ** 31
+    bt.table[2, :] = -1
+    bt.d_table = bt.table.cuda()
+    run(bt, causal=causal)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-30, 2.0])
+def test_scales(scale):
+    run(Batch([100, 200], [200, 1500], 4, 2, 64, 64, 16, seed=3), scale=scale)
+
+
+@pytest.mark.parametrize("dqk,dv", DIMS)
+def test_rising_scores_move_the_reference(dqk, dv):
+    """Keys that grow along the sequence: the reference maximum of a row is exceeded by far in later tiles, which are
+    redone with keys read from their pages."""
+    bt = Batch([90, 120], [1500, 120], 4, 2, dqk, dv, 16, seed=11)
+    for b, n in enumerate(bt.keys):
+        pos = torch.arange(n)
+        pages, slots = bt.table[b, pos // 16].long(), pos % 16
+        grow = (0.2 + 6.0 * pos / n)[:, None, None]
+        bt.k_cache[pages, :, slots] = (bt.k_cache[pages, :, slots].float() * grow).to(torch.bfloat16)
+    bt._to("cuda", "hnd")
+    run(bt)
+    bt.table[0, 40] = -1
+    bt.d_table = bt.table.cuda()
+    run(bt)
+
+
+def test_nhd_cache_and_strided_tensors():
+    bt = Batch([200, 1, 60], [300, 40, 1027], 8, 2, 128, 128, 16, seed=21, order="nhd")
+    qkv = torch.zeros(bt.T, 12, 128, dtype=torch.bfloat16, device="cuda")
+    qkv[:, 2:10] = bt.d_q
+    bt.d_q = qkv[:, 2:10]
+    out = torch.full((8, bt.T, 136), 7.0, dtype=torch.bfloat16, device="cuda")
+    run(bt, out=out[:, :, :128].transpose(0, 1))
+    assert torch.all(out[:, :, 128:] == 7)
+
+
+def test_results_do_not_change_between_runs():
+    bt = Batch([700, 130, 1], [2000, 130, 500], 8, 2, 128, 128, 16, seed=39)
+    first = bt.attend(return_lse=True)
+    for _ in range(3):
+        again = bt.attend(return_lse=True)
+        assert torch.equal(first[0].view(torch.int16), again[0].view(torch.int16)) and torch.equal(first[1], again[1])
+
+
+def test_prompt_equals_fused_forward():
+    """A prompt without a cached part through its pages and through forward(): the same to rounding."""
+    bt = Batch([1000], [1000], 8, 2, 128, 128, 16, seed=51)
+    o, lse = run(bt)
+    pos = torch.arange(1000)
+    k, v = (c[bt.table[0, pos // 16].long(), :, pos % 16].transpose(0, 1)[None].contiguous().cuda()
+            for c in (bt.k_cache, bt.v_cache))
+    ro, rl = fa.forward(bt.d_q.transpose(0, 1)[None].contiguous(), k, v, causal=True, return_lse=True)
+    # Both round P and O to bf16: 2 (2^-8 + 2^-8) max|V|.
+    assert (o.float() - ro[0].transpose(0, 1).float()).abs().max() <= 2.0 ** -6 * v.float().abs().max()
+    assert (lse - rl[0].T).abs().max() <= 1e-4

@@ -4,14 +4,15 @@ import re
 
 import pytest
 
+import test_kernel_asm
 from test_kernel_asm import _asm, _have_hipcc, _in_flight_violations, _kernels
 
 pytestmark = pytest.mark.skipif(not _have_hipcc(), reason="hipcc not installed")
 
 
-@pytest.fixture(scope="module")
-def text():
-    return _asm("fa_paged_kernel.hip")
+@pytest.fixture(scope="module", params=["fa_paged_kernel.hip", "fa_paged_fwd_kernel.hip"])
+def text(request):
+    return _asm(request.param)
 
 
 def test_no_packed_fp32_no_scratch_no_scalar_writes(text):
@@ -34,3 +35,7 @@ def test_no_access_to_registers_of_in_flight_loads(text):
     assert n > 0, "no inline-asm load found: the check would be vacuous"
     report = {name: bad[:5] for name, code in kernels.items() if (bad := _in_flight_violations(code))}
     assert not report, report
+
+
+def test_inline_asm_mfma_operands_settled():
+    test_kernel_asm.test_inline_asm_mfma_operands_settled(_asm("fa_paged_fwd_kernel.hip"))
