@@ -377,9 +377,10 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
                          int Hq, const long long* strides, int max_q, float scale, int causal, void* workspace,
                          size_t workspace_bytes, hipStream_t stream);
 
-/* Workspace bytes of a fa_fwd_paged call with these sizes and this max_q (it does not depend on the lengths; 0 is possible).
- * Host arithmetic only; 0 for sizes <= 0, max_q < 0, Hq not a multiple of Hkv, or an unsupported type or head dimension. */
-size_t fa_fwd_paged_workspace_bytes(int B, int T, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q);
+/* Workspace bytes of a fa_fwd_paged call with these sizes, max_keys = max_blocks * page_size and this max_q (they do not
+ * depend on the lengths; 0 is possible). Host arithmetic only; 0 for sizes <= 0 (max_keys, max_q: < 0), Hq not a multiple of
+ * Hkv, or an unsupported type or head dimension. */
+size_t fa_fwd_paged_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q);
 
 /* Static, human-readable name of a status code ("FA_OK", ...); "unknown status" otherwise. */
 const char* fa_status_str(fa_status_t s);

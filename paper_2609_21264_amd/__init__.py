@@ -175,9 +175,10 @@ def fa_fwd_paged(cache: PagedCache, batch: PagedBatch, Q: int, O: int, LSE: Opti
                                         int(bool(causal)), workspace, int(workspace_bytes), stream))
 
 
-def fa_fwd_paged_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, d_qk: int, d_v: int, type: int, max_q: int) -> int:
-    """C ``fa_fwd_paged_workspace_bytes``."""
-    return int(_lib.load().fa_fwd_paged_workspace_bytes(B, T, Hq, Hkv, d_qk, d_v, type, max_q))
+def fa_fwd_paged_workspace_bytes(B: int, T: int, max_keys: int, Hq: int, Hkv: int, d_qk: int, d_v: int, type: int,
+                                 max_q: int) -> int:
+    """C ``fa_fwd_paged_workspace_bytes`` (``max_keys``: blocks of the table times page size)."""
+    return int(_lib.load().fa_fwd_paged_workspace_bytes(B, T, max_keys, Hq, Hkv, d_qk, d_v, type, max_q))
 
 
 def _ref(s):
@@ -529,7 +530,7 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
             if return_lse and lse is None:
                 lse = torch.empty((T, hq), dtype=torch.float32, device=device)
             if workspace is None:
-                nbytes = fa_fwd_paged_workspace_bytes(batch.B, T, hq, cache.Hkv, dqk, dv, cache.type, int(max_q))
+                nbytes = fa_fwd_paged_workspace_bytes(batch.B, T, batch.max_blocks * cache.page_size, hq, cache.Hkv, dqk, dv, cache.type, int(max_q))
                 workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
         ot, oh = _check_rows("out", out, (T, hq, dv), device, writes=True)
         if lse is not None:

@@ -117,7 +117,7 @@ def load() -> ctypes.CDLL:
     lib.fa_kv_append.restype = i
     lib.fa_fwd_paged.argtypes = [vp, vp, vp, vp, vp, i, vp, i, f, i, vp, ctypes.c_size_t, vp]
     lib.fa_fwd_paged.restype = i
-    lib.fa_fwd_paged_workspace_bytes.argtypes = [i] * 8
+    lib.fa_fwd_paged_workspace_bytes.argtypes = [i] * 9
     lib.fa_fwd_paged_workspace_bytes.restype = ctypes.c_size_t
     _lib = lib
     return lib

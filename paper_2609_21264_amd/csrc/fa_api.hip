@@ -302,20 +302,26 @@ bool token_strides(const long long* s, int n) {
     if (s[i] < 0 || (s[i] & 7) != 0 || s[i] > (1ll << 40)) return false;
   return true;
 }
-// What a call of fa_fwd_paged runs, and its workspace (sizes checked). Sequences with more than kFewCols row-heads per
-// key/value head go to the kernel for many rows, if the host expects any; where it expects no others, all do.
+// What a call of fa_fwd_paged runs, and its workspace (sizes checked).
+//  * The kernel for few rows reads K and V once per item of 32 or 64 row-heads of a key/value head. It runs alone where
+//    the host expects no sequence with more than 64; otherwise it takes the sequences with at most 32 and leaves the
+//    others to the kernel for many rows; where all have max_q tokens, that runs alone.
+//  * Where the table has pages for at most kWholeKeys keys, the kernel for few rows takes whole items, without a join.
 constexpr int kFewCols = 64;
+constexpr int kWholeKeys = 512, kWholeItems = 1 << 16;
 struct PagedPlan {
   bool few, many, split;  // kernels to launch; whether that for many rows splits blocks
-  int few_cols, n_wg, cols, many_wg;
+  bool whole;             // whether that for few rows takes whole items
+  int few_cols, col_blocks, n_wg, cols, many_wg;
   int64_t lse, desc, many_o, many_lse, many_desc, bytes;  // 16-byte aligned offsets
 };
-PagedPlan paged_plan(int B, int T, int Hkv, int group, int d_qk, int d_v, int type, int max_q) {
+PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, int d_v, int type, int max_q) {
   PagedPlan w{};
-  const int64_t rows = static_cast<int64_t>(T) * group;
-  w.many = type == FA_CACHE_BF16 && static_cast<int64_t>(max_q) * group > kFewCols && rows > kFewCols;
+  const int64_t rows = static_cast<int64_t>(T) * group, most = static_cast<int64_t>(max_q) * group;
+  w.many = type == FA_CACHE_BF16 && most > kFewCols && rows > kFewCols;
   w.few = !w.many || static_cast<int64_t>(max_q) * B != T;
-  w.few_cols = !w.many ? INT_MAX : w.few ? kFewCols : 0;
+  w.few_cols = !w.many ? INT_MAX : w.few ? 32 : 0;
+  w.col_blocks = most <= 32 || w.many ? 1 : 2;
   if (w.many) {
     int64_t blocks = 0;
     w.split = fa::paged_many_split(B, T, Hkv, group, w.few_cols, d_qk, &blocks);
@@ -326,8 +332,14 @@ PagedPlan paged_plan(int B, int T, int Hkv, int group, int d_qk, int d_v, int ty
     return at;
   };
   if (w.few) {
-    w.n_wg = fa::paged_workgroups(d_qk, type == FA_CACHE_E4M3);
-    w.cols = rows < 32 ? static_cast<int>(rows) : 32;
+    const int cols = 32 * w.col_blocks;
+    w.n_wg = fa::paged_workgroups(d_qk, type == FA_CACHE_E4M3, w.col_blocks);
+    w.cols = rows < cols ? static_cast<int>(rows) : cols;
+    const int64_t items = (rows / cols + (B < T ? B : T)) * Hkv;  // the most there can be
+    w.whole = max_keys <= kWholeKeys && items <= kWholeItems;
+    if (w.whole) w.n_wg = static_cast<int>(items);
+  }
+  if (w.few && !w.whole) {
     const int64_t places = 2ll * w.n_wg * w.cols;
     place(places * d_v * 4);
     w.lse = place(places * 4);
@@ -383,11 +395,11 @@ fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   return fa::launch_append(p, cache->type == FA_CACHE_E4M3, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 
-size_t fa_fwd_paged_workspace_bytes(int B, int T, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q) {
-  if (B <= 0 || T <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_q < 0 || !dims_supported(d_qk, d_v) ||
+size_t fa_fwd_paged_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q) {
+  if (B <= 0 || T <= 0 || max_keys < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_q < 0 || !dims_supported(d_qk, d_v) ||
       (type != FA_CACHE_BF16 && type != FA_CACHE_E4M3))
     return 0;
-  return static_cast<size_t>(paged_plan(B, T, Hkv, Hq / Hkv, d_qk, d_v, type, max_q).bytes);
+  return static_cast<size_t>(paged_plan(B, T, max_keys, Hkv, Hq / Hkv, d_qk, d_v, type, max_q).bytes);
 }
 
 fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* Q, void* O, float* LSE,
@@ -414,7 +426,8 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
     return FA_ERR_UNSUPPORTED;
   st = check_paged_strides(cache, false);
   if (st != FA_OK) return st;
-  const PagedPlan w = paged_plan(batch->B, batch->T, cache->Hkv, Hq / cache->Hkv, cache->d_qk, cache->d_v, cache->type, max_q);
+  const PagedPlan w = paged_plan(batch->B, batch->T, batch->max_blocks * cache->page_size, cache->Hkv, Hq / cache->Hkv,
+                                 cache->d_qk, cache->d_v, cache->type, max_q);
   if (w.bytes > 0 && (workspace == nullptr || workspace_bytes < static_cast<size_t>(w.bytes))) return FA_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return FA_ERR_UNSUPPORTED;
 
@@ -432,6 +445,7 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   p.few_cols = w.few_cols;
   p.n_wg = w.n_wg;
   p.part_cols = w.cols;
+  p.whole = w.whole;
   p.many_wg = w.many_wg;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   p.o_part = reinterpret_cast<float*>(ws);
@@ -440,10 +454,12 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   p.many_o = reinterpret_cast<float*>(ws + w.many_o);
   p.many_lse = reinterpret_cast<float*>(ws + w.many_lse);
   p.many_desc = reinterpret_cast<fa::PagedItem*>(ws + w.many_desc);
+  // A single item per sequence and head reads K and V once: they are then loaded past the caches.
+  const bool stream_kv = static_cast<int64_t>(max_q) * p.group <= 32 * w.col_blocks;
   hipError_t e = hipSuccess;
   if (w.many) e = fa::launch_paged_many(p, cache->d_qk, stream);
-  if (e == hipSuccess && w.few) e = fa::launch_paged_few(p, cache->d_qk, cache->type == FA_CACHE_E4M3, stream);
-  if (e == hipSuccess && w.few) e = fa::launch_paged_join(p, cache->d_v, false, stream);
+  if (e == hipSuccess && w.few) e = fa::launch_paged_few(p, cache->d_qk, cache->type == FA_CACHE_E4M3, w.col_blocks, stream_kv, stream);
+  if (e == hipSuccess && w.few && !w.whole) e = fa::launch_paged_join(p, cache->d_v, false, stream);
   if (e == hipSuccess && w.split) e = fa::launch_paged_join(p, cache->d_v, true, stream);
   return e == hipSuccess ? FA_OK : FA_ERR_HIP;
 }

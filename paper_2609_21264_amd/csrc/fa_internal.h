@@ -189,7 +189,9 @@ struct PagedParams {
   int64_t q_token, q_head, o_token, o_head;
   int hq, group, causal;
   float cs;              // scale * log2(e)
-  int n_wg, min_units;   // workgroups, fewest units of work of one
+  int n_wg, min_units;   // workgroups (a power of two), fewest units of work of one
+  int wg_log;            // log2 of n_wg, filled by launch_paged_few
+  int whole;             // nonzero: a workgroup takes one whole item, n_wg covers the most there can be; no join
   int part_cols;         // columns of a place in the workspace
   float* o_part;         // fp32 [2 * n_wg][part_cols][d_v]
   float* lse_part;       // fp32 [2 * n_wg][part_cols]
@@ -201,15 +203,16 @@ struct PagedParams {
   float* many_o;         // fp32 [2 * many_wg][paged_block_cols()][d_v]
   float* many_lse;       // fp32 [2 * many_wg][paged_block_cols()]
   PagedItem* many_desc;  // [many_wg]
-  uint32_t m_group, sh_group;  // division by group, filled by launch_paged_many
+  uint32_t m_group, sh_group;  // division by group, filled by the launchers
 };
 
 hipError_t launch_append(AppendParams p, bool fp8, hipStream_t stream);
 // Workgroups of the attention kernel (as many as the chip holds at once).
-int paged_workgroups(int d_qk, bool fp8);
+int paged_workgroups(int d_qk, bool fp8, int col_blocks);
 // The kernels below run on `stream`; (d_qk, d_v) as for the other paths. Few rows: every sequence with at most few_cols
-// row-heads per key/value head.
-hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, hipStream_t stream);
+// row-heads per key/value head, in items of 32 * col_blocks of them (1 or 2). stream_kv: K and V are loaded past the
+// caches (items of 32 always are).
+hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, int col_blocks, bool stream_kv, hipStream_t stream);
 // Joins of split items: of the kernel for few rows, or for many.
 hipError_t launch_paged_join(PagedParams p, int d_v, bool many, hipStream_t stream);
 // Many rows (fa_paged_fwd_kernel.hip; bf16 caches): all other sequences. paged_many_split: whether it splits blocks (and

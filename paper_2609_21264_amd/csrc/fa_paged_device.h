@@ -17,6 +17,9 @@ __device__ __forceinline__ float scalar_load(const float* p) {
   return *(const __attribute__((address_space(4))) float*)(uintptr_t)p;
 }
 
+// A value that is the same for the whole wave, in a scalar register (some divisions and scans would leave it in a vector one).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // One sequence: its new tokens are the packed ones [q0, q_end), the last of its kv keys.
 struct PagedSeq {
   int q0, q_end, n_q, kv;
@@ -36,6 +39,29 @@ __device__ __forceinline__ PagedSeq load_seq(const PagedBatch& bt, int b) {
 __device__ __forceinline__ PagedSeq load_seq_lane(const PagedBatch& bt, int b) {
   return make_seq(bt, bt.q_starts[b], bt.q_starts[b + 1], bt.kv_lens[b]);
 }
+
+__device__ __forceinline__ PagedSeq seq_of_lane(const PagedSeq& s, int l) {
+  return PagedSeq{__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.q_end, l),
+                  __builtin_amdgcn_readlane(s.n_q, l), __builtin_amdgcn_readlane(s.kv, l)};
+}
+
+// Sums over the wave, and inclusive prefix sums, that stop at 2^32 - 1: whatever the batch's arrays hold, a prefix never
+// comes before an earlier one.
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = add_sat(x, (uint32_t)__shfl_xor((int)x, o));
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t y = (uint32_t)__shfl_up((int)x, o);
+    if (lane >= o) x = add_sat(x, y);
+  }
+  return x;
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t x, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); }
 
 }  // namespace
 }  // namespace fa

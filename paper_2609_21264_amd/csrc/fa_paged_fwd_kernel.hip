@@ -85,31 +85,12 @@ __device__ __forceinline__ int n_blocks(const PagedSeq& s, const PagedParams& p)
   const int64_t cols = (int64_t)s.n_q * p.group;
   return cols > p.few_cols ? (int)((cols + kBlockCols - 1) / kBlockCols) : 0;
 }
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-  return __builtin_amdgcn_readfirstlane(x);
-}
-// Inclusive prefix sum over the wave.
-__device__ __forceinline__ int wave_scan(int x, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  return x;
-}
 template <int BN>
 __device__ __forceinline__ int head_units(const PagedSeq& s, int n_cb, const PagedParams& p, int lane) {
-  int sum = 0;
-  for (int c = lane; c < n_cb; c += 64) sum += kBlockCost + Block<BN>(s, c, p).tiles();
-  return wave_sum(sum);
+  uint32_t sum = 0;
+  for (int c = lane; c < n_cb; c += 64) sum += (uint32_t)(kBlockCost + Block<BN>(s, c, p).tiles());
+  return (int)wave_sum(sum);
 }
-__device__ __forceinline__ PagedSeq seq_of_lane(const PagedSeq& s, int l) {
-  return PagedSeq{__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.q_end, l),
-                  __builtin_amdgcn_readlane(s.n_q, l), __builtin_amdgcn_readlane(s.kv, l)};
-}
-
 template <class C>
 __global__ __attribute__((amdgpu_flat_work_group_size(C::NT, C::NT), amdgpu_waves_per_eu(C::WPE, C::WPE)))
 void fa_paged_fwd_kernel(PagedParams p) {
@@ -180,16 +161,16 @@ void fa_paged_fwd_kernel(PagedParams p) {
     }
     if (!found) return;  // not reached: r < total
     for (int c = 0; c < n_cb; c += 64) {
-      const int u = c + lane < n_cb ? kBlockCost + Block<BN>(s, c + lane, p).tiles() : 0;
-      const int incl = wave_scan(u, lane);
-      const uint64_t above = __builtin_amdgcn_ballot_w64(start + incl > r);
+      const uint32_t u = c + lane < n_cb ? (uint32_t)(kBlockCost + Block<BN>(s, c + lane, p).tiles()) : 0u;
+      const uint32_t incl = wave_scan(u, lane);
+      const uint64_t above = __builtin_amdgcn_ballot_w64(incl > (uint32_t)(r - start));
       if (above != 0) {
         const int l = __builtin_ctzll(above);
         cb = c + l;
-        start += __builtin_amdgcn_readlane(incl - u, l);
+        start += (int)lane_of(incl - u, l);
         break;
       }
-      start += __builtin_amdgcn_readlane(incl, 63);
+      start += (int)lane_of(incl, 63);
     }
   } else {
     g = (int)(blockIdx.x % (uint32_t)p.c.hkv);
@@ -198,17 +179,17 @@ void fa_paged_fwd_kernel(PagedParams p) {
     for (int c = 0; c < p.bt.n_seq && !found; c += 64) {
       PagedSeq sl{};
       if (c + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, c + lane);
-      const int n = n_blocks(sl, p), incl = wave_scan(n, lane);
-      const uint64_t above = __builtin_amdgcn_ballot_w64(incl > idx);
+      const uint32_t n = (uint32_t)n_blocks(sl, p), incl = wave_scan(n, lane);
+      const uint64_t above = __builtin_amdgcn_ballot_w64(incl > (uint32_t)idx);
       if (above != 0) {
         const int l = __builtin_ctzll(above);
         b = c + l;
         s = seq_of_lane(sl, l);
-        n_cb = __builtin_amdgcn_readlane(n, l);
-        cb = __builtin_amdgcn_readlane(incl, l) - 1 - idx;  // the last block, with the most keys, first
+        n_cb = (int)lane_of(n, l);
+        cb = (int)lane_of(incl, l) - 1 - idx;  // the last block, with the most keys, first
         found = true;
       } else {
-        idx -= __builtin_amdgcn_readlane(incl, 63);
+        idx -= (int)lane_of(incl, 63);
       }
     }
     if (!found) return;  // the grid is sized for the most blocks there can be

@@ -10,6 +10,7 @@
 #include <stdint.h>
 
 #include "fa_device.h"
+#include "fa_fastdiv.h"
 #include "fa_internal.h"
 #include "fa_paged_device.h"
 
@@ -180,8 +181,8 @@ __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams 
 
 // ---- attention of few rows per sequence -------------------------------------------------------------
 //
-// An item is one column block of one (sequence, key/value head): up to 32 of its group * n_q row-heads
-// (column c = row * group + member) as the columns of 32x32 MFMAs, against the key tiles visible to them.
+// An item is one column block of one (sequence, key/value head): up to 32 or 64 of its group * n_q row-heads
+// (column c = row * group + member) as the columns of one or two 32x32 MFMAs, against the key tiles visible to them.
 // The lengths are on the device, so the host cannot cut the work: all items lie on one line, kItemCost +
 // tiles units each, and workgroup i takes units [i * per, (i + 1) * per) of it, `per` from the line's length.
 // Every workgroup so has the same work whatever the lengths are, a long sequence is split over as many
@@ -191,16 +192,19 @@ __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams 
 // their log-sum-exp weights.
 //
 // Inside an item: the waves take 32 keys each of a tile and stream them HBM -> LDS into a ring of their
-// own (no barrier), two 16-key halves per K and V block, each half inside one page. S^T = K Q^T, exact
-// running maximum per tile, O^T += V^T P^T as in the decode kernel. An e4m3 cache stays 8-bit in LDS and is
+// own (no barrier), two 16-key halves per K and V block, each half inside one page. S^T = K Q^T, the
+// online softmax, O^T += V^T P^T as in the decode kernel. An e4m3 cache stays 8-bit in LDS and is
 // widened (exactly) as fragments are read: K to bf16, V to fp16, so that P keeps 11 bits there; the scales
 // of K and V enter with the scores' scale and with the final division.
 
 constexpr int kItemCost = 1;  // fixed cost of an item in tiles
+constexpr float kRise = 8.f;  // how far (log2) a maximum may rise over its reference
 
-template <int DQK_, int DV_, bool FP8_, int NW_, int SLOTS_>
+template <int DQK_, int DV_, bool FP8_, int QB_, bool STREAM_, int SLOTS_>
 struct FewCfg {
-  static constexpr int DQK = DQK_, DV = DV_, NW = NW_, SLOTS = SLOTS_;
+  static constexpr int QB = QB_, COLS = 32 * QB_;               // 32-column MFMA blocks per wave, columns of an item
+  static constexpr bool STREAM = STREAM_;                       // K and V loaded past the caches
+  static constexpr int DQK = DQK_, DV = DV_, NW = 4, SLOTS = SLOTS_;
   static constexpr bool FP8 = FP8_;
   static constexpr int E = FP8 ? 1 : 2;                         // bytes per element
   static constexpr int KS = DQK / 16, DB = DV / 32;
@@ -211,13 +215,14 @@ struct FewCfg {
   static constexpr int RING = NW * SLOTS * WSLOT;
   static constexpr int TILE = 32 * NW;                          // keys per tile
   static constexpr int OROW = DV + 4;
-  static constexpr int O_BYTES = NW * 32 * OROW * 4;
-  static constexpr int JOIN_BYTES = O_BYTES + 2 * NW * 32 * 4;
+  static constexpr int O_BYTES = NW * COLS * OROW * 4;
+  static constexpr int JOIN_BYTES = O_BYTES + 2 * NW * COLS * 4;
   static constexpr int LDS_BYTES = RING > JOIN_BYTES ? RING : JOIN_BYTES;
   static constexpr int D = SLOTS - 1;                           // tiles loaded ahead
   static constexpr int L = 2 * (KL + VL);                       // loads per tile
   static_assert(LDS_BYTES <= 163840 && KCH % 4 == 0 && VCH % 4 == 0, "LDS budget, whole loads");
   static_assert(2 * VL + D * L < 64, "vmcnt range");
+  static_assert((SLOTS & (SLOTS - 1)) == 0, "a slot's place stays a scalar");
 };
 
 // XOR swizzles of the 16-byte chunks of an 8-bit row, so that lanes served together hit different 16-byte
@@ -250,16 +255,17 @@ __device__ __forceinline__ void load_q16(bf16x8& r, const void* ptr) {
 }
 __device__ __forceinline__ void q_settled(bf16x8& r) { asm volatile("" : "+v"(r)); }
 
-// Units of sequence b on the line of work, and what they are made of.
-template <int TILE>
+// Units of a sequence on the line of work, and what they are made of. Where items are taken whole every item is one unit.
+template <int TILE, int COLS>
 struct SeqWork {
-  int tiles, n_cb;
-  int64_t units;
+  int tiles, cost, n_cb;
+  uint32_t units;  // below 2^31 by the host's check
   __device__ __forceinline__ SeqWork(const PagedSeq& s, const PagedParams& p) {
     const int64_t cols = (int64_t)s.n_q * p.group;
     tiles = (s.kv + TILE - 1) / TILE;
-    n_cb = cols > p.few_cols ? 0 : (int)((cols + 31) / 32);
-    units = (int64_t)n_cb * p.c.hkv * (tiles + kItemCost);
+    cost = kItemCost + (p.whole ? 0 : tiles);
+    n_cb = cols > p.few_cols ? 0 : (int)((cols + COLS - 1) / COLS);
+    units = (uint32_t)n_cb * (uint32_t)p.c.hkv * (uint32_t)cost;
   }
 };
 
@@ -267,6 +273,7 @@ template <class C>
 __global__ __attribute__((amdgpu_flat_work_group_size(C::NW * 64, C::NW * 64)))
 void fa_paged_few_kernel(PagedParams p) {
   constexpr int DQK = C::DQK, DV = C::DV, KS = C::KS, DB = C::DB, NW = C::NW, TILE = C::TILE, D = C::D;
+  constexpr int QB = C::QB, COLS = C::COLS;
   constexpr bool FP8 = C::FP8;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS_BYTES];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -274,41 +281,40 @@ void fa_paged_few_kernel(PagedParams p) {
   const int i32 = lane & 31, h = lane >> 5;
   const int me = blockIdx.x;
 
-  // The line's length, and the sequence that holds this workgroup's first unit (every wave for itself).
-  int64_t mine = 0;
-  for (int b = lane; b < p.bt.n_seq; b += 64)
-    mine += SeqWork<TILE>(load_seq_lane(p.bt, b), p).units;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o);
-  const int total = __builtin_amdgcn_readfirstlane((int)min(mine, (int64_t)INT32_MAX));
-  const int per = max(p.min_units, (int)(((int64_t)total + p.n_wg - 1) / p.n_wg));
-  if (tid == 0) p.desc[me].n_parts = 0;
-  const int64_t r0w = (int64_t)me * per;
-  if (r0w >= total) return;
-  const int r0 = (int)r0w, r1 = (int)min((int64_t)total, r0w + per);
+  // The line's length, and the sequence that holds this workgroup's first unit (every wave for itself). The first 64
+  // sequences stay in registers, one per lane.
+  PagedSeq sl{};
+  if (lane < p.bt.n_seq) sl = load_seq_lane(p.bt, lane);
+  uint32_t mine = SeqWork<TILE, COLS>(sl, p).units, incl = wave_scan(mine, lane);
+  uint32_t sum = lane_of(incl, 63);
+  if (p.bt.n_seq > 64) {
+    uint32_t rest = 0;
+    for (int c = 64 + lane; c < p.bt.n_seq; c += 64) rest = add_sat(rest, SeqWork<TILE, COLS>(load_seq_lane(p.bt, c), p).units);
+    sum = add_sat(sum, wave_sum(rest));
+  }
+  const int total = uniform((int)min(sum, (uint32_t)INT32_MAX));
+  const int per = p.whole ? 1 : max(p.min_units, (int)((uint32_t)(total - 1) >> p.wg_log) + 1);
+  if (!p.whole && tid == 0) p.desc[me].n_parts = 0;
+  if ((int64_t)me * per >= total) return;
+  const int r0 = me * per, r1 = min(total - r0, per) + r0;
   int b = 0, start = 0;
-  for (int c = 0;; c += 64) {
-    const int bl = c + lane;
-    const int64_t u =
-        bl < p.bt.n_seq ? SeqWork<TILE>(load_seq_lane(p.bt, bl), p).units : 0;
-    int64_t incl = u;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t x = __shfl_up(incl, o);
-      if (lane >= o) incl += x;
-    }
-    const uint64_t above = __builtin_amdgcn_ballot_w64(start + incl > r0);
+  while (true) {
+    const uint64_t above = __builtin_amdgcn_ballot_w64(add_sat((uint32_t)start, incl) > (uint32_t)r0);
     if (above != 0) {
       const int l = __builtin_ctzll(above);
-      b = c + l;
-      start += __builtin_amdgcn_readlane((int)(incl - u), l);
+      start += (int)lane_of(incl - mine, l);
+      sl = seq_of_lane(sl, l);
+      b += l;
       break;
     }
-    if (c + 64 >= p.bt.n_seq) return;  // not reached: r0 < total
-    start += __builtin_amdgcn_readlane((int)incl, 63);
+    start += (int)lane_of(incl, 63);
+    b += 64;
+    if (b >= p.bt.n_seq) return;  // not reached: r0 < total
+    sl = PagedSeq{};
+    if (b + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, b + lane);
+    mine = SeqWork<TILE, COLS>(sl, p).units;
+    incl = wave_scan(mine, lane);
   }
-  b = __builtin_amdgcn_readfirstlane(b);
-  start = __builtin_amdgcn_readfirstlane(start);
 
   unsigned char* const ring = smem + wave * C::SLOTS * C::WSLOT;
   const uint32_t ring_lds = __builtin_amdgcn_readfirstlane(lds_offset(ring));
@@ -335,47 +341,55 @@ void fa_paged_few_kernel(PagedParams p) {
   const int v_half = (lane & 1) * 8;
 
   int r = r0;
+  PagedSeq s{uniform(sl.q0), uniform(sl.q_end), uniform(sl.n_q), uniform(sl.kv)};
+  b = uniform(b), start = uniform(start);
   while (r < r1) {
-    PagedSeq s = load_seq(p.bt, b);
-    SeqWork<TILE> sw(s, p);
-    while (sw.units == 0 || r >= start + sw.units) {
+    SeqWork<TILE, COLS> sw(s, p);
+    while (sw.units == 0 || (uint32_t)(r - start) >= sw.units) {
       start += (int)sw.units;
       if (++b >= p.bt.n_seq) return;  // not reached: r < total
       s = load_seq(p.bt, b);
-      sw = SeqWork<TILE>(s, p);
+      sw = SeqWork<TILE, COLS>(s, p);
     }
-    const int cost = sw.tiles + kItemCost;
-    const int item = (r - start) / cost, item0 = start + item * cost;
-    const int g = item / sw.n_cb, cb = item % sw.n_cb;
-    const int end = min(r1, item0 + cost);
+    const int cost = sw.cost;
+    const int item = uniform((int)((uint32_t)(r - start) / (uint32_t)cost)), item0 = start + item * cost;
+    const int g = uniform((int)((uint32_t)item / (uint32_t)sw.n_cb)), cb = item - g * sw.n_cb;
+    const int end = min(r1 - item0, cost) + item0;
     // Tiles of the item in this workgroup; the item belongs to the workgroups that have tiles of it (one without
     // a tile to that of its first unit).
-    const int t0 = max(0, r - item0 - kItemCost), t1 = end - item0 - kItemCost;
-    const bool single = sw.tiles == 0;
+    int t0 = 0, t1 = sw.tiles, first_wg = me, n_parts = 1;
+    bool skip = false;
+    if (!p.whole) {
+      t0 = max(0, r - item0 - kItemCost), t1 = end - item0 - kItemCost;
+      skip = sw.tiles == 0 ? item0 < r0 : t1 <= t0;
+      if (sw.tiles != 0) {
+        first_wg = uniform((int)((uint32_t)(item0 + kItemCost) / (uint32_t)per));
+        n_parts = uniform((int)((uint32_t)(item0 + cost - 1) / (uint32_t)per)) - first_wg + 1;
+      }
+    }
     r = end;
-    if (single ? item0 < r0 : t1 <= t0) continue;
-    const int first_wg = single ? me : (item0 + kItemCost) / per;
-    const int n_parts = single ? 1 : (item0 + cost - 1) / per - first_wg + 1;
+    if (skip) continue;
 
-    // Column of this lane. Columns past the item's rows repeat the last and are never stored.
-    const int cols = s.n_q * p.group, c0 = cb * 32;
-    const int c = min(c0 + i32, cols - 1);
-    const int qi = c / p.group, member = c - qi * p.group;
-    const int last_key = p.causal ? s.kv - s.n_q + qi : s.kv - 1;
-    // Keys visible to the block's last row; tiles behind them are left out.
-    const int last_row = min(c0 + 31, cols - 1) / p.group;
-    const int k_end = p.causal ? max(0, s.kv - s.n_q + last_row + 1) : s.kv;
-    const int nt = max(0, min(t1, (k_end + TILE - 1) / TILE) - t0);
-
-    bf16x8 qf[KS];
-    {
+    // Columns of this lane, one per 32-column block. Columns past the item's rows repeat the last and are never stored.
+    const int cols = s.n_q * p.group, c0 = cb * COLS;
+    int last_key[QB];
+    bf16x8 qf[QB][KS];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int c = min(c0 + 32 * qb + i32, cols - 1);
+      const int qi = (int)fast_div((uint32_t)c, p.m_group, p.sh_group), member = c - qi * p.group;
+      last_key[qb] = p.causal ? s.kv - s.n_q + qi : s.kv - 1;
       const uint16_t* qp = p.q + (int64_t)(s.q0 + qi) * p.q_token + (int64_t)(g * p.group + member) * p.q_head;
       // bf16: k-step ks holds dims 16 ks + 8 h .. + 7. e4m3: a lane reads 16 bytes of K at once, dims 32 m +
       // 16 h .. + 15, which serve k-steps 2 m and 2 m + 1; Q takes the same order.
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        load_q16(qf[ks], qp + (FP8 ? 32 * (ks / 2) + 16 * h + 8 * (ks & 1) : 16 * ks + 8 * h));
+        load_q16(qf[qb][ks], qp + (FP8 ? 32 * (ks / 2) + 16 * h + 8 * (ks & 1) : 16 * ks + 8 * h));
     }
+    // Keys visible to the block's last row; tiles behind them are left out.
+    const int last_row = (int)fast_div((uint32_t)min(c0 + COLS - 1, cols - 1), p.m_group, p.sh_group);
+    const int k_end = p.causal ? max(0, s.kv - s.n_q + last_row + 1) : s.kv;
+    const int nt = max(0, min(t1, (k_end + TILE - 1) / TILE) - t0);
 
     const unsigned char* kbase = static_cast<const unsigned char*>(p.c.k) + (int64_t)g * p.c.k_head * C::E;
     const unsigned char* vbase = static_cast<const unsigned char*>(p.c.v) + (int64_t)g * p.c.v_head * C::E;
@@ -397,19 +411,19 @@ void fa_paged_few_kernel(PagedParams p) {
                    (uint32_t)__builtin_amdgcn_readfirstlane(rows * (int)(slot_str * C::E)), 0x00020000u};
     };
     auto issue = [&](int t, int pg0, int pg1) {
-      const uint32_t l = ring_lds + (uint32_t)((unsigned)t % C::SLOTS) * C::WSLOT;
+      const uint32_t l = (uint32_t)uniform((int)(ring_lds + (uint32_t)((unsigned)t % C::SLOTS) * C::WSLOT));
       const int key0 = t * TILE + 32 * wave;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const u32x4 rs = half_rsrc(kbase, p.c.k_page, p.c.k_slot, u ? pg1 : pg0, key0 + 16 * u);
 #pragma unroll
-        for (int i = 0; i < C::KL; ++i) dma16_buffer(rs, koff[i], l + (u * C::KL + i) * 1024);
+        for (int i = 0; i < C::KL; ++i) dma16_buffer<C::STREAM>(rs, koff[i], l + (u * C::KL + i) * 1024);
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const u32x4 rs = half_rsrc(vbase, p.c.v_page, p.c.v_slot, u ? pg1 : pg0, key0 + 16 * u);
 #pragma unroll
-        for (int i = 0; i < C::VL; ++i) dma16_buffer(rs, voff[i], l + C::K_BYTES + (u * C::VL + i) * 1024);
+        for (int i = 0; i < C::VL; ++i) dma16_buffer<C::STREAM>(rs, voff[i], l + C::K_BYTES + (u * C::VL + i) * 1024);
       }
     };
     // Bits 2 k, 2 k + 1: whether the two halves of the k-th tile from the current one on have a page.
@@ -419,10 +433,14 @@ void fa_paged_few_kernel(PagedParams p) {
     };
 
     const float cs = p.cs * (FP8 && p.c.k_scale != nullptr ? scalar_load(p.c.k_scale + g) : 1.f);
-    f32x16 oacc[DB];
+    f32x16 oacc[DB][QB];
+    float m_run[QB], l_run[QB];
 #pragma unroll
-    for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
-    float m_run = -INFINITY, l_run = 0.f;
+    for (int qb = 0; qb < QB; ++qb) {
+      m_run[qb] = -INFINITY, l_run[qb] = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) oacc[db][qb] = f32x16{};
+    }
     const int n0t = t0, n1t = t0 + nt;
     // (Also without a tile: behind k_end nothing is read, and every path waits for Q the same way.)
 #pragma unroll
@@ -434,7 +452,9 @@ void fa_paged_few_kernel(PagedParams p) {
     int pgn0 = page_of(n0t + D, 0), pgn1 = page_of(n0t + D, 1);
     wait_vmcnt<D * C::L>();  // Q
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) q_settled(qf[ks]);
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) q_settled(qf[qb][ks]);
 
     for (int t = n0t; t < n1t; ++t) {
       compiler_fence();
@@ -448,69 +468,88 @@ void fa_paged_few_kernel(PagedParams p) {
       const unsigned char* sV = sK + C::K_BYTES;
       const int n0 = t * TILE + 32 * wave;
 
-      // Scores: register r holds key n0 + 16 (r / 8) + 8 h + r % 8 of column i32.
-      f32x16 sc;
+      // Scores: register r holds key n0 + 16 (r / 8) + 8 h + r % 8 of column i32 (of block qb).
+      f32x16 sc[QB];
       const unsigned char* krow = sK + perm32(i32) * C::KROW;
-      if constexpr (FP8) {
-        const int ksw = k8_swizzle<C::KCH>(perm32(i32) & 15);
 #pragma unroll
-        for (int m = 0; m < KS / 2; ++m) {
-          const u32x4 a = *reinterpret_cast<const u32x4*>(krow + (((2 * m + h) ^ ksw) << 4));
-          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen_bf16(a[0], a[1]), qf[2 * m], m == 0 ? f32x16{} : sc, 0, 0, 0);
-          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen_bf16(a[2], a[3]), qf[2 * m + 1], sc, 0, 0, 0);
-        }
-      } else {
+      for (int m = 0; m < (FP8 ? KS / 2 : KS); ++m) {
+        const u32x4 a =
+            *reinterpret_cast<const u32x4*>(krow + (((2 * m + h) ^ (FP8 ? k8_swizzle<C::KCH>(perm32(i32) & 15)
+                                                                        : k_lane_swizzle<DQK>(i32))) << 4));
+        if constexpr (FP8) {
+          const bf16x8 lo = widen_bf16(a[0], a[1]), hi = widen_bf16(a[2], a[3]);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const u32x4 a = *reinterpret_cast<const u32x4*>(krow + (((2 * ks + h) ^ k_lane_swizzle<DQK>(i32)) << 4));
-          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bit_cast<bf16x8>(a), qf[ks], ks == 0 ? f32x16{} : sc, 0, 0, 0);
+          for (int qb = 0; qb < QB; ++qb)
+            sc[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, qf[qb][2 * m], m == 0 ? f32x16{} : sc[qb], 0, 0, 0);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+            sc[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, qf[qb][2 * m + 1], sc[qb], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+            sc[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bit_cast<bf16x8>(a), qf[qb][m], m == 0 ? f32x16{} : sc[qb],
+                                                             0, 0, 0);
         }
       }
-      // Mask keys past the column's last visible key and those of halves without a page.
-      const int lim = last_key - n0 - 8 * h;
-      const int lim0 = (valid & 1u) ? lim : -1, lim1 = (valid & 2u) ? lim : -1;
+      const bool there0 = valid & 1u, there1 = valid & 2u;
       valid >>= 2;
-      float mt = -INFINITY;
+      u32x4 pw[QB][2];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float x = (16 * (e >> 3) + (e & 7)) > (e < 8 ? lim0 : lim1) ? -INFINITY : sc[e] * cs;
-        sc[e] = x;
-        mt = fmaxf(mt, x);
+      for (int qb = 0; qb < QB; ++qb) {
+        // Mask keys past the column's last visible key and those of halves without a page.
+        const int lim = last_key[qb] - n0 - 8 * h;
+        const int lim0 = there0 ? lim : -1, lim1 = there1 ? lim : -1;
+        float mt = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = (16 * (e >> 3) + (e & 7)) > (e < 8 ? lim0 : lim1) ? -INFINITY : sc[qb][e] * cs;
+          sc[qb][e] = x;
+          mt = fmaxf(mt, x);
+        }
+        mt = half_swap_max(mt);
+        // The reference follows the maximum only where some column's has risen over it by more than 8 (P then stays
+        // within 2^8, O / l does not depend on it): O is rescaled in few tiles. It starts at the first visible key's tile.
+        if (__builtin_amdgcn_ballot_w64(mt > m_run[qb] + kRise) != 0) {
+          const float m_new = fmaxf(m_run[qb], mt);
+          const float alpha = __builtin_amdgcn_exp2f(m_run[qb] - (m_new == -INFINITY ? 0.f : m_new));
+          m_run[qb] = m_new;
+          l_run[qb] *= alpha;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) oacc[db][qb] *= alpha;
+        }
+        const float mref = m_run[qb] == -INFINITY ? 0.f : m_run[qb];
+        float rs = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float e0 = __builtin_amdgcn_exp2f(sc[qb][2 * e] - mref);
+          const float e1 = __builtin_amdgcn_exp2f(sc[qb][2 * e + 1] - mref);
+          rs += e0 + e1;
+          pw[qb][e / 4][e % 4] = FP8 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
+        }
+        l_run[qb] += rs;
       }
-      mt = half_swap_max(mt);
-      const float m_new = fmaxf(m_run, mt);
-      const float mref = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m_run - mref);  // 0 while nothing was visible
-      m_run = m_new;
-      float rs = 0.f;
-      uint32_t pk[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float e0 = __builtin_amdgcn_exp2f(sc[2 * e] - mref), e1 = __builtin_amdgcn_exp2f(sc[2 * e + 1] - mref);
-        rs += e0 + e1;
-        pk[e] = FP8 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
-      }
-      l_run = l_run * alpha + rs;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
       compiler_fence();
       wait_vmcnt<D * C::L>();  // V(t)
       compiler_fence();
 #pragma unroll
       for (int ps = 0; ps < 2; ++ps) {
-        const u32x4 pw = {pk[4 * ps], pk[4 * ps + 1], pk[4 * ps + 2], pk[4 * ps + 3]};
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           if constexpr (FP8) {
             const unsigned char* vb = sV + (16 * ps + v_key) * C::VROW + (((2 * db) ^ v_t) << 4) + v_half;
             const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vb));
-            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen_f16(w.x, w.y), bit_cast<f16x8>(pw), oacc[db], 0, 0, 0);
+            const f16x8 va = widen_f16(w.x, w.y);
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+              oacc[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, bit_cast<f16x8>(pw[qb][ps]), oacc[db][qb], 0, 0, 0);
           } else {
             const unsigned char* vb = sV + (16 * ps + v_key) * C::VROW + (((4 * db) ^ v_t) << 4) + v_half;
             const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vb));
             const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vb + 4 * C::VROW));
             const bf16x8 va = bit_cast<bf16x8>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, bit_cast<bf16x8>(pw), oacc[db], 0, 0, 0);
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+              oacc[db][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, bit_cast<bf16x8>(pw[qb][ps]), oacc[db][qb], 0, 0, 0);
           }
         }
       }
@@ -524,36 +563,40 @@ void fa_paged_few_kernel(PagedParams p) {
     __syncthreads();
     float* ob = reinterpret_cast<float*>(smem);               // [wave][column][OROW]
     float* mb = reinterpret_cast<float*>(smem + C::O_BYTES);  // [wave][column]
-    float* lb = mb + NW * 32;                                 // [wave][column]
-    const float l_tot = half_swap_sum(l_run);
-    if (h == 0) {
-      mb[wave * 32 + i32] = m_run;
-      lb[wave * 32 + i32] = l_tot;
+    float* lb = mb + NW * COLS;                               // [wave][column]
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int at = wave * COLS + 32 * qb + i32;
+      const float l_tot = half_swap_sum(l_run[qb]);
+      if (h == 0) {
+        mb[at] = m_run[qb];
+        lb[at] = l_tot;
+      }
+      float* orow = ob + at * C::OROW + 4 * h;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4)
+          *reinterpret_cast<f32x4*>(orow + 32 * db + 8 * g4) = f32x4{oacc[db][qb][4 * g4], oacc[db][qb][4 * g4 + 1],
+                                                                     oacc[db][qb][4 * g4 + 2], oacc[db][qb][4 * g4 + 3]};
     }
-    float* orow = ob + (wave * 32 + i32) * C::OROW + 4 * h;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int g4 = 0; g4 < 4; ++g4)
-        *reinterpret_cast<f32x4*>(orow + 32 * db + 8 * g4) =
-            f32x4{oacc[db][4 * g4], oacc[db][4 * g4 + 1], oacc[db][4 * g4 + 2], oacc[db][4 * g4 + 3]};
     __syncthreads();
 
-    constexpr int TPC = NW * 64 / 32;  // threads per column
+    constexpr int TPC = NW * 64 / COLS;  // threads per column
     static_assert(DV % (8 * TPC) == 0, "a thread finishes whole 16-byte chunks of the output");
     const int col = tid / TPC, d0 = (tid % TPC) * (DV / TPC);
     if (c0 + col < cols) {
       float mw[NW], M = -INFINITY;
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
-        mw[w] = mb[w * 32 + col];
+        mw[w] = mb[w * COLS + col];
         M = fmaxf(M, mw[w]);
       }
       float wt[NW], Lsum = 0.f;
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
         wt[w] = mw[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[w] - M);
-        Lsum += wt[w] * lb[w * 32 + col];
+        Lsum += wt[w] * lb[w * COLS + col];
       }
       const bool some = Lsum > 0.f;  // else no visible key, or a score that is no number: O = 0, LSE = -inf
       const float vs = FP8 && p.c.v_scale != nullptr ? scalar_load(p.c.v_scale + g) : 1.f;
@@ -565,11 +608,11 @@ void fa_paged_few_kernel(PagedParams p) {
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w)
-          acc += wt[w] * *reinterpret_cast<const f32x4*>(ob + (w * 32 + col) * C::OROW + d0 + d);
+          acc += wt[w] * *reinterpret_cast<const f32x4*>(ob + (w * COLS + col) * C::OROW + d0 + d);
         o[d / 4] = some ? acc * inv : f32x4{0.f, 0.f, 0.f, 0.f};
       }
       if (n_parts == 1) {
-        const int row = (c0 + col) / p.group, mem = (c0 + col) - row * p.group;
+        const int row = (int)fast_div((uint32_t)(c0 + col), p.m_group, p.sh_group), mem = (c0 + col) - row * p.group;
         const int head = g * p.group + mem;
         const int64_t tok = s.q0 + row;
         uint16_t* dst = p.o + tok * p.o_token + (int64_t)head * p.o_head + d0;
@@ -590,40 +633,66 @@ void fa_paged_few_kernel(PagedParams p) {
       }
     }
     if (n_parts > 1 && me == first_wg && tid == 0)
-      p.desc[me] = PagedItem{n_parts, s.q0, min(32, cols - c0), c0, g};
+      p.desc[me] = PagedItem{n_parts, s.q0, min(COLS, cols - c0), c0, g};
     __syncthreads();  // the next item's loads overwrite the buffers above
   }
 }
 
 // Join of the parts of the item that begins in workgroup blockIdx.x of an attention kernel and goes on in the next ones
-// (none: n_parts 0): O = sum_k w_k O_k / sum_k w_k with w_k = exp(LSE_k - max LSE), added in the order of
-// the parts. DV / 4 threads per column, each with 4 output dims.
+// (none: n_parts 0): O = sum_k w_k O_k / sum_k w_k with w_k = exp(LSE_k - max LSE). DV / 4 threads (4 output dims each)
+// by pg part groups take a column, group j the parts j, j + pg, ...; the groups' sums are added in their order through
+// LDS. pg is the smallest power of two that leaves a group at most four parts (whose loads are in flight together), at
+// most 1024 / DV; the workgroup's other groups take other columns.
 template <int DV>
 __global__ __launch_bounds__(256) void fa_paged_join_kernel(PagedParams p, const PagedItem* desc, const float* o_part,
                                                             const float* lse_part, int part_cols) {
+  constexpr int TD = DV / 4, NG = 256 / TD;
+  __shared__ float s_den[NG];
+  __shared__ f32x4 s_acc[NG][TD];
   const PagedItem it = desc[blockIdx.x];
   if (it.n_parts <= 1) return;
-  constexpr int TD = DV / 4, NG = 256 / TD;  // threads per column, columns at once
-  const int q = threadIdx.x % TD;
+  const int q = threadIdx.x % TD, grp = threadIdx.x / TD;
+  int pg = 1;
+  while (4 * pg < it.n_parts && pg < NG) pg *= 2;
+  const int j = grp & (pg - 1), at_once = NG / pg;
   const int64_t first = 2 * (int64_t)blockIdx.x + 1;
-  for (int col = blockIdx.y * NG + threadIdx.x / TD; col < it.n_cols; col += gridDim.y * NG) {
+  for (int c0 = blockIdx.y * at_once; c0 < it.n_cols; c0 += gridDim.y * at_once) {
+    const int col = c0 + grp / pg;
+    const bool live = col < it.n_cols;
     auto place = [&](int k) { return (k == 0 ? first : first + 2 * k - 1) * part_cols + col; };
     float M = -INFINITY;
-    for (int k = 0; k < it.n_parts; ++k) M = fmaxf(M, lse_part[place(k)]);
+    if (live)
+      for (int k = q; k < it.n_parts; k += TD) M = fmaxf(M, lse_part[place(k)]);
+#pragma unroll
+    for (int o = TD / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float den = 0.f;
-    if (M != -INFINITY)
-      for (int k = 0; k < it.n_parts; ++k) {
+    if (live && M != -INFINITY) {
+#pragma unroll 4
+      for (int k = j; k < it.n_parts; k += pg) {
         const float w = expf(lse_part[place(k)] - M);
         den += w;
         acc += w * *reinterpret_cast<const f32x4*>(o_part + place(k) * DV + 4 * q);
       }
-    acc *= den > 0.f ? 1.f / den : 0.f;
-    const int c = it.c0 + col, row = c / p.group, head = it.g * p.group + c - row * p.group;
-    const int64_t tok = it.q0 + row;
-    *reinterpret_cast<u32x2*>(p.o + tok * p.o_token + (int64_t)head * p.o_head + 4 * q) =
-        u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
-    if (q == 0 && p.lse != nullptr) p.lse[tok * p.hq + head] = den > 0.f ? M + logf(den) : -INFINITY;
+    }
+    if (pg > 1) {
+      __syncthreads();  // the last columns' sums have been read
+      s_acc[grp][q] = acc;
+      if (q == 0) s_den[grp] = den;
+      __syncthreads();
+    }
+    if (live && j == 0) {
+      for (int k = 1; k < pg; ++k) {
+        den += s_den[grp + k];
+        acc += s_acc[grp + k][q];
+      }
+      acc *= den > 0.f ? 1.f / den : 0.f;
+      const int c = it.c0 + col, row = c / p.group, head = it.g * p.group + c - row * p.group;
+      const int64_t tok = it.q0 + row;
+      *reinterpret_cast<u32x2*>(p.o + tok * p.o_token + (int64_t)head * p.o_head + 4 * q) =
+          u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
+      if (q == 0 && p.lse != nullptr) p.lse[tok * p.hq + head] = den > 0.f ? M + logf(den) : -INFINITY;
+    }
   }
 }
 
@@ -643,18 +712,49 @@ hipError_t launch_append(AppendParams p, bool fp8, hipStream_t stream) {
                          dim3(p.bt.n_tokens), dim3(kAppendThreads), args, 0, stream);
 }
 
-int paged_workgroups(int d_qk, bool fp8) { return d_qk == 64 || fp8 ? 512 : 256; }
+// Instances by head dimensions, cache type and 32-column blocks; as many ring slots as leave two workgroups to a CU
+// where the waves' join fits in 80 KiB of LDS, else one.
+template <int DQK, int DV, bool FP8, int QB, bool STREAM>
+struct FewInstance {
+  static constexpr int kSlots = FP8 && (QB == 2 || DQK == 64) ? 4 : 2;
+  using C = FewCfg<DQK, DV, FP8, QB, STREAM, kSlots>;
+  static constexpr int kWorkgroups = C::LDS_BYTES <= 81920 ? 512 : 256;
+};
 
-hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, hipStream_t stream) {
-  p.min_units = 4;
-  hipError_t e;
+int paged_workgroups(int d_qk, bool fp8, int col_blocks) {
+  if (d_qk == 64) return 512;
+  return fp8 && col_blocks == 1 ? 512 : 256;
+}
+static_assert(FewInstance<64, 64, false, 2, true>::kWorkgroups == 512 && FewInstance<64, 64, true, 2, true>::kWorkgroups == 512 &&
+                  FewInstance<64, 64, false, 1, true>::kWorkgroups == 512 && FewInstance<64, 64, true, 1, true>::kWorkgroups == 512 &&
+                  FewInstance<128, 128, true, 1, true>::kWorkgroups == 512 && FewInstance<192, 128, true, 1, true>::kWorkgroups == 512 &&
+                  FewInstance<128, 128, false, 1, true>::kWorkgroups == 256 && FewInstance<128, 128, true, 2, true>::kWorkgroups == 256,
+              "paged_workgroups");
+
+template <int QB, bool STREAM>
+hipError_t launch_few_dims(PagedParams p, int d_qk, bool fp8, hipStream_t stream) {
   if (d_qk == 64)
-    e = fp8 ? launch_few<FewCfg<64, 64, true, 4, 4>>(p, stream) : launch_few<FewCfg<64, 64, false, 4, 2>>(p, stream);
-  else if (d_qk == 128)
-    e = fp8 ? launch_few<FewCfg<128, 128, true, 4, 2>>(p, stream) : launch_few<FewCfg<128, 128, false, 4, 2>>(p, stream);
-  else
-    e = fp8 ? launch_few<FewCfg<192, 128, true, 4, 2>>(p, stream) : launch_few<FewCfg<192, 128, false, 4, 2>>(p, stream);
-  return e;
+    return fp8 ? launch_few<typename FewInstance<64, 64, true, QB, STREAM>::C>(p, stream)
+               : launch_few<typename FewInstance<64, 64, false, QB, STREAM>::C>(p, stream);
+  if (d_qk == 128)
+    return fp8 ? launch_few<typename FewInstance<128, 128, true, QB, STREAM>::C>(p, stream)
+               : launch_few<typename FewInstance<128, 128, false, QB, STREAM>::C>(p, stream);
+  return fp8 ? launch_few<typename FewInstance<192, 128, true, QB, STREAM>::C>(p, stream)
+             : launch_few<typename FewInstance<192, 128, false, QB, STREAM>::C>(p, stream);
+}
+
+hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, int col_blocks, bool stream_kv, hipStream_t stream) {
+#ifndef FA_MIN_UNITS
+#define FA_MIN_UNITS 2
+#endif
+  p.min_units = FA_MIN_UNITS;
+  p.wg_log = 0;
+  while ((1 << p.wg_log) < p.n_wg) ++p.wg_log;
+  const FastDiv fg = make_fastdiv(p.group);
+  p.m_group = fg.m;
+  p.sh_group = fg.sh;
+  if (col_blocks == 1) return launch_few_dims<1, true>(p, d_qk, fp8, stream);
+  return stream_kv ? launch_few_dims<2, true>(p, d_qk, fp8, stream) : launch_few_dims<2, false>(p, d_qk, fp8, stream);
 }
 
 hipError_t launch_paged_join(PagedParams p, int d_v, bool many, hipStream_t stream) {
@@ -664,7 +764,7 @@ hipError_t launch_paged_join(PagedParams p, int d_v, bool many, hipStream_t stre
   void* args[] = {&p, &desc, &o, &lse, &cols};
   return hipLaunchKernel(d_v == 64 ? reinterpret_cast<const void*>(&fa_paged_join_kernel<64>)
                                    : reinterpret_cast<const void*>(&fa_paged_join_kernel<128>),
-                         dim3(many ? p.many_wg : p.n_wg, many ? 32 : 4), dim3(256), args, 0, stream);
+                         dim3(many ? p.many_wg : p.n_wg, many ? 32 : p.part_cols > 8 ? 8 : 4), dim3(256), args, 0, stream);
 }
 
 }  // namespace fa

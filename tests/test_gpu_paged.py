@@ -129,7 +129,7 @@ def test_results_do_not_change_between_runs():
 @pytest.mark.parametrize("max_q", [1, 64])
 def test_captured_call_serves_other_lengths(max_q):
     bt = Batch([1, 1, 1], [900, 40, 300], 8, 2, 128, 128, 16, seed=41)
-    ws = torch.empty(fa.fa_fwd_paged_workspace_bytes(3, 3, 8, 2, 128, 128, fa.FA_CACHE_BF16, max_q), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(fa.fa_fwd_paged_workspace_bytes(3, 3, bt.table.shape[1] * 16, 8, 2, 128, 128, fa.FA_CACHE_BF16, max_q), dtype=torch.uint8, device="cuda")
     out, lse = torch.empty(3, 8, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(3, 8, device="cuda")
     bt.attend(out=out, lse=lse, return_lse=True, workspace=ws, max_q=max_q)  # first call outside the capture
     torch.cuda.synchronize()
@@ -196,3 +196,28 @@ def test_offsets_past_32_bits():
     fa.kv_append(k, v, kc, vc, bt.d_table, bt.d_kv_lens, bt.d_q_starts)
     got = kc[int(bt.d_table[0, 299 // page]), :, 299 % page]
     assert torch.equal(got, k[0]) and np.isfinite(f64(vc[where[-1]])).any()
+
+
+@pytest.mark.parametrize("fp8", TYPES)
+@pytest.mark.parametrize("dqk,dv", DIMS)
+@pytest.mark.parametrize("n", [8, 9, 16, 17])
+def test_draft_tokens(n, dqk, dv, fp8):
+    # 32, 36, 64 and 68 row-heads per key/value head: one item, one of two column blocks, more than one (or the kernel
+    # for many rows); short tables are taken whole, long ones split.
+    run(Batch([n, n, n], [n, 400, 90], 8, 2, dqk, dv, 16, fp8, seed=n))
+    run(Batch([n, n, 1], [n, 5000, 90], 8, 2, dqk, dv, 32, fp8, seed=n + 1))
+
+
+@pytest.mark.parametrize("fp8", TYPES)
+def test_rising_scores_move_the_reference(fp8):
+    """Keys that grow along the sequence, so that a row's maximum rises far over its first tiles'."""
+    bt = Batch([1, 5], [3000, 900], 8, 2, 128, 128, 16, fp8, seed=53)
+    for b, n in enumerate(bt.keys):
+        pos = torch.arange(n)
+        pages, slots = bt.table[b, pos // 16].long(), pos % 16
+        grow = (0.1 + 4.0 * pos / n)[:, None, None]
+        rows = (bt.k_cache.float()[pages, :, slots] * grow).clamp(-448, 448).to(bt.k_cache.dtype)
+        raw = torch.uint8 if fp8 else torch.int16
+        bt.k_cache.view(raw)[pages, :, slots] = rows.view(raw)
+    bt._to("cuda", "hnd")
+    run(bt)

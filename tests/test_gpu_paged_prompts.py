@@ -12,7 +12,8 @@ pytestmark = pytest.mark.gpu
 
 def splits(bt):
     """Whether the call needs a workspace: blocks are split where they would not fill the chip."""
-    return fa.fa_fwd_paged_workspace_bytes(len(bt.new), bt.T, bt.Hq, bt.Hkv, bt.dqk, bt.dv, fa.FA_CACHE_BF16, max(bt.new)) > 0
+    return fa.fa_fwd_paged_workspace_bytes(len(bt.new), bt.T, bt.table.shape[1] * bt.page, bt.Hq, bt.Hkv, bt.dqk, bt.dv,
+                                           fa.FA_CACHE_BF16, max(bt.new)) > 0
 
 
 @pytest.mark.parametrize("causal", [True, False])

@@ -95,18 +95,22 @@ def test_attend_refuses():
         assert attend(scale=scale) == fa.FA_ERR_BAD_SCALE
     assert attend(Q=P + 4) == UNSUPPORTED and attend(O=P + 2) == UNSUPPORTED and attend(LSE=P + 2) == UNSUPPORTED
     assert attend(strides=(512, 128, 512, 100)) == UNSUPPORTED
-    need = fa.fa_fwd_paged_workspace_bytes(3, 5, 4, 2, 128, 128, 0, 2)
-    assert attend(ws=None) == fa.FA_ERR_WORKSPACE and attend(nbytes=need - 1) == fa.FA_ERR_WORKSPACE
-    assert attend(ws=P + 8, nbytes=need) == UNSUPPORTED
+    need = fa.fa_fwd_paged_workspace_bytes(3, 5, 256 * 16, 4, 2, 128, 128, 0, 2)
+    long = batch(max_blocks=256, table_stride=256)
+    assert attend(b=long, ws=None) == fa.FA_ERR_WORKSPACE and attend(b=long, nbytes=need - 1) == fa.FA_ERR_WORKSPACE
+    assert attend(b=long, ws=P + 8, nbytes=need) == UNSUPPORTED
     assert attend(b=batch(T=0)) == fa.FA_OK and attend(b=batch(B=0)) == fa.FA_OK and attend(Hq=0) == fa.FA_OK
 
 
 def test_workspace_bytes():
-    f = fa.fa_fwd_paged_workspace_bytes
+    def f(B, T, *a, keys=4096):
+        return fa.fa_fwd_paged_workspace_bytes(B, T, keys, *a)
+
     assert f(1, 0, 4, 2, 128, 128, 0, 1) == 0 and f(0, 1, 4, 2, 128, 128, 0, 1) == 0 and f(1, 1, 3, 2, 128, 128, 0, 1) == 0
     assert f(1, 1, 4, 2, 96, 96, 0, 1) == 0 and f(1, 1, 4, 2, 64, 64, 7, 1) == 0 and f(1, 1, 4, 2, 64, 64, 0, -1) == 0
     one, most = f(1, 1, 4, 1, 128, 128, 0, 1), f(8, 8, 4, 1, 128, 128, 0, 1)
     assert 0 < one < most == f(10 ** 6, 10 ** 6, 4, 1, 128, 128, 0, 1) and most < 1 << 26
+    assert f(1, 1, 4, 1, 128, 128, 0, 1, keys=-1) == 0
     # A chunk beside single tokens needs places for both kernels; enough equal prompts need none at all.
     assert f(8, 500, 4, 1, 128, 128, 0, 493) > most and f(8, 80000, 32, 8, 128, 128, 0, 10000) == 0
 
