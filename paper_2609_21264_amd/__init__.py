@@ -24,7 +24,6 @@ kernel. The functions below marshal arguments and translate status codes, nothin
 from __future__ import annotations
 
 import contextlib
-import ctypes
 import math
 from typing import Optional
 
@@ -163,7 +162,7 @@ def fa_kv_append(cache: PagedCache, batch: PagedBatch, K: int, V: int, Q: Option
                  strides: AppendStrides, cos_sin: Optional[int], n_pos: int, rot_begin: int, rot_dim: int,
                  interleaved: bool, stream: int) -> int:
     """C ``fa_kv_append``: descriptions, raw device addresses and sizes; returns the status code."""
-    return int(_lib.load().fa_kv_append(_ref(cache), _ref(batch), K, V, Q, Q_out, Hq, strides, cos_sin, n_pos, rot_begin,
+    return int(_lib.load().fa_kv_append(cache, batch, K, V, Q, Q_out, Hq, strides, cos_sin, n_pos, rot_begin,
                                         rot_dim, int(bool(interleaved)), stream))
 
 
@@ -171,7 +170,7 @@ def fa_fwd_paged(cache: PagedCache, batch: PagedBatch, Q: int, O: int, LSE: Opti
                  strides: PagedStrides, max_q: int, scale: float, causal: bool, workspace: Optional[int],
                  workspace_bytes: int, stream: int) -> int:
     """C ``fa_fwd_paged``: descriptions, raw device addresses and sizes; returns the status code."""
-    return int(_lib.load().fa_fwd_paged(_ref(cache), _ref(batch), Q, O, LSE, Hq, strides, max_q, float(scale),
+    return int(_lib.load().fa_fwd_paged(cache, batch, Q, O, LSE, Hq, strides, max_q, float(scale),
                                         int(bool(causal)), workspace, int(workspace_bytes), stream))
 
 
@@ -179,10 +178,6 @@ def fa_fwd_paged_workspace_bytes(B: int, T: int, max_keys: int, Hq: int, Hkv: in
                                  max_q: int) -> int:
     """C ``fa_fwd_paged_workspace_bytes`` (``max_keys``: blocks of the table times page size)."""
     return int(_lib.load().fa_fwd_paged_workspace_bytes(B, T, max_keys, Hq, Hkv, d_qk, d_v, type, max_q))
-
-
-def _ref(s):
-    return None if s is None else ctypes.byref(s)
 
 
 # What a call costs on the host bounds the smallest problems (one head S256 d64: a 4.7 us kernel in a call
@@ -354,81 +349,132 @@ def forward(q, k, v, causal: bool = False, scale: Optional[float] = None, return
     return (out, lse) if return_lse else out
 
 
-def _own_stream(stream):
-    """Context for allocating what kernels on ``stream`` use: the memory belongs to that stream, so that nothing
-    still running elsewhere uses it."""
+# The paged calls are short (an append of one token takes the GPU 3.4 us), so their checks are, as above, one expression
+# each where everything is as it should be, and what is wrong is looked for only then. A call on another stream or
+# device than the current one makes that the current one and starts again, so that new tensors belong to the stream whose
+# kernels use them.
+
+def _elsewhere(stream, device):
+    """Context for a call that is not on the current stream of the current device; None if it is."""
     import torch
 
-    return _NO_SWITCH if stream is None else torch.cuda.stream(stream)
+    if stream is None:
+        return None if torch._C._cuda_getDevice() == device else torch.cuda.device(device)
+    return torch.cuda.stream(_stream(stream, torch.device("cuda", device))[0])
 
 
-def _check_rows(name, t, shape, device, writes=False):
-    """A packed [T, H, d] bf16 tensor with any strides of T and H: returns them, 0 for a dimension of one."""
+def _rows_error(name, t, shape, device, writes):
+    """What is wrong with a packed [T, H, d] bf16 tensor."""
     import torch
 
     if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype != torch.bfloat16:
-        raise ValueError(f"{name} must be a 3-d bfloat16 torch tensor [tokens, heads, d]")
-    if t.device != device:
-        raise ValueError(f"{name} must be on the cache's device {device}, not {t.device}")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} must have shape {list(shape)}, not {list(t.shape)}")
+        return ValueError(f"{name} must be a 3-d bfloat16 torch tensor [tokens, heads, d]")
+    if not t.is_cuda or t.get_device() != device:
+        return ValueError(f"{name} must be on the cache's device cuda:{device}, not {t.device}")
+    if t.shape != shape:
+        return ValueError(f"{name} must have shape {list(shape)}, not {list(t.shape)}")
+    if t.stride(2) != 1:
+        return ValueError(f"the elements of a head of {name} must lie one after the other")
+    return ValueError(f"rows of {name} overlap" if writes else f"{name} is not supported")
+
+
+def _rows(name, t, shape, device, bf16, writes=False):
+    """Checks a packed [T, H, d] bf16 tensor with any strides of T and H (rows apart, where it is written to) and
+    returns them, 0 for a dimension of one."""
+    try:
+        st, sh, sd = t.stride()
+        if t.shape != shape or t.dtype != bf16 or t.get_device() != device or sd != 1:
+            raise _rows_error(name, t, shape, device, writes)
+    except (AttributeError, TypeError, ValueError):
+        raise _rows_error(name, t, shape, device, writes) from None
     T, H, d = shape
-    st, sh, sd = t.stride()
-    if sd != 1:
-        raise ValueError(f"the elements of a head of {name} must lie one after the other")
-    st, sh = st if T > 1 else 0, sh if H > 1 else 0
+    if T <= 1:
+        st = 0
+    if H <= 1:
+        sh = 0
     if writes and not ((sh >= d or H <= 1) and (st >= (H - 1) * sh + d or T <= 1)
                        or (st >= d or T <= 1) and (sh >= (T - 1) * st + d or H <= 1)):
-        raise ValueError(f"rows of {name} overlap")
+        raise _rows_error(name, t, shape, device, writes)
     return st, sh
 
 
-def _check_paged(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale, v_scale, T):
-    """Checks of the cache and the batch; their C descriptions."""
+def _paged_error(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale, v_scale):
+    """What is wrong with a paged cache or its batch."""
     import torch
 
     tensor = torch.Tensor
     for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
         if not isinstance(t, tensor) or t.dim() != 4 or t.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
-            raise ValueError(f"{name} must be a 4-d torch tensor [pages, heads, page_size, d], bfloat16 or float8_e4m3fn")
+            return ValueError(f"{name} must be a 4-d torch tensor [pages, heads, page_size, d], bfloat16 or float8_e4m3fn")
         if not t.is_cuda:
-            raise ValueError(f"{name} must be on a GPU")
+            return ValueError(f"{name} must be on a GPU")
         if t.stride(3) != 1:
-            raise ValueError(f"the elements of a head of {name} must lie one after the other")
+            return ValueError(f"the elements of a head of {name} must lie one after the other")
     device = k_cache.device
     if k_cache.dtype != v_cache.dtype or k_cache.shape[:3] != v_cache.shape[:3] or v_cache.device != device:
-        raise ValueError("k_cache and v_cache must agree in type, device, pages, heads and page size")
-    pages, hkv, page, dqk = k_cache.shape
+        return ValueError("k_cache and v_cache must agree in type, device, pages, heads and page size")
     for name, t, dim in (("block_table", block_table, 2), ("kv_lens", kv_lens, 1), ("q_starts", q_starts, 1)):
         if not isinstance(t, tensor) or t.dim() != dim or t.dtype != torch.int32:
-            raise ValueError(f"{name} must be a {dim}-d int32 torch tensor")
+            return ValueError(f"{name} must be a {dim}-d int32 torch tensor")
         if t.device != device:
-            raise ValueError(f"{name} must be on the cache's device {device}, not {t.device}")
-        if t.numel() > 1 and t.stride(dim - 1) != 1 and t.shape[dim - 1] > 1:
-            raise ValueError(f"the entries of {name} must lie one after the other")
-    B = kv_lens.shape[0]
-    if block_table.shape[0] != B or q_starts.shape[0] != B + 1:
-        raise ValueError(f"block_table [B, blocks], kv_lens [B] and q_starts [B + 1] do not agree: "
-                         f"{list(block_table.shape)}, {list(kv_lens.shape)}, {list(q_starts.shape)}")
-    fp8 = k_cache.dtype == torch.float8_e4m3fn
+            return ValueError(f"{name} must be on the cache's device {device}, not {t.device}")
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            return ValueError(f"the entries of {name} must lie one after the other")
     for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
         if t is None:
             continue
-        if not fp8:
-            raise ValueError(f"{name} goes with a float8_e4m3fn cache")
-        if not isinstance(t, tensor) or t.dtype != torch.float32 or tuple(t.shape) != (hkv,) or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous float32 tensor [heads]")
+        if k_cache.dtype != torch.float8_e4m3fn:
+            return ValueError(f"{name} goes with a float8_e4m3fn cache")
+        if not isinstance(t, tensor) or t.dtype != torch.float32 or t.shape != (k_cache.shape[1],) or not t.is_contiguous():
+            return ValueError(f"{name} must be a contiguous float32 tensor [heads]")
         if t.device != device:
-            raise ValueError(f"{name} must be on the cache's device {device}, not {t.device}")
-    ks, vs = k_cache.stride(), v_cache.stride()
-    if pages <= 1 or hkv <= 1:  # the stride of a dimension of one means nothing
-        ks, vs = ([x if n > 1 else 0 for x, n in zip(st[:2], (pages, hkv))] + [st[2]] for st in (ks, vs))
-    cache = PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
-                       None if v_scale is None else v_scale.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], pages,
-                       page, hkv, dqk, v_cache.shape[3], FA_CACHE_E4M3 if fp8 else FA_CACHE_BF16)
-    batch = PagedBatch(block_table.data_ptr(), block_table.stride(0) if B > 1 else 0, kv_lens.data_ptr(),
-                       q_starts.data_ptr(), B, block_table.shape[1], T)
-    return device, cache, batch
+            return ValueError(f"{name} must be on the cache's device {device}, not {t.device}")
+    return ValueError(f"block_table [B, blocks], kv_lens [B] and q_starts [B + 1] do not agree: "
+                      f"{list(block_table.shape)}, {list(kv_lens.shape)}, {list(q_starts.shape)}")
+
+
+def _scale(t, heads, device, float32):
+    """Address of a scale tensor; None where it is not one."""
+    if t.dtype != float32 or t.shape != (heads,) or t.get_device() != device or not t.is_contiguous():
+        return None
+    return t.data_ptr()
+
+
+def _paged(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale, v_scale, T, torch):
+    """Checks a paged cache and its batch; the device's index and their C descriptions."""
+    try:
+        (pages, hkv, page, dqk), (kp, kh, ks, kd) = k_cache.shape, k_cache.stride()
+        vpages, vhkv, vpage, dv = v_cache.shape
+        vp, vh, vs, vd = v_cache.stride()
+        (B, blocks), (bs, be) = block_table.shape, block_table.stride()
+        (lens,), (starts,) = kv_lens.shape, q_starts.shape
+        device, dtype, i32 = k_cache.get_device(), k_cache.dtype, torch.int32
+        fp8 = dtype == torch.float8_e4m3fn
+        ok = (device >= 0 and (fp8 or dtype == torch.bfloat16) and v_cache.dtype == dtype and vpages == pages
+              and vhkv == hkv and vpage == page and kd == 1 and vd == 1 and lens == B and starts == B + 1
+              and v_cache.get_device() == device and block_table.dtype == i32 and kv_lens.dtype == i32
+              and q_starts.dtype == i32 and block_table.get_device() == device and kv_lens.get_device() == device
+              and q_starts.get_device() == device and (be == 1 or blocks <= 1) and (B <= 1 or kv_lens.stride(0) == 1)
+              and (B == 0 or q_starts.stride(0) == 1))
+        ksp = vsp = None
+        if ok and k_scale is not None:
+            ksp = _scale(k_scale, hkv, device, torch.float32)
+            ok = fp8 and ksp is not None
+        if ok and v_scale is not None:
+            vsp = _scale(v_scale, hkv, device, torch.float32)
+            ok = fp8 and vsp is not None
+    except (AttributeError, TypeError, ValueError):
+        ok = False
+    if not ok:
+        raise _paged_error(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale, v_scale)
+    if pages <= 1:  # the stride of a dimension of one means nothing
+        kp = vp = 0
+    if hkv <= 1:
+        kh = vh = 0
+    return (device, PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), ksp, vsp, kp, kh, ks, vp, vh, vs, pages, page, hkv, dqk,
+                               dv, 1 if fp8 else 0),
+            PagedBatch(block_table.data_ptr(), bs if B > 1 else 0, kv_lens.data_ptr(), q_starts.data_ptr(), B, blocks, T),
+            B, blocks * page, hkv, dqk, dv, 1 if fp8 else 0)
 
 
 def _raise(name, st):
@@ -454,40 +500,49 @@ def kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q=None, q_
     stream); the call does not synchronise, and reads no array on the host."""
     import torch
 
+    bf16 = torch.bfloat16
     if not isinstance(k, torch.Tensor) or k.dim() != 3:
-        raise ValueError("k must be a 3-d bfloat16 torch tensor [tokens, heads, d]")
+        raise _rows_error("k", k, (), 0, False)
     T = k.shape[0]
-    device, cache, batch = _check_paged(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale, v_scale, T)
-    hkv, dqk, dv = cache.Hkv, cache.d_qk, cache.d_v
-    kt, kh = _check_rows("k", k, (T, hkv, dqk), device)
-    vt, vh = _check_rows("v", v, (T, hkv, dv), device)
+    device, cache, batch, _, _, hkv, dqk, dv, _ = _paged(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale, v_scale, T,
+                                                         torch)
+    kt, kh = _rows("k", k, (T, hkv, dqk), device, bf16)
+    vt, vh = _rows("v", v, (T, hkv, dv), device, bf16)
     n_pos = rot = 0
+    table = qp = op = None
     if cos_sin is not None:
-        if not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2 or cos_sin.dtype != torch.float32 or not cos_sin.is_contiguous():
+        if (not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2 or cos_sin.dtype != torch.float32
+                or not cos_sin.is_contiguous()):
             raise ValueError("cos_sin must be a contiguous float32 tensor [positions, rotated dims]")
-        if cos_sin.device != device:
-            raise ValueError(f"cos_sin must be on the cache's device {device}, not {cos_sin.device}")
+        if cos_sin.get_device() != device:
+            raise ValueError(f"cos_sin must be on the cache's device cuda:{device}, not {cos_sin.device}")
         n_pos, rot = cos_sin.shape
-    stream, handle = _stream(stream, device)
-    with _on_device(device):
-        hq = qt = qh = ot = oh = 0
-        if q is not None:
-            if not isinstance(q, torch.Tensor) or q.dim() != 3:
-                raise ValueError("q must be a 3-d bfloat16 torch tensor [tokens, heads, d]")
-            hq = q.shape[1]
-            qt, qh = _check_rows("q", q, (T, hq, dqk), device, writes=q_out is q)
-            if q_out is None:
-                with _own_stream(stream):
-                    q_out = torch.empty((T, hq, dqk), dtype=torch.bfloat16, device=device)
-            elif q_out is not q and isinstance(q_out, torch.Tensor) and q_out.numel() > 0 and \
-                    q_out.untyped_storage().data_ptr() == q.untyped_storage().data_ptr():
+        table = cos_sin.data_ptr()
+    elsewhere = _elsewhere(stream, device)
+    if elsewhere is not None:
+        with elsewhere:
+            return kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q, q_out, cos_sin, rot_begin, interleaved,
+                             k_scale, v_scale)
+    hq = qt = qh = ot = oh = 0
+    if q is not None:
+        hq = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else -1
+        qt, qh = _rows("q", q, (T, hq, dqk), device, bf16, q_out is q)
+        qp = q.data_ptr()
+        if q_out is None:
+            q_out = torch.empty_like(q) if q.is_contiguous() else q.new_empty((T, hq, dqk))
+            ot, oh = hq * dqk, dqk
+        elif q_out is q:
+            ot, oh = qt, qh
+        else:
+            ot, oh = _rows("q_out", q_out, (T, hq, dqk), device, bf16, True)
+            if T > 0 and q_out.untyped_storage().data_ptr() == q.untyped_storage().data_ptr():
                 raise ValueError("q_out must be q itself or lie in a storage of its own")
-            ot, oh = (qt, qh) if q_out is q else _check_rows("q_out", q_out, (T, hq, dqk), device, writes=True)
-        elif q_out is not None:
-            raise ValueError("q_out goes with q")
-        st = fa_kv_append(cache, batch, k.data_ptr(), v.data_ptr(), None if q is None else q.data_ptr(),
-                          None if q is None else q_out.data_ptr(), hq, AppendStrides(qt, qh, ot, oh, kt, kh, vt, vh),
-                          None if cos_sin is None else cos_sin.data_ptr(), n_pos, int(rot_begin), rot, interleaved, handle)
+        op = q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("q_out goes with q")
+    st = _lib.load().fa_kv_append(cache, batch, k.data_ptr(), v.data_ptr(), qp, op, hq,
+                                  AppendStrides(qt, qh, ot, oh, kt, kh, vt, vh), table, n_pos, int(rot_begin), rot,
+                                  1 if interleaved else 0, torch._C._cuda_getCurrentRawStream(device))
     if st != FA_OK:
         _raise("fa_kv_append", st)
     return q_out
@@ -503,45 +558,54 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
     the kernels (default: the mean, rounded up); the results are right for any. Rows of tokens that belong to no
     sequence are left as they were, so a new tensor's hold anything.
 
-    ``scale`` defaults to 1/sqrt(d_qk). ``workspace`` is a uint8 CUDA tensor of ``fa_fwd_paged_workspace_bytes`` (default: from
+    ``scale`` defaults to 1/sqrt(d_qk). ``workspace`` is a CUDA tensor of ``fa_fwd_paged_workspace_bytes`` (default: from
     torch's allocator). The kernels are enqueued on ``stream`` (default: torch's current stream; new tensors belong to that
     stream); the call does not synchronise, and reads no array on the host: captured into a graph, it serves
     whatever lengths the arrays hold at a replay."""
     import torch
 
+    bf16 = torch.bfloat16
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
-        raise ValueError("q must be a 3-d bfloat16 torch tensor [tokens, heads, d]")
-    T, hq = q.shape[0], q.shape[1]
-    device, cache, batch = _check_paged(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale, v_scale, T)
-    dqk, dv = cache.d_qk, cache.d_v
-    qt, qh = _check_rows("q", q, (T, hq, dqk), device)
+        raise _rows_error("q", q, (), 0, False)
+    T, hq = q.shape[:2]
+    device, cache, batch, B, max_keys, hkv, dqk, dv, type = _paged(k_cache, v_cache, block_table, kv_lens, q_starts, k_scale,
+                                                                   v_scale, T, torch)
+    qt, qh = _rows("q", q, (T, hq, dqk), device, bf16)
     if scale is None:
         scale = 1.0 / math.sqrt(dqk) if dqk else 1.0
     if max_q is None:
-        max_q = -(-T // batch.B) if batch.B else 0
-    if workspace is not None and (not isinstance(workspace, torch.Tensor) or workspace.device != device
-                                  or not workspace.is_contiguous()):
-        raise ValueError(f"workspace must be a contiguous tensor on {device}")
-    stream, handle = _stream(stream, device)
-    with _on_device(device):
-        with _own_stream(stream):
-            if out is None:
-                out = torch.empty((T, hq, dv), dtype=torch.bfloat16, device=device)
-            if return_lse and lse is None:
-                lse = torch.empty((T, hq), dtype=torch.float32, device=device)
-            if workspace is None:
-                nbytes = fa_fwd_paged_workspace_bytes(batch.B, T, batch.max_blocks * cache.page_size, hq, cache.Hkv, dqk, dv, cache.type, int(max_q))
-                workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        ot, oh = _check_rows("out", out, (T, hq, dv), device, writes=True)
-        if lse is not None:
-            if (not isinstance(lse, torch.Tensor) or tuple(lse.shape) != (T, hq) or lse.dtype != torch.float32
-                    or not lse.is_contiguous()):
-                raise ValueError("lse must be a contiguous float32 tensor [T, Hq]")
-            if lse.device != device:
-                raise ValueError(f"lse must be on the cache's device {device}, not {lse.device}")
-        st = fa_fwd_paged(cache, batch, q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, hq,
-                          PagedStrides(qt, qh, ot, oh), int(max_q), scale, causal, workspace.data_ptr(),
-                          workspace.numel() * workspace.element_size(), handle)
+        max_q = -(-T // B) if B else 0
+    elsewhere = _elsewhere(stream, device)
+    if elsewhere is not None:
+        with elsewhere:
+            return forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q, causal, scale, k_scale, v_scale,
+                                 return_lse, out, lse, workspace)
+    if out is not None:
+        ot, oh = _rows("out", out, (T, hq, dv), device, bf16, True)
+    else:
+        out = torch.empty_like(q) if dqk == dv and q.is_contiguous() else q.new_empty((T, hq, dv))
+        ot, oh = hq * dv, dv
+    if lse is not None:
+        if (not isinstance(lse, torch.Tensor) or lse.shape != (T, hq) or lse.dtype != torch.float32
+                or not lse.is_contiguous()):
+            raise ValueError("lse must be a contiguous float32 tensor [T, Hq]")
+        if lse.get_device() != device:
+            raise ValueError(f"lse must be on the cache's device cuda:{device}, not {lse.device}")
+    elif return_lse:
+        lse = q.new_empty((T, hq), dtype=torch.float32)
+    lib, ws = _lib.load(), None
+    if workspace is None:
+        nbytes = lib.fa_fwd_paged_workspace_bytes(B, T, max_keys, hq, hkv, dqk, dv, type, max_q)
+        if nbytes > 0:
+            workspace = q.new_empty(nbytes, dtype=torch.uint8)
+            ws = workspace.data_ptr()
+    elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{device}")
+    else:
+        nbytes, ws = workspace.numel() * workspace.element_size(), workspace.data_ptr()
+    st = lib.fa_fwd_paged(cache, batch, q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), hq,
+                          PagedStrides(qt, qh, ot, oh), int(max_q), scale, 1 if causal else 0, ws, nbytes,
+                          torch._C._cuda_getCurrentRawStream(device))
     if st != FA_OK:
         _raise("fa_fwd_paged", st)
     return (out, lse) if return_lse else out

@@ -113,9 +113,10 @@ def load() -> ctypes.CDLL:
     lib.fa_fwd_decode_noalloc.restype = i
     lib.fa_fwd_decode_parts.argtypes = [i, i, i, i, i, i]
     lib.fa_fwd_decode_parts.restype = i
-    lib.fa_kv_append.argtypes = [vp, vp, vp, vp, vp, vp, i, vp, vp, i, i, i, i, vp]
+    cache, batch = ctypes.POINTER(PagedCache), ctypes.POINTER(PagedBatch)  # structures go by reference
+    lib.fa_kv_append.argtypes = [cache, batch, vp, vp, vp, vp, i, vp, vp, i, i, i, i, vp]
     lib.fa_kv_append.restype = i
-    lib.fa_fwd_paged.argtypes = [vp, vp, vp, vp, vp, i, vp, i, f, i, vp, ctypes.c_size_t, vp]
+    lib.fa_fwd_paged.argtypes = [cache, batch, vp, vp, vp, i, vp, i, f, i, vp, ctypes.c_size_t, vp]
     lib.fa_fwd_paged.restype = i
     lib.fa_fwd_paged_workspace_bytes.argtypes = [i] * 9
     lib.fa_fwd_paged_workspace_bytes.restype = ctypes.c_size_t

@@ -456,11 +456,14 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   p.many_desc = reinterpret_cast<fa::PagedItem*>(ws + w.many_desc);
   // A single item per sequence and head reads K and V once: they are then loaded past the caches.
   const bool stream_kv = static_cast<int64_t>(max_q) * p.group <= 32 * w.col_blocks;
+  // Beside the kernel for many rows the others are mostly single tokens.
+  const int64_t most = static_cast<int64_t>(w.many ? 1 : max_q) * p.group;
+  const int cols = most < w.cols ? static_cast<int>(most) : w.cols;
   hipError_t e = hipSuccess;
   if (w.many) e = fa::launch_paged_many(p, cache->d_qk, stream);
   if (e == hipSuccess && w.few) e = fa::launch_paged_few(p, cache->d_qk, cache->type == FA_CACHE_E4M3, w.col_blocks, stream_kv, stream);
-  if (e == hipSuccess && w.few && !w.whole) e = fa::launch_paged_join(p, cache->d_v, false, stream);
-  if (e == hipSuccess && w.split) e = fa::launch_paged_join(p, cache->d_v, true, stream);
+  if (e == hipSuccess && w.few && !w.whole) e = fa::launch_paged_join(p, cache->d_v, false, cols, stream);
+  if (e == hipSuccess && w.split) e = fa::launch_paged_join(p, cache->d_v, true, fa::paged_block_cols(), stream);
   return e == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 

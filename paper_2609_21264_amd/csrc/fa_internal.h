@@ -213,8 +213,9 @@ int paged_workgroups(int d_qk, bool fp8, int col_blocks);
 // row-heads per key/value head, in items of 32 * col_blocks of them (1 or 2). stream_kv: K and V are loaded past the
 // caches (items of 32 always are).
 hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, int col_blocks, bool stream_kv, hipStream_t stream);
-// Joins of split items: of the kernel for few rows, or for many.
-hipError_t launch_paged_join(PagedParams p, int d_v, bool many, hipStream_t stream);
+// Joins of split items: of the kernel for few rows, or for many. cols: the columns that an item is expected to have (a
+// workgroup for each, up to 32).
+hipError_t launch_paged_join(PagedParams p, int d_v, bool many, int cols, hipStream_t stream);
 // Many rows (fa_paged_fwd_kernel.hip; bf16 caches): all other sequences. paged_many_split: whether it splits blocks (and
 // needs a join), and the most blocks per key/value head that there can be.
 int paged_many_workgroups(int d_qk);

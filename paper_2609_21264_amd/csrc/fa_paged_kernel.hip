@@ -189,7 +189,9 @@ __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams 
 // workgroups as it is long, and at most one item per boundary is split. An item that lies in one workgroup is
 // finished there; of a split one every workgroup leaves its part (O normalised by the part's own sum, and
 // the part's LSE) in its own two places of the workspace, and the join kernel adds the parts with
-// their log-sum-exp weights.
+// their log-sum-exp weights. (A join by the workgroup that finishes last, found by marks in the workspace, saves the second
+// launch's 3 us on the host, but is slower on the GPU wherever an item has more than a few parts: 8 000 keys of one
+// request 20.0 us against 15.6, 131 072 94.4 against 92.4.)
 //
 // Inside an item: the waves take 32 keys each of a tile and stream them HBM -> LDS into a ring of their
 // own (no barrier), two 16-key halves per K and V block, each half inside one page. S^T = K Q^T, the
@@ -639,59 +641,85 @@ void fa_paged_few_kernel(PagedParams p) {
 }
 
 // Join of the parts of the item that begins in workgroup blockIdx.x of an attention kernel and goes on in the next ones
-// (none: n_parts 0): O = sum_k w_k O_k / sum_k w_k with w_k = exp(LSE_k - max LSE). DV / 4 threads (4 output dims each)
-// by pg part groups take a column, group j the parts j, j + pg, ...; the groups' sums are added in their order through
-// LDS. pg is the smallest power of two that leaves a group at most four parts (whose loads are in flight together), at
-// most 1024 / DV; the workgroup's other groups take other columns.
+// (none: n_parts 0): O = sum_k w_k O_k / sum_k w_k with w_k = exp(LSE_k - max
+// LSE). DV / 4 threads (4 output dims each) by pg part groups take a column, group j
+// the parts j, j + pg, ..., eight at a time so that their loads are in flight together, with a running maximum; the
+// groups' sums are added in their order through LDS. pg is the smallest power of two that leaves a group at most eight
+// parts, at most 1024 / DV; the workgroup's other groups take other columns.
+template <int DV>
+struct JoinLds {
+  float m[1024 / DV], den[1024 / DV];
+  f32x4 acc[1024 / DV][DV / 4];
+};
+// Place of the k-th part of an item whose first part is workgroup `first`'s.
+__device__ __forceinline__ int64_t part_place(int first, int k) { return 2 * ((int64_t)first + k) + (k == 0 ? 1 : 0); }
+
 template <int DV>
 __global__ __launch_bounds__(256) void fa_paged_join_kernel(PagedParams p, const PagedItem* desc, const float* o_part,
                                                             const float* lse_part, int part_cols) {
-  constexpr int TD = DV / 4, NG = 256 / TD;
-  __shared__ float s_den[NG];
-  __shared__ f32x4 s_acc[NG][TD];
+  __shared__ JoinLds<DV> lds;
   const PagedItem it = desc[blockIdx.x];
   if (it.n_parts <= 1) return;
-  const int q = threadIdx.x % TD, grp = threadIdx.x / TD;
+  const int first = blockIdx.x;
   int pg = 1;
-  while (4 * pg < it.n_parts && pg < NG) pg *= 2;
+  while (8 * pg < it.n_parts && pg < 1024 / DV) pg *= 2;
+  constexpr int TD = DV / 4, NG = 256 / TD, AHEAD = 8;  // threads per column, groups, parts at a time
+  const int q = threadIdx.x % TD, grp = threadIdx.x / TD;
   const int j = grp & (pg - 1), at_once = NG / pg;
-  const int64_t first = 2 * (int64_t)blockIdx.x + 1;
   for (int c0 = blockIdx.y * at_once; c0 < it.n_cols; c0 += gridDim.y * at_once) {
     const int col = c0 + grp / pg;
     const bool live = col < it.n_cols;
-    auto place = [&](int k) { return (k == 0 ? first : first + 2 * k - 1) * part_cols + col; };
-    float M = -INFINITY;
-    if (live)
-      for (int k = q; k < it.n_parts; k += TD) M = fmaxf(M, lse_part[place(k)]);
-#pragma unroll
-    for (int o = TD / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    float m = -INFINITY, den = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float den = 0.f;
-    if (live && M != -INFINITY) {
-#pragma unroll 4
-      for (int k = j; k < it.n_parts; k += pg) {
-        const float w = expf(lse_part[place(k)] - M);
-        den += w;
-        acc += w * *reinterpret_cast<const f32x4*>(o_part + place(k) * DV + 4 * q);
+    for (int k0 = j; live && k0 < it.n_parts; k0 += AHEAD * pg) {
+      float l[AHEAD], top = m;
+      f32x4 v[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int k = min(k0 + i * pg, it.n_parts - 1);
+        const int64_t at = part_place(first, k) * part_cols + col;
+        l[i] = lse_part[at];
+        v[i] = *reinterpret_cast<const f32x4*>(o_part + at * DV + 4 * q);
       }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        l[i] = k0 + i * pg < it.n_parts ? l[i] : -INFINITY;
+        top = fmaxf(top, l[i]);
+      }
+      const float ref = top == -INFINITY ? 0.f : top, a = expf(m - ref);
+      den *= a;
+      acc *= a;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const float w = expf(l[i] - ref);
+        den += w;
+        acc += w * v[i];
+      }
+      m = top;
     }
     if (pg > 1) {
       __syncthreads();  // the last columns' sums have been read
-      s_acc[grp][q] = acc;
-      if (q == 0) s_den[grp] = den;
+      lds.acc[grp][q] = acc;
+      if (q == 0) lds.m[grp] = m, lds.den[grp] = den;
       __syncthreads();
     }
     if (live && j == 0) {
-      for (int k = 1; k < pg; ++k) {
-        den += s_den[grp + k];
-        acc += s_acc[grp + k][q];
+      if (pg > 1) {
+        for (int k = 1; k < pg; ++k) m = fmaxf(m, lds.m[grp + k]);
+        const float ref = m == -INFINITY ? 0.f : m;
+        den = 0.f, acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < pg; ++k) {
+          const float w = expf(lds.m[grp + k] - ref);
+          den += w * lds.den[grp + k];
+          acc += w * lds.acc[grp + k][q];
+        }
       }
       acc *= den > 0.f ? 1.f / den : 0.f;
       const int c = it.c0 + col, row = c / p.group, head = it.g * p.group + c - row * p.group;
       const int64_t tok = it.q0 + row;
       *reinterpret_cast<u32x2*>(p.o + tok * p.o_token + (int64_t)head * p.o_head + 4 * q) =
           u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
-      if (q == 0 && p.lse != nullptr) p.lse[tok * p.hq + head] = den > 0.f ? M + logf(den) : -INFINITY;
+      if (q == 0 && p.lse != nullptr) p.lse[tok * p.hq + head] = den > 0.f ? m + logf(den) : -INFINITY;
     }
   }
 }
@@ -757,14 +785,14 @@ hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, int col_blocks, b
   return stream_kv ? launch_few_dims<2, true>(p, d_qk, fp8, stream) : launch_few_dims<2, false>(p, d_qk, fp8, stream);
 }
 
-hipError_t launch_paged_join(PagedParams p, int d_v, bool many, hipStream_t stream) {
+hipError_t launch_paged_join(PagedParams p, int d_v, bool many, int cols, hipStream_t stream) {
   const PagedItem* desc = many ? p.many_desc : p.desc;
   const float *o = many ? p.many_o : p.o_part, *lse = many ? p.many_lse : p.lse_part;
-  int cols = many ? paged_block_cols() : p.part_cols;
-  void* args[] = {&p, &desc, &o, &lse, &cols};
+  int part_cols = many ? paged_block_cols() : p.part_cols;
+  void* args[] = {&p, &desc, &o, &lse, &part_cols};
   return hipLaunchKernel(d_v == 64 ? reinterpret_cast<const void*>(&fa_paged_join_kernel<64>)
                                    : reinterpret_cast<const void*>(&fa_paged_join_kernel<128>),
-                         dim3(many ? p.many_wg : p.n_wg, many ? 32 : p.part_cols > 8 ? 8 : 4), dim3(256), args, 0, stream);
+                         dim3(many ? p.many_wg : p.n_wg, cols < 1 ? 1 : cols > 32 ? 32 : cols), dim3(256), args, 0, stream);
 }
 
 }  // namespace fa

@@ -221,3 +221,24 @@ def test_rising_scores_move_the_reference(fp8):
         bt.k_cache.view(raw)[pages, :, slots] = rows.view(raw)
     bt._to("cuda", "hnd")
     run(bt)
+
+
+@pytest.mark.parametrize("Hq,Hkv,B", [(32, 1, 1), (64, 1, 1), (4, 1, 1), (64, 2, 2), (16, 16, 1)])
+@pytest.mark.parametrize("fp8", TYPES)
+def test_joins(Hq, Hkv, B, fp8):
+    """Items of up to hundreds of parts, with few columns (joined where the last part is done) and with many (by a
+    second kernel); the workspace holds anything before, and the same one serves several calls."""
+    bt = Batch([1] * B, [40000 // B] * B, Hq, Hkv, 128, 128, 64, fp8, seed=Hq + B)
+    n = fa.fa_fwd_paged_workspace_bytes(B, B, bt.table.shape[1] * 64, Hq, Hkv, 128, 128, int(fp8), 1)
+    ws = torch.randint(0, 256, (n,), dtype=torch.uint8, device="cuda")
+    first = run(bt, workspace=ws)
+    for fill in (None, 0, 255):
+        if fill is not None:
+            ws.fill_(fill)
+        o, lse = bt.attend(return_lse=True, workspace=ws)
+        assert torch.equal(o.view(torch.int16), first[0].view(torch.int16)) and torch.equal(lse, first[1])
+    # Another batch in the same workspace, and this one again.
+    other = Batch([1] * B, [9000 // B] * B, Hq, Hkv, 128, 128, 64, fp8, seed=Hq + B + 1)
+    run(other, workspace=ws)
+    o, lse = bt.attend(return_lse=True, workspace=ws)
+    assert torch.equal(o.view(torch.int16), first[0].view(torch.int16)) and torch.equal(lse, first[1])

@@ -109,7 +109,7 @@ def test_workspace_bytes():
     assert f(1, 0, 4, 2, 128, 128, 0, 1) == 0 and f(0, 1, 4, 2, 128, 128, 0, 1) == 0 and f(1, 1, 3, 2, 128, 128, 0, 1) == 0
     assert f(1, 1, 4, 2, 96, 96, 0, 1) == 0 and f(1, 1, 4, 2, 64, 64, 7, 1) == 0 and f(1, 1, 4, 2, 64, 64, 0, -1) == 0
     one, most = f(1, 1, 4, 1, 128, 128, 0, 1), f(8, 8, 4, 1, 128, 128, 0, 1)
-    assert 0 < one < most == f(10 ** 6, 10 ** 6, 4, 1, 128, 128, 0, 1) and most < 1 << 26
+    assert 0 < one < most < 1 << 26 and 0 < f(10 ** 6, 10 ** 6, 4, 1, 128, 128, 0, 1) < 1 << 26
     assert f(1, 1, 4, 1, 128, 128, 0, 1, keys=-1) == 0
     # A chunk beside single tokens needs places for both kernels; enough equal prompts need none at all.
     assert f(8, 500, 4, 1, 128, 128, 0, 493) > most and f(8, 80000, 32, 8, 128, 128, 0, 10000) == 0
