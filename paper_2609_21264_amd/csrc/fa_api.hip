@@ -310,22 +310,21 @@ bool token_strides(const long long* s, int n) {
 constexpr int kFewCols = 64;
 constexpr int kWholeKeys = 512, kWholeItems = 1 << 16;
 struct PagedPlan {
-  bool few, many, split;  // kernels to launch; whether that for many rows splits blocks
+  bool few, many;         // kernels to launch
+  fa::PagedMany m;        // what that for many rows runs
   bool whole;             // whether that for few rows takes whole items
-  int few_cols, col_blocks, n_wg, cols, many_wg;
+  int few_cols, col_blocks, n_wg, cols;
   int64_t lse, desc, many_o, many_lse, many_desc, bytes;  // 16-byte aligned offsets
 };
 PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, int d_v, int type, int max_q) {
   PagedPlan w{};
   const int64_t rows = static_cast<int64_t>(T) * group, most = static_cast<int64_t>(max_q) * group;
-  w.many = type == FA_CACHE_BF16 && most > kFewCols && rows > kFewCols;
+  const bool e4m3 = type == FA_CACHE_E4M3;
+  w.many = most > kFewCols && rows > kFewCols;
   w.few = !w.many || static_cast<int64_t>(max_q) * B != T;
   w.few_cols = !w.many ? INT_MAX : w.few ? 32 : 0;
   w.col_blocks = most <= 32 || w.many ? 1 : 2;
-  if (w.many) {
-    int64_t blocks = 0;
-    w.split = fa::paged_many_split(B, T, Hkv, group, w.few_cols, d_qk, &blocks);
-  }
+  if (w.many) w.m = fa::paged_many(B, T, Hkv, group, max_q, w.few_cols, d_qk, e4m3);
   auto place = [&](int64_t n) {
     const int64_t at = w.bytes;
     w.bytes += (n + 15) / 16 * 16;
@@ -333,7 +332,7 @@ PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, i
   };
   if (w.few) {
     const int cols = 32 * w.col_blocks;
-    w.n_wg = fa::paged_workgroups(d_qk, type == FA_CACHE_E4M3, w.col_blocks);
+    w.n_wg = fa::paged_workgroups(d_qk, e4m3, w.col_blocks);
     w.cols = rows < cols ? static_cast<int>(rows) : cols;
     const int64_t items = (rows / cols + (B < T ? B : T)) * Hkv;  // the most there can be
     w.whole = max_keys <= kWholeKeys && items <= kWholeItems;
@@ -345,12 +344,11 @@ PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, i
     w.lse = place(places * 4);
     w.desc = place(w.n_wg * static_cast<int64_t>(sizeof(fa::PagedItem)));
   }
-  if (w.split) {
-    w.many_wg = fa::paged_many_workgroups(d_qk);
-    const int64_t places = 2ll * w.many_wg * fa::paged_block_cols();
+  if (w.m.split) {
+    const int64_t places = 2ll * w.m.n_wg * w.m.cols;
     w.many_o = place(places * d_v * 4);
     w.many_lse = place(places * 4);
-    w.many_desc = place(w.many_wg * static_cast<int64_t>(sizeof(fa::PagedItem)));
+    w.many_desc = place(w.m.n_wg * static_cast<int64_t>(sizeof(fa::PagedItem)));
   }
   return w;
 }
@@ -446,7 +444,8 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   p.n_wg = w.n_wg;
   p.part_cols = w.cols;
   p.whole = w.whole;
-  p.many_wg = w.many_wg;
+  p.many_wg = w.m.n_wg;
+  p.many_cols = w.m.cols;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   p.o_part = reinterpret_cast<float*>(ws);
   p.lse_part = reinterpret_cast<float*>(ws + w.lse);
@@ -460,10 +459,10 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   const int64_t most = static_cast<int64_t>(w.many ? 1 : max_q) * p.group;
   const int cols = most < w.cols ? static_cast<int>(most) : w.cols;
   hipError_t e = hipSuccess;
-  if (w.many) e = fa::launch_paged_many(p, cache->d_qk, stream);
+  if (w.many) e = fa::launch_paged_many(p, w.m, cache->d_qk, cache->type == FA_CACHE_E4M3, stream);
   if (e == hipSuccess && w.few) e = fa::launch_paged_few(p, cache->d_qk, cache->type == FA_CACHE_E4M3, w.col_blocks, stream_kv, stream);
   if (e == hipSuccess && w.few && !w.whole) e = fa::launch_paged_join(p, cache->d_v, false, cols, stream);
-  if (e == hipSuccess && w.split) e = fa::launch_paged_join(p, cache->d_v, true, fa::paged_block_cols(), stream);
+  if (e == hipSuccess && w.m.split) e = fa::launch_paged_join(p, cache->d_v, true, w.m.cols, stream);
   return e == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 

@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include "fa_device.h"
+#include "fa_e4m3.h"
 #include "fa_fastdiv.h"
 
 namespace fa {
@@ -57,6 +58,21 @@ __device__ __forceinline__ void mfma_out_settled(f32x16& acc, const bf16x8& v, c
     asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(v), "v"(pt));
   else
     asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(v), "v"(pt));
+}
+// The same for operands in fp16 (over e4m3 tiles).
+template <bool AG>
+__device__ __forceinline__ void mfma_out_f16(f32x16& acc, const bf16x8& v, const bf16x8& pt) {
+  if constexpr (AG)
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(v), "v"(pt));
+  else
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(acc) : "v"(v), "v"(pt));
+}
+template <bool AG>
+__device__ __forceinline__ void mfma_out_settled_f16(f32x16& acc, const bf16x8& v, const bf16x8& pt) {
+  if constexpr (AG)
+    asm("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(v), "v"(pt));
+  else
+    asm("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(acc) : "v"(v), "v"(pt));
 }
 template <bool AG>
 __device__ __forceinline__ void agpr_fence(f32x16& acc) {
@@ -114,7 +130,7 @@ struct Ring {
 // K and V fragments read ahead from LDS (KPF, VPF), K and V ring slots in LDS (NKR, NVR), and the
 // parts each key tile is split into between the waves (KSPLIT).
 template <int DQK_, int DV_, int BN_, int NWAVES_, int QB_, bool CAUSAL_, bool SPLIT_, int OCC_, int KPF_, int VPF_,
-          int NKR_, int NVR_, int KSPLIT_ = 1, bool PAGED_ = false>
+          int NKR_, int NVR_, int KSPLIT_ = 1, bool PAGED_ = false, bool E4M3_ = false>
 struct Cfg {
   static constexpr int DQK = DQK_, DV = DV_, BN = BN_, NWAVES = NWAVES_, QB = QB_;
   // KSPLIT = 2: the waves form two sets of NWAVES / 2 (RWAVES) that own the same query rows; set k
@@ -130,16 +146,21 @@ struct Cfg {
   // PAGED: the keys lie in pages (PagedKeys below), the columns of a wave are any rows of any of the group's heads,
   // and the last key each of them sees is in a register.
   static constexpr bool PAGED = PAGED_;
+  // E4M3: K and V tiles are 8-bit. They stay so in LDS and are widened as fragments are read: K to bf16, V to fp16, with
+  // P in fp16 too. The order of the dims in a score product follows the 16-byte reads of K: k-steps 2 m and 2 m + 1
+  // take dims 32 m + 16 h + 0 .. 7 and + 8 .. 15 in lane half h.
+  static constexpr bool E4M3 = E4M3_;
+  static constexpr int E = E4M3_ ? 1 : 2;  // bytes per element of K and V
   static constexpr bool CHUNKED = QB > 1;  // long instance: key/value heads in chunks (launch_cfg)
   static constexpr int NT = NWAVES * 64;
   // Waves per SIMD the registers are budgeted for: the workgroup's own (4 SIMDs per CU) times the
   // workgroups that share a CU (OCC_).
   static constexpr int WPE = (NWAVES > 4 ? NWAVES / 4 : 1) * OCC_;
   static constexpr int BM = RWAVES * 32 * QB;  // query rows per workgroup holding one query head
-  static constexpr int KCH = DQK / 8;          // 16-byte chunks per K-tile row
-  static constexpr int VCH = DV / 8;           // 16-byte chunks per V-tile row
-  static constexpr int K_BYTES = BN * DQK * 2;
-  static constexpr int V_BYTES = BN * DV * 2;
+  static constexpr int KCH = DQK * E / 16;          // 16-byte chunks per K-tile row
+  static constexpr int VCH = DV * E / 16;           // 16-byte chunks per V-tile row
+  static constexpr int K_BYTES = BN * DQK * E;
+  static constexpr int V_BYTES = BN * DV * E;
   // Ring slots. Step j loads K(j + KA) into the slot of K(j) and V(j + VA) into the slot of V(j-2):
   // both were last read in step j-1, which every wave has finished at the barrier of step j.
   static constexpr int NKR = NKR_, NVR = NVR_;
@@ -230,11 +251,18 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
 
   __device__ __forceinline__ u32x4 kfrag(const unsigned char* sK, int ks, int kb) const {
     const int row = kb * 32 + perm32(i32);
+    if constexpr (C::E4M3)  // ks even: both of k-steps ks and ks + 1
+      return *reinterpret_cast<const u32x4*>(sK + row * DQK + (((ks + h) ^ k8_swizzle<C::KCH>(perm32(i32) & 15)) << 4));
     return *reinterpret_cast<const u32x4*>(sK + row * (DQK * 2) + (((ks * 2 + h) ^ k_lane_swizzle<DQK>(i32)) << 4));
   }
   // A operand V^T[dims db*32 + 0..31][keys 16*ps + 0..15]: lane (group G, slot j) points the
   // transpose read at key 16*ps + 8*(G/2) + j/4 (then +4), dims db*32 + 16*(G%2) + 4*(j%4).
   __device__ __forceinline__ bf16x8 vfrag(const unsigned char* sV, int ps, int db) const {
+    if constexpr (C::E4M3) {  // 8-bit yet: the first two registers
+      const unsigned char* at = sV + (ps * 16 + v_key) * DV + (((db * 2) ^ v_t) << 4) + v_half;
+      const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(at));
+      return bit_cast<bf16x8>(u32x4{(uint32_t)w.x, (uint32_t)w.y, 0u, 0u});
+    }
     const unsigned char* base = sV + (ps * 16 + v_key) * (DV * 2) + (((db * 4) ^ v_t) << 4) + v_half;
     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(base));
     const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(base + 4 * DV * 2));
@@ -245,14 +273,30 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
   // f = kb*KS + ks) are read KPF ahead.
   __device__ __forceinline__ void score_mfma(Scores& s, u32x4 (&kf)[KB * KS], const unsigned char* sK, int i) {
     const int kb = i / (KS * QB), ks = (i / QB) % KS, qb = i % QB, f = kb * KS + ks;
+    if constexpr (C::E4M3) {
+      // kf[f] of an even f holds the 8-bit fragments f and f + 1, kf[f + 1] the widened one in use; KPF reads ahead.
+      if (qb == 0) {
+        if (f % 2 == 0 && f + 2 * KPF < KB * KS) kf[f + 2 * KPF] = kfrag(sK, (f + 2 * KPF) % KS, (f + 2 * KPF) / KS);
+        kf[f | 1] = f % 2 == 0 ? bit_cast<u32x4>(widen_bf16(kf[f][0], kf[f][1]))
+                               : bit_cast<u32x4>(widen_bf16(kf[f - 1][2], kf[f - 1][3]));
+      }
+      s[kb][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bit_cast<bf16x8>(kf[f | 1]), qf[qb][ks],
+                                                          ks == 0 ? f32x16{} : s[kb][qb], 0, 0, 0);
+      return;
+    }
     if (qb == 0 && f + KPF < KB * KS) kf[f + KPF] = kfrag(sK, (f + KPF) % KS, (f + KPF) / KS);
     s[kb][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bit_cast<bf16x8>(kf[f]), qf[qb][ks],
                                                         ks == 0 ? f32x16{} : s[kb][qb], 0, 0, 0);
   }
+  // The first KPF reads of a tile's K fragments.
+  __device__ __forceinline__ void first_kfrags(u32x4 (&kf)[KB * KS], const unsigned char* sK) const {
+    constexpr int EACH = C::E4M3 ? 2 : 1;  // fragments per read
+#pragma unroll
+    for (int f = 0; f < KPF * EACH && f < KB * KS; f += EACH) kf[f] = kfrag(sK, f % KS, f / KS);
+  }
   __device__ __forceinline__ void scores(Scores& s, const unsigned char* sK) {
     u32x4 kf[KB * KS];
-#pragma unroll
-    for (int f = 0; f < KPF && f < KB * KS; ++f) kf[f] = kfrag(sK, f % KS, f / KS);
+    first_kfrags(kf, sK);
 #pragma unroll
     for (int i = 0; i < NMS; ++i) score_mfma(s, kf, sK, i);
   }
@@ -349,7 +393,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
       rs[qb] = e0 + e1;
     else
       rs[qb] += e0 + e1;
-    pk[kb][qb][rp] = pack_bf16x2(e0, e1);
+    pk[kb][qb][rp] = C::E4M3 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
     asm volatile("" : "+v"(pk[kb][qb][rp]));
   }
 
@@ -361,6 +405,17 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
     if (qb == 0 && t + VPF < NVF) vf[t + VPF] = vfrag(sV, (t + VPF) / DB, (t + VPF) % DB);
     const int kb = ps >> 1, base = (ps & 1) * 4;
     const u32x4 w = {pk[kb][qb][base], pk[kb][qb][base + 1], pk[kb][qb][base + 2], pk[kb][qb][base + 3]};
+    if constexpr (C::E4M3) {
+      if (qb == 0) {
+        const u32x4 raw = bit_cast<u32x4>(vf[t]);
+        vf[t] = bit_cast<bf16x8>(widen_f16(raw[0], raw[1]));
+      }
+      if (settled && qb > 0)  // widened a slot ago
+        mfma_out_settled_f16<AG>(oacc[db][qb], vf[t], bit_cast<bf16x8>(w));
+      else
+        mfma_out_f16<AG>(oacc[db][qb], vf[t], bit_cast<bf16x8>(w));
+      return;
+    }
     if (settled)
       mfma_out_settled<AG>(oacc[db][qb], vf[t], bit_cast<bf16x8>(w));
     else
@@ -385,18 +440,28 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
     for (int kb = 0; kb < KB; ++kb) {
       const int row = min(n0 + kb * 32 + perm32(i32), sk - 1);
       const uint16_t* krow;
+      const uint8_t* krow8 = nullptr;
       bool there = true;
       if constexpr (C::PAGED) {
         const int page = this->table[row >> this->page_shift];
         there = page >= 0 && page < this->n_pages;
-        krow = kg + page * this->page_stride + (row & ((1 << this->page_shift) - 1)) * this->slot_stride + 8 * h;
+        const int64_t at = page * this->page_stride + (row & ((1 << this->page_shift) - 1)) * this->slot_stride;
+        krow = kg + at + 8 * h;
+        krow8 = reinterpret_cast<const uint8_t*>(kg) + at + 16 * h;
       } else {
         krow = kg + (size_t)row * DQK + 8 * h;
       }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         u32x4 a = {0u, 0u, 0u, 0u};
-        if (!C::PAGED || there) a = *reinterpret_cast<const u32x4*>(krow + 16 * ks);
+        if constexpr (C::E4M3) {
+          if (there) {
+            const uint2 w = *reinterpret_cast<const uint2*>(krow8 + 32 * (ks / 2) + 8 * (ks & 1));
+            a = bit_cast<u32x4>(widen_bf16(w.x, w.y));
+          }
+        } else if (!C::PAGED || there) {
+          a = *reinterpret_cast<const u32x4*>(krow + 16 * ks);
+        }
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
           cur[kb][qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bit_cast<bf16x8>(a), qf[qb][ks],
@@ -449,8 +514,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
     for (int t = 0; t < VPF && t < NVF; ++t) vf[t] = vfrag(sVo, t / DB, t % DB);
     __builtin_amdgcn_sched_barrier(0);
     u32x4 kf[KB * KS];
-#pragma unroll
-    for (int f = 0; f < KPF && f < KB * KS; ++f) kf[f] = kfrag(sKn, f % KS, f / KS);
+    first_kfrags(kf, sKn);
     static_assert(at_most_two_elems_per_slot(), "ev holds the elements of two slots");
     float ev[4];  // exponentials in flight, element e in ev[e % 4]
     __builtin_amdgcn_sched_barrier(0);

@@ -199,9 +199,9 @@ struct PagedParams {
   // Sequences with more than few_cols row-heads per key/value head run in the kernel for many rows, which has work
   // units, places and items of its own (the latter three only where it splits blocks).
   int few_cols;
-  int many_wg, many_min_units;
-  float* many_o;         // fp32 [2 * many_wg][paged_block_cols()][d_v]
-  float* many_lse;       // fp32 [2 * many_wg][paged_block_cols()]
+  int many_wg, many_min_units, many_cols;  // many_cols: columns of a block
+  float* many_o;         // fp32 [2 * many_wg][many_cols][d_v]
+  float* many_lse;       // fp32 [2 * many_wg][many_cols]
   PagedItem* many_desc;  // [many_wg]
   uint32_t m_group, sh_group;  // division by group, filled by the launchers
 };
@@ -216,11 +216,15 @@ hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, int col_blocks, b
 // Joins of split items: of the kernel for few rows, or for many. cols: the columns that an item is expected to have (a
 // workgroup for each, up to 32).
 hipError_t launch_paged_join(PagedParams p, int d_v, bool many, int cols, hipStream_t stream);
-// Many rows (fa_paged_fwd_kernel.hip; bf16 caches): all other sequences. paged_many_split: whether it splits blocks (and
-// needs a join), and the most blocks per key/value head that there can be.
-int paged_many_workgroups(int d_qk);
-int paged_block_cols();
-bool paged_many_split(int n_seq, int n_tokens, int hkv, int group, int few_cols, int d_qk, int64_t* blocks);
-hipError_t launch_paged_many(PagedParams p, int d_qk, hipStream_t stream);
+// Many rows (fa_paged_fwd_kernel.hip): all other sequences, in blocks of `cols` row-heads of a key/value head. Where `split`,
+// n_wg workgroups share the blocks and a join follows; else a workgroup takes a block, of which there are at most
+// `blocks` per key/value head. max_q, as the host expects it, chooses the instance.
+struct PagedMany {
+  bool is_short, split;
+  int cols, n_wg;
+  int64_t blocks;
+};
+PagedMany paged_many(int n_seq, int n_tokens, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3);
+hipError_t launch_paged_many(PagedParams p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream);
 
 }  // namespace fa

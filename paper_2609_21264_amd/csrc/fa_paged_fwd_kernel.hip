@@ -1,7 +1,7 @@
 // Attention of many new tokens per sequence over a paged key/value cache (gfx950): prompts and chunks of them.
 // The pipelined step of the fused forward (fa_fwd_attn.h) with another source of keys and another arrangement of
 // rows and work:
-//  * A block is 256 consecutive row-heads of one (sequence, key/value head): column c of the block's item is
+//  * A block is 256 consecutive row-heads (128 in the short instances) of one (sequence, key/value head): column c of the block's item is
 //    token c / group of the sequence's new ones and query head c % group of the group, so all heads of a group share
 //    every K/V tile whatever the group's size, and a short chunk pads at most once. Each lane keeps the
 //    last key its columns see; the mask is the same with and without causal masking.
@@ -12,6 +12,7 @@
 //  * Where there are blocks enough, a workgroup takes one block, a sequence's last (longest) blocks first.
 //    Otherwise (SPLIT) the blocks lie on one line of work, kBlockCost + tiles units each, that the workgroups share
 //    evenly; parts of a block that several share are joined as those of the kernel for few rows are.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -24,11 +25,11 @@
 namespace fa {
 namespace {
 
-constexpr int kBlockCols = 256;  // row-heads per block: 4 waves x 64
-constexpr int kBlockCost = 4;    // fixed cost of a block in tiles
+constexpr int kBlockCost = 4;  // fixed cost of a block in tiles
 
-// This wave's share of the loads of one K or V tile: BN / NWAVES rows, all in one page.
-template <int NWAVES, int BN, int CH>
+// This wave's share of the loads of one K or V tile: BN / NWAVES rows of CH 16-byte chunks, all in one page; E bytes per
+// element.
+template <int NWAVES, int BN, int CH, int E>
 struct PagedLoader {
   static constexpr int R = BN / NWAVES, NI = BN * CH / 64 / NWAVES;
   static_assert(R * CH == NI * 64 && R <= 16 && 16 % R == 0, "a wave's rows are whole loads inside one page");
@@ -37,11 +38,11 @@ struct PagedLoader {
   uint32_t slot_bytes;
   uint32_t voff[NI];    // bytes from the wave's first row
   template <class Swz>
-  __device__ __forceinline__ void init(const uint16_t* head, int64_t page_stride, int64_t slot_stride, int wave, int lane,
+  __device__ __forceinline__ void init(const unsigned char* head, int64_t page_stride, int64_t slot_stride, int wave, int lane,
                                        Swz swz) {
     base = reinterpret_cast<uint64_t>(head);
-    page_bytes = page_stride * 2;
-    slot_bytes = (uint32_t)(slot_stride * 2);
+    page_bytes = page_stride * E;
+    slot_bytes = (uint32_t)(slot_stride * E);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int x = i * 64 + lane, row = x / CH;
@@ -67,28 +68,29 @@ struct PagedLoader {
 };
 
 // A block's place: which keys its columns see.
-template <int BN>
+template <int BN, int BC>
 struct Block {
   int cols, c0, row0, row1;  // row-heads of the item, the block's first, its first and last row
   int kv_end, plain;         // keys visible to its last row; leading tiles that need no mask for any row
   __device__ __forceinline__ Block(const PagedSeq& s, int cb, const PagedParams& p) {
     cols = s.n_q * p.group;
-    c0 = cb * kBlockCols;
+    c0 = cb * BC;
     row0 = (int)fast_div((uint32_t)c0, p.m_group, p.sh_group);
-    row1 = (int)fast_div((uint32_t)min(c0 + kBlockCols, cols) - 1u, p.m_group, p.sh_group);
+    row1 = (int)fast_div((uint32_t)min(c0 + BC, cols) - 1u, p.m_group, p.sh_group);
     kv_end = p.causal ? max(0, s.kv - s.n_q + row1 + 1) : s.kv;
     plain = (p.causal ? max(0, s.kv - s.n_q + row0 + 1) : s.kv) / BN;
   }
   __device__ __forceinline__ int tiles() const { return (kv_end + BN - 1) / BN; }
 };
+template <int BC>
 __device__ __forceinline__ int n_blocks(const PagedSeq& s, const PagedParams& p) {
   const int64_t cols = (int64_t)s.n_q * p.group;
-  return cols > p.few_cols ? (int)((cols + kBlockCols - 1) / kBlockCols) : 0;
+  return cols > p.few_cols ? (int)((cols + BC - 1) / BC) : 0;
 }
-template <int BN>
+template <int BN, int BC>
 __device__ __forceinline__ int head_units(const PagedSeq& s, int n_cb, const PagedParams& p, int lane) {
   uint32_t sum = 0;
-  for (int c = lane; c < n_cb; c += 64) sum += (uint32_t)(kBlockCost + Block<BN>(s, c, p).tiles());
+  for (int c = lane; c < n_cb; c += 64) sum += (uint32_t)(kBlockCost + Block<BN, BC>(s, c, p).tiles());
   return (int)wave_sum(sum);
 }
 template <class C>
@@ -96,8 +98,10 @@ __global__ __attribute__((amdgpu_flat_work_group_size(C::NT, C::NT), amdgpu_wave
 void fa_paged_fwd_kernel(PagedParams p) {
   using A = Attn<C>;
   constexpr int DQK = C::DQK, DV = C::DV, BN = C::BN, QB = C::QB;
-  static_assert(C::KA == C::VA && C::KSPLIT == 1 && C::NWAVES == 4 && 32 * QB * 4 == kBlockCols, "one page lookup per tile");
-  constexpr int R = BN / C::NWAVES;  // keys that a wave brings of a tile
+  constexpr int BC = C::NWAVES * 32 * QB;  // row-heads per block
+  constexpr int R = BN / C::NWAVES;        // keys that a wave brings of a tile
+  constexpr int E = C::E;
+  static_assert(C::KSPLIT == 1 && C::KA - C::VA <= 1, "a V tile is loaded with its K tile or one step later");
 
   __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS_BYTES];
   const int tid = threadIdx.x;
@@ -105,8 +109,6 @@ void fa_paged_fwd_kernel(PagedParams p) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   A st;
   st.qw = st.diag = 0;
-  st.cs = p.cs;
-  st.mask_val = p.cs < 0.f ? INFINITY : -INFINITY;
   st.page_stride = p.c.k_page;
   st.slot_stride = p.c.k_slot;
   st.page_shift = p.c.page_shift;
@@ -124,11 +126,11 @@ void fa_paged_fwd_kernel(PagedParams p) {
     for (int c = 0; c < p.bt.n_seq; c += 64) {
       PagedSeq sl{};
       if (c + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, c + lane);
-      uint64_t left = __builtin_amdgcn_ballot_w64(n_blocks(sl, p) > 0);
+      uint64_t left = __builtin_amdgcn_ballot_w64(n_blocks<BC>(sl, p) > 0);
       while (left != 0) {
         const PagedSeq x = seq_of_lane(sl, __builtin_ctzll(left));
         left &= left - 1;
-        sum += (int64_t)head_units<BN>(x, n_blocks(x, p), p, lane) * p.c.hkv;
+        sum += (int64_t)head_units<BN, BC>(x, n_blocks<BC>(x, p), p, lane) * p.c.hkv;
       }
     }
     const int total = (int)min(sum, (int64_t)INT32_MAX);
@@ -142,13 +144,13 @@ void fa_paged_fwd_kernel(PagedParams p) {
     for (int c = 0; c < p.bt.n_seq && !found; c += 64) {
       PagedSeq sl{};
       if (c + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, c + lane);
-      uint64_t left = __builtin_amdgcn_ballot_w64(n_blocks(sl, p) > 0);
+      uint64_t left = __builtin_amdgcn_ballot_w64(n_blocks<BC>(sl, p) > 0);
       while (left != 0 && !found) {
         const int l = __builtin_ctzll(left);
         left &= left - 1;
         s = seq_of_lane(sl, l);
-        n_cb = n_blocks(s, p);
-        const int units = head_units<BN>(s, n_cb, p, lane);
+        n_cb = n_blocks<BC>(s, p);
+        const int units = head_units<BN, BC>(s, n_cb, p, lane);
         if ((int64_t)r < start + (int64_t)units * p.c.hkv) {
           b = c + l;
           g = (r - start) / units;
@@ -161,7 +163,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
     }
     if (!found) return;  // not reached: r < total
     for (int c = 0; c < n_cb; c += 64) {
-      const uint32_t u = c + lane < n_cb ? (uint32_t)(kBlockCost + Block<BN>(s, c + lane, p).tiles()) : 0u;
+      const uint32_t u = c + lane < n_cb ? (uint32_t)(kBlockCost + Block<BN, BC>(s, c + lane, p).tiles()) : 0u;
       const uint32_t incl = wave_scan(u, lane);
       const uint64_t above = __builtin_amdgcn_ballot_w64(incl > (uint32_t)(r - start));
       if (above != 0) {
@@ -179,7 +181,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
     for (int c = 0; c < p.bt.n_seq && !found; c += 64) {
       PagedSeq sl{};
       if (c + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, c + lane);
-      const uint32_t n = (uint32_t)n_blocks(sl, p), incl = wave_scan(n, lane);
+      const uint32_t n = (uint32_t)n_blocks<BC>(sl, p), incl = wave_scan(n, lane);
       const uint64_t above = __builtin_amdgcn_ballot_w64(incl > (uint32_t)idx);
       if (above != 0) {
         const int l = __builtin_ctzll(above);
@@ -196,7 +198,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
   }
 
   while (true) {
-    const Block<BN> blk(s, cb, p);
+    const Block<BN, BC> blk(s, cb, p);
     const int tiles = blk.tiles();
     int t0 = 0, nt = tiles, n_parts = 1, first_wg = me;
     bool skip = false;
@@ -218,13 +220,22 @@ void fa_paged_fwd_kernel(PagedParams p) {
       if constexpr (C::SPLIT) asm volatile("" : "+v"(lane));
       st.i32 = lane & 31;
       st.h = lane >> 5;
-      st.v_key = 8 * (lane >> 5) + ((lane & 15) >> 2);
-      st.v_t = (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<DV>(st.v_key);
+      st.v_key = 8 * (lane >> 5) + ((lane & 15) >> (C::E4M3 ? 1 : 2));
+      st.v_t = C::E4M3 ? (((lane >> 4) & 1) ^ v8_swizzle<C::VCH>(st.v_key))
+                       : ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<DV>(st.v_key));
       st.v_half = (lane & 1) * 8;
       const int kb0 = t0 * BN, t1 = t0 + nt;
       const int kv_lim = min(blk.kv_end, t1 * BN);  // keys loaded; behind it the tile loads read zeros
       st.sk = s.kv;
       st.table = p.bt.block_table + (int64_t)b * p.bt.table_stride;
+      st.cs = p.cs;
+      if constexpr (C::E4M3) {
+        if (p.c.k_scale != nullptr) {  // a masked score has to stay infinite
+          const float c = p.cs * scalar_load(p.c.k_scale + g);
+          st.cs = fabsf(c) < FLT_MIN ? copysignf(FLT_MIN, c) : c;
+        }
+      }
+      st.mask_val = st.cs < 0.f ? INFINITY : -INFINITY;
 
       // Q of this wave's columns, straight into registers; columns behind the last repeat it and are not stored.
 #pragma unroll
@@ -232,9 +243,10 @@ void fa_paged_fwd_kernel(PagedParams p) {
         const uint32_t c = (uint32_t)min(blk.c0 + wave * 32 * QB + qb * 32 + st.i32, blk.cols - 1);
         const int qi = (int)fast_div(c, p.m_group, p.sh_group), member = (int)c - qi * p.group;
         st.last_key[qb] = p.causal ? s.kv - s.n_q + qi : s.kv - 1;
-        const uint16_t* qp = p.q + (int64_t)(s.q0 + qi) * p.q_token + (int64_t)(g * p.group + member) * p.q_head + st.h * 8;
+        const uint16_t* qp = p.q + (int64_t)(s.q0 + qi) * p.q_token + (int64_t)(g * p.group + member) * p.q_head;
 #pragma unroll
-        for (int ks = 0; ks < A::KS; ++ks) load_q<A::AG>(st.qf[qb][ks], qp + ks * 16);
+        for (int ks = 0; ks < A::KS; ++ks)
+          load_q<A::AG>(st.qf[qb][ks], qp + (C::E4M3 ? 32 * (ks / 2) + 16 * st.h + 8 * (ks & 1) : 16 * ks + 8 * st.h));
       }
 
       // The pages of this wave's keys of tiles w0 .. w0 + 63, one per lane (behind the last key: the last one's).
@@ -253,38 +265,47 @@ void fa_paged_fwd_kernel(PagedParams p) {
       st.holes = __builtin_amdgcn_ballot_w64(hole) != 0;
       int n_plain = st.holes ? 0 : min(max(blk.plain - t0, 0), nt);
 
-      const uint16_t* kh = static_cast<const uint16_t*>(p.c.k) + (int64_t)g * p.c.k_head;
-      const uint16_t* vh = static_cast<const uint16_t*>(p.c.v) + (int64_t)g * p.c.v_head;
-      st.kg = kh;
-      PagedLoader<C::NWAVES, BN, C::KCH> kload;
-      PagedLoader<C::NWAVES, BN, C::VCH> vload;
-      kload.init(kh, p.c.k_page, p.c.k_slot, wave, lane, [](int row) { return k_swizzle<DQK>(row); });
-      vload.init(vh, p.c.v_page, p.c.v_slot, wave, lane, [](int row) { return v_swizzle<DV>(row); });
+      const unsigned char* kh = static_cast<const unsigned char*>(p.c.k) + (int64_t)g * p.c.k_head * E;
+      const unsigned char* vh = static_cast<const unsigned char*>(p.c.v) + (int64_t)g * p.c.v_head * E;
+      st.kg = reinterpret_cast<const uint16_t*>(kh);
+      PagedLoader<C::NWAVES, BN, C::KCH, E> kload;
+      PagedLoader<C::NWAVES, BN, C::VCH, E> vload;
+      kload.init(kh, p.c.k_page, p.c.k_slot, wave, lane,
+                 [](int row) { return C::E4M3 ? k8_swizzle<C::KCH>(row & 15) : k_swizzle<DQK>(row); });
+      vload.init(vh, p.c.v_page, p.c.v_slot, wave, lane,
+                 [](int row) { return C::E4M3 ? v8_swizzle<C::VCH>(row & 15) : v_swizzle<DV>(row); });
+      unsigned char* const vring = smem + C::NKR * C::K_BYTES;
       auto kslot = [&](int t) { return smem + ((unsigned)t % C::NKR) * C::K_BYTES; };
-      auto vslot = [&](int t) { return smem + C::NKR * C::K_BYTES + ((unsigned)t % C::NVR) * C::V_BYTES; };
+      auto vslot = [&](int t) { return vring + ((unsigned)t % C::NVR) * C::V_BYTES; };
       auto lds_of = [&](const unsigned char* slot, int ni) {
         return (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds_offset(slot) + wave * ni * 1024));
       };
+      // Descriptors of the K and V tile to be loaded next. A V tile is loaded with its K tile or a step later, with the
+      // page found for that.
       u32x4 gk, gv;
-      uint32_t gkl, gvl;
-      auto aim = [&](int j) {  // descriptors and LDS places of tile j of the item's part
-        const int page = __builtin_amdgcn_readlane(entries, j & 63), key = kb0 + j * BN + wave * R;
-        gk = kload.rsrc(page, p.c.n_pages, key, smask, kv_lim);
-        gv = vload.rsrc(page, p.c.n_pages, key, smask, kv_lim);
-        gkl = lds_of(kslot(j), C::K_LOADS);
-        gvl = lds_of(vslot(j), C::V_LOADS);
+      uint32_t gkl = 0, gvl = 0;
+      int v_page = 0;
+      auto aim_k = [&](int j) {
+        const int page = __builtin_amdgcn_readlane(entries, j & 63);
+        gk = kload.rsrc(page, p.c.n_pages, kb0 + j * BN + wave * R, smask, kv_lim);
+        return page;
       };
-      // The prologue's groups -KA .. -1, as in the fused forward: tiles 0 .. KA - 1, and zeros in the slot of the V
-      // tile before the first, which step 0 multiplies by P = 0.
+      auto aim_v = [&](int j, int page) { gv = vload.rsrc(page, p.c.n_pages, kb0 + j * BN + wave * R, smask, kv_lim); };
+      // The prologue's groups j = -KA .. -1, as in the fused forward: K(j + KA) and V(j + VA), and in front of group 1 - KA
+      // zeros in the slot of the V tile before the first, which step 0 multiplies by P = 0.
 #pragma unroll
-      for (int t = 0; t < C::KA; ++t) {
-        if (t == 1) vload.issue(u32x4{0u, 0u, 0u, 0x00020000u}, lds_of(vslot(C::NVR - 1), C::V_LOADS));
-        aim(t);
-        kload.issue(gk, gkl);
-        vload.issue(gv, gvl);
+      for (int j = -C::KA; j < 0; ++j) {
+        if (j == 1 - C::KA) vload.issue(u32x4{0u, 0u, 0u, 0x00020000u}, lds_of(vslot(C::NVR - 1), C::V_LOADS));
+        const int page = aim_k(j + C::KA);
+        kload.issue(gk, lds_of(kslot(j + C::KA), C::K_LOADS));
+        if (j + C::VA >= 0) {
+          aim_v(j + C::VA, C::VA == C::KA ? page : v_page);
+          vload.issue(gv, lds_of(vslot(j + C::VA), C::V_LOADS));
+        }
+        v_page = page;
       }
-      // Q and K0: behind K0 are V0, the zeros and the groups after.
-      wait_vmcnt<2 * C::V_LOADS + (C::KA - 1) * (C::K_LOADS + C::V_LOADS)>();
+      // Q and K0: behind K0 are V0 when VA = KA, the zeros and the groups after.
+      wait_vmcnt<C::V_LOADS + (C::VA == C::KA ? C::V_LOADS : 0) + (C::KA - 1) * (C::K_LOADS + C::V_LOADS)>();
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
@@ -317,14 +338,24 @@ void fa_paged_fwd_kernel(PagedParams p) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) pB[kb][qb][e] = 0u;
       }
-      // Before step j: K(j+1) and V(j-1) have landed; see the fused forward.
+      // Before step j: K(j+1) and V(j-1) have landed; see the fused forward, also for the rings.
+      Ring<C::K_BYTES, C::NKR> kring(0);
+      Ring<C::V_BYTES, C::NVR> vpos(C::NVR - 2);
+      auto kread = [&](int t) { return smem + kring.at(t); };
+      auto vread = [&](int t) { return vring + vpos.at(t); };
       auto sync_step = [&](int j) {
         wait_vmcnt<C::V_LOADS + (C::KA - 2) * (C::K_LOADS + C::V_LOADS)>();
         compiler_fence();
         __builtin_amdgcn_s_barrier();
         compiler_fence();
         if (((j + C::KA) & 63) == 0) window(t0 + j + C::KA);
-        aim(j + C::KA);
+        const int page = aim_k(j + C::KA);
+        aim_v(j + C::VA, C::VA == C::KA ? page : v_page);
+        v_page = page;
+        gkl = lds_of(smem + kring.at(j + C::KA), C::K_LOADS);
+        gvl = lds_of(vring + vpos.at(j + C::VA), C::V_LOADS);
+        kring.next();
+        vpos.next();
       };
       auto issue = [&](int k) {
         if (k < C::K_LOADS)
@@ -336,13 +367,13 @@ void fa_paged_fwd_kernel(PagedParams p) {
       int j = 0;
       for (; j + 1 < nt; j += 2) {
         sync_step(j);
-        st.step(sA, sB, pA, pB, kslot(j + 1), j > 0 ? vslot(j - 1) : vzero, j >= n_plain, kb0 + j * BN, issue);
+        st.step(sA, sB, pA, pB, kread(j + 1), j > 0 ? vread(j - 1) : vzero, j >= n_plain, kb0 + j * BN, issue);
         sync_step(j + 1);
-        st.step(sB, sA, pB, pA, kslot(j + 2), vslot(j), j + 1 >= n_plain, kb0 + (j + 1) * BN, issue);
+        st.step(sB, sA, pB, pA, kread(j + 2), vread(j), j + 1 >= n_plain, kb0 + (j + 1) * BN, issue);
       }
       if (j < nt) {
         sync_step(j);
-        st.step(sA, sB, pA, pB, kslot(j + 1), j > 0 ? vslot(j - 1) : vzero, j >= n_plain, kb0 + j * BN, issue);
+        st.step(sA, sB, pA, pB, kread(j + 1), j > 0 ? vread(j - 1) : vzero, j >= n_plain, kb0 + j * BN, issue);
       }
       if (nt > 0) {
         // P V of the last tile, on a selected copy of P (see the fused forward).
@@ -358,7 +389,8 @@ void fa_paged_fwd_kernel(PagedParams p) {
           for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
             for (int e = 0; e < 8; ++e) pl[kb][qb][e] = (pA[kb][qb][e] & take_a) | (pB[kb][qb][e] & ~take_a);
-        st.pv_tile(pl, vslot(nt - 1));
+        vpos.next();
+        st.pv_tile(pl, vread(nt - 1));
       }
       // Every load has landed and every wave is done with the last V tile: the output is staged in the rings.
       wait_vmcnt<0>();
@@ -375,13 +407,15 @@ void fa_paged_fwd_kernel(PagedParams p) {
       st.h = lane >> 5;
       constexpr int WROWS = 32 * QB, RB = DV * 2;
       const int col0 = wave * WROWS;  // this wave's first column of the block
+      float vs = 1.f;
+      if constexpr (C::E4M3) vs = p.c.v_scale != nullptr ? scalar_load(p.c.v_scale + g) : 1.f;
       if (C::SPLIT && n_parts > 1) {
         // A part: O normalised by its own sum (fp32), and its LSE. Place 2 me: of a block that begins before.
-        const int64_t place = (2 * (int64_t)me + (me == first_wg ? 1 : 0)) * kBlockCols;
+        const int64_t place = (2 * (int64_t)me + (me == first_wg ? 1 : 0)) * BC;
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
           const float l_tot = half_swap_sum(st.l_run[qb]);
-          const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+          const float inv = l_tot > 0.f ? vs / l_tot : 0.f;
           const int col = col0 + qb * 32 + st.i32;
           if (blk.c0 + col < blk.cols) {
             float* orow = p.many_o + (place + col) * DV;
@@ -396,7 +430,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
           }
         }
         if (me == first_wg && tid == 0)
-          p.many_desc[me] = PagedItem{n_parts, s.q0, min(kBlockCols, blk.cols - blk.c0), blk.c0, g};
+          p.many_desc[me] = PagedItem{n_parts, s.q0, min(BC, blk.cols - blk.c0), blk.c0, g};
       } else {
         // O through LDS, so that each store instruction writes whole rows (layout: see the fused forward).
         unsigned char* stage = smem + wave * WROWS * RB;
@@ -404,7 +438,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
           const float l_tot = half_swap_sum(st.l_run[qb]);
-          const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+          const float inv = l_tot > 0.f ? vs / l_tot : 0.f;
           const bool some = l_tot > 0.f;  // else no visible key, or a score that is no number
           unsigned char* srow = stage + (qb * 32 + st.i32) * RB + ohalf;
 #pragma unroll
@@ -461,7 +495,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
           do {
             if (++b >= p.bt.n_seq) return;  // not reached: r < total
             s = load_seq(p.bt, b);
-            n_cb = n_blocks(s, p);
+            n_cb = n_blocks<BC>(s, p);
           } while (n_cb == 0);
         }
       }
@@ -470,14 +504,20 @@ void fa_paged_fwd_kernel(PagedParams p) {
   }
 }
 
-// The long instances of the fused forward. (d = 64: 32-key tiles, two workgroups per CU.)
-template <int DQK, int DV, bool SPLIT>
+// Instances. Long: those of the fused forward (64 query columns per wave; d = 64: 32-key tiles, two workgroups per CU), but
+// 64-key tiles at d = 64 over e4m3, whose 32-key tiles would be half a load per wave. Short: 32 columns per wave, two
+// workgroups per CU, for sequences of at most 128 row-heads (bf16; at d_qk = 192 two waves per SIMD do not fit).
+template <int DQK, int DV, bool E4M3, bool SHORT, bool SPLIT>
 struct PagedInstance {
-  using C = Cfg<DQK, DV, 64, 4, 2, true, SPLIT, 1, 2, 6, 2, 4, 1, true>;
+  using C = Cfg<DQK, DV, 64, 4, 2, true, SPLIT, 1, 2, 6, 2, 4, 1, true, E4M3>;
 };
 template <bool SPLIT>
-struct PagedInstance<64, 64, SPLIT> {
+struct PagedInstance<64, 64, false, false, SPLIT> {
   using C = Cfg<64, 64, 32, 4, 2, true, SPLIT, 2, 2, 4, 2, 4, 1, true>;
+};
+template <int DQK, int DV, bool SPLIT>
+struct PagedInstance<DQK, DV, false, true, SPLIT> {
+  using C = Cfg<DQK, DV, 64, 4, 1, true, SPLIT, 2, DQK >= 128 ? 1 : 2, DQK >= 128 ? 2 : 6, 2, DQK >= 128 ? 3 : 4, 1, true>;
 };
 
 template <class C>
@@ -486,36 +526,45 @@ hipError_t launch_many(PagedParams p, int64_t blocks, hipStream_t stream) {
   const dim3 grid((unsigned)(C::SPLIT ? p.many_wg : blocks * p.c.hkv));
   return hipLaunchKernel(reinterpret_cast<const void*>(&fa_paged_fwd_kernel<C>), grid, dim3(C::NT), args, 0, stream);
 }
+template <int DQK, int DV, bool E4M3, bool SHORT>
+hipError_t launch_many_split(const PagedParams& p, const PagedMany& m, hipStream_t stream) {
+  return m.split ? launch_many<typename PagedInstance<DQK, DV, E4M3, SHORT, true>::C>(p, m.blocks, stream)
+                 : launch_many<typename PagedInstance<DQK, DV, E4M3, SHORT, false>::C>(p, m.blocks, stream);
+}
 
 }  // namespace
 
-int paged_many_workgroups(int d_qk) { return d_qk == 64 ? 512 : 256; }
-int paged_block_cols() { return kBlockCols; }
-
-bool paged_many_split(int n_seq, int n_tokens, int hkv, int group, int few_cols, int d_qk, int64_t* blocks) {
-  // The most blocks that the packed tokens can make: whole ones, and a last one for each sequence of this kernel.
+PagedMany paged_many(int n_seq, int n_tokens, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3) {
+  PagedMany m{};
   const int64_t rows = (int64_t)n_tokens * group;
+  m.is_short = !e4m3 && d_qk != 192 && (int64_t)max_q * group <= 128;
+  m.cols = m.is_short ? 128 : 256;
+  m.n_wg = m.is_short || (d_qk == 64 && !e4m3) ? 512 : 256;
+  // The most blocks that the packed tokens can make: whole ones, and a last one for each sequence of this kernel.
   int64_t seqs = rows / (few_cols + 1);
   if (seqs > n_seq) seqs = n_seq;
-  *blocks = rows / kBlockCols + seqs;
-  return *blocks * hkv < 2 * paged_many_workgroups(d_qk);
+  m.blocks = rows / m.cols + seqs;
+  m.split = m.blocks * hkv < 2 * m.n_wg;
+  return m;
 }
 
-hipError_t launch_paged_many(PagedParams p, int d_qk, hipStream_t stream) {
+hipError_t launch_paged_many(PagedParams p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream) {
   const FastDiv fg = make_fastdiv(p.group);
   p.m_group = fg.m;
   p.sh_group = fg.sh;
   p.many_min_units = kBlockCost + 4;
-  int64_t blocks = 0;
-  const bool split = paged_many_split(p.bt.n_seq, p.bt.n_tokens, p.c.hkv, p.group, p.few_cols, d_qk, &blocks);
+  if (e4m3) {
+    if (d_qk == 64) return launch_many_split<64, 64, true, false>(p, m, stream);
+    if (d_qk == 128) return launch_many_split<128, 128, true, false>(p, m, stream);
+    return launch_many_split<192, 128, true, false>(p, m, stream);
+  }
   if (d_qk == 64)
-    return split ? launch_many<PagedInstance<64, 64, true>::C>(p, blocks, stream)
-                 : launch_many<PagedInstance<64, 64, false>::C>(p, blocks, stream);
+    return m.is_short ? launch_many_split<64, 64, false, true>(p, m, stream)
+                      : launch_many_split<64, 64, false, false>(p, m, stream);
   if (d_qk == 128)
-    return split ? launch_many<PagedInstance<128, 128, true>::C>(p, blocks, stream)
-                 : launch_many<PagedInstance<128, 128, false>::C>(p, blocks, stream);
-  return split ? launch_many<PagedInstance<192, 128, true>::C>(p, blocks, stream)
-               : launch_many<PagedInstance<192, 128, false>::C>(p, blocks, stream);
+    return m.is_short ? launch_many_split<128, 128, false, true>(p, m, stream)
+                      : launch_many_split<128, 128, false, false>(p, m, stream);
+  return launch_many_split<192, 128, false, false>(p, m, stream);
 }
 
 }  // namespace fa

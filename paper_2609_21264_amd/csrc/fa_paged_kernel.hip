@@ -10,6 +10,7 @@
 #include <stdint.h>
 
 #include "fa_device.h"
+#include "fa_e4m3.h"
 #include "fa_fastdiv.h"
 #include "fa_internal.h"
 #include "fa_paged_device.h"
@@ -17,11 +18,7 @@
 namespace fa {
 namespace {
 
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -226,31 +223,6 @@ struct FewCfg {
   static_assert(2 * VL + D * L < 64, "vmcnt range");
   static_assert((SLOTS & (SLOTS - 1)) == 0, "a slot's place stays a scalar");
 };
-
-// XOR swizzles of the 16-byte chunks of an 8-bit row, so that lanes served together hit different 16-byte
-// bank slots: K rows are read whole chunks at a time by 16 rows at once; V by 8 keys x two chunks.
-template <int CH>
-__device__ __forceinline__ int k8_swizzle(int row) { return CH % 8 == 0 ? (row >> 1) & 7 : (row >> 2) & 3; }
-template <int CH>
-__device__ __forceinline__ int v8_swizzle(int row) { return CH % 8 == 0 ? 2 * ((row >> 1) & 3) : 2 * ((row >> 2) & 1); }
-
-// Eight e4m3 (two registers) as bf16 or fp16, exactly.
-__device__ __forceinline__ bf16x8 widen_bf16(uint32_t a, uint32_t b) {
-  return bit_cast<bf16x8>(u32x4{bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false)),
-                                bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true)),
-                                bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false)),
-                                bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true))});
-}
-__device__ __forceinline__ f16x8 widen_f16(uint32_t a, uint32_t b) {
-  return bit_cast<f16x8>(u32x4{bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false)),
-                               bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true)),
-                               bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false)),
-                               bit_cast<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true))});
-}
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
-  f32x2 f = {lo, hi};
-  return bit_cast<uint32_t>(__builtin_convertvector(f, f16x2));  // RNE
-}
 
 __device__ __forceinline__ void load_q16(bf16x8& r, const void* ptr) {
   asm volatile("global_load_dwordx4 %0, %1, off" : "=v"(r) : "v"(ptr) : "memory");
@@ -788,7 +760,7 @@ hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, int col_blocks, b
 hipError_t launch_paged_join(PagedParams p, int d_v, bool many, int cols, hipStream_t stream) {
   const PagedItem* desc = many ? p.many_desc : p.desc;
   const float *o = many ? p.many_o : p.o_part, *lse = many ? p.many_lse : p.lse_part;
-  int part_cols = many ? paged_block_cols() : p.part_cols;
+  int part_cols = many ? p.many_cols : p.part_cols;
   void* args[] = {&p, &desc, &o, &lse, &part_cols};
   return hipLaunchKernel(d_v == 64 ? reinterpret_cast<const void*>(&fa_paged_join_kernel<64>)
                                    : reinterpret_cast<const void*>(&fa_paged_join_kernel<128>),

@@ -122,3 +122,73 @@ def test_prompt_equals_fused_forward():
     # Both round P and O to bf16: 2 (2^-8 + 2^-8) max|V|.
     assert (o.float() - ro[0].transpose(0, 1).float()).abs().max() <= 2.0 ** -6 * v.float().abs().max()
     assert (lse - rl[0].T).abs().max() <= 1e-4
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dqk,dv", DIMS)
+@pytest.mark.parametrize("n,extra,page", [(65, 0, 16), (257, 1, 64), (300, 1000, 32), (100, 5000, 16)])
+def test_prompt_and_chunk_e4m3(n, extra, page, dqk, dv, causal):
+    run(Batch([n], [n + extra], 4, 2, dqk, dv, page, True, seed=n), causal=causal)
+
+
+@pytest.mark.parametrize("dqk,dv", DIMS)
+def test_mixed_lengths_e4m3(dqk, dv):
+    run(Batch([1, 300, 0, 5, 131, 1, 200], [1000, 300, 40, 77, 2000, 1, 90], 8, 2, dqk, dv, 16, True, seed=7))
+    bt = Batch([150, 90, 200], [700, 333, 200], 14, 2, dqk, dv, 16, True, seed=31)
+    bt.table[0, 3], bt.table[0, 43] = -1, bt.n_pages
+    bt.table[1, 0:4], bt.table[1, 20] = 2 ** 31 - 1, -2 ** 31
+    bt.table[2, :] = -1
+    bt.d_table = bt.table.cuda()
+    run(bt)
+
+
+def test_whole_blocks_e4m3():
+    bt = Batch([1111, 1111], [1111, 1500], 64, 64, 128, 128, 32, True, seed=3)
+    run(bt)
+
+
+@pytest.mark.parametrize("ks", [0.0, -0.02, 1e-42])
+def test_e4m3_scales(ks):
+    """Scales that are zero, negative or tiny (masked scores stay masked), in both kernels."""
+    for n in (1, 90):
+        bt = Batch([n, n], [n, 300], 4, 2, 128, 128, 16, True, seed=61)
+        bt.k_scale = torch.tensor([ks, 0.01])
+        bt.d_k_scale = bt.k_scale.cuda()
+        run(bt)
+
+
+@pytest.mark.parametrize("dqk,dv", DIMS)
+def test_rising_scores_move_the_reference_e4m3(dqk, dv):
+    bt = Batch([90, 120], [1500, 120], 4, 2, dqk, dv, 16, True, seed=11)
+    for b, n in enumerate(bt.keys):
+        pos = torch.arange(n)
+        pages, slots = bt.table[b, pos // 16].long(), pos % 16
+        grow = (0.1 + 2.0 * pos / n)[:, None, None]
+        rows = (bt.k_cache.float()[pages, :, slots] * grow).clamp(-448, 448).to(bt.k_cache.dtype)
+        bt.k_cache.view(torch.uint8)[pages, :, slots] = rows.view(torch.uint8)
+    bt._to("cuda", "hnd")
+    run(bt)
+    bt.table[0, 40] = -1
+    bt.d_table = bt.table.cuda()
+    run(bt)
+
+
+@pytest.mark.parametrize("dqk,dv", DIMS[:2])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n", [17, 31, 32])
+def test_short_blocks(n, dqk, dv, causal):
+    """Up to 128 row-heads per key/value head: blocks of 128, split, beside other lengths and whole."""
+    run(Batch([n], [4000], 8, 2, dqk, dv, 16, seed=n), causal=causal)
+    run(Batch([n, 1, 0, n], [n, 700, 30, 1501], 8, 2, dqk, dv, 64, seed=n), causal=causal)
+    bt = Batch([n] * 20, [n + 37 * i for i in range(20)], 256, 64, dqk, dv, 16, seed=n)
+    assert not splits(bt)
+    run(bt, causal=causal)
+
+
+def test_short_blocks_page_windows_and_holes():
+    bt = Batch([32], [70 * 64], 4, 1, 128, 128, 16, seed=71)  # more tiles than a register of page numbers holds
+    run(bt)
+    bt.table[0, 0:8] = -1
+    bt.table[0, 200], bt.table[0, -1] = bt.n_pages, -1
+    bt.d_table = bt.table.cuda()
+    run(bt)
