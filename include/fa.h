@@ -351,6 +351,15 @@ fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
                          const void* Q, void* Q_out, int Hq, const long long* strides, const float* cos_sin, int n_pos,
                          int rot_begin, int rot_dim, int interleaved, hipStream_t stream);
 
+/* The kernels of fa_fwd_paged: one reads K and V once per 32 or 64 row-heads of a key/value head (query rows times the
+ * heads that share it) and splits every sequence over the chip, for single tokens, draft tokens and short prompts; one computes
+ * in blocks of 128 or 256 row-heads, for longer prompts and chunks. Each is right for any lengths. */
+typedef enum {
+  FA_PAGED_AUTO = 0, /* chosen by max_q, the sizes and, on the device, the lengths */
+  FA_PAGED_FEW = 1,
+  FA_PAGED_MANY = 2
+} fa_paged_path_t;
+
 /*
  * fa_fwd_paged -- attention of the new tokens over the paged cache: for token t of sequence b at position p,
  *     O[t,h] = softmax over visible j of (scale * q[t,h] . K[b,g,j]) * V[b,g,j],   g = h / (Hq / Hkv),
@@ -359,8 +368,9 @@ fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
  *   Q, O        bf16 [T][Hq][d_qk], [T][Hq][d_v]; element (t, h, 0) at t * q_token + h * q_head
  *   LSE         float32 [T][Hq] (contiguous), or NULL
  *   strides     {q_token, q_head, o_token, o_head}, in elements, multiples of 8
- *   max_q       the most new tokens of one sequence, as far as the host knows: it chooses the kernels, the results
+ *   max_q       the most new tokens of one sequence, as far as the host knows: it helps to choose the kernels, the results
  *               are right for any
+ *   path        fa_paged_path_t
  *   workspace   16-byte aligned, at least fa_fwd_paged_workspace_bytes(...) bytes, overwritten; nothing needs to be in
  *               it before, and it must not be used elsewhere until the call's work has completed. NULL only when no
  *               byte is needed.
@@ -368,19 +378,20 @@ fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
  * hold at a replay.
  *
  * Errors, in this order: cache, batch or strides NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE: as for fa_kv_append, max_q < 0,
- * Hkv * (T * Hq / Hkv / 32 + B) * (max_blocks * page_size / 128 + 2) >= 2^31); head dimensions, page size, type
+ * Hkv * (T * Hq / Hkv / 32 + B) * (max_blocks * page_size / 128 + 2) >= 2^31); head dimensions, page size, type, path
  * (FA_ERR_UNSUPPORTED); NULL buffers (FA_ERR_NULL_POINTER); scale (FA_ERR_BAD_SCALE); alignment (FA_ERR_UNSUPPORTED); cache
  * strides (FA_ERR_BAD_SHAPE); workspace NULL or too small (FA_ERR_WORKSPACE), not aligned (FA_ERR_UNSUPPORTED). T == 0, B == 0 or
  * Hq == 0 returns FA_OK without a launch.
  */
 fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* Q, void* O, float* LSE,
-                         int Hq, const long long* strides, int max_q, float scale, int causal, void* workspace,
+                         int Hq, const long long* strides, int max_q, int path, float scale, int causal, void* workspace,
                          size_t workspace_bytes, hipStream_t stream);
 
-/* Workspace bytes of a fa_fwd_paged call with these sizes, max_keys = max_blocks * page_size and this max_q (they do not
- * depend on the lengths; 0 is possible). Host arithmetic only; 0 for sizes <= 0 (max_keys, max_q: < 0), Hq not a multiple of
- * Hkv, or an unsupported type or head dimension. */
-size_t fa_fwd_paged_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q);
+/* Workspace bytes of a fa_fwd_paged call with these sizes, max_keys = max_blocks * page_size, this max_q and this path (they do
+ * not depend on the lengths; 0 is possible). Host arithmetic only; 0 for sizes <= 0 (max_keys, max_q: < 0), Hq not a multiple of
+ * Hkv, or an unsupported type, path or head dimension. */
+size_t fa_fwd_paged_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q,
+                                    int path);
 
 /* Static, human-readable name of a status code ("FA_OK", ...); "unknown status" otherwise. */
 const char* fa_status_str(fa_status_t s);

@@ -29,6 +29,7 @@ from typing import Optional
 
 from . import _lib
 from ._lib import (AppendStrides, PagedBatch, PagedCache, PagedStrides, FA_CACHE_BF16, FA_CACHE_E4M3,  # noqa: F401
+                   FA_PAGED_AUTO, FA_PAGED_FEW, FA_PAGED_MANY,
                    FA_ERR_BAD_SCALE, FA_ERR_BAD_SHAPE, FA_ERR_HIP, FA_ERR_NULL_POINTER,
                    FA_ERR_UNSUPPORTED, FA_ERR_WORKSPACE, FA_INSTANCE_HALVES, FA_INSTANCE_LONG, FA_INSTANCE_NONE,
                    FA_INSTANCE_QUARTERS, FA_INSTANCE_SHORT, FA_INSTANCE_SHORT_WIDE, FA_NOALLOC_SCRATCH_BYTES, FA_OK,
@@ -39,7 +40,8 @@ __all__ = ["fa_fwd", "fa_fwd_ex", "fa_fwd_split", "fa_fwd_split_workspace_bytes"
            "fa_lbl_workspace_bytes", "fa_fwd_unfused", "fa_fwd_decode", "fa_fwd_decode_parts",
            "fa_fwd_decode_noalloc", "fa_fwd_instance", "forward", "forward_unfused", "FaError", "LIB_PATH", "FA_NOALLOC_SCRATCH_BYTES",
            "fa_kv_append", "fa_fwd_paged", "fa_fwd_paged_workspace_bytes", "PagedCache", "PagedBatch", "AppendStrides",
-           "PagedStrides", "FA_CACHE_BF16", "FA_CACHE_E4M3", "kv_append", "forward_paged"]
+           "PagedStrides", "FA_CACHE_BF16", "FA_CACHE_E4M3", "FA_PAGED_AUTO", "FA_PAGED_FEW",
+           "FA_PAGED_MANY", "kv_append", "forward_paged"]
 
 
 class FaError(RuntimeError):
@@ -167,17 +169,17 @@ def fa_kv_append(cache: PagedCache, batch: PagedBatch, K: int, V: int, Q: Option
 
 
 def fa_fwd_paged(cache: PagedCache, batch: PagedBatch, Q: int, O: int, LSE: Optional[int], Hq: int,
-                 strides: PagedStrides, max_q: int, scale: float, causal: bool, workspace: Optional[int],
+                 strides: PagedStrides, max_q: int, path: int, scale: float, causal: bool, workspace: Optional[int],
                  workspace_bytes: int, stream: int) -> int:
     """C ``fa_fwd_paged``: descriptions, raw device addresses and sizes; returns the status code."""
-    return int(_lib.load().fa_fwd_paged(cache, batch, Q, O, LSE, Hq, strides, max_q, float(scale),
+    return int(_lib.load().fa_fwd_paged(cache, batch, Q, O, LSE, Hq, strides, max_q, path, float(scale),
                                         int(bool(causal)), workspace, int(workspace_bytes), stream))
 
 
 def fa_fwd_paged_workspace_bytes(B: int, T: int, max_keys: int, Hq: int, Hkv: int, d_qk: int, d_v: int, type: int,
-                                 max_q: int) -> int:
+                                 max_q: int, path: int = FA_PAGED_AUTO) -> int:
     """C ``fa_fwd_paged_workspace_bytes`` (``max_keys``: blocks of the table times page size)."""
-    return int(_lib.load().fa_fwd_paged_workspace_bytes(B, T, max_keys, Hq, Hkv, d_qk, d_v, type, max_q))
+    return int(_lib.load().fa_fwd_paged_workspace_bytes(B, T, max_keys, Hq, Hkv, d_qk, d_v, type, max_q, path))
 
 
 # What a call costs on the host bounds the smallest problems (one head S256 d64: a 4.7 us kernel in a call
@@ -550,12 +552,13 @@ def kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q=None, q_
 
 def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Optional[int] = None, causal: bool = True,
                   scale: Optional[float] = None, k_scale=None, v_scale=None, return_lse: bool = False, out=None, lse=None,
-                  workspace=None, stream=None):
+                  workspace=None, stream=None, path: Optional[str] = None):
     """Attention of the new tokens q [T, Hq, d_qk] over a paged cache (see :func:`kv_append` for the cache and the
     batch, whose new tokens are in the cache already): returns O [T, Hq, d_v] (bf16) and, with ``return_lse``, LSE
     [T, Hq] (float32, natural log). Token i of the n new ones of sequence b sees the keys up to its position
-    ``kv_lens[b] - n + i`` (all ``kv_lens[b]`` where not ``causal``). ``max_q``, the most new tokens of one sequence, chooses
-    the kernels (default: the mean, rounded up); the results are right for any. Rows of tokens that belong to no
+    ``kv_lens[b] - n + i`` (all ``kv_lens[b]`` where not ``causal``). ``max_q``, the most new tokens of one sequence, helps to
+    choose the kernels (default: the mean, rounded up), ``path`` ("few", "many") chooses them: for single tokens and short
+    prompts, or for longer ones; the results are right for any. Rows of tokens that belong to no
     sequence are left as they were, so a new tensor's hold anything.
 
     ``scale`` defaults to 1/sqrt(d_qk). ``workspace`` is a CUDA tensor of ``fa_fwd_paged_workspace_bytes`` (default: from
@@ -575,11 +578,16 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
         scale = 1.0 / math.sqrt(dqk) if dqk else 1.0
     if max_q is None:
         max_q = -(-T // B) if B else 0
+    way = 0
+    if path is not None:
+        if path not in ("few", "many"):
+            raise ValueError(f'path must be "few", "many" or None, not {path!r}')
+        way = FA_PAGED_FEW if path == "few" else FA_PAGED_MANY
     elsewhere = _elsewhere(stream, device)
     if elsewhere is not None:
         with elsewhere:
             return forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q, causal, scale, k_scale, v_scale,
-                                 return_lse, out, lse, workspace)
+                                 return_lse, out, lse, workspace, path=path)
     if out is not None:
         ot, oh = _rows("out", out, (T, hq, dv), device, bf16, True)
     else:
@@ -595,7 +603,7 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
         lse = q.new_empty((T, hq), dtype=torch.float32)
     lib, ws = _lib.load(), None
     if workspace is None:
-        nbytes = lib.fa_fwd_paged_workspace_bytes(B, T, max_keys, hq, hkv, dqk, dv, type, max_q)
+        nbytes = lib.fa_fwd_paged_workspace_bytes(B, T, max_keys, hq, hkv, dqk, dv, type, max_q, way)
         if nbytes > 0:
             workspace = q.new_empty(nbytes, dtype=torch.uint8)
             ws = workspace.data_ptr()
@@ -604,7 +612,7 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
     else:
         nbytes, ws = workspace.numel() * workspace.element_size(), workspace.data_ptr()
     st = lib.fa_fwd_paged(cache, batch, q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), hq,
-                          PagedStrides(qt, qh, ot, oh), int(max_q), scale, 1 if causal else 0, ws, nbytes,
+                          PagedStrides(qt, qh, ot, oh), int(max_q), way, scale, 1 if causal else 0, ws, nbytes,
                           torch._C._cuda_getCurrentRawStream(device))
     if st != FA_OK:
         _raise("fa_fwd_paged", st)

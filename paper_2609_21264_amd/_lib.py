@@ -42,6 +42,11 @@ EXPORTED = ("fa_fwd", "fa_fwd_ex", "fa_fwd_split", "fa_fwd_split_workspace_bytes
 FA_CACHE_BF16 = 0
 FA_CACHE_E4M3 = 1
 
+# Values of fa_paged_path_t.
+FA_PAGED_AUTO = 0
+FA_PAGED_FEW = 1
+FA_PAGED_MANY = 2
+
 
 class PagedCache(ctypes.Structure):
     """fa_paged_cache_t."""
@@ -116,9 +121,9 @@ def load() -> ctypes.CDLL:
     cache, batch = ctypes.POINTER(PagedCache), ctypes.POINTER(PagedBatch)  # structures go by reference
     lib.fa_kv_append.argtypes = [cache, batch, vp, vp, vp, vp, i, vp, vp, i, i, i, i, vp]
     lib.fa_kv_append.restype = i
-    lib.fa_fwd_paged.argtypes = [cache, batch, vp, vp, vp, i, vp, i, f, i, vp, ctypes.c_size_t, vp]
+    lib.fa_fwd_paged.argtypes = [cache, batch, vp, vp, vp, i, vp, i, i, f, i, vp, ctypes.c_size_t, vp]
     lib.fa_fwd_paged.restype = i
-    lib.fa_fwd_paged_workspace_bytes.argtypes = [i] * 9
+    lib.fa_fwd_paged_workspace_bytes.argtypes = [i] * 10
     lib.fa_fwd_paged_workspace_bytes.restype = ctypes.c_size_t
     _lib = lib
     return lib

@@ -303,27 +303,49 @@ bool token_strides(const long long* s, int n) {
   return true;
 }
 // What a call of fa_fwd_paged runs, and its workspace (sizes checked).
-//  * The kernel for few rows reads K and V once per item of 32 or 64 row-heads of a key/value head. It runs alone where
-//    the host expects no sequence with more than 64; otherwise it takes the sequences with at most 32 and leaves the
-//    others to the kernel for many rows; where all have max_q tokens, that runs alone.
-//  * Where the table has pages for at most kWholeKeys keys, the kernel for few rows takes whole items, without a join.
+//  By path, or (FA_PAGED_AUTO) thus:
+//  * The kernel for few rows reads K and V once per item of 32 or 64 row-heads of a key/value head, and starts fast; the
+//    kernel for many rows computes at three times its rate, and takes 20 us more to start. The former runs alone where the
+//    host expects no sequence with more than 64 row-heads, or where the table holds too few keys for kManyPairs visible
+//    (query, key) pairs over all query heads; the latter where all sequences have max_q tokens and with them as many
+//    pairs. Else both are launched and find from the lengths whether the sequences with more than 32 row-heads have
+//    kManyPairs together: if so the kernel for many rows takes these, else that for few takes all.
+//    Few (64 row-heads) against many, one box: d = 128 32/8 heads 4 x 300 x 300 (5.8 M pairs) 36.9 us against 44.0,
+//    1024 x 1024 (17 M) 50.1 : 49.5, 4 x 128 x 2000 (32 M) 53.9 : 50.2, 300 x 4000 (37 M) 66.7 : 49.1; d = 64 16/16 heads
+//    2048 x 2048 (34 M) 41.6 : 51.4, 1024 x 4096 (59 M) 59.5 : 76.9, 64 x 300 x 300 (46 M) 92.8 : 82.0, 4 x 300 x 4000
+//    (74 M) 73.7 : 64.6; d_qk = 192 16/16 1024 x 1024 (8.4 M) 33.6 : 43.9, 16 x 300 x 300 (12 M) 74.6 : 50.9, 300 x 4000
+//    (18 M) 49.9 : 46.0.
+//  * Items of 64 where sequences have more than 32 row-heads, so that K and V are read half as often (8 x 35 row-heads x 3 001
+//    keys 13.4 us against 15.7), except where items of 32 are no more than the CUs and the keys few, or read several
+//    times anyway (40 tokens x 40 keys of one sequence, 32/8 heads: 7.2 us in items of 32, 9.6 of 64; 16 of 128 x 128
+//    56.0 and 42.7).
+//  * Where the table has pages for at most kWholeKeys keys, the kernel for few rows takes whole items, without a join
+//    (one token, 32/8 heads, 512 keys 9.9 us against 11.0 with the join; 1 000 keys 15.0 against 11.2).
 constexpr int kFewCols = 64;
+constexpr double kManyPairs64 = 40e6, kManyPairs128 = 16e6, kManyPairs192 = 10e6;
 constexpr int kWholeKeys = 512, kWholeItems = 1 << 16;
 struct PagedPlan {
   bool few, many;         // kernels to launch
   fa::PagedMany m;        // what that for many rows runs
   bool whole;             // whether that for few rows takes whole items
   int few_cols, col_blocks, n_wg, cols;
+  uint32_t many_work;
   int64_t lse, desc, many_o, many_lse, many_desc, bytes;  // 16-byte aligned offsets
 };
-PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, int d_v, int type, int max_q) {
+PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, int d_v, int type, int max_q,
+                     int path) {
   PagedPlan w{};
   const int64_t rows = static_cast<int64_t>(T) * group, most = static_cast<int64_t>(max_q) * group;
   const bool e4m3 = type == FA_CACHE_E4M3;
-  w.many = most > kFewCols && rows > kFewCols;
-  w.few = !w.many || static_cast<int64_t>(max_q) * B != T;
+  const double pairs = d_qk == 64 ? kManyPairs64 : d_qk == 128 ? kManyPairs128 : kManyPairs192;
+  const double heads = static_cast<double>(Hkv) * group;
+  w.many_work = static_cast<uint32_t>(pairs / 1024);
+  w.many = path == FA_PAGED_MANY ||
+           (path == FA_PAGED_AUTO && most > kFewCols && rows > kFewCols && heads * T * max_keys >= pairs);
+  w.few = !w.many || (path == FA_PAGED_AUTO && (static_cast<int64_t>(max_q) * B != T || heads * T * max_q / 2 < pairs));
   w.few_cols = !w.many ? INT_MAX : w.few ? 32 : 0;
-  w.col_blocks = most <= 32 || w.many ? 1 : 2;
+  const int64_t items32 = (rows / 32 + (B < T ? B : T)) * Hkv;
+  w.col_blocks = most <= 32 || w.many || (items32 <= 256 && (most > kFewCols || max_keys <= kWholeKeys)) ? 1 : 2;
   if (w.many) w.m = fa::paged_many(B, T, Hkv, group, max_q, w.few_cols, d_qk, e4m3);
   auto place = [&](int64_t n) {
     const int64_t at = w.bytes;
@@ -393,15 +415,16 @@ fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   return fa::launch_append(p, cache->type == FA_CACHE_E4M3, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 
-size_t fa_fwd_paged_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q) {
+size_t fa_fwd_paged_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q,
+                                    int path) {
   if (B <= 0 || T <= 0 || max_keys < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_q < 0 || !dims_supported(d_qk, d_v) ||
-      (type != FA_CACHE_BF16 && type != FA_CACHE_E4M3))
+      (type != FA_CACHE_BF16 && type != FA_CACHE_E4M3) || path < FA_PAGED_AUTO || path > FA_PAGED_MANY)
     return 0;
-  return static_cast<size_t>(paged_plan(B, T, max_keys, Hkv, Hq / Hkv, d_qk, d_v, type, max_q).bytes);
+  return static_cast<size_t>(paged_plan(B, T, max_keys, Hkv, Hq / Hkv, d_qk, d_v, type, max_q, path).bytes);
 }
 
 fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* Q, void* O, float* LSE,
-                         int Hq, const long long* strides, int max_q, float scale, int causal, void* workspace,
+                         int Hq, const long long* strides, int max_q, int path, float scale, int causal, void* workspace,
                          size_t workspace_bytes, hipStream_t stream) {
   if (cache == nullptr || batch == nullptr || strides == nullptr) return FA_ERR_NULL_POINTER;
   fa_status_t st = check_paged_shape(cache, batch, Hq);
@@ -415,6 +438,7 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   }
   st = check_paged_support(cache);
   if (st != FA_OK) return st;
+  if (path < FA_PAGED_AUTO || path > FA_PAGED_MANY) return FA_ERR_UNSUPPORTED;
   if (batch->T == 0 || batch->B == 0 || Hq == 0) return FA_OK;
   if (!paged_pointers(cache, batch) || Q == nullptr || O == nullptr) return FA_ERR_NULL_POINTER;
   if (!isfinite(scale)) return FA_ERR_BAD_SCALE;
@@ -425,7 +449,7 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   st = check_paged_strides(cache, false);
   if (st != FA_OK) return st;
   const PagedPlan w = paged_plan(batch->B, batch->T, batch->max_blocks * cache->page_size, cache->Hkv, Hq / cache->Hkv,
-                                 cache->d_qk, cache->d_v, cache->type, max_q);
+                                 cache->d_qk, cache->d_v, cache->type, max_q, path);
   if (w.bytes > 0 && (workspace == nullptr || workspace_bytes < static_cast<size_t>(w.bytes))) return FA_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return FA_ERR_UNSUPPORTED;
 
@@ -441,6 +465,7 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   const float cmag = fabs(c) < FLT_MIN ? FLT_MIN : static_cast<float>(fabs(c));  // a masked score stays infinite
   p.cs = c < 0 ? -cmag : cmag;
   p.few_cols = w.few_cols;
+  p.many_work = w.many_work;
   p.n_wg = w.n_wg;
   p.part_cols = w.cols;
   p.whole = w.whole;

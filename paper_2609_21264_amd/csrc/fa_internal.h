@@ -196,9 +196,12 @@ struct PagedParams {
   float* o_part;         // fp32 [2 * n_wg][part_cols][d_v]
   float* lse_part;       // fp32 [2 * n_wg][part_cols]
   PagedItem* desc;       // [n_wg]
-  // Sequences with more than few_cols row-heads per key/value head run in the kernel for many rows, which has work
-  // units, places and items of its own (the latter three only where it splits blocks).
+  // Sequences with more than few_cols row-heads per key/value head run in the kernel for many rows if all of them together
+  // have many_work units of work (big_work in fa_paged_device.h), else in that for few rows. few_cols INT32_MAX: only the
+  // latter is launched; 0: only the former. It has work units, places and items of its own (the latter three only
+  // where it splits blocks).
   int few_cols;
+  uint32_t many_work;
   int many_wg, many_min_units, many_cols;  // many_cols: columns of a block
   float* many_o;         // fp32 [2 * many_wg][many_cols][d_v]
   float* many_lse;       // fp32 [2 * many_wg][many_cols]

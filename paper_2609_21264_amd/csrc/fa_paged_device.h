@@ -63,5 +63,19 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane) {
 }
 __device__ __forceinline__ uint32_t lane_of(uint32_t x, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); }
 
+// The work of the sequences with more than few_cols row-heads per key/value head: visible (query, key) pairs of all query
+// heads, in units of 1024, counted alike by both attention kernels. sl: the first 64 sequences, one per lane.
+__device__ __forceinline__ uint32_t big_work(const PagedParams& p, const PagedSeq& sl, int lane) {
+  auto of = [&](const PagedSeq& s) {
+    if ((int64_t)s.n_q * p.group <= p.few_cols) return 0u;
+    const int64_t n = s.n_q, pairs = n * s.kv - (p.causal ? n * (n - 1) / 2 : 0);
+    const int64_t units = (min(max(pairs, (int64_t)0), (int64_t)1 << 40) >> 10) * p.hq;  // < 2^61
+    return (uint32_t)min(units, (int64_t)UINT32_MAX);
+  };
+  uint32_t sum = of(sl);
+  for (int c = 64 + lane; c < p.bt.n_seq; c += 64) sum = add_sat(sum, of(load_seq_lane(p.bt, c)));
+  return wave_sum(sum);
+}
+
 }  // namespace
 }  // namespace fa

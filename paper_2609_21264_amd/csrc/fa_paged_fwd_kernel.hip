@@ -122,6 +122,14 @@ void fa_paged_fwd_kernel(PagedParams p) {
   int b = 0, g = 0, cb = 0, n_cb = 0, start = 0, r = 0, r1 = 0, per = 1;
   PagedSeq s{};
   if constexpr (C::SPLIT) {
+    if (tid == 0) p.many_desc[me].n_parts = 0;
+  }
+  if (p.few_cols != 0) {
+    PagedSeq sl{};
+    if (lane < p.bt.n_seq) sl = load_seq_lane(p.bt, lane);
+    if (big_work(p, sl, lane) < p.many_work) return;  // all sequences run in the kernel for few rows
+  }
+  if constexpr (C::SPLIT) {
     int64_t sum = 0;
     for (int c = 0; c < p.bt.n_seq; c += 64) {
       PagedSeq sl{};
@@ -135,7 +143,6 @@ void fa_paged_fwd_kernel(PagedParams p) {
     }
     const int total = (int)min(sum, (int64_t)INT32_MAX);
     per = max(p.many_min_units, (int)(((int64_t)total + p.many_wg - 1) / p.many_wg));
-    if (tid == 0) p.many_desc[me].n_parts = 0;
     if ((int64_t)me * per >= total) return;
     r = me * per;
     r1 = (int)min((int64_t)total, (int64_t)r + per);

@@ -234,11 +234,11 @@ template <int TILE, int COLS>
 struct SeqWork {
   int tiles, cost, n_cb;
   uint32_t units;  // below 2^31 by the host's check
-  __device__ __forceinline__ SeqWork(const PagedSeq& s, const PagedParams& p) {
+  __device__ __forceinline__ SeqWork(const PagedSeq& s, const PagedParams& p, int few_cols) {
     const int64_t cols = (int64_t)s.n_q * p.group;
     tiles = (s.kv + TILE - 1) / TILE;
     cost = kItemCost + (p.whole ? 0 : tiles);
-    n_cb = cols > p.few_cols ? 0 : (int)((cols + COLS - 1) / COLS);
+    n_cb = cols > few_cols ? 0 : (int)((cols + COLS - 1) / COLS);
     units = (uint32_t)n_cb * (uint32_t)p.c.hkv * (uint32_t)cost;
   }
 };
@@ -259,11 +259,13 @@ void fa_paged_few_kernel(PagedParams p) {
   // sequences stay in registers, one per lane.
   PagedSeq sl{};
   if (lane < p.bt.n_seq) sl = load_seq_lane(p.bt, lane);
-  uint32_t mine = SeqWork<TILE, COLS>(sl, p).units, incl = wave_scan(mine, lane);
+  int few_cols = p.few_cols;
+  if (few_cols != INT32_MAX && big_work(p, sl, lane) < p.many_work) few_cols = INT32_MAX;  // all sequences run here
+  uint32_t mine = SeqWork<TILE, COLS>(sl, p, few_cols).units, incl = wave_scan(mine, lane);
   uint32_t sum = lane_of(incl, 63);
   if (p.bt.n_seq > 64) {
     uint32_t rest = 0;
-    for (int c = 64 + lane; c < p.bt.n_seq; c += 64) rest = add_sat(rest, SeqWork<TILE, COLS>(load_seq_lane(p.bt, c), p).units);
+    for (int c = 64 + lane; c < p.bt.n_seq; c += 64) rest = add_sat(rest, SeqWork<TILE, COLS>(load_seq_lane(p.bt, c), p, few_cols).units);
     sum = add_sat(sum, wave_sum(rest));
   }
   const int total = uniform((int)min(sum, (uint32_t)INT32_MAX));
@@ -286,7 +288,7 @@ void fa_paged_few_kernel(PagedParams p) {
     if (b >= p.bt.n_seq) return;  // not reached: r0 < total
     sl = PagedSeq{};
     if (b + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, b + lane);
-    mine = SeqWork<TILE, COLS>(sl, p).units;
+    mine = SeqWork<TILE, COLS>(sl, p, few_cols).units;
     incl = wave_scan(mine, lane);
   }
 
@@ -318,12 +320,12 @@ void fa_paged_few_kernel(PagedParams p) {
   PagedSeq s{uniform(sl.q0), uniform(sl.q_end), uniform(sl.n_q), uniform(sl.kv)};
   b = uniform(b), start = uniform(start);
   while (r < r1) {
-    SeqWork<TILE, COLS> sw(s, p);
+    SeqWork<TILE, COLS> sw(s, p, few_cols);
     while (sw.units == 0 || (uint32_t)(r - start) >= sw.units) {
       start += (int)sw.units;
       if (++b >= p.bt.n_seq) return;  // not reached: r < total
       s = load_seq(p.bt, b);
-      sw = SeqWork<TILE, COLS>(s, p);
+      sw = SeqWork<TILE, COLS>(s, p, few_cols);
     }
     const int cost = sw.cost;
     const int item = uniform((int)((uint32_t)(r - start) / (uint32_t)cost)), item0 = start + item * cost;

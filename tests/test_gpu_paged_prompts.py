@@ -5,15 +5,21 @@ import torch
 
 import paper_2609_21264_amd as fa
 from paged import Batch
-from test_gpu_paged import DIMS, run
+from test_gpu_paged import DIMS, run as run_any
 
 pytestmark = pytest.mark.gpu
 
 
+def run(bt, **kw):
+    """The kernel for many rows, whatever the sizes; and what the call chooses by itself."""
+    run_any(bt, **kw)
+    return run_any(bt, path="many", **kw)
+
+
 def splits(bt):
-    """Whether the call needs a workspace: blocks are split where they would not fill the chip."""
+    """Whether the kernel for many rows needs a workspace: blocks are split where they would not fill the chip."""
     return fa.fa_fwd_paged_workspace_bytes(len(bt.new), bt.T, bt.table.shape[1] * bt.page, bt.Hq, bt.Hkv, bt.dqk, bt.dv,
-                                           fa.FA_CACHE_BF16, max(bt.new)) > 0
+                                           fa.FA_CACHE_BF16, max(bt.new), fa.FA_PAGED_MANY) > 0
 
 
 @pytest.mark.parametrize("causal", [True, False])
@@ -105,9 +111,9 @@ def test_nhd_cache_and_strided_tensors():
 
 def test_results_do_not_change_between_runs():
     bt = Batch([700, 130, 1], [2000, 130, 500], 8, 2, 128, 128, 16, seed=39)
-    first = bt.attend(return_lse=True)
+    first = bt.attend(return_lse=True, path="many")
     for _ in range(3):
-        again = bt.attend(return_lse=True)
+        again = bt.attend(return_lse=True, path="many")
         assert torch.equal(first[0].view(torch.int16), again[0].view(torch.int16)) and torch.equal(first[1], again[1])
 
 
@@ -192,3 +198,37 @@ def test_short_blocks_page_windows_and_holes():
     bt.table[0, 200], bt.table[0, -1] = bt.n_pages, -1
     bt.d_table = bt.table.cuda()
     run(bt)
+
+
+@pytest.mark.parametrize("path", [None, "few", "many"])
+@pytest.mark.parametrize("dqk,dv,Hq,Hkv", [(64, 64, 128, 16), (128, 128, 64, 8), (192, 128, 64, 32)])
+def test_paths_by_work(path, dqk, dv, Hq, Hkv):
+    """Batches around the work from which prompts go to the kernel for many rows, beside single tokens (by themselves the
+    two kernels share the sequences then), and a table wider than its lengths."""
+    for keys in (400, 2100):
+        bt = Batch([230, 1, 0, 9, 120], [keys, 500, 3, 80, 333], Hq, Hkv, dqk, dv, 32, seed=keys, blocks=100)
+        run_any(bt, path=path)
+
+
+def test_paths_many_sequences():
+    new = [1 + (31 * i) % 60 for i in range(150)]
+    run_any(Batch(new, [n + 10 * (i % 50) for i, n in enumerate(new)], 64, 4, 64, 64, 16, seed=77, blocks=60))
+
+
+@pytest.mark.parametrize("keys", [[2000, 1], [300, 300], [64, 2048]])
+def test_captured_call_serves_short_and_long_prompts(keys):
+    """Which kernel takes the prompts is decided on the device, so a captured call serves both."""
+    bt = Batch([150, 150], [2048, 2048], 64, 8, 128, 128, 16, seed=79)
+    T = bt.T
+    out, lse = torch.empty(T, 64, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(T, 64, device="cuda")
+    bt.attend(out=out, lse=lse, return_lse=True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bt.attend(out=out, lse=lse, return_lse=True)
+    for lens in ([2048, 2048], keys, [2048, 150], keys):
+        bt.kv_lens = torch.tensor(lens, dtype=torch.int32)
+        bt.d_kv_lens.copy_(bt.kv_lens)
+        out.fill_(float("nan"))
+        graph.replay()
+        bt.check(out, lse, 128 ** -0.5, True, str(lens))

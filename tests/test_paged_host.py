@@ -33,8 +33,8 @@ def append(c=None, b=None, K=P, V=P, Q=P, Q_out=P, Hq=4, strides=(512, 128) * 2 
                            n_pos, begin, rot, inter, None)
 
 
-def attend(c=None, b=None, Q=P, O=P, LSE=P, Hq=4, strides=(512, 128, 512, 128), max_q=2, scale=0.1, ws=P, nbytes=1 << 30):
-    return fa.fa_fwd_paged(c or cache(), b or batch(), Q, O, LSE, Hq, strides and fa.PagedStrides(*strides), max_q, scale, True,
+def attend(c=None, b=None, Q=P, O=P, LSE=P, Hq=4, strides=(512, 128, 512, 128), max_q=2, path=0, scale=0.1, ws=P, nbytes=1 << 30):
+    return fa.fa_fwd_paged(c or cache(), b or batch(), Q, O, LSE, Hq, strides and fa.PagedStrides(*strides), max_q, path, scale, True,
                            ws, nbytes, None)
 
 
@@ -87,8 +87,9 @@ def test_append_refuses():
 
 def test_attend_refuses():
     assert attend(strides=None) == NULL
-    assert fa.fa_fwd_paged(cache(), None, P, P, P, 4, fa.PagedStrides(), 1, 0.1, True, P, 1 << 30, None) == NULL
+    assert fa.fa_fwd_paged(cache(), None, P, P, P, 4, fa.PagedStrides(), 1, 0, 0.1, True, P, 1 << 30, None) == NULL
     assert attend(Hq=3) == SHAPE and attend(max_q=-1) == SHAPE
+    assert attend(path=3) == UNSUPPORTED and attend(path=-1) == UNSUPPORTED
     assert attend(cache(Hkv=1), batch(T=2 ** 24, max_blocks=2 ** 20), Hq=64) == SHAPE  # more work than 32 bits count
     assert attend(Q=None) == NULL and attend(O=None) == NULL
     for scale in (float("nan"), float("inf"), 3e38):
@@ -103,16 +104,21 @@ def test_attend_refuses():
 
 
 def test_workspace_bytes():
-    def f(B, T, *a, keys=4096):
-        return fa.fa_fwd_paged_workspace_bytes(B, T, keys, *a)
+    def f(B, T, *a, keys=4096, path=0):
+        return fa.fa_fwd_paged_workspace_bytes(B, T, keys, *a, path)
 
     assert f(1, 0, 4, 2, 128, 128, 0, 1) == 0 and f(0, 1, 4, 2, 128, 128, 0, 1) == 0 and f(1, 1, 3, 2, 128, 128, 0, 1) == 0
     assert f(1, 1, 4, 2, 96, 96, 0, 1) == 0 and f(1, 1, 4, 2, 64, 64, 7, 1) == 0 and f(1, 1, 4, 2, 64, 64, 0, -1) == 0
     one, most = f(1, 1, 4, 1, 128, 128, 0, 1), f(8, 8, 4, 1, 128, 128, 0, 1)
     assert 0 < one < most < 1 << 26 and 0 < f(10 ** 6, 10 ** 6, 4, 1, 128, 128, 0, 1) < 1 << 26
     assert f(1, 1, 4, 1, 128, 128, 0, 1, keys=-1) == 0
-    # A chunk beside single tokens needs places for both kernels; enough equal prompts need none at all.
-    assert f(8, 500, 4, 1, 128, 128, 0, 493) > most and f(8, 80000, 32, 8, 128, 128, 0, 10000) == 0
+    # A chunk beside single tokens needs places for both kernels, unless the table holds too little for that for many
+    # rows; enough equal prompts need none at all.
+    assert f(8, 500, 4, 1, 128, 128, 0, 493, keys=65536) > f(8, 500, 4, 1, 128, 128, 0, 493, keys=1024)
+    assert f(8, 80000, 32, 8, 128, 128, 0, 10000) == 0
+    assert f(1, 1, 4, 1, 128, 128, 0, 1, path=3) == 0
+    few, many = (f(8, 500, 4, 1, 128, 128, 0, 493, keys=65536, path=x) for x in (1, 2))
+    assert 0 < few < many and few + many >= f(8, 500, 4, 1, 128, 128, 0, 493, keys=65536)
 
 
 def test_structures_match_the_header():
