@@ -202,7 +202,8 @@ struct PagedParams {
   // where it splits blocks).
   int few_cols;
   uint32_t many_work;
-  int many_wg, many_min_units, many_cols;  // many_cols: columns of a block
+  int many_wg, many_min_units, many_cols;  // many_wg: a power of two; many_cols: columns of a block
+  int many_log;          // log2 of many_wg, filled by launch_paged_many
   float* many_o;         // fp32 [2 * many_wg][many_cols][d_v]
   float* many_lse;       // fp32 [2 * many_wg][many_cols]
   PagedItem* many_desc;  // [many_wg]

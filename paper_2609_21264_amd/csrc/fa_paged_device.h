@@ -48,18 +48,22 @@ __device__ __forceinline__ PagedSeq seq_of_lane(const PagedSeq& s, int l) {
 // Sums over the wave, and inclusive prefix sums, that stop at 2^32 - 1: whatever the batch's arrays hold, a prefix never
 // comes before an earlier one.
 __device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
-__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = add_sat(x, (uint32_t)__shfl_xor((int)x, o));
-  return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+// (Lane moves inside the vector instructions: exchanges through LDS would be 0.3 us a scan.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t add_moved(uint32_t x) {
+  return add_sat(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false));
 }
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t y = (uint32_t)__shfl_up((int)x, o);
-    if (lane >= o) x = add_sat(x, y);
-  }
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x = add_moved<0x111, 0xf>(x);  // from 1, 2, 4 and 8 lanes before, within the rows of 16
+  x = add_moved<0x112, 0xf>(x);
+  x = add_moved<0x114, 0xf>(x);
+  x = add_moved<0x118, 0xf>(x);
+  x = add_moved<0x142, 0xa>(x);  // the last lane of rows 0 and 2 to rows 1 and 3
+  x = add_moved<0x143, 0xc>(x);  // lane 31 to rows 2 and 3
   return x;
+}
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(x), 63);
 }
 __device__ __forceinline__ uint32_t lane_of(uint32_t x, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); }
 

@@ -124,33 +124,39 @@ void fa_paged_fwd_kernel(PagedParams p) {
   if constexpr (C::SPLIT) {
     if (tid == 0) p.many_desc[me].n_parts = 0;
   }
-  if (p.few_cols != 0) {
-    PagedSeq sl{};
-    if (lane < p.bt.n_seq) sl = load_seq_lane(p.bt, lane);
-    if (big_work(p, sl, lane) < p.many_work) return;  // all sequences run in the kernel for few rows
-  }
+  // The first 64 sequences stay in registers, one per lane; those behind them are read again for each use.
+  PagedSeq first{};
+  if (lane < p.bt.n_seq) first = load_seq_lane(p.bt, lane);
+  auto seqs_from = [&](int c) {
+    PagedSeq x{};
+    if (c == 0)
+      x = first;
+    else if (c + lane < p.bt.n_seq)
+      x = load_seq_lane(p.bt, c + lane);
+    return x;
+  };
+  if (p.few_cols != 0 && big_work(p, first, lane) < p.many_work) return;  // all sequences run in the kernel for few rows
   if constexpr (C::SPLIT) {
-    int64_t sum = 0;
+    uint32_t sum = 0;
     for (int c = 0; c < p.bt.n_seq; c += 64) {
-      PagedSeq sl{};
-      if (c + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, c + lane);
+      const PagedSeq sl = seqs_from(c);
       uint64_t left = __builtin_amdgcn_ballot_w64(n_blocks<BC>(sl, p) > 0);
       while (left != 0) {
         const PagedSeq x = seq_of_lane(sl, __builtin_ctzll(left));
         left &= left - 1;
-        sum += (int64_t)head_units<BN, BC>(x, n_blocks<BC>(x, p), p, lane) * p.c.hkv;
+        sum = add_sat(sum, (uint32_t)min((int64_t)head_units<BN, BC>(x, n_blocks<BC>(x, p), p, lane) * p.c.hkv,
+                                         (int64_t)UINT32_MAX));
       }
     }
-    const int total = (int)min(sum, (int64_t)INT32_MAX);
-    per = max(p.many_min_units, (int)(((int64_t)total + p.many_wg - 1) / p.many_wg));
+    const int total = uniform((int)min(sum, (uint32_t)INT32_MAX));
+    per = max(p.many_min_units, (int)((uint32_t)(total - 1) >> p.many_log) + 1);
     if ((int64_t)me * per >= total) return;
     r = me * per;
-    r1 = (int)min((int64_t)total, (int64_t)r + per);
+    r1 = min(total - r, per) + r;
     // The sequence, head and block that hold unit r.
     bool found = false;
     for (int c = 0; c < p.bt.n_seq && !found; c += 64) {
-      PagedSeq sl{};
-      if (c + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, c + lane);
+      const PagedSeq sl = seqs_from(c);
       uint64_t left = __builtin_amdgcn_ballot_w64(n_blocks<BC>(sl, p) > 0);
       while (left != 0 && !found) {
         const int l = __builtin_ctzll(left);
@@ -160,7 +166,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
         const int units = head_units<BN, BC>(s, n_cb, p, lane);
         if ((int64_t)r < start + (int64_t)units * p.c.hkv) {
           b = c + l;
-          g = (r - start) / units;
+          g = uniform((int)((uint32_t)(r - start) / (uint32_t)units));
           start += g * units;
           found = true;
         } else {
@@ -171,7 +177,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
     if (!found) return;  // not reached: r < total
     for (int c = 0; c < n_cb; c += 64) {
       const uint32_t u = c + lane < n_cb ? (uint32_t)(kBlockCost + Block<BN, BC>(s, c + lane, p).tiles()) : 0u;
-      const uint32_t incl = wave_scan(u, lane);
+      const uint32_t incl = wave_scan(u);
       const uint64_t above = __builtin_amdgcn_ballot_w64(incl > (uint32_t)(r - start));
       if (above != 0) {
         const int l = __builtin_ctzll(above);
@@ -186,9 +192,8 @@ void fa_paged_fwd_kernel(PagedParams p) {
     int idx = (int)(blockIdx.x / (uint32_t)p.c.hkv);
     bool found = false;
     for (int c = 0; c < p.bt.n_seq && !found; c += 64) {
-      PagedSeq sl{};
-      if (c + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, c + lane);
-      const uint32_t n = (uint32_t)n_blocks<BC>(sl, p), incl = wave_scan(n, lane);
+      const PagedSeq sl = seqs_from(c);
+      const uint32_t n = (uint32_t)n_blocks<BC>(sl, p), incl = wave_scan(n);
       const uint64_t above = __builtin_amdgcn_ballot_w64(incl > (uint32_t)idx);
       if (above != 0) {
         const int l = __builtin_ctzll(above);
@@ -216,8 +221,8 @@ void fa_paged_fwd_kernel(PagedParams p) {
       // The block belongs to the workgroups that have tiles of it (one without a tile: to that of its first unit).
       skip = tiles == 0 ? start < r : nt == 0;
       if (tiles != 0) {
-        first_wg = (start + kBlockCost) / per;
-        n_parts = (start + cost - 1) / per - first_wg + 1;
+        first_wg = uniform((int)((uint32_t)(start + kBlockCost) / (uint32_t)per));
+        n_parts = uniform((int)((uint32_t)(start + cost - 1) / (uint32_t)per)) - first_wg + 1;
       }
       r = end;
     }
@@ -263,9 +268,14 @@ void fa_paged_fwd_kernel(PagedParams p) {
         entries = key >= 0 ? st.table[key >> p.c.page_shift] : -1;
         asm volatile("" : "+v"(entries));  // waited for here, not at every use
       };
+      // Whether a page of the range is not there. (The first 64 are read beside the window, so that both are waited for
+      // once.)
+      const int e0 = (kb0 >> p.c.page_shift) + lane, e1 = (kv_lim + smask) >> p.c.page_shift;
+      int page0 = 0;
+      if (e0 < e1) page0 = st.table[e0];
       window(t0);
-      bool hole = false;
-      for (int e = (kb0 >> p.c.page_shift) + lane; e < (kv_lim + smask) >> p.c.page_shift; e += 64) {
+      bool hole = e0 < e1 && (page0 < 0 || page0 >= p.c.n_pages);
+      for (int e = e0 + 64; e < e1; e += 64) {
         const int page = st.table[e];
         hole = hole || page < 0 || page >= p.c.n_pages;
       }
@@ -463,9 +473,17 @@ void fa_paged_fwd_kernel(PagedParams p) {
                 some ? (st.m_run[qb] + log2f(l_tot)) * kLn2 : -INFINITY;
           }
         }
-        // Each wave reads back only its own rows, so no barrier.
+        // Each wave reads back only its own rows, so no barrier. A lane's next column is RPI further on: its address
+        // moves by that many heads, and to the next token where the group ends (products of 64 bits for every row
+        // would take longer than the stores).
         constexpr int CPR = RB / 16, RPI = 64 / CPR, NIT = WROWS / RPI;
         const int ch = lane % CPR;
+        const int rows_on = (int)fast_div(RPI, p.m_group, p.sh_group), heads_on = RPI - rows_on * p.group;
+        const int64_t step = rows_on * p.o_token + heads_on * p.o_head, wrap = p.o_token - p.group * p.o_head;
+        int c = blk.c0 + col0 + lane / CPR;
+        const int qi = (int)fast_div((uint32_t)c, p.m_group, p.sh_group);
+        int member = c - qi * p.group;
+        uint16_t* dst = p.o + (int64_t)(s.q0 + qi) * p.o_token + (int64_t)(g * p.group + member) * p.o_head + ch * 8;
         u32x4 ov[NIT];
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
@@ -480,12 +498,13 @@ void fa_paged_fwd_kernel(PagedParams p) {
         for (int it = 0; it < NIT; ++it) asm volatile("" : "+v"(ov[it]));
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
-          const uint32_t c = (uint32_t)(blk.c0 + col0 + it * RPI + lane / CPR);
-          if ((int)c < blk.cols) {
-            const int qi = (int)fast_div(c, p.m_group, p.sh_group);
-            uint16_t* dst = p.o + (int64_t)(s.q0 + qi) * p.o_token + (int64_t)(g * p.group + ((int)c - qi * p.group)) * p.o_head;
-            *reinterpret_cast<u32x4*>(dst + ch * 8) = ov[it];
-          }
+          if (c < blk.cols) *reinterpret_cast<u32x4*>(dst) = ov[it];
+          c += RPI;
+          dst += step;
+          member += heads_on;
+          const bool over = member >= p.group;
+          member -= over ? p.group : 0;
+          dst += over ? wrap : 0;
         }
       }
     }
@@ -560,6 +579,8 @@ hipError_t launch_paged_many(PagedParams p, const PagedMany& m, int d_qk, bool e
   p.m_group = fg.m;
   p.sh_group = fg.sh;
   p.many_min_units = kBlockCost + 4;
+  p.many_log = 0;
+  while ((1 << p.many_log) < p.many_wg) ++p.many_log;
   if (e4m3) {
     if (d_qk == 64) return launch_many_split<64, 64, true, false>(p, m, stream);
     if (d_qk == 128) return launch_many_split<128, 128, true, false>(p, m, stream);

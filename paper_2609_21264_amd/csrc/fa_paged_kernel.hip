@@ -261,7 +261,7 @@ void fa_paged_few_kernel(PagedParams p) {
   if (lane < p.bt.n_seq) sl = load_seq_lane(p.bt, lane);
   int few_cols = p.few_cols;
   if (few_cols != INT32_MAX && big_work(p, sl, lane) < p.many_work) few_cols = INT32_MAX;  // all sequences run here
-  uint32_t mine = SeqWork<TILE, COLS>(sl, p, few_cols).units, incl = wave_scan(mine, lane);
+  uint32_t mine = SeqWork<TILE, COLS>(sl, p, few_cols).units, incl = wave_scan(mine);
   uint32_t sum = lane_of(incl, 63);
   if (p.bt.n_seq > 64) {
     uint32_t rest = 0;
@@ -289,7 +289,7 @@ void fa_paged_few_kernel(PagedParams p) {
     sl = PagedSeq{};
     if (b + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, b + lane);
     mine = SeqWork<TILE, COLS>(sl, p, few_cols).units;
-    incl = wave_scan(mine, lane);
+    incl = wave_scan(mine);
   }
 
   unsigned char* const ring = smem + wave * C::SLOTS * C::WSLOT;
