@@ -338,10 +338,11 @@ typedef struct {
  * e4m3 cache, after division by the head's scale to e4m3 (nearest even; what passes +-448 becomes +-448, NaN
  * stays NaN). V, and dims that do not turn, are copied (or divided and rounded). n_pos >= max_blocks * page_size, so that
  * every position has its row. A token before position 0 (more new tokens than keys) is left out, and nothing is
- * written for it. Inputs must not overlap the cache. Enqueues one kernel.
+ * written for it. Neither inputs nor Q_out may overlap the cache, nor Q_out K
+ * or V. Enqueues one kernel.
  *
  * Errors, in this order: cache, batch, strides or cos_sin description NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE: negative
- * (table_stride too), Hkv <= 0 with T > 0, Hq not a multiple of Hkv, max_blocks * page_size or T * Hq >= 2^31, n_pos too small, the rotated dims
+ * (table_stride too), Hkv <= 0 with T > 0, Hq not a multiple of Hkv, max_blocks * page_size > 2^30, T * Hq >= 2^31, n_pos too small, the rotated dims
  * outside [0, d_qk)); head dimensions, page size, type or rotation not supported (FA_ERR_UNSUPPORTED); a NULL buffer that
  * has elements (FA_ERR_NULL_POINTER); alignment (FA_ERR_UNSUPPORTED: 16 bytes for buffers and strides, 4 for the int
  * and scale arrays); cache strides negative, too large, or letting two elements of the cache overlap (FA_ERR_BAD_SHAPE).
@@ -364,7 +365,8 @@ typedef enum {
  * fa_fwd_paged -- attention of the new tokens over the paged cache: for token t of sequence b at position p,
  *     O[t,h] = softmax over visible j of (scale * q[t,h] . K[b,g,j]) * V[b,g,j],   g = h / (Hq / Hkv),
  * j <= p when causal, j < kv_lens[b] else. Arithmetic as for fa_fwd_ex (e4m3 caches: K and V are widened exactly, P is
- * rounded to fp16). A row with no visible key gets O = 0, LSE = -inf.
+ * rounded to fp16). A row with no visible key, or whose sum is no number, gets O = 0, LSE = -inf. An infinity or a NaN in a
+ * key reaches only the rows that see the key; one in a value may reach other rows of its sequence.
  *   Q, O        bf16 [T][Hq][d_qk], [T][Hq][d_v]; element (t, h, 0) at t * q_token + h * q_head
  *   LSE         float32 [T][Hq] (contiguous), or NULL
  *   strides     {q_token, q_head, o_token, o_head}, in elements, multiples of 8

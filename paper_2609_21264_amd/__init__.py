@@ -578,6 +578,7 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
         scale = 1.0 / math.sqrt(dqk) if dqk else 1.0
     if max_q is None:
         max_q = -(-T // B) if B else 0
+    max_q = int(max_q)
     way = 0
     if path is not None:
         if path not in ("few", "many"):
@@ -612,7 +613,7 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
     else:
         nbytes, ws = workspace.numel() * workspace.element_size(), workspace.data_ptr()
     st = lib.fa_fwd_paged(cache, batch, q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), hq,
-                          PagedStrides(qt, qh, ot, oh), int(max_q), way, scale, 1 if causal else 0, ws, nbytes,
+                          PagedStrides(qt, qh, ot, oh), max_q, way, scale, 1 if causal else 0, ws, nbytes,
                           torch._C._cuda_getCurrentRawStream(device))
     if st != FA_OK:
         _raise("fa_fwd_paged", st)

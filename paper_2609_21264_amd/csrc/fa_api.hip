@@ -228,12 +228,15 @@ fa::LblParams lbl_params(int B, int Hq, int Hkv, int Sq, int Sk, float scale, in
 
 bool dims_supported(int d_qk, int d_v) { return fa::block_rows(d_qk, d_v, true) != 0; }
 
+// Keys of one sequence: the kernels count keys in 32 bits, some tiles past the last.
+constexpr int64_t kMaxPagedKeys = 1 << 30;
+
 // Checks that both paged entry points begin with, in the order fa.h documents: sizes, then what is supported. Hq may be
 // 0 (no queries). On FA_OK fills the kernels' view of the cache and the batch.
 fa_status_t check_paged_shape(const fa_paged_cache_t* c, const fa_paged_batch_t* bt, int Hq) {
   if (bt->B < 0 || bt->T < 0 || bt->max_blocks < 0 || c->n_pages < 0 || c->Hkv < 0 || Hq < 0) return FA_ERR_BAD_SHAPE;
   if ((bt->T > 0 || Hq > 0) && (c->Hkv <= 0 || Hq % c->Hkv != 0)) return FA_ERR_BAD_SHAPE;
-  if (bt->table_stride < 0 || static_cast<int64_t>(bt->max_blocks) * c->page_size > INT_MAX) return FA_ERR_BAD_SHAPE;
+  if (bt->table_stride < 0 || static_cast<int64_t>(bt->max_blocks) * c->page_size > kMaxPagedKeys) return FA_ERR_BAD_SHAPE;
   const int64_t heads = Hq > c->Hkv ? Hq : c->Hkv;
   if (static_cast<int64_t>(bt->T) * heads > INT_MAX || bt->B == INT_MAX) return FA_ERR_BAD_SHAPE;
   return FA_OK;
@@ -296,7 +299,7 @@ void paged_view(const fa_paged_cache_t* c, const fa_paged_batch_t* bt, fa::Paged
   *w = fa::PagedBatch{bt->block_table, bt->kv_lens, bt->q_starts, bt->table_stride,
                       bt->B,           bt->T,       bt->max_blocks * c->page_size};
 }
-// Element strides of a packed input or output: multiples of 16 bytes that double-checked offsets can hold.
+// Element strides of a packed input or output: multiples of 16 bytes, offsets within 64 bits.
 bool token_strides(const long long* s, int n) {
   for (int i = 0; i < n; ++i)
     if (s[i] < 0 || (s[i] & 7) != 0 || s[i] > (1ll << 40)) return false;

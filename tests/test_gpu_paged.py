@@ -242,3 +242,45 @@ def test_joins(Hq, Hkv, B, fp8):
     run(other, workspace=ws)
     o, lse = bt.attend(return_lse=True, workspace=ws)
     assert torch.equal(o.view(torch.int16), first[0].view(torch.int16)) and torch.equal(lse, first[1])
+
+
+def test_empty_table_and_empty_cache():
+    """A table without columns holds no key; a cache without pages has none to hold: rows without a visible key."""
+    for what in ("table", "cache"):
+        bt = Batch([1, 70], [0, 0] if what == "table" else [40, 100], 4, 2, 128, 128, 16, seed=55)
+        if what == "table":
+            bt.d_table = bt.d_table[:, :0]
+        else:
+            bt.d_k_cache, bt.d_v_cache = bt.d_k_cache[:0], bt.d_v_cache[:0]
+        bt.append()
+        for path in ("few", "many", None):
+            out, lse = torch.full_like(bt.d_q, 3.0), torch.full((71, 4), 3.0, device="cuda")
+            bt.attend(out=out, lse=lse, return_lse=True, path=path)
+            torch.cuda.synchronize()
+            assert torch.all(out == 0) and torch.all(torch.isneginf(lse)), (what, path)
+
+
+def test_first_call_in_a_capture():
+    """A process whose first call of the library is captured."""
+    import subprocess
+    import sys
+
+    code = """
+import torch, paper_2609_21264_amd as fa
+g = torch.Generator(device="cuda").manual_seed(1)
+r = lambda *s: torch.randn(s, device="cuda", generator=g).bfloat16()
+i = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+q, k, v, kc, vc = r(2, 4, 128), r(2, 2, 128), r(2, 2, 128), r(300, 2, 16, 128), r(300, 2, 16, 128)
+a = (kc, vc, torch.arange(300, dtype=torch.int32, device="cuda").view(2, 150), i([2000, 77]), i([0, 1, 2]))
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    o = fa.forward_paged(fa.kv_append(k, v, *a, q=q), *a)
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(o, fa.forward_paged(q, *a)) and torch.isfinite(o).all()
+print("same")
+"""
+    root = __file__.rsplit("/tests/", 1)[0]
+    res = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=100)
+    assert res.returncode == 0 and "same" in res.stdout, res.stderr[-2000:]

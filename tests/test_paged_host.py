@@ -42,7 +42,7 @@ SHAPE, UNSUPPORTED, NULL = fa.FA_ERR_BAD_SHAPE, fa.FA_ERR_UNSUPPORTED, fa.FA_ERR
 BOTH = [  # (cache changes, batch changes, status) of both entry points
     (dict(n_pages=-1), {}, SHAPE), (dict(Hkv=0), {}, SHAPE), (dict(Hkv=3), {}, SHAPE),
     ({}, dict(B=-1), SHAPE), ({}, dict(T=-1), SHAPE), ({}, dict(max_blocks=-1), SHAPE), ({}, dict(table_stride=-1), SHAPE),
-    (dict(page_size=1 << 20), dict(max_blocks=2048), SHAPE), ({}, dict(T=2 ** 30), SHAPE),
+    (dict(page_size=1 << 20), dict(max_blocks=1025), SHAPE), ({}, dict(T=2 ** 30), SHAPE),
     (dict(d_qk=96), {}, UNSUPPORTED), (dict(d_v=64), {}, UNSUPPORTED),
     (dict(page_size=0), {}, UNSUPPORTED), (dict(page_size=8), {}, UNSUPPORTED), (dict(page_size=48), {}, UNSUPPORTED),
     (dict(type=2), {}, UNSUPPORTED), (dict(k_scale=P), {}, UNSUPPORTED),
