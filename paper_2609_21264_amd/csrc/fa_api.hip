@@ -308,16 +308,16 @@ bool token_strides(const long long* s, int n) {
 // What a call of fa_fwd_paged runs, and its workspace (sizes checked).
 //  By path, or (FA_PAGED_AUTO) thus:
 //  * The kernel for few rows reads K and V once per item of 32 or 64 row-heads of a key/value head, and starts fast; the
-//    kernel for many rows computes at three times its rate, and takes 20 us more to start. The former runs alone where the
-//    host expects no sequence with more than 64 row-heads, or where the table holds too few keys for kManyPairs visible
-//    (query, key) pairs over all query heads; the latter where all sequences have max_q tokens and with them as many
-//    pairs. Else both are launched and find from the lengths whether the sequences with more than 32 row-heads have
-//    kManyPairs together: if so the kernel for many rows takes these, else that for few takes all.
-//    Few (64 row-heads) against many, one box: d = 128 32/8 heads 4 x 300 x 300 (5.8 M pairs) 36.9 us against 44.0,
-//    1024 x 1024 (17 M) 50.1 : 49.5, 4 x 128 x 2000 (32 M) 53.9 : 50.2, 300 x 4000 (37 M) 66.7 : 49.1; d = 64 16/16 heads
-//    2048 x 2048 (34 M) 41.6 : 51.4, 1024 x 4096 (59 M) 59.5 : 76.9, 64 x 300 x 300 (46 M) 92.8 : 82.0, 4 x 300 x 4000
-//    (74 M) 73.7 : 64.6; d_qk = 192 16/16 1024 x 1024 (8.4 M) 33.6 : 43.9, 16 x 300 x 300 (12 M) 74.6 : 50.9, 300 x 4000
-//    (18 M) 49.9 : 46.0.
+//    kernel for many rows computes at three times its rate, and takes some 10 us more to start. The former runs alone where
+//    the host expects no sequence with more than 64 row-heads, or where the table holds too few keys for kManyUnits units
+//    of work (items of 64 row-heads, 5 units each and one per 128 keys); the latter where all sequences have max_q tokens
+//    and with as few keys kSureUnits. Else both are launched and find from the lengths whether the sequences with more than
+//    32 row-heads have kManyUnits together: if so the kernel for many rows takes these, else that for few takes all.
+//    Few against many, us, one box (units): d = 128 32/8 heads 512 x 512 (1.8 K) 17.0 : 22.2, 128 x 2000 (1.3 K) 31.7 : 45.6,
+//    4 x 200 x 200 (2.5 K) 22.8 : 18.8, 700 x 700 (2.8 K) 40.9 : 24.9, 4 x 128 x 2000 (5.4 K) 48.6 : 50.2, 300 x 4000 (5.5 K)
+//    60.3 : 43.6; d = 64 16/16 4 x 128 x 2000 (2.7 K) 27.0 : 34.4, 300 x 4000 (2.9 K) 35.7 : 28.1, 4 x 512 x 512 (4.1 K)
+//    16.6 : 19.0, 16 x 200 x 200 (6.1 K) 20.8 : 13.2; d_qk = 192 16/16 1024 x 1024 (2.6 K) 32.2 : 43.4, 300 x 4000 (2.9 K)
+//    75.0 : 44.5, 4 x 512 x 512 (4.1 K) 39.3 : 33.9; e4m3 d = 128 32/8 512 x 512 16.8 : 26.7, 700 x 700 41.4 : 30.5.
 //  * Items of 64 where sequences have more than 32 row-heads, so that K and V are read half as often (8 x 35 row-heads x 3 001
 //    keys 13.4 us against 15.7), except where items of 32 are no more than the CUs and the keys few, or read several
 //    times anyway (40 tokens x 40 keys of one sequence, 32/8 heads: 7.2 us in items of 32, 9.6 of 64; 16 of 128 x 128
@@ -325,7 +325,7 @@ bool token_strides(const long long* s, int n) {
 //  * Where the table has pages for at most kWholeKeys keys, the kernel for few rows takes whole items, without a join
 //    (one token, 32/8 heads, 512 keys 9.9 us against 11.0 with the join; 1 000 keys 15.0 against 11.2).
 constexpr int kFewCols = 64;
-constexpr double kManyPairs64 = 40e6, kManyPairs128 = 16e6, kManyPairs192 = 10e6;
+constexpr uint32_t kManyUnits = 2750, kSureUnits = 2000;
 constexpr int kWholeKeys = 512, kWholeItems = 1 << 16;
 struct PagedPlan {
   bool few, many;         // kernels to launch
@@ -340,12 +340,12 @@ PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, i
   PagedPlan w{};
   const int64_t rows = static_cast<int64_t>(T) * group, most = static_cast<int64_t>(max_q) * group;
   const bool e4m3 = type == FA_CACHE_E4M3;
-  const double pairs = d_qk == 64 ? kManyPairs64 : d_qk == 128 ? kManyPairs128 : kManyPairs192;
-  const double heads = static_cast<double>(Hkv) * group;
-  w.many_work = static_cast<uint32_t>(pairs / 1024);
-  w.many = path == FA_PAGED_MANY ||
-           (path == FA_PAGED_AUTO && most > kFewCols && rows > kFewCols && heads * T * max_keys >= pairs);
-  w.few = !w.many || (path == FA_PAGED_AUTO && (static_cast<int64_t>(max_q) * B != T || heads * T * max_q / 2 < pairs));
+  w.many_work = kManyUnits;
+  // The most units that the call can have, and the fewest with max_q new tokens (and so keys) in every sequence.
+  const double most_units = (static_cast<double>(rows) / 64 + B) * Hkv * (6 + max_keys / 128);
+  const double least_units = static_cast<double>(most + 63) / 64 * Hkv * B * (6 + max_q / 256);
+  w.many = path == FA_PAGED_MANY || (path == FA_PAGED_AUTO && most > kFewCols && rows > kFewCols && most_units >= kManyUnits);
+  w.few = !w.many || (path == FA_PAGED_AUTO && (static_cast<int64_t>(max_q) * B != T || least_units < kSureUnits));
   w.few_cols = !w.many ? INT_MAX : w.few ? 32 : 0;
   const int64_t items32 = (rows / 32 + (B < T ? B : T)) * Hkv;
   w.col_blocks = most <= 32 || w.many || (items32 <= 256 && (most > kFewCols || max_keys <= kWholeKeys)) ? 1 : 2;
@@ -370,7 +370,7 @@ PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, i
     w.desc = place(w.n_wg * static_cast<int64_t>(sizeof(fa::PagedItem)));
   }
   if (w.m.split) {
-    const int64_t places = 2ll * w.m.n_wg * w.m.cols;
+    const int64_t places = 2ll * w.m.n_wg * fa::many_place_cols(w.m.cols);
     w.many_o = place(places * d_v * 4);
     w.many_lse = place(places * 4);
     w.many_desc = place(w.m.n_wg * static_cast<int64_t>(sizeof(fa::PagedItem)));
@@ -485,12 +485,13 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   const bool stream_kv = static_cast<int64_t>(max_q) * p.group <= 32 * w.col_blocks;
   // Beside the kernel for many rows the others are mostly single tokens.
   const int64_t most = static_cast<int64_t>(w.many ? 1 : max_q) * p.group;
-  const int cols = most < w.cols ? static_cast<int>(most) : w.cols;
+  const int cols = most < 1 ? 1 : most < w.cols ? static_cast<int>(most) : w.cols;
   hipError_t e = hipSuccess;
   if (w.many) e = fa::launch_paged_many(p, w.m, cache->d_qk, cache->type == FA_CACHE_E4M3, stream);
   if (e == hipSuccess && w.few) e = fa::launch_paged_few(p, cache->d_qk, cache->type == FA_CACHE_E4M3, w.col_blocks, stream_kv, stream);
-  if (e == hipSuccess && w.few && !w.whole) e = fa::launch_paged_join(p, cache->d_v, false, cols, stream);
-  if (e == hipSuccess && w.m.split) e = fa::launch_paged_join(p, cache->d_v, true, w.m.cols, stream);
+  const bool few_joins = w.few && !w.whole;
+  if (e == hipSuccess && (few_joins || w.m.split))
+    e = fa::launch_paged_join(p, cache->d_v, few_joins ? cols : 0, w.m.split ? w.m.cols : 0, stream);
   return e == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 

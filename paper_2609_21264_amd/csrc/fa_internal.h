@@ -172,12 +172,17 @@ struct AppendParams {
   int rot, begin, inter; // rotated dims (0: none), the first of them, neighbouring pairs
 };
 
+// Columns of a place of the kernel for many rows. One more than a block has: with places 128 KiB apart the workgroups that
+// write and read the same column of theirs at one time would all meet in the same memory channels.
+__host__ __device__ constexpr int many_place_cols(int cols) { return cols + 1; }
+
 // An item of the attention that several workgroups share, written by the first of them for the join kernel.
 struct PagedItem {
   int n_parts;  // 0 or 1: nothing to join
   int q0;       // first packed token of the sequence
   int n_cols, c0, g;
-  int pad[3];
+  int first;    // that workgroup's index on the line of work: its places and those of the next ones hold the parts
+  int pad[2];
 };
 
 struct PagedParams {
@@ -204,8 +209,8 @@ struct PagedParams {
   uint32_t many_work;
   int many_wg, many_min_units, many_cols;  // many_wg: a power of two; many_cols: columns of a block
   int many_log;          // log2 of many_wg, filled by launch_paged_many
-  float* many_o;         // fp32 [2 * many_wg][many_cols][d_v]
-  float* many_lse;       // fp32 [2 * many_wg][many_cols]
+  float* many_o;         // fp32 [2 * many_wg][many_place_cols(many_cols)][d_v]
+  float* many_lse;       // fp32 [2 * many_wg][many_place_cols(many_cols)]
   PagedItem* many_desc;  // [many_wg]
   uint32_t m_group, sh_group;  // division by group, filled by the launchers
 };
@@ -217,12 +222,13 @@ int paged_workgroups(int d_qk, bool fp8, int col_blocks);
 // row-heads per key/value head, in items of 32 * col_blocks of them (1 or 2). stream_kv: K and V are loaded past the
 // caches (items of 32 always are).
 hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, int col_blocks, bool stream_kv, hipStream_t stream);
-// Joins of split items: of the kernel for few rows, or for many. cols: the columns that an item is expected to have (a
-// workgroup for each, up to 32).
-hipError_t launch_paged_join(PagedParams p, int d_v, bool many, int cols, hipStream_t stream);
+// Join of split items of the kernel for few rows and of that for many: the columns that an item of each is expected to have, 0
+// where there is nothing to join.
+hipError_t launch_paged_join(PagedParams p, int d_v, int few_cols, int many_cols, hipStream_t stream);
 // Many rows (fa_paged_fwd_kernel.hip): all other sequences, in blocks of `cols` row-heads of a key/value head. Where `split`,
-// n_wg workgroups share the blocks and a join follows; else a workgroup takes a block, of which there are at most
-// `blocks` per key/value head. max_q, as the host expects it, chooses the instance.
+// n_wg workgroups share the blocks, which are split if the lengths make it worth it, and a join follows; else a workgroup
+// takes a block, of which there are at most `blocks` per key/value head. max_q, as the host expects it, helps to choose the
+// instance.
 struct PagedMany {
   bool is_short, split;
   int cols, n_wg;

@@ -67,13 +67,15 @@ __device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
 }
 __device__ __forceinline__ uint32_t lane_of(uint32_t x, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); }
 
-// The work of the sequences with more than few_cols row-heads per key/value head: visible (query, key) pairs of all query
-// heads, in units of 1024, counted alike by both attention kernels. sl: the first 64 sequences, one per lane.
+// The work of the sequences with more than few_cols row-heads per key/value head, as the kernel for few rows would have
+// it: items of 64 row-heads, each 5 units and one per 128 keys that its rows see on average (one for the rest). Counted
+// alike by both attention kernels. sl: the first 64 sequences, one per lane.
 __device__ __forceinline__ uint32_t big_work(const PagedParams& p, const PagedSeq& sl, int lane) {
   auto of = [&](const PagedSeq& s) {
-    if ((int64_t)s.n_q * p.group <= p.few_cols) return 0u;
-    const int64_t n = s.n_q, pairs = n * s.kv - (p.causal ? n * (n - 1) / 2 : 0);
-    const int64_t units = (min(max(pairs, (int64_t)0), (int64_t)1 << 40) >> 10) * p.hq;  // < 2^61
+    const int64_t cols = (int64_t)s.n_q * p.group;
+    if (cols <= p.few_cols) return 0u;
+    const int64_t keys2 = 2 * (int64_t)s.kv - (p.causal ? min(s.n_q, s.kv) : 0);
+    const int64_t units = (cols + 63) / 64 * p.c.hkv * (6 + (keys2 >> 8));  // below 2^62: cols * hkv < 2^31 + 2^31
     return (uint32_t)min(units, (int64_t)UINT32_MAX);
   };
   uint32_t sum = of(sl);

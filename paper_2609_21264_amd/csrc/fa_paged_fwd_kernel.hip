@@ -10,8 +10,10 @@
 //    of the wave's next 64 tiles, one per lane; a step reads its own with a lane read, so no step waits for the table.
 //  * Pages that are not there are rare: each item looks for one first, and only then masks every tile by pages.
 //  * Where there are blocks enough, a workgroup takes one block, a sequence's last (longest) blocks first.
-//    Otherwise (SPLIT) the blocks lie on one line of work, kBlockCost + tiles units each, that the workgroups share
-//    evenly; parts of a block that several share are joined as those of the kernel for few rows are.
+//    Otherwise (SPLIT) the lengths decide: where the longest block is much longer than an even share of the work (a chunk of
+//    a prompt against a long cache), the blocks lie on one line of work, kBlockCost + tiles units each, that the
+//    workgroups share evenly, and parts of a block that several share are joined as those of the kernel for few
+//    rows are; else a workgroup takes one block here too.
 #include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -26,6 +28,13 @@ namespace fa {
 namespace {
 
 constexpr int kBlockCost = 4;  // fixed cost of a block in tiles
+// Splitting costs a second block's start, writing and reading the parts and the join, 20-40 us in all, so it pays where the
+// longest block has 32 units more than an even share, and 1.9 times as many. Measured, a block per workgroup against
+// split, 128-row-head blocks, one box: d = 128 32/8 heads 1024 x 1024 26 us against 42, 256 x 4096 (8 times the share) 73 : 42,
+// 512 x 4096 (4 times) 74 : 56, 3 x 512 x 4096 (1.4) 112 : 123, 1024 x 8192 (2.0) 148 : 145; d = 64 16/16 2048 x 2048 (26 units
+// more) 28 : 36, 256 x 4096 47 : 28, 3 x 1024 x 8192 (1.3) 145 : 135; blocks of 256, d = 128: 2048 x 2048 57 : 79, 1024 x 8192
+// (2.0) 176 : 137, 3 x 512 x 4096 101 : 119.
+constexpr int kSplitUnits = 32;
 
 // This wave's share of the loads of one K or V tile: BN / NWAVES rows of CH 16-byte chunks, all in one page; E bytes per
 // element.
@@ -116,13 +125,12 @@ void fa_paged_fwd_kernel(PagedParams p) {
   const int smask = (1 << p.c.page_shift) - 1;
 
   // ---- this workgroup's work ----
-  // SPLIT: units [r, r1) of the line; consecutive workgroups run on different XCDs, so the line is dealt to the XCDs
-  // in eighths, and what shares a key/value head mostly shares an L2.
-  const int me = C::SPLIT ? (int)(blockIdx.x % kNumXcd) * (p.many_wg / kNumXcd) + (int)(blockIdx.x / kNumXcd) : 0;
-  int b = 0, g = 0, cb = 0, n_cb = 0, start = 0, r = 0, r1 = 0, per = 1;
+  int b = 0, g = 0, cb = 0, n_cb = 0;
+  int me = 0, start = 0, r = 0, r1 = 0, per = 1;  // split: place on the line, the block's first unit, units [r, r1)
+  bool split = false;
   PagedSeq s{};
   if constexpr (C::SPLIT) {
-    if (tid == 0) p.many_desc[me].n_parts = 0;
+    if (tid == 0) p.many_desc[blockIdx.x].n_parts = 0;
   }
   // The first 64 sequences stay in registers, one per lane; those behind them are read again for each use.
   PagedSeq first{};
@@ -137,22 +145,37 @@ void fa_paged_fwd_kernel(PagedParams p) {
   };
   if (p.few_cols != 0 && big_work(p, first, lane) < p.many_work) return;  // all sequences run in the kernel for few rows
   if constexpr (C::SPLIT) {
-    uint32_t sum = 0;
+    uint32_t sum = 0, blocks = 0;
+    int longest = 0;
     for (int c = 0; c < p.bt.n_seq; c += 64) {
       const PagedSeq sl = seqs_from(c);
+      blocks = add_sat(blocks, wave_sum((uint32_t)n_blocks<BC>(sl, p)));
       uint64_t left = __builtin_amdgcn_ballot_w64(n_blocks<BC>(sl, p) > 0);
       while (left != 0) {
         const PagedSeq x = seq_of_lane(sl, __builtin_ctzll(left));
         left &= left - 1;
-        sum = add_sat(sum, (uint32_t)min((int64_t)head_units<BN, BC>(x, n_blocks<BC>(x, p), p, lane) * p.c.hkv,
-                                         (int64_t)UINT32_MAX));
+        const int n = n_blocks<BC>(x, p);
+        sum = add_sat(sum, (uint32_t)min((int64_t)head_units<BN, BC>(x, n, p, lane) * p.c.hkv, (int64_t)UINT32_MAX));
+        longest = max(longest, kBlockCost + Block<BN, BC>(x, n - 1, p).tiles());
       }
     }
     const int total = uniform((int)min(sum, (uint32_t)INT32_MAX));
+    longest = uniform(longest);
     per = max(p.many_min_units, (int)((uint32_t)(total - 1) >> p.many_log) + 1);
-    if ((int64_t)me * per >= total) return;
-    r = me * per;
-    r1 = min(total - r, per) + r;
+    const int64_t items = (int64_t)uniform((int)min(blocks, (uint32_t)INT32_MAX)) * p.c.hkv;
+    split = items > p.many_wg || (longest - per > kSplitUnits && 10ll * longest >= 19ll * per);
+    if (split) {
+      // Consecutive workgroups run on different XCDs, so the line is dealt to the XCDs in eighths: what shares a
+      // key/value head mostly shares an L2.
+      const int active = (int)((uint32_t)(total + per - 1) / (uint32_t)per), eighth = (active + kNumXcd - 1) / kNumXcd;
+      const int slot = (int)(blockIdx.x / kNumXcd);
+      me = uniform((int)(blockIdx.x % kNumXcd) * eighth + slot);
+      if (slot >= eighth || (int64_t)me * per >= total) return;
+      r = me * per;
+      r1 = min(total - r, per) + r;
+    }
+  }
+  if (C::SPLIT && split) {
     // The sequence, head and block that hold unit r.
     bool found = false;
     for (int c = 0; c < p.bt.n_seq && !found; c += 64) {
@@ -214,8 +237,8 @@ void fa_paged_fwd_kernel(PagedParams p) {
     const int tiles = blk.tiles();
     int t0 = 0, nt = tiles, n_parts = 1, first_wg = me;
     bool skip = false;
-    if constexpr (C::SPLIT) {
-      const int cost = kBlockCost + tiles, end = min(r1, start + cost);
+    if (C::SPLIT && split) {
+      const int cost = kBlockCost + tiles, end = min(r1 - start, cost) + start;
       t0 = max(0, r - start - kBlockCost);
       nt = max(0, end - start - kBlockCost - t0);
       // The block belongs to the workgroups that have tiles of it (one without a tile: to that of its first unit).
@@ -428,7 +451,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
       if constexpr (C::E4M3) vs = p.c.v_scale != nullptr ? scalar_load(p.c.v_scale + g) : 1.f;
       if (C::SPLIT && n_parts > 1) {
         // A part: O normalised by its own sum (fp32), and its LSE. Place 2 me: of a block that begins before.
-        const int64_t place = (2 * (int64_t)me + (me == first_wg ? 1 : 0)) * BC;
+        const int64_t place = (2 * (int64_t)me + (me == first_wg ? 1 : 0)) * many_place_cols(BC);
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
           const float l_tot = half_swap_sum(st.l_run[qb]);
@@ -447,7 +470,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
           }
         }
         if (me == first_wg && tid == 0)
-          p.many_desc[me] = PagedItem{n_parts, s.q0, min(BC, blk.cols - blk.c0), blk.c0, g};
+          p.many_desc[blockIdx.x] = PagedItem{n_parts, s.q0, min(BC, blk.cols - blk.c0), blk.c0, g, me};
       } else {
         // O through LDS, so that each store instruction writes whole rows (layout: see the fused forward).
         unsigned char* stage = smem + wave * WROWS * RB;
@@ -511,7 +534,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
     if constexpr (!C::SPLIT) {
       break;
     } else {
-      if (r >= r1) break;
+      if (!split || r >= r1) break;
       // The next block: of this head, of the next, of the next sequence with any.
       start += kBlockCost + tiles;
       if (++cb == n_cb) {
@@ -552,10 +575,13 @@ hipError_t launch_many(PagedParams p, int64_t blocks, hipStream_t stream) {
   const dim3 grid((unsigned)(C::SPLIT ? p.many_wg : blocks * p.c.hkv));
   return hipLaunchKernel(reinterpret_cast<const void*>(&fa_paged_fwd_kernel<C>), grid, dim3(C::NT), args, 0, stream);
 }
+// Where there is a short instance, the long one runs only grids that fill the chip (paged_many): it is never split.
 template <int DQK, int DV, bool E4M3, bool SHORT>
 hipError_t launch_many_split(const PagedParams& p, const PagedMany& m, hipStream_t stream) {
-  return m.split ? launch_many<typename PagedInstance<DQK, DV, E4M3, SHORT, true>::C>(p, m.blocks, stream)
-                 : launch_many<typename PagedInstance<DQK, DV, E4M3, SHORT, false>::C>(p, m.blocks, stream);
+  if constexpr (SHORT || E4M3 || DQK == 192) {
+    if (m.split) return launch_many<typename PagedInstance<DQK, DV, E4M3, SHORT, true>::C>(p, m.blocks, stream);
+  }
+  return launch_many<typename PagedInstance<DQK, DV, E4M3, SHORT, false>::C>(p, m.blocks, stream);
 }
 
 }  // namespace
@@ -563,14 +589,19 @@ hipError_t launch_many_split(const PagedParams& p, const PagedMany& m, hipStream
 PagedMany paged_many(int n_seq, int n_tokens, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3) {
   PagedMany m{};
   const int64_t rows = (int64_t)n_tokens * group;
-  m.is_short = !e4m3 && d_qk != 192 && (int64_t)max_q * group <= 128;
+  int64_t seqs = rows / (few_cols + 1);
+  if (seqs > n_seq) seqs = n_seq;
+  // Short blocks where sequences have no more, and where long ones would not fill the chip twice (d = 128; at d = 64, with
+  // two long workgroups per CU, as often). Long against short, a block per workgroup, one box: d = 128 32/8 heads 512 x 512
+  // 22.3 : 17.1 us, 2048 x 2048 (256 long blocks) 56.6 : 51.2, 4096 x 4096 (512) 133 : 143, 2048 x 8192 219 : 228; d = 64 16/16
+  // 2048 x 2048 48.0 : 28.4, 4096 x 4096 87.1 : 55.8, 3 x 4096 x 4096 (768) 155 : 144.
+  const int64_t fill = d_qk == 64 ? 1024 : 512;
+  m.is_short = !e4m3 && d_qk != 192 && ((int64_t)max_q * group <= 128 || (rows / 256 + seqs) * hkv < fill);
   m.cols = m.is_short ? 128 : 256;
   m.n_wg = m.is_short || (d_qk == 64 && !e4m3) ? 512 : 256;
   // The most blocks that the packed tokens can make: whole ones, and a last one for each sequence of this kernel.
-  int64_t seqs = rows / (few_cols + 1);
-  if (seqs > n_seq) seqs = n_seq;
   m.blocks = rows / m.cols + seqs;
-  m.split = m.blocks * hkv < 2 * m.n_wg;
+  m.split = m.blocks * hkv < m.n_wg;  // never with long blocks where there are short ones: fill is n_wg at least
   return m;
 }
 

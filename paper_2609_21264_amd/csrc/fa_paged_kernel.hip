@@ -9,6 +9,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fa_device.h"
 #include "fa_e4m3.h"
 #include "fa_fastdiv.h"
@@ -609,17 +611,28 @@ void fa_paged_few_kernel(PagedParams p) {
       }
     }
     if (n_parts > 1 && me == first_wg && tid == 0)
-      p.desc[me] = PagedItem{n_parts, s.q0, min(COLS, cols - c0), c0, g};
+      p.desc[me] = PagedItem{n_parts, s.q0, min(COLS, cols - c0), c0, g, me};
     __syncthreads();  // the next item's loads overwrite the buffers above
   }
 }
 
-// Join of the parts of the item that begins in workgroup blockIdx.x of an attention kernel and goes on in the next ones
-// (none: n_parts 0): O = sum_k w_k O_k / sum_k w_k with w_k = exp(LSE_k - max
+// What a join reads: the items of one attention kernel, a workgroup (of the grid's first dimension) for each of its
+// workgroups times cols (columns that an item is expected to have).
+struct JoinSource {
+  const PagedItem* desc;  // [n]
+  const float* o_part;
+  const float* lse_part;
+  int part_cols, n, cols;
+};
+
+// Join of the parts of an item (none: n_parts 0): O = sum_k w_k O_k / sum_k w_k with w_k = exp(LSE_k - max
 // LSE). DV / 4 threads (4 output dims each) by pg part groups take a column, group j
-// the parts j, j + pg, ..., eight at a time so that their loads are in flight together, with a running maximum; the
-// groups' sums are added in their order through LDS. pg is the smallest power of two that leaves a group at most eight
-// parts, at most 1024 / DV; the workgroup's other groups take other columns.
+// the parts j, j + pg, ... with a running maximum, up to six at a time whose loads are in flight together (exactly as many
+// as there are: their latency, and for blocks of the kernel for many rows their bytes, are the kernel's time); the groups'
+// sums are added in their order through LDS. pg is the smallest power of two that leaves a group at most six parts, at most
+// 1024 / DV; the workgroup's other groups take other columns. BOTH: one launch joins the items of both attention kernels (a second one would take 4 us more, this
+// form costs 1 us where there is one): the first a.n * a.cols workgroups take those of `a`, the rest those of `b`. Else
+// the grid is a.n by a.cols.
 template <int DV>
 struct JoinLds {
   float m[1024 / DV], den[1024 / DV];
@@ -628,48 +641,68 @@ struct JoinLds {
 // Place of the k-th part of an item whose first part is workgroup `first`'s.
 __device__ __forceinline__ int64_t part_place(int first, int k) { return 2 * ((int64_t)first + k) + (k == 0 ? 1 : 0); }
 
-template <int DV>
-__global__ __launch_bounds__(256) void fa_paged_join_kernel(PagedParams p, const PagedItem* desc, const float* o_part,
-                                                            const float* lse_part, int part_cols) {
+template <int DV, bool BOTH>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(8))) void fa_paged_join_kernel(PagedParams p, JoinSource a, JoinSource b) {
   __shared__ JoinLds<DV> lds;
-  const PagedItem it = desc[blockIdx.x];
+  JoinSource src = a;
+  int item = (int)blockIdx.x, share = (int)blockIdx.y;
+  if constexpr (BOTH) {
+    const int n_a = a.n * a.cols;
+    if (item >= n_a) src = b, item -= n_a;
+    share = (int)((uint32_t)item / (uint32_t)src.n);
+    item -= share * src.n;
+  }
+  const PagedItem it = src.desc[item];
   if (it.n_parts <= 1) return;
-  const int first = blockIdx.x;
+  const int first = it.first, part_cols = src.part_cols;
+  const float* const o_part = src.o_part;
+  const float* const lse_part = src.lse_part;
   int pg = 1;
-  while (8 * pg < it.n_parts && pg < 1024 / DV) pg *= 2;
-  constexpr int TD = DV / 4, NG = 256 / TD, AHEAD = 8;  // threads per column, groups, parts at a time
+  while (6 * pg < it.n_parts && pg < 1024 / DV) pg *= 2;
+  constexpr int TD = DV / 4, NG = 256 / TD;  // threads per column, groups
   const int q = threadIdx.x % TD, grp = threadIdx.x / TD;
   const int j = grp & (pg - 1), at_once = NG / pg;
-  for (int c0 = blockIdx.y * at_once; c0 < it.n_cols; c0 += gridDim.y * at_once) {
+  for (int c0 = share * at_once; c0 < it.n_cols; c0 += src.cols * at_once) {
     const int col = c0 + grp / pg;
     const bool live = col < it.n_cols;
     float m = -INFINITY, den = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int k0 = j; live && k0 < it.n_parts; k0 += AHEAD * pg) {
-      float l[AHEAD], top = m;
-      f32x4 v[AHEAD];
+    // N parts of each group, base + j + pg * i (the last group's last may lie behind the item's last part).
+    auto batch = [&](auto n, int base) {
+      constexpr int N = decltype(n)::value;
+      float l[N], top = m;
+      f32x4 v[N];
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const int k = min(k0 + i * pg, it.n_parts - 1);
-        const int64_t at = part_place(first, k) * part_cols + col;
+      for (int i = 0; i < N; ++i) {
+        const int64_t at = part_place(first, min(base + j + pg * i, it.n_parts - 1)) * part_cols + (live ? col : 0);
         l[i] = lse_part[at];
         v[i] = *reinterpret_cast<const f32x4*>(o_part + at * DV + 4 * q);
       }
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        l[i] = k0 + i * pg < it.n_parts ? l[i] : -INFINITY;
+      for (int i = 0; i < N; ++i) {
+        l[i] = base + j + pg * i < it.n_parts ? l[i] : -INFINITY;
         top = fmaxf(top, l[i]);
       }
       const float ref = top == -INFINITY ? 0.f : top, a = expf(m - ref);
       den *= a;
       acc *= a;
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
+      for (int i = 0; i < N; ++i) {
         const float w = expf(l[i] - ref);
         den += w;
         acc += w * v[i];
       }
       m = top;
+    };
+    for (int base = 0; base < it.n_parts; base += 6 * pg) {
+      switch ((it.n_parts - base + pg - 1) / pg) {  // for the whole workgroup the same
+        case 1: batch(std::integral_constant<int, 1>{}, base); break;
+        case 2: batch(std::integral_constant<int, 2>{}, base); break;
+        case 3: batch(std::integral_constant<int, 3>{}, base); break;
+        case 4: batch(std::integral_constant<int, 4>{}, base); break;
+        case 5: batch(std::integral_constant<int, 5>{}, base); break;
+        default: batch(std::integral_constant<int, 6>{}, base);
+      }
     }
     if (pg > 1) {
       __syncthreads();  // the last columns' sums have been read
@@ -759,14 +792,20 @@ hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, int col_blocks, b
   return stream_kv ? launch_few_dims<2, true>(p, d_qk, fp8, stream) : launch_few_dims<2, false>(p, d_qk, fp8, stream);
 }
 
-hipError_t launch_paged_join(PagedParams p, int d_v, bool many, int cols, hipStream_t stream) {
-  const PagedItem* desc = many ? p.many_desc : p.desc;
-  const float *o = many ? p.many_o : p.o_part, *lse = many ? p.many_lse : p.lse_part;
-  int part_cols = many ? p.many_cols : p.part_cols;
-  void* args[] = {&p, &desc, &o, &lse, &part_cols};
-  return hipLaunchKernel(d_v == 64 ? reinterpret_cast<const void*>(&fa_paged_join_kernel<64>)
-                                   : reinterpret_cast<const void*>(&fa_paged_join_kernel<128>),
-                         dim3(many ? p.many_wg : p.n_wg, cols < 1 ? 1 : cols > 32 ? 32 : cols), dim3(256), args, 0, stream);
+hipError_t launch_paged_join(PagedParams p, int d_v, int few_cols, int many_cols, hipStream_t stream) {
+  auto clamped = [](int cols) { return cols < 1 ? 1 : cols > 32 ? 32 : cols; };
+  many_cols = many_cols * d_v / 1024;  // blocks have few parts each, so a workgroup takes 1024 / d_v columns at once
+  JoinSource few{p.desc, p.o_part, p.lse_part, p.part_cols, p.n_wg, clamped(few_cols)};
+  JoinSource many{p.many_desc, p.many_o, p.many_lse, many_place_cols(p.many_cols), p.many_wg, clamped(many_cols)};
+  const bool both = few_cols > 0 && many_cols > 0;
+  JoinSource* first = few_cols > 0 ? &few : &many;
+  void* args[] = {&p, first, &many};
+  const dim3 grid = both ? dim3((unsigned)(few.n * few.cols + many.n * many.cols)) : dim3(first->n, first->cols);
+  const void* k = both ? (d_v == 64 ? reinterpret_cast<const void*>(&fa_paged_join_kernel<64, true>)
+                                    : reinterpret_cast<const void*>(&fa_paged_join_kernel<128, true>))
+                       : (d_v == 64 ? reinterpret_cast<const void*>(&fa_paged_join_kernel<64, false>)
+                                    : reinterpret_cast<const void*>(&fa_paged_join_kernel<128, false>));
+  return hipLaunchKernel(k, grid, dim3(256), args, 0, stream);
 }
 
 }  // namespace fa
