@@ -369,7 +369,8 @@ typedef enum {
  * key reaches only the rows that see the key; one in a value may reach other rows of its sequence.
  *   Q, O        bf16 [T][Hq][d_qk], [T][Hq][d_v]; element (t, h, 0) at t * q_token + h * q_head
  *   LSE         float32 [T][Hq] (contiguous), or NULL
- *   strides     {q_token, q_head, o_token, o_head}, in elements, multiples of 8
+ *   strides     {q_token, q_head, o_token, o_head}, in elements, multiples of 8. O and LSE overlap neither each other nor
+ *               an input (O may be Q itself with the same strides, where d_qk = d_v)
  *   max_q       the most new tokens of one sequence, as far as the host knows: it helps to choose the kernels, the results
  *               are right for any
  *   path        fa_paged_path_t

@@ -456,17 +456,21 @@ void fa_paged_fwd_kernel(PagedParams p) {
         for (int qb = 0; qb < QB; ++qb) {
           const float l_tot = half_swap_sum(st.l_run[qb]);
           const float inv = l_tot > 0.f ? vs / l_tot : 0.f;
+          const bool some = l_tot > 0.f;
           const int col = col0 + qb * 32 + st.i32;
           if (blk.c0 + col < blk.cols) {
             float* orow = p.many_o + (place + col) * DV;
 #pragma unroll
             for (int db = 0; db < A::DB; ++db)
 #pragma unroll
-              for (int g4 = 0; g4 < 4; ++g4)
-                *reinterpret_cast<f32x4*>(orow + db * 32 + 8 * g4 + 4 * st.h) =
-                    f32x4{st.oacc[db][qb][4 * g4] * inv, st.oacc[db][qb][4 * g4 + 1] * inv,
-                          st.oacc[db][qb][4 * g4 + 2] * inv, st.oacc[db][qb][4 * g4 + 3] * inv};
-            if (st.h == 0) p.many_lse[place + col] = l_tot > 0.f ? (st.m_run[qb] + log2f(l_tot)) * kLn2 : -INFINITY;
+              for (int g4 = 0; g4 < 4; ++g4) {
+                const f32x4 o = {st.oacc[db][qb][4 * g4] * inv, st.oacc[db][qb][4 * g4 + 1] * inv,
+                                 st.oacc[db][qb][4 * g4 + 2] * inv, st.oacc[db][qb][4 * g4 + 3] * inv};
+                *reinterpret_cast<f32x4*>(orow + db * 32 + 8 * g4 + 4 * st.h) = some ? o : f32x4{0.f, 0.f, 0.f, 0.f};
+              }
+            if (st.h == 0)  // a sum that is no number stays one in the join
+              p.many_lse[place + col] =
+                  some ? (st.m_run[qb] + log2f(l_tot)) * kLn2 : isnan(l_tot) ? NAN : -INFINITY;
           }
         }
         if (me == first_wg && tid == 0)

@@ -199,6 +199,7 @@ __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams 
 // of K and V enter with the scores' scale and with the final division.
 
 constexpr int kItemCost = 1;  // fixed cost of an item in tiles
+constexpr int kMinUnits = 2;  // least work of a workgroup: one token over 1 023 keys 12.0 us with 2, 15.6 with 4
 constexpr float kRise = 8.f;  // how far (log2) a maximum may rise over its reference
 
 template <int DQK_, int DV_, bool FP8_, int QB_, bool STREAM_, int SLOTS_>
@@ -607,7 +608,7 @@ void fa_paged_few_kernel(PagedParams p) {
         float* dst = p.o_part + (place * p.part_cols + col) * DV + d0;
 #pragma unroll
         for (int d = 0; d < DV / TPC; d += 4) *reinterpret_cast<f32x4*>(dst + d) = o[d / 4];
-        if (tid % TPC == 0) p.lse_part[place * p.part_cols + col] = lse;
+        if (tid % TPC == 0) p.lse_part[place * p.part_cols + col] = isnan(Lsum) ? NAN : lse;
       }
     }
     if (n_parts > 1 && me == first_wg && tid == 0)
@@ -721,12 +722,13 @@ __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_pe
           acc += w * lds.acc[grp + k][q];
         }
       }
-      acc *= den > 0.f ? 1.f / den : 0.f;
+      const bool some = den > 0.f;  // else no part with a visible key, or one whose sum is no number
+      acc = some ? acc * (1.f / den) : f32x4{0.f, 0.f, 0.f, 0.f};
       const int c = it.c0 + col, row = c / p.group, head = it.g * p.group + c - row * p.group;
       const int64_t tok = it.q0 + row;
       *reinterpret_cast<u32x2*>(p.o + tok * p.o_token + (int64_t)head * p.o_head + 4 * q) =
           u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
-      if (q == 0 && p.lse != nullptr) p.lse[tok * p.hq + head] = den > 0.f ? m + logf(den) : -INFINITY;
+      if (q == 0 && p.lse != nullptr) p.lse[tok * p.hq + head] = some ? m + logf(den) : -INFINITY;
     }
   }
 }
@@ -779,10 +781,7 @@ hipError_t launch_few_dims(PagedParams p, int d_qk, bool fp8, hipStream_t stream
 }
 
 hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, int col_blocks, bool stream_kv, hipStream_t stream) {
-#ifndef FA_MIN_UNITS
-#define FA_MIN_UNITS 2
-#endif
-  p.min_units = FA_MIN_UNITS;
+  p.min_units = kMinUnits;
   p.wg_log = 0;
   while ((1 << p.wg_log) < p.n_wg) ++p.wg_log;
   const FastDiv fg = make_fastdiv(p.group);

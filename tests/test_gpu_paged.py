@@ -180,6 +180,41 @@ def test_not_finite_values_stay_in_their_rows():
     assert torch.all(o[0, :2] == 0) and torch.all(torch.isneginf(lse[0, :2]))
 
 
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("new,keys,Hq,Hkv,path", [(1, 5000, 8, 2, "few"), (3, 20000, 8, 2, "few"), (300, 4000, 64, 8, "many")])
+def test_no_number_where_the_keys_are_split(new, keys, Hq, Hkv, path, dqk, dv):
+    """A row whose sum is no number has O = 0 and LSE = -inf also where other workgroups have the rest of its keys."""
+    bt = Batch([new], [keys], Hq, Hkv, dqk, dv, 16, seed=46)
+    clean, clean_lse = bt.attend(return_lse=True, path=path)
+    kc, group = bt.d_k_cache, Hq // Hkv
+    for head, key in ((0, 1000), (1, keys - (new + 1) // 2)):
+        kc[int(bt.table[0, key // 16]), head, key % 16, 7] = float("nan")
+    o, lse = bt.attend(return_lse=True, path=path)
+    torch.cuda.synchronize()
+    seen = torch.zeros(new, Hq, dtype=torch.bool, device="cuda")
+    seen[:, :group] = True
+    seen[new - (new + 1) // 2:, group:2 * group] = True
+    assert torch.all(o[seen] == 0) and torch.all(torch.isneginf(lse[seen]))
+    if seen.all():
+        return
+    # The others may be rescaled at other tiles: two roundings of P and O apart in each run; of the same scores.
+    o, clean = o[~seen].float(), clean[~seen].float()
+    assert (o - clean).abs().max() <= 2 * (2 ** -7 + 1e-5) * bt.d_v_cache[bt.d_table[bt.d_table >= 0].long()].float().nan_to_num().abs().max()
+    lse, clean_lse = lse[~seen], clean_lse[~seen]
+    assert (lse - clean_lse).abs().max() <= 2 * 2 ** -20 * (1 + 2 * clean_lse.abs().max() + math.log(keys))
+
+
+@pytest.mark.parametrize("dqk", [64, 128])
+@pytest.mark.parametrize("path", [None, "few", "many"])
+def test_output_over_the_queries(path, dqk):
+    bt = Batch([1, 70, 300, 3], [3000, 90, 1500, 40], 32, 8, dqk, dqk, 16, seed=48)
+    o, lse = bt.attend(return_lse=True, path=path)
+    q = bt.d_q.clone()
+    o2, lse2 = fa.forward_paged(q, bt.d_k_cache, bt.d_v_cache, bt.d_table, bt.d_kv_lens, bt.d_q_starts, max_q=300, out=q,
+                                return_lse=True, path=path)
+    assert o2 is q and torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
 def test_offsets_past_32_bits():
     """A cache of 4.5 GiB per buffer, its last pages in use."""
     pages, page = 73728, 64
