@@ -15,9 +15,11 @@ Contents (all NumPy float64 or plain Python, no GPU):
 * :mod:`oracle.layer_by_layer` -- the paper's unfused layer-by-layer mapping as three operators with
   bfloat16 intermediates (score matrix, probabilities), the oracle of the unfused GPU baseline, with
   a direct float64 -> bfloat16 rounding and the error bound of the three roundings.
+* :mod:`oracle.paged` -- the paged key/value cache: the rotation of a token by its position, where its keys lie, and
+  the attention over the keys gathered from a sequence's pages.
 * :func:`bf16_bits_to_f64` -- exact decoding of bfloat16 bit patterns.
 
-Every function is pinned by ``tests/test_oracle_*.py`` against facts that do not come from the
+Every function is pinned by ``tests/test_oracle_*.py`` (:mod:`oracle.paged` by ``tests/test_paged_host.py``) against facts that do not come from the
 oracle itself: torch's float64 CPU attention routine, closed forms, invariances, the brute force.
 """
 

@@ -1,6 +1,6 @@
 // Internal interface between the C-ABI layer (fa_api.hip) and the kernel launchers (fa_fwd_kernel.hip:
-// fused forward and split mode; fa_lbl_kernel.hip: layer-by-layer operators). Not installed; callers
-// use include/fa.h.
+// fused forward and split mode; fa_decode_kernel.hip: decode; fa_lbl_kernel.hip: layer-by-layer operators;
+// fa_paged_kernel.hip and fa_paged_fwd_kernel.hip: the paged cache). Not installed; callers use include/fa.h.
 #pragma once
 
 #include <hip/hip_runtime.h>
