@@ -46,11 +46,12 @@ sys.path.insert(0, ROOT)
 
 PEAK_BF16_TFLOPS = 2516.6  # 256 CUs x 4096 dense bf16 FLOP/clk/CU x 2.4 GHz
 PEAK_HBM_GBS = 8000.0      # HBM3E
-# Device code whose measurements the committed profiles certify: every kernel and the headers they
-# share (the host-side argument checks of fa_api.hip are not part of it).
+# Device code whose measurements the committed profiles certify: the kernels that the workloads run and the
+# headers they share (the host-side argument checks of fa_api.hip are not part of it).
 KERNEL_SOURCES = ["paper_2609_21264_amd/csrc/fa_fwd_kernel.hip", "paper_2609_21264_amd/csrc/fa_decode_kernel.hip",
                   "paper_2609_21264_amd/csrc/fa_lbl_kernel.hip", "paper_2609_21264_amd/csrc/fa_internal.h",
-                  "paper_2609_21264_amd/csrc/fa_device.h"]
+                  "paper_2609_21264_amd/csrc/fa_device.h", "paper_2609_21264_amd/csrc/fa_fwd_attn.h",
+                  "paper_2609_21264_amd/csrc/fa_fastdiv.h", "paper_2609_21264_amd/csrc/fa_e4m3.h"]
 
 
 def _code_tokens(text: str) -> str:
