@@ -310,8 +310,9 @@ bool token_strides(const long long* s, int n) {
 //  * The kernel for few rows reads K and V once per item of 32 or 64 row-heads of a key/value head, and starts fast; the
 //    kernel for many rows computes at three times its rate, and takes some 10 us more to start. The former runs alone where
 //    the host expects no sequence with more than 64 row-heads, or where the table holds too few keys for kManyUnits units
-//    of work (items of 64 row-heads, 5 units each and one per 128 keys); the latter where all sequences have max_q tokens
-//    and with as few keys kSureUnits. Else both are launched and find from the lengths whether the sequences with more than
+//    of work (items of 64 row-heads, 5 units each and one per 128 keys); the latter where no sequence can have as few as 64
+//    row-heads if none has more than max_q tokens, and where even without cached keys they have kSureUnits (prompts of 4 096
+//    and 3 001 tokens, 32/8 heads, d = 128: 200 us alone, 206 with the others' launches; 2 000 and 1 500: 61.5 against 65.5). Else both are launched and find from the lengths whether the sequences with more than
 //    32 row-heads have kManyUnits together: if so the kernel for many rows takes these, else that for few takes all.
 //    Few against many, us, one box (units): d = 128 32/8 heads 512 x 512 (1.8 K) 17.0 : 22.2, 128 x 2000 (1.3 K) 31.7 : 45.6,
 //    4 x 200 x 200 (2.5 K) 22.8 : 18.8, 700 x 700 (2.8 K) 40.9 : 24.9, 4 x 128 x 2000 (5.4 K) 48.6 : 50.2, 300 x 4000 (5.5 K)
@@ -341,11 +342,13 @@ PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, i
   const int64_t rows = static_cast<int64_t>(T) * group, most = static_cast<int64_t>(max_q) * group;
   const bool e4m3 = type == FA_CACHE_E4M3;
   w.many_work = kManyUnits;
-  // The most units that the call can have, and the fewest with max_q new tokens (and so keys) in every sequence.
+  // The most units that the call can have, and the fewest (sequences of equal length, without cached keys); the fewest
+  // row-heads of a sequence where none has more than max_q tokens.
   const double most_units = (static_cast<double>(rows) / 64 + B) * Hkv * (6 + max_keys / 128);
-  const double least_units = static_cast<double>(most + 63) / 64 * Hkv * B * (6 + max_q / 256);
+  const double least_units = static_cast<double>(rows) / 64 * Hkv * (6 + T / B / 256);
+  const double least = static_cast<double>(rows) - (B - 1.0) * static_cast<double>(most);
   w.many = path == FA_PAGED_MANY || (path == FA_PAGED_AUTO && most > kFewCols && rows > kFewCols && most_units >= kManyUnits);
-  w.few = !w.many || (path == FA_PAGED_AUTO && (static_cast<int64_t>(max_q) * B != T || least_units < kSureUnits));
+  w.few = !w.many || (path == FA_PAGED_AUTO && (least <= kFewCols || least_units < kSureUnits));
   w.few_cols = !w.many ? INT_MAX : w.few ? 32 : 0;
   const int64_t items32 = (rows / 32 + (B < T ? B : T)) * Hkv;
   w.col_blocks = most <= 32 || w.many || (items32 <= 256 && (most > kFewCols || max_keys <= kWholeKeys)) ? 1 : 2;
