@@ -352,7 +352,7 @@ PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, i
   w.few_cols = !w.many ? INT_MAX : w.few ? 32 : 0;
   const int64_t items32 = (rows / 32 + (B < T ? B : T)) * Hkv;
   w.col_blocks = most <= 32 || w.many || (items32 <= 256 && (most > kFewCols || max_keys <= kWholeKeys)) ? 1 : 2;
-  if (w.many) w.m = fa::paged_many(B, T, Hkv, group, max_q, w.few_cols, d_qk, e4m3);
+  if (w.many) w.m = fa::paged_many(B, T, max_keys, Hkv, group, max_q, w.few_cols, d_qk, e4m3);
   auto place = [&](int64_t n) {
     const int64_t at = w.bytes;
     w.bytes += (n + 15) / 16 * 16;

@@ -234,7 +234,7 @@ struct PagedMany {
   int cols, n_wg;
   int64_t blocks;
 };
-PagedMany paged_many(int n_seq, int n_tokens, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3);
+PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3);
 hipError_t launch_paged_many(PagedParams p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream);
 
 }  // namespace fa

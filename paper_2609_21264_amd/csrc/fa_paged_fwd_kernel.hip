@@ -32,6 +32,7 @@ namespace fa {
 namespace {
 
 constexpr int kBlockCost = 4;  // fixed cost of a block in tiles
+constexpr int kSplitTile = 64;  // keys of a tile where blocks are split
 // Splitting costs a second block's start, writing and reading the parts and the join, 20-40 us in all, so it pays where the
 // longest block has 32 units more than an even share, and 1.9 times as many. Measured, a block per workgroup against
 // split, 128-row-head blocks, one box: d = 128 32/8 heads 1024 x 1024 26 us against 42, 256 x 4096 (8 times the share) 73 : 42,
@@ -115,6 +116,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
   constexpr int R = BN / C::NWAVES;        // keys that a wave brings of a tile
   constexpr int E = C::E;
   static_assert(C::KSPLIT == 1 && C::KA - C::VA <= 1, "a V tile is loaded with its K tile or one step later");
+  static_assert(!C::SPLIT || BN == kSplitTile, "the host counts the line's units");
 
   __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS_BYTES];
   const int tid = threadIdx.x;
@@ -594,7 +596,7 @@ hipError_t launch_many_split(const PagedParams& p, const PagedMany& m, hipStream
 
 }  // namespace
 
-PagedMany paged_many(int n_seq, int n_tokens, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3) {
+PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3) {
   PagedMany m{};
   const int64_t rows = (int64_t)n_tokens * group;
   int64_t seqs = rows / (few_cols + 1);
@@ -609,7 +611,10 @@ PagedMany paged_many(int n_seq, int n_tokens, int hkv, int group, int max_q, int
   m.n_wg = m.is_short || (d_qk == 64 && !e4m3) ? 512 : 256;
   // The most blocks that the packed tokens can make: whole ones, and a last one for each sequence of this kernel.
   m.blocks = rows / m.cols + seqs;
-  m.split = m.blocks * hkv < m.n_wg;  // never with long blocks where there are short ones: fill is n_wg at least
+  // Never with long blocks where there are short ones: fill is n_wg at least. The line of work is counted in 32 bits: where
+  // the table has pages for more units than that (128 blocks over 2^30 keys each) no block is split.
+  const int64_t units = kBlockCost + (static_cast<int64_t>(max_keys) + kSplitTile - 1) / kSplitTile;  // of a block, at most
+  m.split = m.blocks * hkv < m.n_wg && m.blocks * hkv * units <= INT32_MAX;
   return m;
 }
 

@@ -1,0 +1,26 @@
+"""Sizes at the borders of what the paged calls count and launch, on the host (no GPU needed)."""
+
+import pytest
+
+import paper_2609_21264_amd as fa
+
+MANY = fa.FA_PAGED_MANY
+
+
+def workspace(B, T, keys, Hq, Hkv, d=128, type=0, max_q=1, path=MANY):
+    return fa.fa_fwd_paged_workspace_bytes(B, T, keys, Hq, Hkv, d, d, type, max_q, path)
+
+
+@pytest.mark.parametrize("type", [0, 1])
+@pytest.mark.parametrize("d", [64, 128])
+def test_split_blocks_lie_on_a_line_that_32_bits_count(d, type):
+    """The kernel for many rows splits blocks (and needs a workspace) only where all of them, 4 units and one per 64
+    keys each, are fewer than 2^31 units: what lay behind would not be run."""
+    assert workspace(248, 248, 2 ** 30, 1, 1, d, type) == 0      # 248 sequences of one token and 2^30 keys: 4.2e9 units
+    assert workspace(100, 100, 2 ** 30, 1, 1, d, type) > 0       # 1.7e9
+    for blocks in (1, 7, 100, 127, 128, 129, 200, 250):
+        for keys in (2 ** 20, 2 ** 28, 2 ** 29, 2 ** 30 - 2 ** 20, 2 ** 30):
+            units = 4 + -(-keys // 64)
+            split = workspace(blocks, blocks, keys, 1, 1, d, type) > 0
+            assert split or (blocks + blocks // 128) * units >= 2 ** 31, (blocks, keys)  # what the host takes for the most
+            assert not split or blocks * units < 2 ** 31, (blocks, keys)
