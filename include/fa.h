@@ -365,8 +365,9 @@ typedef enum {
  * fa_fwd_paged -- attention of the new tokens over the paged cache: for token t of sequence b at position p,
  *     O[t,h] = softmax over visible j of (scale * q[t,h] . K[b,g,j]) * V[b,g,j],   g = h / (Hq / Hkv),
  * j <= p when causal, j < kv_lens[b] else. Arithmetic as for fa_fwd_ex (e4m3 caches: K and V are widened exactly, P is
- * rounded to fp16). A row with no visible key, or whose sum is no number, gets O = 0, LSE = -inf. An infinity or a NaN in a
- * key reaches only the rows that see the key; one in a value may reach other rows of its sequence.
+ * rounded to fp16, by 2^-11 of it or 2^-32 of the row's largest at most). A row with no visible key, or whose sum is no
+ * number, gets O = 0, LSE = -inf. An infinity or a NaN in a key reaches only the rows that see the key; one in a value may
+ * reach other rows of its sequence.
  *   Q, O        bf16 [T][Hq][d_qk], [T][Hq][d_v]; element (t, h, 0) at t * q_token + h * q_head
  *   LSE         float32 [T][Hq] (contiguous), or NULL
  *   strides     {q_token, q_head, o_token, o_head}, in elements, multiples of 8. O and LSE overlap neither each other nor

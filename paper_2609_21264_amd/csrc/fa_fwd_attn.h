@@ -151,6 +151,8 @@ struct Cfg {
   // take dims 32 m + 16 h + 0 .. 7 and + 8 .. 15 in lane half h.
   static constexpr bool E4M3 = E4M3_;
   static constexpr int E = E4M3_ ? 1 : 2;  // bytes per element of K and V
+  static constexpr float P_LOG2 = E4M3_ ? kE4m3PLog2 : 0.f;  // probabilities and their sums are held times 2^P_LOG2
+  static constexpr float OVERFLOW_SUM = kOverflowSum * (E4M3_ ? 1 << (int)kE4m3PLog2 : 1);
   static constexpr bool CHUNKED = QB > 1;  // long instance: key/value heads in chunks (launch_cfg)
   static constexpr int NT = NWAVES * 64;
   // Waves per SIMD the registers are budgeted for: the workgroup's own (4 SIMDs per CU) times the
@@ -482,7 +484,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
         oacc[db][qb] *= alpha;
         agpr_fence<AG>(oacc[db][qb]);
       }
-      mref[qb] = m_new == -INFINITY ? 0.f : m_new;
+      mref[qb] = m_new == -INFINITY ? 0.f : m_new - C::P_LOG2;
     }
 #pragma unroll
     for (int u = 0; u < NEP; ++u) {
@@ -503,7 +505,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
     float mref[QB], rs[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      mref[qb] = m_run[qb] == -INFINITY ? 0.f : m_run[qb];
+      mref[qb] = m_run[qb] == -INFINITY ? 0.f : m_run[qb] - C::P_LOG2;
       rs[qb] = 0.f;
     }
     // V fragments first: the step's first MFMAs are P V's, so with one wave per SIMD every LDS read in
@@ -544,7 +546,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
       if (e & 1) pack_pair(e >> 1, ev[(e - 1) % 4], ev[e % 4], pk_new, rs);
     bool over = false;
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) over = over || !(rs[qb] <= kOverflowSum);
+    for (int qb = 0; qb < QB; ++qb) over = over || !(rs[qb] <= C::OVERFLOW_SUM);
     // Without pages that are not there a row that sees any key of its range sees the first, so it has a reference from
     // tile 0 on; with them it takes one as soon as a tile has a key for it.
     if constexpr (C::PAGED) {

@@ -476,7 +476,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
               }
             if (st.h == 0)  // a sum that is no number stays one in the join
               p.many_lse[place + col] =
-                  some ? (st.m_run[qb] + log2f(l_tot)) * kLn2 : isnan(l_tot) ? NAN : -INFINITY;
+                  some ? (st.m_run[qb] - C::P_LOG2 + log2f(l_tot)) * kLn2 : isnan(l_tot) ? NAN : -INFINITY;
           }
         }
         if (me == first_wg && tid == 0)
@@ -503,7 +503,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
           if (p.lse != nullptr && st.h == 0 && (int)c < blk.cols) {
             const int qi = (int)fast_div(c, p.m_group, p.sh_group);
             p.lse[(int64_t)(s.q0 + qi) * p.hq + g * p.group + ((int)c - qi * p.group)] =
-                some ? (st.m_run[qb] + log2f(l_tot)) * kLn2 : -INFINITY;
+                some ? (st.m_run[qb] - C::P_LOG2 + log2f(l_tot)) * kLn2 : -INFINITY;
           }
         }
         // Each wave reads back only its own rows, so no barrier. A lane's next column is RPI further on: its address

@@ -214,6 +214,7 @@ struct FewCfg {
   static constexpr int DQK = DQK_, DV = DV_, NW = 4, SLOTS = SLOTS_;
   static constexpr bool FP8 = FP8_;
   static constexpr int E = FP8 ? 1 : 2;                         // bytes per element
+  static constexpr float P_LOG2 = FP8 ? kE4m3PLog2 : 0.f;       // probabilities and their sums are held times 2^P_LOG2
   static constexpr int KS = DQK / 16, DB = DV / 32;
   static constexpr int KROW = DQK * E, VROW = DV * E;           // bytes per LDS row
   static constexpr int KCH = KROW / 16, VCH = VROW / 16;        // 16-byte chunks per row
@@ -501,7 +502,7 @@ void fa_paged_few_kernel(PagedParams p) {
 #pragma unroll
           for (int db = 0; db < DB; ++db) oacc[db][qb] *= alpha;
         }
-        const float mref = m_run[qb] == -INFINITY ? 0.f : m_run[qb];
+        const float mref = m_run[qb] == -INFINITY ? 0.f : m_run[qb] - C::P_LOG2;
         float rs = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -585,7 +586,7 @@ void fa_paged_few_kernel(PagedParams p) {
       const bool some = Lsum > 0.f;  // else no visible key, or a score that is no number: O = 0, LSE = -inf
       const float vs = FP8 && p.c.v_scale != nullptr ? scalar_load(p.c.v_scale + g) : 1.f;
       const float inv = some ? vs / Lsum : 0.f;
-      const float lse = some ? (M + log2f(Lsum)) * kLn2 : -INFINITY;
+      const float lse = some ? (M - C::P_LOG2 + log2f(Lsum)) * kLn2 : -INFINITY;
       f32x4 o[DV / TPC / 4];
 #pragma unroll
       for (int d = 0; d < DV / TPC; d += 4) {
