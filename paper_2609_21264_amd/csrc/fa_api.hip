@@ -234,7 +234,8 @@ constexpr int64_t kMaxPagedKeys = 1 << 30;
 // Checks that both paged entry points begin with, in the order fa.h documents: sizes, then what is supported. Hq may be
 // 0 (no queries). On FA_OK fills the kernels' view of the cache and the batch.
 fa_status_t check_paged_shape(const fa_paged_cache_t* c, const fa_paged_batch_t* bt, int Hq) {
-  if (bt->B < 0 || bt->T < 0 || bt->max_blocks < 0 || c->n_pages < 0 || c->Hkv < 0 || Hq < 0) return FA_ERR_BAD_SHAPE;
+  if (bt->B < 0 || bt->T < 0 || bt->max_blocks < 0 || c->n_pages < 0 || c->page_size < 0 || c->Hkv < 0 || Hq < 0)
+    return FA_ERR_BAD_SHAPE;
   if ((bt->T > 0 || Hq > 0) && (c->Hkv <= 0 || Hq % c->Hkv != 0)) return FA_ERR_BAD_SHAPE;
   if (bt->table_stride < 0 || static_cast<int64_t>(bt->max_blocks) * c->page_size > kMaxPagedKeys) return FA_ERR_BAD_SHAPE;
   const int64_t heads = Hq > c->Hkv ? Hq : c->Hkv;

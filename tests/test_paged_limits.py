@@ -24,3 +24,14 @@ def test_split_blocks_lie_on_a_line_that_32_bits_count(d, type):
             split = workspace(blocks, blocks, keys, 1, 1, d, type) > 0
             assert split or (blocks + blocks // 128) * units >= 2 ** 31, (blocks, keys)  # what the host takes for the most
             assert not split or blocks * units < 2 ** 31, (blocks, keys)
+
+
+def test_a_negative_page_size_is_refused():
+    """Before any product or quotient is formed from it: max_blocks * page_size / 128 + 2 is 0 for -256."""
+    import test_paged_host as host
+
+    for page in (-1, -16, -255, -256, -383, -2 ** 31):
+        for blocks in (0, 1, 4):
+            bt = host.batch(max_blocks=blocks)
+            assert host.attend(host.cache(page_size=page), bt) == fa.FA_ERR_BAD_SHAPE, page
+            assert host.append(host.cache(page_size=page), bt) == fa.FA_ERR_BAD_SHAPE, page
