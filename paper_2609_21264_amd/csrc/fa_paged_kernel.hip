@@ -82,10 +82,13 @@ __device__ __forceinline__ u32x2 pack8_e4m3(const F8& f, float scale) {
 }
 
 constexpr int kAppendThreads = 256;
+// Tokens of a row of the grid: a dimension of it holds fewer than 2^32 threads, so 2^24 tokens and more need a second one.
+constexpr int kAppendRowLog = 22;
 
 template <bool FP8>
 __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams p) {
-  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int t = (int)(blockIdx.y << kAppendRowLog | blockIdx.x), tid = threadIdx.x, lane = tid & 63;  // below 2^31
+  if (t >= p.bt.n_tokens) return;
   const int b = __builtin_amdgcn_readfirstlane(sequence_of(p.bt.q_starts, p.bt.n_seq, t, lane));
   if (b < 0 || b >= p.bt.n_seq) return;
   const PagedSeq s = load_seq(p.bt, b);
@@ -751,9 +754,12 @@ hipError_t launch_few(PagedParams p, hipStream_t stream) {
 
 hipError_t launch_append(AppendParams p, bool fp8, hipStream_t stream) {
   void* args[] = {&p};
+  constexpr unsigned kRow = 1u << kAppendRowLog;
+  const unsigned n = (unsigned)p.bt.n_tokens;
+  const dim3 grid(n < kRow ? n : kRow, (n + kRow - 1) / kRow);
   return hipLaunchKernel(fp8 ? reinterpret_cast<const void*>(&fa_append_kernel<true>)
                              : reinterpret_cast<const void*>(&fa_append_kernel<false>),
-                         dim3(p.bt.n_tokens), dim3(kAppendThreads), args, 0, stream);
+                         grid, dim3(kAppendThreads), args, 0, stream);
 }
 
 // Instances by head dimensions, cache type and 32-column blocks; as many ring slots as leave two workgroups to a CU

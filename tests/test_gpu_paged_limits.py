@@ -1,0 +1,36 @@
+"""GPU tests of the paged calls at sizes where a grid or a count passes a limit."""
+
+import pytest
+import torch
+
+import paper_2609_21264_amd as fa
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("T", [2 ** 22 - 1, 2 ** 22, 2 ** 22 + 1, 2 ** 24 + 5])
+def test_append_of_very_many_tokens(T):
+    """2^24 workgroups of 256 threads are more than one dimension of a grid holds. Two sequences: nearly all tokens, and
+    the last three."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    page, split = 64, T - 3
+    # Rows 8 elements apart, so that every token has its own and the buffers stay small.
+    k, v, q = (torch.randn(8 * (T + 8), device="cuda", generator=g).bfloat16().as_strided((T, 1, 64), (8, 8, 1)) for _ in range(3))
+    blocks = -(-split // page)
+    kc, vc = (torch.zeros(blocks + 1, 1, page, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = torch.zeros(2, blocks, dtype=torch.int32, device="cuda")
+    table[0] = torch.arange(blocks, dtype=torch.int32, device="cuda")
+    table[1, 0] = blocks
+    q_out = torch.zeros(T, 1, 64, dtype=torch.bfloat16, device="cuda")
+    fa.kv_append(k, v, kc, vc, table, ints([split, 3]), ints([0, split, T]), q=q, q_out=q_out)
+    torch.cuda.synchronize()
+    for x, cache in ((k, kc), (v, vc)):
+        rows = cache.view(-1, 64)
+        assert torch.equal(rows[:split], x[:split, 0]), "the first sequence"
+        assert torch.equal(rows[blocks * page:blocks * page + 3], x[split:, 0]), "the second"
+        assert not rows[split:blocks * page].any() and not rows[blocks * page + 3:].any()
+    assert torch.equal(q_out, q)
