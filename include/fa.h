@@ -382,7 +382,8 @@ typedef enum {
  * hold at a replay.
  *
  * Errors, in this order: cache, batch or strides NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE: as for fa_kv_append, max_q < 0,
- * Hkv * (T * Hq / Hkv / 32 + B) * (max_blocks * page_size / 128 + 2) >= 2^31); head dimensions, page size, type, path
+ * Hkv * (T * Hq / Hkv / 32 + B) * (max_blocks * page_size / 128 + 2) >= 2^31, with FA_PAGED_MANY also
+ * Hkv * (rows / 128 + min(B, rows)) >= 2^24 for rows = T * Hq / Hkv); head dimensions, page size, type, path
  * (FA_ERR_UNSUPPORTED); NULL buffers (FA_ERR_NULL_POINTER); scale (FA_ERR_BAD_SCALE); alignment (FA_ERR_UNSUPPORTED); cache
  * strides (FA_ERR_BAD_SHAPE); workspace NULL or too small (FA_ERR_WORKSPACE), not aligned (FA_ERR_UNSUPPORTED). T == 0, B == 0 or
  * Hq == 0 returns FA_OK without a launch.

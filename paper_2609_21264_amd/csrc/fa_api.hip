@@ -329,6 +329,12 @@ bool token_strides(const long long* s, int n) {
 constexpr int kFewCols = 64;
 constexpr uint32_t kManyUnits = 2750, kSureUnits = 2000;
 constexpr int kWholeKeys = 512, kWholeItems = 1 << 16;
+// Whether the kernel for many rows may be launched: it has a workgroup of 256 threads per block, whole ones of 128 row-heads and
+// a last one of every sequence, and one dimension of a grid holds fewer than 2^32 threads.
+bool many_fits(int B, int T, int Hkv, int group) {
+  const int64_t rows = static_cast<int64_t>(T) * group;
+  return (rows / 128 + (B < rows ? B : rows)) * Hkv < 1 << 24;
+}
 struct PagedPlan {
   bool few, many;         // kernels to launch
   fa::PagedMany m;        // what that for many rows runs
@@ -348,7 +354,8 @@ PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, i
   const double most_units = (static_cast<double>(rows) / 64 + B) * Hkv * (6 + max_keys / 128);
   const double least_units = static_cast<double>(rows) / 64 * Hkv * (6 + T / B / 256);
   const double least = static_cast<double>(rows) - (B - 1.0) * static_cast<double>(most);
-  w.many = path == FA_PAGED_MANY || (path == FA_PAGED_AUTO && most > kFewCols && rows > kFewCols && most_units >= kManyUnits);
+  w.many = path == FA_PAGED_MANY || (path == FA_PAGED_AUTO && most > kFewCols && rows > kFewCols && most_units >= kManyUnits &&
+                                      many_fits(B, T, Hkv, group));
   w.few = !w.many || (path == FA_PAGED_AUTO && (least <= kFewCols || least_units < kSureUnits));
   w.few_cols = !w.many ? INT_MAX : w.few ? 32 : 0;
   const int64_t items32 = (rows / 32 + (B < T ? B : T)) * Hkv;
@@ -442,6 +449,7 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
     const int64_t blocks = (static_cast<int64_t>(batch->T) * (Hq / cache->Hkv) / 32 + batch->B) * cache->Hkv;  // < 2^58
     const int64_t tiles = static_cast<int64_t>(batch->max_blocks) * cache->page_size / 128 + 2;
     if (blocks > INT_MAX / tiles) return FA_ERR_BAD_SHAPE;
+    if (path == FA_PAGED_MANY && !many_fits(batch->B, batch->T, cache->Hkv, Hq / cache->Hkv)) return FA_ERR_BAD_SHAPE;
   }
   st = check_paged_support(cache);
   if (st != FA_OK) return st;

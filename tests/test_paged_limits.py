@@ -35,3 +35,20 @@ def test_a_negative_page_size_is_refused():
             bt = host.batch(max_blocks=blocks)
             assert host.attend(host.cache(page_size=page), bt) == fa.FA_ERR_BAD_SHAPE, page
             assert host.append(host.cache(page_size=page), bt) == fa.FA_ERR_BAD_SHAPE, page
+
+
+def test_more_blocks_than_a_grid_holds():
+    """The kernel for many rows launches up to (T * group / 128 + sequences with rows) * Hkv workgroups of 256 threads,
+    fewer than 2^24: the path refuses more, and without a path such a call runs in the kernel for few rows."""
+    import test_paged_host as host
+
+    heads = dict(Hkv=8, k_page=8 * 16 * 128, v_page=8 * 16 * 128)
+    many = host.batch(B=2 ** 21, T=2 ** 21, max_blocks=1, table_stride=1)
+    assert host.attend(host.cache(**heads), many, Hq=8, path=MANY) == fa.FA_ERR_BAD_SHAPE
+    fewer = host.batch(B=2 ** 21 - 2 ** 14, T=2 ** 21 - 2 ** 14, max_blocks=1, table_stride=1)
+    assert host.attend(host.cache(**heads), fewer, Hq=8, path=MANY, Q=None) == fa.FA_ERR_NULL_POINTER  # sizes are right
+    # Sequences of 65 and more row-heads alone, if max_q is right: the kernel for many rows needs no workspace, that for few does.
+    n, keys = 2 ** 21, 1024
+    few, auto = (workspace(n, 9 * n, keys, 64, 8, max_q=9, path=x) for x in (fa.FA_PAGED_FEW, fa.FA_PAGED_AUTO))
+    assert auto == few > 0
+    assert workspace(n // 2, 9 * (n // 2), keys, 64, 8, max_q=9, path=fa.FA_PAGED_AUTO) == 0
