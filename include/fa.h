@@ -372,8 +372,8 @@ typedef enum {
  *   LSE         float32 [T][Hq] (contiguous), or NULL
  *   strides     {q_token, q_head, o_token, o_head}, in elements, multiples of 8. O and LSE overlap neither each other nor
  *               an input (O may be Q itself with the same strides, where d_qk = d_v)
- *   max_q       the most new tokens of one sequence, as far as the host knows: it helps to choose the kernels, the results
- *               are right for any
+ *   max_q       the most new tokens of one sequence, as far as the host knows, 0 if it does not: it helps to choose the
+ *               kernels, the results are right for any
  *   path        fa_paged_path_t
  *   workspace   16-byte aligned, at least fa_fwd_paged_workspace_bytes(...) bytes, overwritten; nothing needs to be in
  *               it before, and it must not be used elsewhere until the call's work has completed. NULL only when no

@@ -557,8 +557,8 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
     batch, whose new tokens are in the cache already): returns O [T, Hq, d_v] (bf16) and, with ``return_lse``, LSE
     [T, Hq] (float32, natural log). Token i of the n new ones of sequence b sees the keys up to its position
     ``kv_lens[b] - n + i`` (all ``kv_lens[b]`` where not ``causal``). ``max_q``, the most new tokens of one sequence, helps to
-    choose the kernels (default: the mean, rounded up), ``path`` ("few", "many") chooses them: for single tokens and short
-    prompts, or for longer ones; the results are right for any. Rows of tokens that belong to no
+    choose the kernels (default: not known), ``path`` ("few", "many") chooses them: for single tokens and short prompts, or for
+    longer ones; the results are right for any. Rows of tokens that belong to no
     sequence are left as they were, so a new tensor's hold anything.
 
     ``scale`` defaults to 1/sqrt(d_qk). ``workspace`` is a CUDA tensor of ``fa_fwd_paged_workspace_bytes`` (default: from
@@ -577,7 +577,7 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
     if scale is None:
         scale = 1.0 / math.sqrt(dqk) if dqk else 1.0
     if max_q is None:
-        max_q = -(-T // B) if B else 0
+        max_q = 0
     max_q = int(max_q)
     way = 0
     if path is not None:

@@ -315,6 +315,10 @@ bool token_strides(const long long* s, int n) {
 //    row-heads if none has more than max_q tokens, and where even without cached keys they have kSureUnits (prompts of 4 096
 //    and 3 001 tokens, 32/8 heads, d = 128: 200 us alone, 206 with the others' launches; 2 000 and 1 500: 61.5 against 65.5). Else both are launched and find from the lengths whether the sequences with more than
 //    32 row-heads have kManyUnits together: if so the kernel for many rows takes these, else that for few takes all.
+//    A call without max_q (0) is planned as if every other sequence had one token: mostly the lengths then decide. (The
+//    mean in its place would be taken for a bound: 4 096 + 255 x 1 tokens, 2 heads a group, d = 128, ran in the kernel for few
+//    rows alone, 440 us against 195. Where all tokens in one sequence would have fewer than kManyUnits, few alone: 16 x 9 over 2 000
+//    keys, 32/8 heads, 37 us, launched with the other kernel 51.)
 //    Few against many, us, one box (units): d = 128 32/8 heads 512 x 512 (1.8 K) 17.0 : 22.2, 128 x 2000 (1.3 K) 31.7 : 45.6,
 //    4 x 200 x 200 (2.5 K) 22.8 : 18.8, 700 x 700 (2.8 K) 40.9 : 24.9, 4 x 128 x 2000 (5.4 K) 48.6 : 50.2, 300 x 4000 (5.5 K)
 //    60.3 : 43.6; d = 64 16/16 4 x 128 x 2000 (2.7 K) 27.0 : 34.4, 300 x 4000 (2.9 K) 35.7 : 28.1, 4 x 512 x 512 (4.1 K)
@@ -340,26 +344,32 @@ struct PagedPlan {
   fa::PagedMany m;        // what that for many rows runs
   bool whole;             // whether that for few rows takes whole items
   int few_cols, col_blocks, n_wg, cols;
+  int64_t usual;          // row-heads that a sequence is taken to have in the kernel for few rows
   uint32_t many_work;
   int64_t lse, desc, many_o, many_lse, many_desc, bytes;  // 16-byte aligned offsets
 };
 PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, int d_v, int type, int max_q,
                      int path) {
   PagedPlan w{};
+  const bool known = max_q > 0;
+  if (!known) max_q = T > B ? T - B + 1 : 1;
   const int64_t rows = static_cast<int64_t>(T) * group, most = static_cast<int64_t>(max_q) * group;
+  w.usual = known ? most : (static_cast<int64_t>(T) + B - 1) / B * group;
   const bool e4m3 = type == FA_CACHE_E4M3;
   w.many_work = kManyUnits;
-  // The most units that the call can have, and the fewest (sequences of equal length, without cached keys); the fewest
-  // row-heads of a sequence where none has more than max_q tokens.
-  const double most_units = (static_cast<double>(rows) / 64 + B) * Hkv * (6 + max_keys / 128);
+  // The most units that the call can have (without max_q: that its longest sequence can have), and the fewest (sequences of
+  // equal length, without cached keys); the fewest row-heads of a sequence where none has more than max_q tokens (without
+  // max_q: of one that has any).
+  const double items64 = known ? static_cast<double>(rows) / 64 + B : static_cast<double>((most + 63) / 64);
+  const double most_units = items64 * Hkv * (6 + max_keys / 128);
   const double least_units = static_cast<double>(rows) / 64 * Hkv * (6 + T / B / 256);
-  const double least = static_cast<double>(rows) - (B - 1.0) * static_cast<double>(most);
+  const double least = known || B == 1 ? static_cast<double>(rows) - (B - 1.0) * static_cast<double>(most) : group;
   w.many = path == FA_PAGED_MANY || (path == FA_PAGED_AUTO && most > kFewCols && rows > kFewCols && most_units >= kManyUnits &&
                                       many_fits(B, T, Hkv, group));
   w.few = !w.many || (path == FA_PAGED_AUTO && (least <= kFewCols || least_units < kSureUnits));
   w.few_cols = !w.many ? INT_MAX : w.few ? 32 : 0;
   const int64_t items32 = (rows / 32 + (B < T ? B : T)) * Hkv;
-  w.col_blocks = most <= 32 || w.many || (items32 <= 256 && (most > kFewCols || max_keys <= kWholeKeys)) ? 1 : 2;
+  w.col_blocks = w.usual <= 32 || w.many || (items32 <= 256 && (w.usual > kFewCols || max_keys <= kWholeKeys)) ? 1 : 2;
   if (w.many) w.m = fa::paged_many(B, T, max_keys, Hkv, group, max_q, w.few_cols, d_qk, e4m3);
   auto place = [&](int64_t n) {
     const int64_t at = w.bytes;
@@ -494,10 +504,10 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   p.many_lse = reinterpret_cast<float*>(ws + w.many_lse);
   p.many_desc = reinterpret_cast<fa::PagedItem*>(ws + w.many_desc);
   // A single item per sequence and head reads K and V once: they are then loaded past the caches.
-  const bool stream_kv = static_cast<int64_t>(max_q) * p.group <= 32 * w.col_blocks;
+  const bool stream_kv = w.usual <= 32 * w.col_blocks;
   // Beside the kernel for many rows the others are mostly single tokens.
-  const int64_t most = static_cast<int64_t>(w.many ? 1 : max_q) * p.group;
-  const int cols = most < 1 ? 1 : most < w.cols ? static_cast<int>(most) : w.cols;
+  const int64_t usual = w.many ? p.group : w.usual;
+  const int cols = usual < w.cols ? static_cast<int>(usual) : w.cols;
   hipError_t e = hipSuccess;
   if (w.many) e = fa::launch_paged_many(p, w.m, cache->d_qk, cache->type == FA_CACHE_E4M3, stream);
   if (e == hipSuccess && w.few) e = fa::launch_paged_few(p, cache->d_qk, cache->type == FA_CACHE_E4M3, w.col_blocks, stream_kv, stream);

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2609_21264_amd as fa
+from paged import Batch
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +35,16 @@ def test_append_of_very_many_tokens(T):
         assert torch.equal(rows[blocks * page:blocks * page + 3], x[split:, 0]), "the second"
         assert not rows[split:blocks * page].any() and not rows[blocks * page + 3:].any()
     assert torch.equal(q_out, q)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("new,keys,Hq,Hkv", [([1024] + [1] * 24, [3000] + [700] * 24, 8, 2), ([1] * 40 + [600], [90] * 41, 4, 2),
+                                             ([1] * 33, [40 * i + 1 for i in range(33)], 8, 2), ([0, 0, 3], [5, 0, 900], 8, 2),
+                                             ([300, 280, 290], [300, 280, 1290], 4, 4)], ids=str)
+def test_without_max_q(new, keys, Hq, Hkv, fp8):
+    """The call as most programs write it first: no hint at all."""
+    keys = [max(n, k) for n, k in zip(new, keys)]
+    bt = Batch(new, keys, Hq, Hkv, 128, 128, 16, fp8, seed=len(new))
+    for causal in (True, False):
+        o, lse = bt.attend(max_q=None, causal=causal, return_lse=True)
+        bt.check(o, lse, 128 ** -0.5, causal, str(new[:3]))

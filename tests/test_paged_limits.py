@@ -52,3 +52,24 @@ def test_more_blocks_than_a_grid_holds():
     few, auto = (workspace(n, 9 * n, keys, 64, 8, max_q=9, path=x) for x in (fa.FA_PAGED_FEW, fa.FA_PAGED_AUTO))
     assert auto == few > 0
     assert workspace(n // 2, 9 * (n // 2), keys, 64, 8, max_q=9, path=fa.FA_PAGED_AUTO) == 0
+
+
+@pytest.mark.parametrize("new,Hq,Hkv", [((1024,) + (1,) * 24, 32, 8), ((4096,) + (1,) * 255, 16, 8), ((700, 0, 0, 2), 8, 8)], ids=("a", "b", "c"))
+@pytest.mark.parametrize("type", [0, 1])
+def test_without_max_q_both_kernels_are_launched_for_a_mix(new, Hq, Hkv, type):
+    """max_q 0 says nothing of the longest sequence: the places of both kernels are in the workspace, as with the true
+    max_q."""
+    T, B, keys = sum(new), len(new), 16384
+    unknown, true, few = (workspace(B, T, keys, Hq, Hkv, type=type, max_q=q, path=path)
+                          for q, path in ((0, fa.FA_PAGED_AUTO), (max(new), fa.FA_PAGED_AUTO), (max(new), fa.FA_PAGED_FEW)))
+    if (B, Hkv) == (25, 8) and type == 0:
+        assert few < true  # a chunk's blocks are split: their places too
+    assert unknown == true > 0
+
+
+@pytest.mark.parametrize("n,B", [(1, 1), (1, 64), (5, 8), (9, 16), (2, 64)])
+def test_without_max_q_few_tokens_are_taken_for_what_they_are(n, B):
+    """Too few tokens for the kernel for many rows however they lie: planned as with the true max_q."""
+    for heads in ((32, 8), (14, 2), (8, 1)):
+        assert workspace(B, n * B, 2000, *heads, max_q=0, path=0) == workspace(B, n * B, 2000, *heads, max_q=n, path=1)
+    assert workspace(1, 4096, 4096, 32, 8, max_q=0, path=0) == workspace(1, 4096, 4096, 32, 8, max_q=4096, path=0)
