@@ -495,8 +495,9 @@ def kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q=None, q_
     ``v_scale[h]``); ``block_table`` [B, blocks] names every sequence's pages in order (int32, like the lengths). Any strides
     of the outer dimensions. ``cos_sin`` float32 [positions, rot_dim] holds the cosines and then the sines of a
     position's angles; dims ``rot_begin`` to ``rot_begin + rot_dim - 1`` of k and q turn, in pairs (c, c + rot_dim / 2) or,
-    ``interleaved``, (2c, 2c + 1). With ``q`` [T, Hq, d_qk] returns the turned queries, in ``q_out`` (which may be ``q``) or a
-    new tensor; rows of tokens that belong to no sequence are left as they were, so a new tensor's hold anything.
+    ``interleaved``, (2c, 2c + 1). With ``q`` [T, Hq, d_qk] returns the turned queries, in ``q_out`` (``q`` itself, or apart
+    from it in memory) or a new tensor; rows of tokens that belong to no sequence are left as they were, so a new tensor's
+    hold anything.
 
     The kernel is enqueued on ``stream`` (default: torch's current stream; a new tensor belongs to that
     stream); the call does not synchronise, and reads no array on the host."""
@@ -537,8 +538,11 @@ def kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q=None, q_
             ot, oh = qt, qh
         else:
             ot, oh = _rows("q_out", q_out, (T, hq, dqk), device, bf16, True)
-            if T > 0 and q_out.untyped_storage().data_ptr() == q.untyped_storage().data_ptr():
-                raise ValueError("q_out must be q itself or lie in a storage of its own")
+            # Bytes from the first element to behind the last, of q and of q_out.
+            q0, o0, n, m = q.data_ptr(), q_out.data_ptr(), T - 1, hq - 1
+            if (T > 0 and hq > 0 and q0 < o0 + 2 * (n * ot + m * oh + dqk) and o0 < q0 + 2 * (n * qt + m * qh + dqk)
+                    and (q0, qt, qh) != (o0, ot, oh)):
+                raise ValueError("q_out must be q itself or lie before or behind it in memory")
         op = q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out goes with q")
