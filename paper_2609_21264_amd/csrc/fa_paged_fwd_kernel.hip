@@ -151,11 +151,10 @@ void fa_paged_fwd_kernel(PagedParams p) {
   };
   if (p.few_cols != 0 && big_work(p, first, lane) < p.many_work) return;  // all sequences run in the kernel for few rows
   if constexpr (C::SPLIT) {
-    uint32_t sum = 0, blocks = 0;
+    uint32_t sum = 0;
     int longest = 0;
     for (int c = 0; c < p.bt.n_seq; c += 64) {
       const PagedSeq sl = seqs_from(c);
-      blocks = add_sat(blocks, wave_sum((uint32_t)n_blocks<BC>(sl, p)));
       uint64_t left = __builtin_amdgcn_ballot_w64(n_blocks<BC>(sl, p) > 0);
       while (left != 0) {
         const PagedSeq x = seq_of_lane(sl, __builtin_ctzll(left));
@@ -168,8 +167,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
     const int total = uniform((int)min(sum, (uint32_t)INT32_MAX));
     longest = uniform(longest);
     per = max(p.many_min_units, (int)((uint32_t)(total - 1) >> p.many_log) + 1);
-    const int64_t items = (int64_t)uniform((int)min(blocks, (uint32_t)INT32_MAX)) * p.c.hkv;
-    split = items > p.many_wg || (longest - per > kSplitUnits && 10ll * longest >= 19ll * per);
+    split = longest - per > kSplitUnits && 10ll * longest >= 19ll * per;  // else there are workgroups for all blocks (paged_many)
     if (split) {
       // Consecutive workgroups run on different XCDs, so the line is dealt to the XCDs in eighths: what shares a
       // key/value head mostly shares an L2.
