@@ -132,7 +132,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
 
   // ---- this workgroup's work ----
   int b = 0, g = 0, cb = 0, n_cb = 0;
-  int me = 0, start = 0, r = 0, r1 = 0, per = 1;  // split: place on the line, the block's first unit, units [r, r1)
+  int me = 0, start = 0, r = 0, r1 = 0, per = 1, total = 0;  // split: place on the line, the block's first unit, units [r, r1)
   bool split = false;
   PagedSeq s{};
   if constexpr (C::SPLIT) {
@@ -164,7 +164,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
         longest = max(longest, kBlockCost + Block<BN, BC>(x, n - 1, p).tiles());
       }
     }
-    const int total = uniform((int)min(sum, (uint32_t)INT32_MAX));
+    total = uniform((int)min(sum, (uint32_t)INT32_MAX));
     longest = uniform(longest);
     per = max(p.many_min_units, (int)((uint32_t)(total - 1) >> p.many_log) + 1);
     split = longest - per > kSplitUnits && 10ll * longest >= 19ll * per;  // else there are workgroups for all blocks (paged_many)
@@ -249,7 +249,8 @@ void fa_paged_fwd_kernel(PagedParams p) {
       skip = tiles == 0 ? start < r : nt == 0;
       if (tiles != 0) {
         first_wg = uniform((int)((uint32_t)(start + kBlockCost) / (uint32_t)per));
-        n_parts = uniform((int)((uint32_t)(start + cost - 1) / (uint32_t)per)) - first_wg + 1;
+        // (The line ends inside a block only if q_starts decreases and so many sequences share tokens that it was cut.)
+        n_parts = uniform((int)((min((uint32_t)start + (uint32_t)cost, (uint32_t)total) - 1u) / (uint32_t)per)) - first_wg + 1;
       }
       r = end;
     }

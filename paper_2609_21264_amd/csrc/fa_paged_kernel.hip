@@ -352,7 +352,8 @@ void fa_paged_few_kernel(PagedParams p) {
       skip = sw.tiles == 0 ? item0 < r0 : t1 <= t0;
       if (sw.tiles != 0) {
         first_wg = uniform((int)((uint32_t)(item0 + kItemCost) / (uint32_t)per));
-        n_parts = uniform((int)((uint32_t)(item0 + cost - 1) / (uint32_t)per)) - first_wg + 1;
+        // (The line ends inside an item only if q_starts decreases and so many sequences share tokens that it was cut.)
+        n_parts = uniform((int)((min((uint32_t)item0 + (uint32_t)cost, (uint32_t)total) - 1u) / (uint32_t)per)) - first_wg + 1;
       }
     }
     r = end;

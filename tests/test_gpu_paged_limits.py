@@ -48,3 +48,25 @@ def test_without_max_q(new, keys, Hq, Hkv, fp8):
     for causal in (True, False):
         o, lse = bt.attend(max_q=None, causal=causal, return_lse=True)
         bt.check(o, lse, 128 ** -0.5, causal, str(new[:3]))
+
+
+@pytest.mark.parametrize("keys", [300, 6000])
+@pytest.mark.parametrize("path", ["few", "many", None])
+def test_starts_that_decrease_stay_inside_the_buffers(path, keys):
+    """Results are undefined where q_starts decreases; what lies around the outputs and the workspace is not touched, and the
+    next call is right."""
+    bt = Batch([40, 1, 60, 3], [keys] * 4, 8, 2, 128, 128, 16, seed=keys)
+    want = bt.attend(return_lse=True, path=path)
+    o, lse = (torch.full((bt.T + 2, 8, *x), 7.0, dtype=t, device="cuda") for x, t in (((128,), torch.bfloat16), ((), torch.float32)))
+    n = fa.fa_fwd_paged_workspace_bytes(4, bt.T, bt.table.shape[1] * 16, 8, 2, 128, 128, 0, 60,
+                                        {"few": 1, "many": 2, None: 0}[path])
+    ws = torch.full((n + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    right = bt.d_q_starts.clone()
+    for starts in ([0, bt.T, 0, bt.T, 0], [bt.T, 0, bt.T, 50, 60], [-5, 2 ** 31 - 1, -2 ** 31, 70, 30]):
+        bt.d_q_starts.copy_(ints(starts))
+        bt.attend(out=o[1:-1], lse=lse[1:-1], workspace=ws[:n], path=path, return_lse=True)
+        torch.cuda.synchronize()
+        assert all((t[i] == 7).all() for t in (o, lse) for i in (0, -1)) and (ws[n:] == 0x5A).all()
+    bt.d_q_starts.copy_(right)
+    again = bt.attend(return_lse=True, path=path)
+    assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
