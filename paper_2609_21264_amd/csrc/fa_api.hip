@@ -319,11 +319,15 @@ bool token_strides(const long long* s, int n) {
 //    mean in its place would be taken for a bound: 4 096 + 255 x 1 tokens, 2 heads a group, d = 128, ran in the kernel for few
 //    rows alone, 440 us against 195. Where all tokens in one sequence would have fewer than kManyUnits, few alone: 16 x 9 over 2 000
 //    keys, 32/8 heads, 37 us, launched with the other kernel 51.)
-//    Few against many, us, one box (units): d = 128 32/8 heads 512 x 512 (1.8 K) 17.0 : 22.2, 128 x 2000 (1.3 K) 31.7 : 45.6,
-//    4 x 200 x 200 (2.5 K) 22.8 : 18.8, 700 x 700 (2.8 K) 40.9 : 24.9, 4 x 128 x 2000 (5.4 K) 48.6 : 50.2, 300 x 4000 (5.5 K)
-//    60.3 : 43.6; d = 64 16/16 4 x 128 x 2000 (2.7 K) 27.0 : 34.4, 300 x 4000 (2.9 K) 35.7 : 28.1, 4 x 512 x 512 (4.1 K)
-//    16.6 : 19.0, 16 x 200 x 200 (6.1 K) 20.8 : 13.2; d_qk = 192 16/16 1024 x 1024 (2.6 K) 32.2 : 43.4, 300 x 4000 (2.9 K)
-//    75.0 : 44.5, 4 x 512 x 512 (4.1 K) 39.3 : 33.9; e4m3 d = 128 32/8 512 x 512 16.8 : 26.7, 700 x 700 41.4 : 30.5.
+//    Few against many, us, one box (units): d = 128 32/8 heads 512 x 512 (1.8 K) 17.1 : 20.1, 128 x 2000 (1.3 K) 30.5 : 44.2,
+//    4 x 200 x 200 (2.5 K) 22.6 : 16.9, 700 x 700 (2.8 K) 39.9 : 23.4, 4 x 128 x 2000 (5.4 K) 50.4 : 48.6, 300 x 4000 (5.5 K)
+//    60.7 : 45.4; d = 64 16/16 4 x 128 x 2000 (2.7 K) 26.5 : 31.9, 300 x 4000 (2.9 K) 35.2 : 29.5, 4 x 512 x 512 (4.1 K)
+//    16.7 : 16.0, 16 x 200 x 200 (6.1 K) 20.7 : 13.3; d_qk = 192 16/16 1024 x 1024 (2.6 K) 32.0 : 43.2, 300 x 4000 (2.9 K)
+//    72.4 : 47.0, 4 x 512 x 512 (4.1 K) 39.7 : 33.8; e4m3 d = 128 32/8 512 x 512 17.2 : 26.9, 700 x 700 40.0 : 30.7.
+//    The thresholds are the same for all head dimensions and types, and so are off for some. Where most (the better kernel :
+//    what runs): d = 64 16/16 16 x 100 x 100 9.4 : 15.0, 700 x 700 15.8 : 20.8, 4 x 128 x 2000 26.5 : 35.0; d_qk = 192 16/16
+//    1024 x 1024 32.0 : 43.3, 4 x 128 x 2000 44.7 : 61.5; e4m3 32/8 d = 128 4 x 128 x 2000 45.4 : 68.6; e4m3 14/2 d = 64
+//    4 x 400 x 400 13.8 : 19.9, 4 x 512 x 512 14.3 : 21.2. A caller who knows better names the path.
 //  * Items of 64 where sequences have more than 32 row-heads, so that K and V are read half as often (8 x 35 row-heads x 3 001
 //    keys 13.4 us against 15.7), except where items of 32 are no more than the CUs and the keys few, or read several
 //    times anyway (40 tokens x 40 keys of one sequence, 32/8 heads: 7.2 us in items of 32, 9.6 of 64; 16 of 128 x 128

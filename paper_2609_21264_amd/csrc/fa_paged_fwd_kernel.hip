@@ -564,7 +564,8 @@ void fa_paged_fwd_kernel(PagedParams p) {
 
 // Instances. Long: those of the fused forward (64 query columns per wave; d = 64: 32-key tiles, two workgroups per CU), but
 // 64-key tiles at d = 64 over e4m3, whose 32-key tiles would be half a load per wave. Short: 32 columns per wave, two
-// workgroups per CU, for sequences of at most 128 row-heads (bf16; at d_qk = 192 two waves per SIMD do not fit).
+// workgroups per CU, where sequences have at most 128 row-heads or long blocks would not fill the chip (paged_many; bf16, d_qk 64
+// and 128: in 64-key tiles two waves per SIMD do not fit at d_qk = 192).
 template <int DQK, int DV, bool E4M3, bool SHORT, bool SPLIT>
 struct PagedInstance {
   using C = Cfg<DQK, DV, 64, 4, 2, true, SPLIT, 1, 2, 6, 2, 4, 1, true, E4M3>;
@@ -610,8 +611,11 @@ PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, 
   m.n_wg = m.is_short || (d_qk == 64 && !e4m3) ? 512 : 256;
   // The most blocks that the packed tokens can make: whole ones, and a last one for each sequence of this kernel.
   m.blocks = rows / m.cols + seqs;
-  // Never with long blocks where there are short ones: fill is n_wg at least. The line of work is counted in 32 bits: where
-  // the table has pages for more units than that (128 blocks over 2^30 keys each) no block is split.
+  // Never with long blocks where there are short ones: fill is n_wg at least. Every sequence that may have rows here counts as a
+  // block, single tokens too, so a chunk is no longer split beside many of them: 32/8 heads, d = 128, 1 024 tokens over
+  // 9 000 keys beside 24 over 2 000 194 us, beside 31 217; e4m3 beside 4 166, beside 15 236; 32/32 heads, d_qk = 192, 512 over
+  // 4 500 beside 4 over 1 000 96, beside 5 146. The line of work is counted in 32 bits: where the table has pages for more
+  // units than that (128 blocks over 2^30 keys each) no block is split.
   const int64_t units = kBlockCost + (static_cast<int64_t>(max_keys) + kSplitTile - 1) / kSplitTile;  // of a block, at most
   m.split = m.blocks * hkv < m.n_wg && m.blocks * hkv * units <= INT32_MAX;
   return m;
