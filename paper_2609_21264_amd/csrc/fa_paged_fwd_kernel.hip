@@ -15,7 +15,7 @@
 //    workgroups share evenly, and parts of a block that several share are joined as those of the kernel for few
 //    rows are; else a workgroup takes one block here too.
 // What bounds it: MFMA and the softmax between them, as in the fused forward. 32/8 heads, d = 128, prompts of 4 096 and 3 001
-// tokens 200-204 us (1 035-1 055 TFLOP/s), a chunk of 1 024 over 9 000 keys, split, 140 (1 000) and its
+// tokens 200-215 us by box (985-1 055 TFLOP/s; over an e4m3 cache 218, 969), a chunk of 1 024 over 9 000 keys, split, 140 (1 000) and its
 // part of the join; 32/32 heads, d_qk = 192, 512 tokens over 4 500 keys, split, 64 (700) and 13 for the join. Over contiguous keys the fused forward takes 1/1.03 to 1/1.06 of its time from 8 192 tokens
 // on, 1/1.10 at 2 048 (d = 128), 1/1.26 at 4 096 of 16/16 heads with d = 64.
 #include <float.h>

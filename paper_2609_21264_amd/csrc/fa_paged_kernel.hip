@@ -205,7 +205,7 @@ __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams 
 // against 1.6-1.7e-3 with P in fp32; over e4m3 caches, in fp16, it does not show.
 //
 // What bounds it: reading K and V once. 32/8 heads, d = 128: one token over 131 072 keys 83-85 us (6.3-6.5 TB/s) and 5 for
-// the join; 64 tokens over 20 000 to 130 keys each 124-128 (6.0-6.2) and 5; 16 over 16 384 and 10 001 in e4m3 71-74 (5.8-6.1) and
+// the join; 64 tokens over 20 000 to 130 keys each 124-128 (6.0-6.2) and 5; 16 over 16 384 and 10 001 in e4m3 71-75 (5.8-6.1) and
 // 5. Short ones are bound by the chain of line, table, Q, K, V and join: one token over 1 023 keys 8 us and 3.
 
 constexpr int kItemCost = 1;  // fixed cost of an item in tiles
