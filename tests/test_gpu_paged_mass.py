@@ -15,10 +15,11 @@ pytestmark = pytest.mark.gpu
 DIMS = [(64, 64), (128, 128), (192, 128)]
 
 
-def run(bt, causal=True, **kw):
-    o, lse = bt.attend(causal=causal, return_lse=True, **kw)
+def run(bt, causal=True, scale=None, **kw):
+    scale = bt.dqk ** -0.5 if scale is None else scale
+    o, lse = bt.attend(causal=causal, scale=scale, return_lse=True, **kw)
     torch.cuda.synchronize()
-    check_mass(bt, o, bt.dqk ** -0.5, causal)
+    check_mass(bt, o, scale, causal)
     return o, lse
 
 
@@ -69,6 +70,31 @@ def test_pages_that_are_not_there(path):
     bt.table[0, 100:140], bt.table[0, 562], bt.table[1, 0], bt.table[1, 60] = -1, bt.n_pages, -5, 2 ** 31 - 1
     bt.d_table = bt.table.cuda()
     run(bt, path=path)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("path", ["few", "many"])
+@pytest.mark.parametrize("scale", [0.0, -0.1, 1e-30, 0.5])
+def test_scales(scale, path, fp8):
+    run(mass_batch("residues", [1, 50, 3], [5000, 700, 90], 8, 2, 128, 128, 16, fp8, seed=12), scale=scale, path=path)
+
+
+@pytest.mark.parametrize("path", ["few", "many"])
+def test_requests_that_share_their_pages(path):
+    """One table row for all requests (a row stride of 0), each with its own length: the sequences of a shared prompt."""
+    one = mass_batch("blocks", [0], [3000], 8, 2, 128, 128, 16, seed=15)
+    lens = [3000, 1, 17, 2999, 640]
+    bt = mass_batch("blocks", [1, 1, 9, 30, 1], lens, 8, 2, 128, 128, 16, seed=16)  # for its queries and starts
+    table = one.d_table.expand(len(lens), -1)
+    o = fa.forward_paged(bt.d_q, one.d_k_cache, one.d_v_cache, table, bt.d_kv_lens, bt.d_q_starts, path=path)
+    own = fa.forward_paged(bt.d_q, one.d_k_cache, one.d_v_cache, table.contiguous(), bt.d_kv_lens, bt.d_q_starts, path=path)
+    assert table.stride(0) == 0 and torch.equal(o, own)
+    for b, n in enumerate(lens):  # each against the check, as a batch of its own (classes by its own length: as all 3 000 keys have)
+        q0, q1 = int(bt.q_starts[b]), int(bt.q_starts[b + 1])
+        alone = fa.forward_paged(bt.d_q[q0:q1], one.d_k_cache, one.d_v_cache, one.d_table, bt.d_kv_lens[b:b + 1],
+                                 torch.tensor([0, q1 - q0], dtype=torch.int32, device="cuda"), path=path)
+        # Cut elsewhere and joined: P and O rounded twice, in each run.
+        assert (o[q0:q1].double() - alone.double()).abs().le(2 * (2.0 ** -8 + 2.0 ** -8 + 1e-3) * alone.double() + 1e-6).all(), n
 
 
 @pytest.mark.parametrize("dqk,dv,page,fp8", [(128, 128, 16, False), (64, 64, 32, True), (192, 128, 64, False)])
