@@ -352,6 +352,93 @@ fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
                          const void* Q, void* Q_out, int Hq, const long long* strides, const float* cos_sin, int n_pos,
                          int rot_begin, int rot_dim, int interleaved, hipStream_t stream);
 
+/*
+ * Positions by device arrays: token t stands at positions[t * token + a * axis] on axis a of n_axes (int32), for images and
+ * video (time, height, width) and for drafted tokens, whose place in the cache is not their position. pair_axes
+ * (uint8, 4-byte aligned, one for each of the rot_dim / 2 pairs) names the axis whose position turns a pair; NULL: the first.
+ * Strides in elements, 0 to 2^40; `batch` is that of the batch in fa_rotate, and unused elsewhere. The device clamps: an axis
+ * behind the last counts as the last, a position outside the table of angles as its first or last row.
+ */
+typedef struct {
+  const int* positions;
+  const unsigned char* pair_axes;
+  long long batch, token, axis;
+  int n_axes;
+} fa_positions_t;
+
+/*
+ * fa_kv_append_at -- fa_kv_append with the angles by `positions` (token t: the packed one) instead of the tokens' places
+ * among their sequences' keys. What it writes where is the same. n_pos >= 1 rows of angles with rot_dim > 0.
+ * Errors: positions NULL (FA_ERR_NULL_POINTER), then as fa_kv_append, with n_axes < 1 and strides out of range among the
+ * sizes, NULL arrays and alignment (4 bytes) of the positions among the others.
+ */
+fa_status_t fa_kv_append_at(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* K, const void* V,
+                            const void* Q, void* Q_out, int Hq, const long long* strides, const fa_positions_t* positions,
+                            const float* cos_sin, int n_pos, int rot_begin, int rot_dim, int interleaved, hipStream_t stream);
+
+/*
+ * fa_rotate -- the position rotation of fa_kv_append for queries or keys that are in no cache (bf16): Y[b,h,s] is X[b,h,s] with
+ * the pairs of its dims rot_begin .. rot_begin + rot_dim - 1 turned, its other dims copied. inverse != 0 turns by the negative
+ * angles, which takes a rotation back and is its gradient.
+ *   X, Y        element (b, h, s, 0) at b * strides[0] + h * strides[1] + s * strides[2], of Y likewise by strides[3 .. 5]; in
+ *               elements, multiples of 8. Y is X itself with the same strides, or does not overlap it
+ *   d           a multiple of 8, up to 1024
+ *   positions   of token (b, s); NULL, or positions->positions NULL: token s stands at s (n_pos >= S)
+ *   cos_sin, n_pos, rot_begin, rot_dim, interleaved   as in fa_kv_append
+ * Enqueues one kernel. Errors, in this order: strides NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE: negative,
+ * B * H * S >= 2^31, rotated dims outside [0, d), n_pos, positions as above); d or rotation not supported
+ * (FA_ERR_UNSUPPORTED); NULL buffers (FA_ERR_NULL_POINTER); alignment (FA_ERR_UNSUPPORTED: 16 bytes for buffers, strides and cos_sin, 4
+ * for the positions). No element returns FA_OK without a launch.
+ */
+fa_status_t fa_rotate(const void* X, void* Y, int B, int H, int S, int d, const long long* strides,
+                      const fa_positions_t* positions, const float* cos_sin, int n_pos, int rot_begin, int rot_dim,
+                      int interleaved, int inverse, hipStream_t stream);
+
+/* Most 32-bit words of a row of a tree's mask (2048 drafted tokens). */
+#define FA_TREE_WORDS 64
+
+/*
+ * fa_tree_mask -- mask and positions of trees of drafted tokens, as fa_fwd_paged_ex and fa_kv_append_at take them. The new tokens
+ * of sequence b (by q_starts and kv_lens as above, kv_lens counting them, clamped to max_keys) are a tree: token i's
+ * parent is token parents[t] of the same sequence, one before it; anything else (-1) makes it a root, whose
+ * parent is the last cached key. Bit j % 32 of word j / 32 of mask[t] is set where token j is token t itself or an ancestor (those
+ * from 32 * words on have no bit); positions[t] = kv_lens[b] - n + its number of ancestors, for the n new ones.
+ *   parents, mask, positions   int32 [T], 32-bit words [T] in rows mask_stride apart, int32 [T]
+ * Rows of tokens that belong to no sequence are left as they were. Enqueues one kernel. Errors: sizes (FA_ERR_BAD_SHAPE: negative,
+ * max_keys > 2^30, words outside [1, FA_TREE_WORDS], mask_stride < words), NULL arrays (FA_ERR_NULL_POINTER), alignment of 4 bytes
+ * (FA_ERR_UNSUPPORTED). T == 0 or B == 0 returns FA_OK without a launch.
+ */
+fa_status_t fa_tree_mask(const int* parents, const int* q_starts, const int* kv_lens, int B, int T, int max_keys, void* mask,
+                         int words, long long mask_stride, int* positions, hipStream_t stream);
+
+/*
+ * fa_kv_compact -- close up the new tokens that a sequence keeps (of drafted ones those that were accepted): of the n new tokens
+ * of sequence b, which are in the cache, number kept[b][i] moves to the i-th place behind its cached keys, key kv_lens[b] - n + i, for
+ * i < n_kept[b]; kv_lens_out[b] = kv_lens[b] - n + n_kept[b]. Keys keep the rotation that they were written with.
+ *   cache, batch    as above (T is not used: there are no packed tokens here)
+ *   kept            int32 [B][max_kept], rows kept_stride apart: numbers of new tokens, which increase (else the moved keys hold
+ *                   what any of the sequence's new tokens held); one outside [0, n) moves nothing
+ *   n_kept          int32 [B], clamped to [0, min(max_kept, n)]
+ *   kv_lens_out     int32 [B], apart from all inputs
+ * Nothing moves to or from a page that is not there. A cache whose layers lie in one buffer, [n_pages][layers][Hkv] .., closes up in
+ * one call with layers * Hkv heads. Enqueues one kernel. Errors: as fa_kv_append's of cache and batch, in that order (sizes
+ * also: max_kept or kept_stride < 0, Hkv >= 2^25). B == 0 returns FA_OK without a launch.
+ */
+fa_status_t fa_kv_compact(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const int* kept, long long kept_stride,
+                          int max_kept, const int* n_kept, int* kv_lens_out, hipStream_t stream);
+
+/*
+ * fa_kv_copy -- copy pages: keys and values of all heads and slots of page src[i] to page dst[i], i < n (int32 device arrays), for
+ * sequences that fork and write on in pages of their own. A pair with a page number outside [0, n_pages) or of one page
+ * does nothing. A page that is copied to twice, or copied to and from, holds afterwards, 16 bytes by 16 bytes, what any order of
+ * the copies could leave. The scales of an e4m3 cache are per head and stay. Layers in one buffer count as heads, as above.
+ * Enqueues one kernel. Errors: cache NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE); head dimensions, page size or type
+ * not supported (FA_ERR_UNSUPPORTED); NULL buffers (FA_ERR_NULL_POINTER); alignment (FA_ERR_UNSUPPORTED); cache strides, or
+ * n * ceil(Hkv * page_size * max(d_qk, d_v) * element bytes / 32768) >= 2^24 (FA_ERR_BAD_SHAPE). n == 0 returns FA_OK
+ * without a launch.
+ */
+fa_status_t fa_kv_copy(const fa_paged_cache_t* cache, const int* src, const int* dst, int n, hipStream_t stream);
+
 /* The kernels of fa_fwd_paged: one reads K and V once per 32 or 64 row-heads of a key/value head (query rows times the
  * heads that share it) and splits every sequence over the chip, for single tokens, draft tokens and short prompts; one computes
  * in blocks of 128 or 256 row-heads, for longer prompts and chunks. Each is right for any lengths. */

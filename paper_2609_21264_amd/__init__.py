@@ -18,7 +18,10 @@ kernel. The functions below marshal arguments and translate status codes, nothin
 * :func:`forward_unfused` -- the same over the unfused path (``fa_fwd_unfused``).
 * :func:`kv_append`, :func:`forward_paged` -- a paged key/value cache: appending new tokens to it with their
   position rotation, and their attention over it (C: ``fa_kv_append``, ``fa_fwd_paged``, whose descriptions are the
-  ctypes structures :class:`PagedCache` and :class:`PagedBatch`).
+  ctypes structures :class:`PagedCache` and :class:`PagedBatch`; with positions ``fa_kv_append_at``, :class:`Positions`).
+* :func:`rotate` -- the position rotation alone, and the way back (``fa_rotate``).
+* :func:`tree_mask`, :func:`kv_compact`, :func:`kv_copy` -- around the paged cache: mask and positions of drafted
+  trees, closing up the tokens that are kept, copies of pages (``fa_tree_mask``, ``fa_kv_compact``, ``fa_kv_copy``).
 """
 
 from __future__ import annotations
@@ -28,8 +31,8 @@ import math
 from typing import Optional
 
 from . import _lib
-from ._lib import (AppendStrides, PagedBatch, PagedCache, PagedStrides, FA_CACHE_BF16, FA_CACHE_E4M3,  # noqa: F401
-                   FA_PAGED_AUTO, FA_PAGED_FEW, FA_PAGED_MANY,
+from ._lib import (AppendStrides, PagedBatch, PagedCache, PagedStrides, Positions, RotateStrides,  # noqa: F401
+                   FA_CACHE_BF16, FA_CACHE_E4M3, FA_PAGED_AUTO, FA_PAGED_FEW, FA_PAGED_MANY, FA_TREE_WORDS,
                    FA_ERR_BAD_SCALE, FA_ERR_BAD_SHAPE, FA_ERR_HIP, FA_ERR_NULL_POINTER,
                    FA_ERR_UNSUPPORTED, FA_ERR_WORKSPACE, FA_INSTANCE_HALVES, FA_INSTANCE_LONG, FA_INSTANCE_NONE,
                    FA_INSTANCE_QUARTERS, FA_INSTANCE_SHORT, FA_INSTANCE_SHORT_WIDE, FA_NOALLOC_SCRATCH_BYTES, FA_OK,
@@ -41,7 +44,8 @@ __all__ = ["fa_fwd", "fa_fwd_ex", "fa_fwd_split", "fa_fwd_split_workspace_bytes"
            "fa_fwd_decode_noalloc", "fa_fwd_instance", "forward", "forward_unfused", "FaError", "LIB_PATH", "FA_NOALLOC_SCRATCH_BYTES",
            "fa_kv_append", "fa_fwd_paged", "fa_fwd_paged_workspace_bytes", "PagedCache", "PagedBatch", "AppendStrides",
            "PagedStrides", "FA_CACHE_BF16", "FA_CACHE_E4M3", "FA_PAGED_AUTO", "FA_PAGED_FEW",
-           "FA_PAGED_MANY", "kv_append", "forward_paged"]
+           "FA_PAGED_MANY", "kv_append", "forward_paged", "fa_kv_append_at", "fa_rotate", "fa_tree_mask", "fa_kv_compact",
+           "fa_kv_copy", "Positions", "RotateStrides", "FA_TREE_WORDS", "rotate", "tree_mask", "kv_compact", "kv_copy"]
 
 
 class FaError(RuntimeError):
@@ -166,6 +170,39 @@ def fa_kv_append(cache: PagedCache, batch: PagedBatch, K: int, V: int, Q: Option
     """C ``fa_kv_append``: descriptions, raw device addresses and sizes; returns the status code."""
     return int(_lib.load().fa_kv_append(cache, batch, K, V, Q, Q_out, Hq, strides, cos_sin, n_pos, rot_begin,
                                         rot_dim, int(bool(interleaved)), stream))
+
+
+def fa_kv_append_at(cache: PagedCache, batch: PagedBatch, K: int, V: int, Q: Optional[int], Q_out: Optional[int], Hq: int,
+                    strides: AppendStrides, positions: Positions, cos_sin: Optional[int], n_pos: int, rot_begin: int,
+                    rot_dim: int, interleaved: bool, stream: int) -> int:
+    """C ``fa_kv_append_at``: descriptions, raw device addresses and sizes; returns the status code."""
+    return int(_lib.load().fa_kv_append_at(cache, batch, K, V, Q, Q_out, Hq, strides, positions, cos_sin, n_pos, rot_begin,
+                                           rot_dim, int(bool(interleaved)), stream))
+
+
+def fa_rotate(X: int, Y: int, B: int, H: int, S: int, d: int, strides: RotateStrides, positions: Optional[Positions],
+              cos_sin: Optional[int], n_pos: int, rot_begin: int, rot_dim: int, interleaved: bool, inverse: bool,
+              stream: int) -> int:
+    """C ``fa_rotate``: raw device addresses and sizes; returns the status code."""
+    return int(_lib.load().fa_rotate(X, Y, B, H, S, d, strides, positions, cos_sin, n_pos, rot_begin, rot_dim,
+                                     int(bool(interleaved)), int(bool(inverse)), stream))
+
+
+def fa_tree_mask(parents: int, q_starts: int, kv_lens: int, B: int, T: int, max_keys: int, mask: int, words: int,
+                 mask_stride: int, positions: int, stream: int) -> int:
+    """C ``fa_tree_mask``: raw device addresses and sizes; returns the status code."""
+    return int(_lib.load().fa_tree_mask(parents, q_starts, kv_lens, B, T, max_keys, mask, words, mask_stride, positions, stream))
+
+
+def fa_kv_compact(cache: PagedCache, batch: PagedBatch, kept: Optional[int], kept_stride: int, max_kept: int, n_kept: int,
+                  kv_lens_out: int, stream: int) -> int:
+    """C ``fa_kv_compact``: descriptions, raw device addresses and sizes; returns the status code."""
+    return int(_lib.load().fa_kv_compact(cache, batch, kept, kept_stride, max_kept, n_kept, kv_lens_out, stream))
+
+
+def fa_kv_copy(cache: PagedCache, src: int, dst: int, n: int, stream: int) -> int:
+    """C ``fa_kv_copy``: description, raw device addresses and the number of pairs; returns the status code."""
+    return int(_lib.load().fa_kv_copy(cache, src, dst, n, stream))
 
 
 def fa_fwd_paged(cache: PagedCache, batch: PagedBatch, Q: int, O: int, LSE: Optional[int], Hq: int,
@@ -486,7 +523,8 @@ def _raise(name, st):
 
 
 def kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q=None, q_out=None, cos_sin=None,
-              rot_begin: int = 0, interleaved: bool = False, k_scale=None, v_scale=None, stream=None):
+              rot_begin: int = 0, interleaved: bool = False, k_scale=None, v_scale=None, stream=None, positions=None,
+              pair_axes=None):
     """Write the keys and values of new tokens to a paged cache, turning keys and queries by their positions.
 
     k [T, Hkv, d_qk] and v [T, Hkv, d_v] (bf16) hold the packed new tokens; those of sequence b are
@@ -498,6 +536,10 @@ def kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q=None, q_
     ``interleaved``, (2c, 2c + 1). With ``q`` [T, Hq, d_qk] returns the turned queries, in ``q_out`` (``q`` itself, or apart
     from it in memory) or a new tensor; rows of tokens that belong to no sequence are left as they were, so a new tensor's
     hold anything.
+
+    ``positions`` (int32 [T], or [T, axes] with ``pair_axes`` uint8 [rot_dim / 2], the axis of each pair; any strides)
+    are where the tokens stand if not at their places among their sequence's keys: drafted tokens (:func:`tree_mask`), images
+    and video (time, height, width). A position outside the table counts as its first or last row.
 
     The kernel is enqueued on ``stream`` (default: torch's current stream; a new tensor belongs to that
     stream); the call does not synchronise, and reads no array on the host."""
@@ -521,11 +563,16 @@ def kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q=None, q_
             raise ValueError(f"cos_sin must be on the cache's device cuda:{device}, not {cos_sin.device}")
         n_pos, rot = cos_sin.shape
         table = cos_sin.data_ptr()
+    at = None
+    if positions is not None or pair_axes is not None:
+        if cos_sin is None:
+            raise ValueError("positions and pair_axes go with cos_sin")
+        at = _positions(positions, pair_axes, (T,), rot, device)
     elsewhere = _elsewhere(stream, device)
     if elsewhere is not None:
         with elsewhere:
             return kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q, q_out, cos_sin, rot_begin, interleaved,
-                             k_scale, v_scale)
+                             k_scale, v_scale, None, positions, pair_axes)
     hq = qt = qh = ot = oh = 0
     if q is not None:
         hq = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else -1
@@ -546,12 +593,258 @@ def kv_append(k, v, k_cache, v_cache, block_table, kv_lens, q_starts, q=None, q_
         op = q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out goes with q")
-    st = _lib.load().fa_kv_append(cache, batch, k.data_ptr(), v.data_ptr(), qp, op, hq,
-                                  AppendStrides(qt, qh, ot, oh, kt, kh, vt, vh), table, n_pos, int(rot_begin), rot,
-                                  1 if interleaved else 0, torch._C._cuda_getCurrentRawStream(device))
+    strides, stream = AppendStrides(qt, qh, ot, oh, kt, kh, vt, vh), torch._C._cuda_getCurrentRawStream(device)
+    inter = 1 if interleaved else 0
+    if at is None:
+        st = _lib.load().fa_kv_append(cache, batch, k.data_ptr(), v.data_ptr(), qp, op, hq, strides, table, n_pos,
+                                      int(rot_begin), rot, inter, stream)
+    else:
+        st = _lib.load().fa_kv_append_at(cache, batch, k.data_ptr(), v.data_ptr(), qp, op, hq, strides, at, table, n_pos,
+                                         int(rot_begin), rot, inter, stream)
     if st != FA_OK:
-        _raise("fa_kv_append", st)
+        _raise("fa_kv_append" if at is None else "fa_kv_append_at", st)
     return q_out
+
+
+def _positions(positions, pair_axes, tokens, rot, device):
+    """The C description of positions [*tokens] or [*tokens, axes] and of the axes of the pairs."""
+    import torch
+
+    n = len(tokens)
+    if (not isinstance(positions, torch.Tensor) or positions.dtype != torch.int32 or positions.dim() not in (n, n + 1)
+            or positions.shape[:n] != tokens):
+        raise ValueError(f"positions must be an int32 tensor of shape {list(tokens)} or {list(tokens)} + [axes]")
+    if positions.get_device() != device:
+        raise ValueError(f"positions must be on the device cuda:{device}, not {positions.device}")
+    strides = positions.stride()
+    axes, axis = (positions.shape[n], strides[n]) if positions.dim() > n else (1, 0)
+    where = None
+    if pair_axes is not None:
+        if (not isinstance(pair_axes, torch.Tensor) or pair_axes.dtype != torch.uint8 or pair_axes.shape != (rot // 2,)
+                or not pair_axes.is_contiguous()):
+            raise ValueError(f"pair_axes must be a contiguous uint8 tensor [{rot // 2}], an axis for each pair of turned dims")
+        if pair_axes.get_device() != device:
+            raise ValueError(f"pair_axes must be on the device cuda:{device}, not {pair_axes.device}")
+        where = pair_axes.data_ptr()
+    elif axes > 1:
+        raise ValueError("positions of several axes need pair_axes")
+    return Positions(positions.data_ptr(), where, strides[0] if n > 1 else 0, strides[n - 1], axis, axes)
+
+
+def _apart(shape, strides):
+    """Whether no two elements of a tensor share a place in memory."""
+    reach = 1
+    for st, n in sorted((st, n) for st, n in zip(strides, shape) if n > 1):
+        if st < reach:
+            return False
+        reach += (n - 1) * st
+    return True
+
+
+def rotate(x, cos_sin, positions=None, pair_axes=None, rot_begin: int = 0, interleaved: bool = False, inverse: bool = False,
+           out=None, stream=None):
+    """The position rotation of :func:`kv_append` for queries or keys x [B, H, S, d] or [T, H, d] (bf16, any strides of
+    whole rows) that are in no cache, as :func:`forward` takes them: dims ``rot_begin`` to ``rot_begin + rot_dim - 1`` turn by the
+    angles of ``cos_sin`` float32 [positions, rot_dim], the others are copied. ``inverse`` turns back; the
+    gradient with respect to x is that of the output's gradient.
+
+    ``positions`` int32 [B, S] or [B, S, axes] ([T] or [T, axes]; any strides, so one row may be expanded over the batch) with
+    ``pair_axes`` as in :func:`kv_append`; default: token s stands at s. Returns ``out`` (x itself, or apart from it in
+    memory) or a new contiguous tensor. The kernel is enqueued on ``stream`` (default: torch's current stream; a new tensor
+    belongs to that stream); the call does not synchronise, and reads no array on the host."""
+    import torch
+
+    if not isinstance(x, torch.Tensor) or x.dim() not in (3, 4) or x.dtype != torch.bfloat16:
+        raise ValueError("x must be a bfloat16 torch tensor [B, H, S, d] or [T, H, d]")
+    if not x.is_cuda:
+        raise ValueError("x must be on a GPU")
+    device = x.get_device()
+
+    def strides(name, t):
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            raise ValueError(f"the elements of a head of {name} must lie one after the other")
+        st = [s if n > 1 else 0 for s, n in zip(t.stride(), t.shape)]
+        return st[:3] if t.dim() == 4 else [0, st[1], st[0]]
+
+    if x.dim() == 4:
+        B, H, S, d = x.shape
+        tokens = (B, S)
+    else:
+        B, (S, H, d) = 1, x.shape
+        tokens = (S,)
+    if (not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2 or cos_sin.dtype != torch.float32
+            or not cos_sin.is_contiguous()):
+        raise ValueError("cos_sin must be a contiguous float32 tensor [positions, rotated dims]")
+    if cos_sin.get_device() != device:
+        raise ValueError(f"cos_sin must be on x's device {x.device}, not {cos_sin.device}")
+    at = None
+    if positions is not None:
+        at = _positions(positions, pair_axes, tokens, cos_sin.shape[1], device)
+    elif pair_axes is not None:
+        raise ValueError("pair_axes goes with positions")
+    elsewhere = _elsewhere(stream, device)
+    if elsewhere is not None:
+        with elsewhere:
+            return rotate(x, cos_sin, positions, pair_axes, rot_begin, interleaved, inverse, out)
+    if out is None:
+        out = x.new_empty(x.shape)
+    elif out is not x:
+        if not isinstance(out, torch.Tensor) or out.shape != x.shape or out.dtype != x.dtype or out.get_device() != device:
+            raise ValueError(f"out must be a bfloat16 tensor {list(x.shape)} on {x.device}")
+        n = x.numel() and 1 + sum((m - 1) * s for m, s in zip(x.shape, x.stride()))
+        m = out.numel() and 1 + sum((m - 1) * s for m, s in zip(out.shape, out.stride()))
+        x0, o0 = x.data_ptr(), out.data_ptr()
+        if x0 < o0 + 2 * m and o0 < x0 + 2 * n and (x0, strides("x", x)) != (o0, strides("out", out)):
+            raise ValueError("out must be x itself or lie before or behind it in memory")
+    if not _apart(out.shape, out.stride()):
+        raise ValueError("rows of out overlap")
+    st = _lib.load().fa_rotate(x.data_ptr(), out.data_ptr(), B, H, S, d, RotateStrides(*strides("x", x), *strides("out", out)),
+                               at, cos_sin.data_ptr(), cos_sin.shape[0], int(rot_begin), cos_sin.shape[1],
+                               1 if interleaved else 0, 1 if inverse else 0, torch._C._cuda_getCurrentRawStream(device))
+    if st != FA_OK:
+        _raise("fa_rotate", st)
+    return out
+
+
+def _int32(name, t, dim, device):
+    """Checks a contiguous (in its last dimension) int32 tensor of `dim` dimensions on the device (None: on some GPU)."""
+    import torch
+
+    if not isinstance(t, torch.Tensor) or t.dim() != dim or t.dtype != torch.int32:
+        raise ValueError(f"{name} must be a {dim}-d int32 torch tensor")
+    if not t.is_cuda or (device is not None and t.get_device() != device):
+        raise ValueError(f"{name} must be on {'a GPU' if device is None else f'the device cuda:{device}'}, not {t.device}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the entries of {name} must lie one after the other")
+
+
+def tree_mask(parents, q_starts, kv_lens, words: int = 1, max_keys: Optional[int] = None, mask=None, positions=None, stream=None):
+    """Mask and positions of trees of drafted tokens. ``parents`` int32 [T] (packed as in :func:`kv_append`, with its
+    ``q_starts`` [B + 1] and ``kv_lens`` [B], which count the drafted tokens) holds the number of each token's parent among its
+    sequence's new tokens, a smaller one than its own, or -1: it follows the cached keys. Returns (mask, positions): int32
+    [T, ``words``], whose bit j % 32 of word j / 32 says whether the sequence's new token j is the token or one of its ancestors,
+    for :func:`forward_paged`, and int32 [T], cached keys + ancestors, for :func:`kv_append`. ``words`` (up to 64) has to cover the
+    largest tree. Rows of tokens that belong to no sequence are left as they were, so new tensors' hold anything.
+
+    ``max_keys`` clamps ``kv_lens`` (default 2^30). The kernel is enqueued on ``stream`` (default: torch's current stream; new
+    tensors belong to that stream); the call does not synchronise, and reads no array on the host."""
+    import torch
+
+    _int32("parents", parents, 1, None)
+    device = parents.get_device()
+    _int32("q_starts", q_starts, 1, device)
+    _int32("kv_lens", kv_lens, 1, device)
+    T, B, words = parents.shape[0], kv_lens.shape[0], int(words)
+    if q_starts.shape[0] != B + 1:
+        raise ValueError(f"q_starts [B + 1] and kv_lens [B] do not agree: {list(q_starts.shape)}, {list(kv_lens.shape)}")
+    if not 1 <= words <= FA_TREE_WORDS:
+        raise ValueError(f"words must be 1 to {FA_TREE_WORDS}, not {words}")
+    elsewhere = _elsewhere(stream, device)
+    if elsewhere is not None:
+        with elsewhere:
+            return tree_mask(parents, q_starts, kv_lens, words, max_keys, mask, positions)
+    if mask is None:
+        mask = parents.new_empty((T, words))
+    else:
+        _int32("mask", mask, 2, device)
+        if mask.shape != (T, words) or (T > 1 and mask.stride(0) < words):
+            raise ValueError(f"mask must have shape {[T, words]}, its rows apart")
+    if positions is None:
+        positions = parents.new_empty(T)
+    else:
+        _int32("positions", positions, 1, device)
+        if positions.shape != (T,):
+            raise ValueError(f"positions must have shape {[T]}")
+    st = _lib.load().fa_tree_mask(parents.data_ptr(), q_starts.data_ptr(), kv_lens.data_ptr(), B, T,
+                                  1 << 30 if max_keys is None else int(max_keys), mask.data_ptr(), words,
+                                  mask.stride(0) if T > 1 else words, positions.data_ptr(),
+                                  torch._C._cuda_getCurrentRawStream(device))
+    if st != FA_OK:
+        _raise("fa_tree_mask", st)
+    return mask, positions
+
+
+def _cache(k_cache, v_cache, device):
+    """Checks a paged cache alone; its C description."""
+    import torch
+
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 4 or t.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise ValueError(f"{name} must be a 4-d torch tensor [pages, heads, page_size, d], bfloat16 or float8_e4m3fn")
+        if t.get_device() != device:
+            raise ValueError(f"{name} must be on the device cuda:{device}, not {t.device}")
+        if t.stride(3) != 1:
+            raise ValueError(f"the elements of a head of {name} must lie one after the other")
+    if k_cache.dtype != v_cache.dtype or k_cache.shape[:3] != v_cache.shape[:3]:
+        raise ValueError("k_cache and v_cache must agree in type, pages, heads and page size")
+    (pages, hkv, page, dqk), dv = k_cache.shape, v_cache.shape[3]
+    (kp, kh, ks, _), (vp, vh, vs, _) = ([0 if n <= 1 and i < 2 else s for i, (s, n) in enumerate(zip(t.stride(), t.shape))]
+                                        for t in (k_cache, v_cache))
+    return PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), None, None, kp, kh, ks, vp, vh, vs, pages, page, hkv, dqk, dv,
+                      1 if k_cache.dtype == torch.float8_e4m3fn else 0)
+
+
+def kv_compact(k_cache, v_cache, block_table, kv_lens, q_starts, kept, n_kept, new_lens=None, stream=None):
+    """Close up the new tokens that each sequence keeps, such as the accepted ones of a drafted tree: of the new tokens of
+    sequence b, which :func:`kv_append` has written, number ``kept[b, i]`` moves to the i-th place behind the cached keys, for i <
+    ``n_kept[b]``. ``kept`` int32 [B, m] holds increasing numbers, ``n_kept`` is int32 [B]; cache, table and lengths as in
+    :func:`kv_append`. Returns int32 [B], ``kv_lens - new + n_kept``, in ``new_lens`` (not ``kv_lens`` itself) or a new tensor. Keys
+    keep the rotation that they were written with.
+
+    A buffer that holds the caches of all layers, [pages, layers, Hkv, page_size, d], closes up in one call as
+    ``k_all.flatten(1, 2)``. The kernel is enqueued on ``stream`` (default: torch's current stream; a new tensor belongs to
+    that stream); the call does not synchronise, and reads no array on the host."""
+    import torch
+
+    device, cache, batch, B, *_ = _paged(k_cache, v_cache, block_table, kv_lens, q_starts, None, None, 0, torch)
+    _int32("kept", kept, 2, device)
+    _int32("n_kept", n_kept, 1, device)
+    if kept.shape[0] != B or n_kept.shape[0] != B:
+        raise ValueError(f"kept [B, m] and n_kept [B] do not agree with B = {B}: {list(kept.shape)}, {list(n_kept.shape)}")
+    elsewhere = _elsewhere(stream, device)
+    if elsewhere is not None:
+        with elsewhere:
+            return kv_compact(k_cache, v_cache, block_table, kv_lens, q_starts, kept, n_kept, new_lens)
+    if new_lens is None:
+        new_lens = kv_lens.new_empty(B)
+    else:
+        _int32("new_lens", new_lens, 1, device)
+        if new_lens.shape != (B,):
+            raise ValueError(f"new_lens must have shape {[B]}")
+        at = new_lens.data_ptr()
+        for name, t in (("kv_lens", kv_lens), ("q_starts", q_starts), ("kept", kept), ("n_kept", n_kept),
+                        ("block_table", block_table)):
+            n = t.numel() and 1 + sum((m - 1) * s for m, s in zip(t.shape, t.stride()))
+            if at < t.data_ptr() + 4 * n and t.data_ptr() < at + 4 * B:
+                raise ValueError(f"new_lens must not overlap {name}")
+    st = _lib.load().fa_kv_compact(cache, batch, kept.data_ptr(), kept.stride(0) if B > 1 else 0, kept.shape[1],
+                                   n_kept.data_ptr(), new_lens.data_ptr(), torch._C._cuda_getCurrentRawStream(device))
+    if st != FA_OK:
+        _raise("fa_kv_compact", st)
+    return new_lens
+
+
+def kv_copy(k_cache, v_cache, src, dst, stream=None):
+    """Copy pages of a paged cache: page ``src[i]`` to page ``dst[i]`` (int32 [n]), keys and values of all heads, for sequences
+    that fork and go on in pages of their own. A pair with a page number that is none of the cache's does nothing; no page
+    should be copied to twice, or copied both to and from. All layers of one buffer are copied as ``k_all.flatten(1, 2)``, see
+    :func:`kv_compact`. The kernel is enqueued on ``stream`` (default: torch's current stream); the call does not
+    synchronise, and reads no array on the host."""
+    import torch
+
+    _int32("src", src, 1, None)
+    device = src.get_device()
+    _int32("dst", dst, 1, device)
+    if src.shape != dst.shape:
+        raise ValueError(f"src and dst must have as many pages: {list(src.shape)}, {list(dst.shape)}")
+    cache = _cache(k_cache, v_cache, device)
+    elsewhere = _elsewhere(stream, device)
+    if elsewhere is not None:
+        with elsewhere:
+            return kv_copy(k_cache, v_cache, src, dst)
+    st = _lib.load().fa_kv_copy(cache, src.data_ptr(), dst.data_ptr(), src.shape[0], torch._C._cuda_getCurrentRawStream(device))
+    if st != FA_OK:
+        _raise("fa_kv_copy", st)
 
 
 def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Optional[int] = None, causal: bool = True,

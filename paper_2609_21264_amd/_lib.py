@@ -36,7 +36,8 @@ FA_NOALLOC_SCRATCH_BYTES = 32 << 20
 EXPORTED = ("fa_fwd", "fa_fwd_ex", "fa_fwd_split", "fa_fwd_split_workspace_bytes", "fa_fwd_split_parts",
             "fa_status_str", "fa_block_rows", "fa_fwd_rows", "fa_lbl_scores", "fa_lbl_softmax", "fa_lbl_pv", "fa_lbl_ld",
             "fa_lbl_workspace_bytes", "fa_fwd_unfused", "fa_fwd_decode", "fa_fwd_decode_parts",
-            "fa_fwd_decode_noalloc", "fa_fwd_instance", "fa_kv_append", "fa_fwd_paged", "fa_fwd_paged_workspace_bytes")
+            "fa_fwd_decode_noalloc", "fa_fwd_instance", "fa_kv_append", "fa_fwd_paged", "fa_fwd_paged_workspace_bytes",
+            "fa_kv_append_at", "fa_rotate", "fa_tree_mask", "fa_kv_compact", "fa_kv_copy")
 
 # Values of fa_cache_type_t.
 FA_CACHE_BF16 = 0
@@ -63,9 +64,20 @@ class PagedBatch(ctypes.Structure):
                 ("q_starts", ctypes.c_void_p), *((n, ctypes.c_int) for n in ("B", "max_blocks", "T"))]
 
 
-#: Element strides of fa_kv_append and of fa_fwd_paged.
+class Positions(ctypes.Structure):
+    """fa_positions_t."""
+
+    _fields_ = [("positions", ctypes.c_void_p), ("pair_axes", ctypes.c_void_p),
+                *((n, ctypes.c_longlong) for n in ("batch", "token", "axis")), ("n_axes", ctypes.c_int)]
+
+
+#: Element strides of fa_kv_append, of fa_fwd_paged and of fa_rotate.
 AppendStrides = ctypes.c_longlong * 8
 PagedStrides = ctypes.c_longlong * 4
+RotateStrides = ctypes.c_longlong * 6
+
+#: FA_TREE_WORDS of include/fa.h: most words of a row of a tree's mask.
+FA_TREE_WORDS = 64
 
 _lib = None
 
@@ -125,5 +137,16 @@ def load() -> ctypes.CDLL:
     lib.fa_fwd_paged.restype = i
     lib.fa_fwd_paged_workspace_bytes.argtypes = [i] * 10
     lib.fa_fwd_paged_workspace_bytes.restype = ctypes.c_size_t
+    pos, ll = ctypes.POINTER(Positions), ctypes.c_longlong
+    lib.fa_kv_append_at.argtypes = [cache, batch, vp, vp, vp, vp, i, vp, pos, vp, i, i, i, i, vp]
+    lib.fa_kv_append_at.restype = i
+    lib.fa_rotate.argtypes = [vp, vp, i, i, i, i, vp, pos, vp, i, i, i, i, i, vp]
+    lib.fa_rotate.restype = i
+    lib.fa_tree_mask.argtypes = [vp, vp, vp, i, i, i, vp, i, ll, vp, vp]
+    lib.fa_tree_mask.restype = i
+    lib.fa_kv_compact.argtypes = [cache, batch, vp, ll, i, vp, vp, vp]
+    lib.fa_kv_compact.restype = i
+    lib.fa_kv_copy.argtypes = [cache, vp, vp, i, vp]
+    lib.fa_kv_copy.restype = i
     _lib = lib
     return lib

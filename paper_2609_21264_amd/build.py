@@ -11,6 +11,7 @@ import shutil
 import subprocess
 import sys
 import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
@@ -19,7 +20,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libfa.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 SOURCES = ["fa_api.hip", "fa_fwd_kernel.hip", "fa_lbl_kernel.hip", "fa_decode_kernel.hip", "fa_paged_kernel.hip",
-           "fa_paged_fwd_kernel.hip"]
+           "fa_paged_fwd_kernel.hip", "fa_paged_moves_kernel.hip", "fa_rotate_kernel.hip"]
 # Measurement-only microbenchmarks (measured ceilings), a library of their own.
 CEIL_LIB_PATH = os.path.join(PKG_DIR, "libfa_ceilings.so")
 CEIL_SOURCES = ["fa_ceilings.hip"]
@@ -52,15 +53,13 @@ def _device_flags() -> list:
     ]
 
 
-def compile_command(out: str, extra=(), sources=SOURCES) -> list:
-    return [
-        hipcc(), *_device_flags(), "-fPIC", "-shared",
-        "-Wall", "-Wno-unused-command-line-argument",
-        "-Wl,-rpath,/opt/rocm/lib",
-        *extra,
-        "-o", out,
-        *[os.path.join(CSRC, s) for s in sources],
-    ]
+def object_command(source: str, out: str, extra=()) -> list:
+    return [hipcc(), *_device_flags(), "-fPIC", "-Wall", "-Wno-unused-command-line-argument", *extra,
+            "-c", "-o", out, os.path.join(CSRC, source)]
+
+
+def link_command(objects, out: str) -> list:
+    return [hipcc(), f"--offload-arch={ARCH}", "-fPIC", "-shared", "-Wl,-rpath,/opt/rocm/lib", "-o", out, *objects]
 
 
 def kernel_asm(out: str, source: str = "fa_fwd_kernel.hip") -> None:
@@ -73,23 +72,34 @@ def kernel_asm(out: str, source: str = "fa_fwd_kernel.hip") -> None:
         raise RuntimeError("hipcc -S failed:\n" + (res.stdout or "") + (res.stderr or ""))
 
 
+def _run(cmd, verbose: bool) -> str:
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    # hipcc's host pass does not know the packed-fp32 feature name; that warning is expected.
+    out = "\n".join(ln for ln in ((res.stdout or "") + (res.stderr or "")).splitlines()
+                    if "packed-fp32-ops" not in ln or "error" in ln)
+    if res.returncode != 0:
+        raise RuntimeError("hipcc failed:\n" + out)
+    return out
+
+
 def _link(path: str, sources, extra, verbose: bool, show: bool) -> None:
+    """Compile the sources side by side and link them."""
     fd, tmp = tempfile.mkstemp(prefix="." + os.path.basename(path) + ".", suffix=".so.tmp", dir=PKG_DIR)
     os.close(fd)
+    objects = tempfile.mkdtemp(prefix="fa_build_")
     try:
-        cmd = compile_command(tmp, extra, sources)
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        res = subprocess.run(cmd, capture_output=True, text=True)
-        out = (res.stdout or "") + (res.stderr or "")
-        # hipcc's host pass does not know the packed-fp32 feature name; that warning is expected.
-        lines = [ln for ln in out.splitlines() if "packed-fp32-ops" not in ln or "error" in ln]
-        if res.returncode != 0:
-            raise RuntimeError("hipcc failed:\n" + "\n".join(lines))
+        outs = [os.path.join(objects, s + ".o") for s in sources]
+        with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            jobs = [pool.submit(_run, object_command(s, o, extra), verbose) for s, o in zip(sources, outs)]
+            logs = [j.result() for j in jobs]
+        logs.append(_run(link_command(outs, tmp), verbose))
         if verbose or show:
-            print("\n".join(lines), flush=True)
+            print("\n".join(filter(None, logs)), flush=True)
         os.replace(tmp, path)
     finally:
+        shutil.rmtree(objects, ignore_errors=True)
         if os.path.exists(tmp):
             os.unlink(tmp)
 

@@ -403,27 +403,48 @@ PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, i
   return w;
 }
 
-}  // namespace
+// Positions of tokens by device arrays (fa.h): sizes, then what is supported. rot: the rotated dims.
+fa_status_t check_positions(const fa_positions_t* ps, int n_pos, int rot) {
+  if (ps->n_axes < 1 || n_pos < (rot > 0 ? 1 : 0)) return FA_ERR_BAD_SHAPE;
+  const long long most = 1ll << 40;
+  for (const long long s : {ps->batch, ps->token, ps->axis})
+    if (s < 0 || s > most) return FA_ERR_BAD_SHAPE;
+  return FA_OK;
+}
+bool rotation_fits(int rot_begin, int rot_dim, int d, int n_pos) {
+  return rot_dim >= 0 && rot_begin >= 0 && static_cast<int64_t>(rot_begin) + rot_dim <= d && n_pos >= 0;
+}
+bool rotation_supported(int rot_begin, int rot_dim, int interleaved) {
+  return rot_dim == 0 || (rot_begin % 8 == 0 && rot_dim % (interleaved != 0 ? 8 : 16) == 0);
+}
+fa::Positions positions_view(const fa_positions_t* ps, int n_pos) {
+  return fa::Positions{ps->positions, ps->pair_axes, ps->batch, ps->token, ps->axis, ps->n_axes, n_pos};
+}
 
-extern "C" {
-
-fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* K, const void* V,
-                         const void* Q, void* Q_out, int Hq, const long long* strides, const float* cos_sin, int n_pos,
-                         int rot_begin, int rot_dim, int interleaved, hipStream_t stream) {
+// fa_kv_append, and with positions fa_kv_append_at.
+fa_status_t append(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* K, const void* V, const void* Q,
+                   void* Q_out, int Hq, const long long* strides, const fa_positions_t* positions, const float* cos_sin,
+                   int n_pos, int rot_begin, int rot_dim, int interleaved, hipStream_t stream) {
   if (cache == nullptr || batch == nullptr || strides == nullptr) return FA_ERR_NULL_POINTER;
   fa_status_t st = check_paged_shape(cache, batch, Hq);
   if (st != FA_OK) return st;
-  if (rot_dim < 0 || rot_begin < 0 || static_cast<int64_t>(rot_begin) + rot_dim > cache->d_qk || n_pos < 0) return FA_ERR_BAD_SHAPE;
-  if (rot_dim > 0 && n_pos < static_cast<int64_t>(batch->max_blocks) * cache->page_size) return FA_ERR_BAD_SHAPE;
+  if (!rotation_fits(rot_begin, rot_dim, cache->d_qk, n_pos)) return FA_ERR_BAD_SHAPE;
+  if (positions != nullptr) {
+    st = check_positions(positions, n_pos, rot_dim);
+    if (st != FA_OK) return st;
+  } else if (rot_dim > 0 && n_pos < static_cast<int64_t>(batch->max_blocks) * cache->page_size) {
+    return FA_ERR_BAD_SHAPE;
+  }
   st = check_paged_support(cache);
   if (st != FA_OK) return st;
-  if (rot_dim > 0 && (rot_begin % 8 != 0 || rot_dim % (interleaved != 0 ? 8 : 16) != 0)) return FA_ERR_UNSUPPORTED;
+  if (!rotation_supported(rot_begin, rot_dim, interleaved)) return FA_ERR_UNSUPPORTED;
   if (batch->T == 0 || batch->B == 0) return FA_OK;
   if (!paged_pointers(cache, batch) || K == nullptr || V == nullptr || (Hq > 0 && (Q == nullptr || Q_out == nullptr)) ||
-      (rot_dim > 0 && cos_sin == nullptr))
+      (rot_dim > 0 && (cos_sin == nullptr || (positions != nullptr && positions->positions == nullptr))))
     return FA_ERR_NULL_POINTER;
   if (!paged_aligned(cache, batch) || !aligned(K, 16) || !aligned(V, 16) || !aligned(Q, 16) || !aligned(Q_out, 16) ||
-      !aligned(cos_sin, 16) || !token_strides(strides, 8))
+      !aligned(cos_sin, 16) || !token_strides(strides, 8) ||
+      (positions != nullptr && (!aligned(positions->positions, 4) || !aligned(positions->pair_axes, 4))))
     return FA_ERR_UNSUPPORTED;
   st = check_paged_strides(cache, true);
   if (st != FA_OK) return st;
@@ -440,7 +461,129 @@ fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
   p.rot = rot_dim;
   p.begin = rot_dim > 0 ? rot_begin : 0;
   p.inter = rot_dim > 0 && interleaved != 0;
+  if (positions != nullptr) p.pos = positions_view(positions, n_pos);
   return fa::launch_append(p, cache->type == FA_CACHE_E4M3, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* K, const void* V,
+                         const void* Q, void* Q_out, int Hq, const long long* strides, const float* cos_sin, int n_pos,
+                         int rot_begin, int rot_dim, int interleaved, hipStream_t stream) {
+  return append(cache, batch, K, V, Q, Q_out, Hq, strides, nullptr, cos_sin, n_pos, rot_begin, rot_dim, interleaved, stream);
+}
+
+fa_status_t fa_kv_append_at(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* K, const void* V,
+                            const void* Q, void* Q_out, int Hq, const long long* strides, const fa_positions_t* positions,
+                            const float* cos_sin, int n_pos, int rot_begin, int rot_dim, int interleaved, hipStream_t stream) {
+  if (positions == nullptr) return FA_ERR_NULL_POINTER;
+  return append(cache, batch, K, V, Q, Q_out, Hq, strides, positions, cos_sin, n_pos, rot_begin, rot_dim, interleaved, stream);
+}
+
+fa_status_t fa_rotate(const void* X, void* Y, int B, int H, int S, int d, const long long* strides,
+                      const fa_positions_t* positions, const float* cos_sin, int n_pos, int rot_begin, int rot_dim,
+                      int interleaved, int inverse, hipStream_t stream) {
+  if (strides == nullptr) return FA_ERR_NULL_POINTER;
+  if (B < 0 || H < 0 || S < 0 || d < 0) return FA_ERR_BAD_SHAPE;
+  if (static_cast<double>(B) * H * S > INT_MAX) return FA_ERR_BAD_SHAPE;
+  if (!rotation_fits(rot_begin, rot_dim, d, n_pos)) return FA_ERR_BAD_SHAPE;
+  const bool at = positions != nullptr && positions->positions != nullptr;
+  if (at) {
+    const fa_status_t st = check_positions(positions, n_pos, rot_dim);
+    if (st != FA_OK) return st;
+  } else if (rot_dim > 0 && n_pos < S) {
+    return FA_ERR_BAD_SHAPE;
+  }
+  if (d % 8 != 0 || d > 1024 || !rotation_supported(rot_begin, rot_dim, interleaved)) return FA_ERR_UNSUPPORTED;
+  if (B == 0 || H == 0 || S == 0 || d == 0) return FA_OK;
+  if (X == nullptr || Y == nullptr || (rot_dim > 0 && cos_sin == nullptr)) return FA_ERR_NULL_POINTER;
+  if (!aligned(X, 16) || !aligned(Y, 16) || !aligned(cos_sin, 16) || !token_strides(strides, 6) ||
+      (at && (!aligned(positions->positions, 4) || !aligned(positions->pair_axes, 4))))
+    return FA_ERR_UNSUPPORTED;
+  fa::RotateParams p{};
+  p.x = static_cast<const uint16_t*>(X);
+  p.y = static_cast<uint16_t*>(Y);
+  p.cos_sin = cos_sin;
+  if (at && rot_dim > 0) p.pos = positions_view(positions, n_pos);
+  p.x_b = strides[0], p.x_h = strides[1], p.x_s = strides[2], p.y_b = strides[3], p.y_h = strides[4], p.y_s = strides[5];
+  p.batch = B, p.h = H, p.s = S, p.d = d;
+  p.rot = rot_dim;
+  p.begin = rot_dim > 0 ? rot_begin : 0;
+  p.inter = rot_dim > 0 && interleaved != 0;
+  p.in_place = X == Y;
+  p.sign = inverse != 0 ? -1.f : 1.f;
+  if (p.in_place && rot_dim == 0) return FA_OK;
+  return fa::launch_rotate(p, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
+
+fa_status_t fa_tree_mask(const int* parents, const int* q_starts, const int* kv_lens, int B, int T, int max_keys, void* mask,
+                         int words, long long mask_stride, int* positions, hipStream_t stream) {
+  if (B < 0 || T < 0 || B == INT_MAX || max_keys < 0 || max_keys > kMaxPagedKeys || words < 1 || words > FA_TREE_WORDS ||
+      mask_stride < words || mask_stride > (1ll << 40))
+    return FA_ERR_BAD_SHAPE;
+  if (B == 0 || T == 0) return FA_OK;
+  if (parents == nullptr || q_starts == nullptr || kv_lens == nullptr || mask == nullptr || positions == nullptr)
+    return FA_ERR_NULL_POINTER;
+  if (!aligned(parents, 4) || !aligned(q_starts, 4) || !aligned(kv_lens, 4) || !aligned(mask, 4) || !aligned(positions, 4))
+    return FA_ERR_UNSUPPORTED;
+  fa::TreeParams p{};
+  p.bt.kv_lens = kv_lens, p.bt.q_starts = q_starts;
+  p.bt.n_seq = B, p.bt.n_tokens = T, p.bt.max_keys = max_keys;
+  p.parents = parents;
+  p.mask = static_cast<uint32_t*>(mask);
+  p.mask_stride = mask_stride;
+  p.words = words;
+  p.positions = positions;
+  return fa::launch_tree_mask(p, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
+
+fa_status_t fa_kv_compact(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const int* kept, long long kept_stride,
+                          int max_kept, const int* n_kept, int* kv_lens_out, hipStream_t stream) {
+  if (cache == nullptr || batch == nullptr) return FA_ERR_NULL_POINTER;
+  fa_paged_batch_t untold = *batch;  // there are no packed tokens here
+  untold.T = 0;
+  fa_status_t st = check_paged_shape(cache, &untold, 0);
+  if (st != FA_OK) return st;
+  if (max_kept < 0 || kept_stride < 0 || kept_stride > (1ll << 40) || cache->Hkv > INT_MAX / 64) return FA_ERR_BAD_SHAPE;
+  st = check_paged_support(cache);
+  if (st != FA_OK) return st;
+  if (batch->B == 0) return FA_OK;
+  if (!paged_pointers(cache, batch) || (max_kept > 0 && kept == nullptr) || n_kept == nullptr || kv_lens_out == nullptr)
+    return FA_ERR_NULL_POINTER;
+  if (!paged_aligned(cache, batch) || !aligned(kept, 4) || !aligned(n_kept, 4) || !aligned(kv_lens_out, 4)) return FA_ERR_UNSUPPORTED;
+  st = check_paged_strides(cache, true);
+  if (st != FA_OK) return st;
+  fa::CompactParams p{};
+  paged_view(cache, batch, &p.c, &p.bt);
+  p.bt.n_tokens = INT_MAX;
+  p.kept = kept, p.n_kept = n_kept, p.kept_stride = kept_stride, p.max_kept = max_kept;
+  p.elem = cache->type == FA_CACHE_E4M3 ? 1 : 2;
+  p.lens_out = kv_lens_out;
+  return fa::launch_kv_compact(p, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
+
+fa_status_t fa_kv_copy(const fa_paged_cache_t* cache, const int* src, const int* dst, int n, hipStream_t stream) {
+  if (cache == nullptr) return FA_ERR_NULL_POINTER;
+  const fa_paged_batch_t none{};
+  fa_status_t st = check_paged_shape(cache, &none, 0);
+  if (st != FA_OK) return st;
+  if (n < 0) return FA_ERR_BAD_SHAPE;
+  st = check_paged_support(cache);
+  if (st != FA_OK) return st;
+  if (n == 0 || cache->Hkv == 0 || cache->n_pages == 0) return FA_OK;
+  if (cache->K == nullptr || cache->V == nullptr || src == nullptr || dst == nullptr) return FA_ERR_NULL_POINTER;
+  if (!paged_aligned(cache, &none) || !aligned(src, 4) || !aligned(dst, 4)) return FA_ERR_UNSUPPORTED;
+  st = check_paged_strides(cache, true);
+  if (st != FA_OK) return st;
+  fa::PagedCache c{};
+  fa::PagedBatch bt{};
+  paged_view(cache, &none, &c, &bt);
+  const int elem = cache->type == FA_CACHE_E4M3 ? 1 : 2;
+  const int64_t blocks = fa::kv_copy_blocks(c, elem, n);
+  if (blocks < 0 || blocks >= 1 << 24) return FA_ERR_BAD_SHAPE;  // one dimension of a grid, 256 threads each
+  return fa::launch_kv_copy(c, elem, src, dst, n, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 
 size_t fa_fwd_paged_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q,

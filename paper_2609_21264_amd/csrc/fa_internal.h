@@ -159,6 +159,14 @@ struct PagedBatch {
   int max_keys;            // keys that a row of the table has pages for
 };
 
+// Where a token's rows of the table of angles come from, if not from its place: device arrays.
+struct Positions {
+  const int* positions;            // token t's position on axis a at t * token + a * axis (batch: the rotation alone)
+  const unsigned char* pair_axes;  // [rot / 2]: the axis of each pair; nullptr: the first
+  int64_t batch, token, axis;
+  int n_axes, n_pos;
+};
+
 struct AppendParams {
   PagedCache c;
   PagedBatch bt;
@@ -170,6 +178,7 @@ struct AppendParams {
   int64_t q_token, q_head, qo_token, qo_head, k_token, k_head, v_token, v_head;
   int hq;                // 0: no queries
   int rot, begin, inter; // rotated dims (0: none), the first of them, neighbouring pairs
+  Positions pos;         // positions nullptr: the row of a token is its place among its sequence's keys
 };
 
 // Columns of a place of the kernel for many rows. One more than a block has: with places 128 KiB apart the workgroups that
@@ -214,6 +223,64 @@ struct PagedParams {
   PagedItem* many_desc;  // [many_wg]
   uint32_t m_group, sh_group;  // division by group, filled by the launchers
 };
+
+// ---- rotation alone (fa_rotate_kernel.hip) --------------------------------------------------------
+
+struct RotateParams {
+  const uint16_t* x;
+  uint16_t* y;
+  const float* cos_sin;
+  Positions pos;          // positions nullptr: the row of token s is s
+  int64_t x_b, x_h, x_s, y_b, y_h, y_s;
+  int batch, h, s, d, rot, begin, inter, in_place;
+  float sign;             // of the angles
+  int per, n_blocks, heads;  // filled by launch_rotate: blocks of tokens of a batch and in all, heads of a workgroup
+  uint32_t m_per, sh_per;
+};
+hipError_t launch_rotate(RotateParams p, hipStream_t stream);
+
+// ---- around the paged cache (fa_paged_moves_kernel.hip) --------------------------------------------
+
+struct TreeParams {
+  PagedBatch bt;          // block_table unused
+  const int* parents;     // [n_tokens]
+  uint32_t* mask;         // [n_tokens], rows mask_stride apart
+  int64_t mask_stride;
+  int words;
+  int* positions;         // [n_tokens]
+};
+hipError_t launch_tree_mask(TreeParams p, hipStream_t stream);
+
+// Sequences of one row of the grid (its second dimension; the third counts rows).
+constexpr int kMoveRows = 1 << 15;
+struct CompactParams {
+  PagedCache c;
+  PagedBatch bt;
+  const int* kept;        // [n_seq], rows kept_stride apart
+  const int* n_kept;      // [n_seq]
+  int64_t kept_stride;
+  int max_kept, elem;     // entries of a row, bytes of an element
+  int* lens_out;          // [n_seq]
+  uint32_t k_chunks, v_chunks, m_k, sh_k, m_v, sh_v;  // filled by launch_kv_compact: 16-byte chunks of a row
+};
+hipError_t launch_kv_compact(CompactParams p, hipStream_t stream);
+
+// K or V of a page as heads of rows of `run` 16-byte chunks; strides in bytes.
+struct CopySide {
+  unsigned char* base;
+  int64_t page, head, row;
+  uint32_t chunks, rows, run, m_run, sh_run, m_rows, sh_rows;
+};
+struct CopyParams {
+  CopySide side[2];
+  const int* src;
+  const int* dst;
+  int n_pages;
+  uint32_t parts, m_parts, sh_parts;  // workgroups of a pair of pages
+};
+// Workgroups of a copy of n pages (of K, and as many of V); -1 where a page is too large.
+int64_t kv_copy_blocks(const PagedCache& c, int elem, int n);
+hipError_t launch_kv_copy(const PagedCache& c, int elem, const int* src, const int* dst, int n, hipStream_t stream);
 
 hipError_t launch_append(AppendParams p, bool fp8, hipStream_t stream);
 // Workgroups of the attention kernel (as many as the chip holds at once).

@@ -16,6 +16,7 @@
 #include "fa_fastdiv.h"
 #include "fa_internal.h"
 #include "fa_paged_device.h"
+#include "fa_turn.h"
 
 namespace fa {
 namespace {
@@ -48,23 +49,6 @@ __device__ __forceinline__ int sequence_of(const int* q_starts, int n_seq, int t
   }
 }
 
-// Eight bf16 as fp32 and back (RNE).
-struct F8 {
-  float x[8];
-};
-__device__ __forceinline__ F8 unpack8(const u32x4& w) {
-  F8 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r.x[2 * i] = __uint_as_float(w[i] << 16);
-    r.x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-  return r;
-}
-__device__ __forceinline__ u32x4 pack8(const F8& f) {
-  return u32x4{pack_bf16x2(f.x[0], f.x[1]), pack_bf16x2(f.x[2], f.x[3]), pack_bf16x2(f.x[4], f.x[5]),
-               pack_bf16x2(f.x[6], f.x[7])};
-}
 // x / scale in e4m3, rounded to nearest even; what passes the largest finite value (448) becomes it, NaN
 // stays NaN.
 __device__ __forceinline__ u32x2 pack8_e4m3(const F8& f, float scale) {
@@ -85,7 +69,8 @@ constexpr int kAppendThreads = 256;
 // Tokens of a row of the grid: a dimension of it holds fewer than 2^32 threads, so 2^24 tokens and more need a second one.
 constexpr int kAppendRowLog = 22;
 
-template <bool FP8>
+// AT: the rows of the table go by p.pos, not by the keys' places.
+template <bool FP8, bool AT>
 __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams p) {
   const int t = (int)(blockIdx.y << kAppendRowLog | blockIdx.x), tid = threadIdx.x, lane = tid & 63;  // below 2^31
   if (t >= p.bt.n_tokens) return;
@@ -99,30 +84,24 @@ __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams 
   const bool held = page >= 0 && page < p.c.n_pages;
   const int64_t slot = pos & ((1 << p.c.page_shift) - 1);
 
-  const int half = p.inter ? 0 : p.rot / 16;  // chunks between the partners of a pair
-  const int first = p.begin / 8, turned = p.inter ? p.rot / 8 : half;
-  // Q and K: thread (h0, j) takes chunk j of every kHeads-th head; the first `turned` chunks are those that
-  // turn (each with its partner `half` chunks on), the others are copied.
-  const int tasks = p.c.d_qk / 8 - half, lanes = kAppendThreads / tasks;
-  const int j = tid % tasks, h0 = tid / tasks;
+  // Q and K: thread (h0, j) takes task j of every kHeads-th head.
+  const TurnTasks w(p.c.d_qk, p.rot, p.begin, p.inter);
+  const int half = w.half, lanes = kAppendThreads / w.tasks;
+  const int j = tid % w.tasks, h0 = tid / w.tasks;
   if (h0 < lanes) {
-    const bool turn = j < turned;
-    int ch = first + j;
-    if (!turn) {
-      const int o = j - turned;  // o-th of the chunks outside [first, first + turned + half)
-      ch = o < first ? o : o + turned + half;
-    }
+    const bool turn = j < w.turned;
+    const int ch = w.chunk(j);
     F8 cs{}, sn{};
     if (turn) {
       // Half-split: cos and sin of 8 pairs; neighbouring pairs: of the chunk's 4.
-      const float* row = p.cos_sin + pos * p.rot + (p.inter ? 4 * j : 8 * j);
-      const float* srow = row + p.rot / 2;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if (i > 0 && p.inter) break;
-        const f32x4 c4 = *reinterpret_cast<const f32x4*>(row + 4 * i), s4 = *reinterpret_cast<const f32x4*>(srow + 4 * i);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) cs.x[4 * i + e] = c4[e], sn.x[4 * i + e] = s4[e];
+        const int four = p.inter ? j : 2 * j + i;
+        if constexpr (AT)
+          angles_at(cs, sn, i, p.pos, p.pos.positions + t * p.pos.token, p.cos_sin, p.rot, four);
+        else
+          angles_of_row(cs, sn, i, p.cos_sin + pos * p.rot, p.rot, four);
       }
     }
     const bool pair = turn && !p.inter;
@@ -135,19 +114,9 @@ __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams 
       F8 x = unpack8(*reinterpret_cast<const u32x4*>(src)), y;
       if (pair) {
         y = unpack8(*reinterpret_cast<const u32x4*>(src + 8 * half));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float a = x.x[e], c = y.x[e];
-          x.x[e] = a * cs.x[e] - c * sn.x[e];
-          y.x[e] = c * cs.x[e] + a * sn.x[e];
-        }
+        turn_halves(x, y, cs, sn);
       } else if (turn) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float a = x.x[2 * e], c = x.x[2 * e + 1];
-          x.x[2 * e] = a * cs.x[e] - c * sn.x[e];
-          x.x[2 * e + 1] = c * cs.x[e] + a * sn.x[e];
-        }
+        turn_neighbours(x, cs, sn);
       }
       if (is_q) {
         uint16_t* dst = p.q_out + t * p.qo_token + h * p.qo_head + 8 * ch;
@@ -760,9 +729,12 @@ hipError_t launch_append(AppendParams p, bool fp8, hipStream_t stream) {
   constexpr unsigned kRow = 1u << kAppendRowLog;
   const unsigned n = (unsigned)p.bt.n_tokens;
   const dim3 grid(n < kRow ? n : kRow, (n + kRow - 1) / kRow);
-  return hipLaunchKernel(fp8 ? reinterpret_cast<const void*>(&fa_append_kernel<true>)
-                             : reinterpret_cast<const void*>(&fa_append_kernel<false>),
-                         grid, dim3(kAppendThreads), args, 0, stream);
+  const bool at = p.pos.positions != nullptr && p.rot > 0;
+  const void* k = fp8 ? (at ? reinterpret_cast<const void*>(&fa_append_kernel<true, true>)
+                            : reinterpret_cast<const void*>(&fa_append_kernel<true, false>))
+                      : (at ? reinterpret_cast<const void*>(&fa_append_kernel<false, true>)
+                            : reinterpret_cast<const void*>(&fa_append_kernel<false, false>));
+  return hipLaunchKernel(k, grid, dim3(kAppendThreads), args, 0, stream);
 }
 
 // Instances by head dimensions, cache type and 32-column blocks; as many ring slots as leave two workgroups to a CU
