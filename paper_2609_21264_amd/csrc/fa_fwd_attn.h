@@ -15,7 +15,6 @@
 namespace fa {
 namespace {
 
-constexpr float kLn2 = 0.69314718055994530942f;
 // A tile's exponentials are accepted when every lane's sum of them is at most 2^8: then no
 // probability exceeds 2^8 relative to the reference maximum.
 constexpr float kOverflowSum = 256.0f;
