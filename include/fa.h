@@ -485,6 +485,49 @@ fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* 
 size_t fa_fwd_paged_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q,
                                     int path);
 
+/* The largest cap of scores. */
+#define FA_MAX_SOFTCAP 1024.0f
+
+/*
+ * How fa_fwd_paged_ex changes scores and hides keys. For the token at position p (its place among its sequence's kv_lens[b] keys)
+ * and key j, with x = scale * q . k:
+ *   softcap      > 0: x becomes softcap * tanh(x / softcap), up to FA_MAX_SOFTCAP; 0: none
+ *   slopes       float32 [Hq] or NULL: then slopes[h] * |p - j| is taken off
+ *   window       > 0: key j is hidden where |p - j| >= window (the token itself counts); 0: none
+ *   prefix_lens  int32 [B] or NULL: keys j < prefix_lens[b] (clamped to [0, kv_lens[b]]) are visible to all tokens of the
+ *                sequence, whatever window and causal masking say: a bidirectional prefix, or first tokens kept beside a window
+ *   tree_mask    32-bit words [T][mask_words], rows mask_stride >= mask_words apart, up to FA_TREE_WORDS words; or NULL. The new tokens
+ *                are drafted ones: token t sees all cached keys j < kv_lens[b] - n, and the sequence's i-th new token where
+ *                bit i % 32 of word i / 32 is set (new tokens from 32 * mask_words on are hidden). Only causal calls, and not with
+ *                slopes, a window or a prefix, whose distances would be those of places in the cache.
+ */
+typedef struct {
+  float softcap;
+  int window;
+  const float* slopes;
+  const int* prefix_lens;
+  const void* tree_mask;
+  long long mask_stride;
+  int mask_words;
+} fa_paged_scores_t;
+
+/*
+ * fa_fwd_paged_ex -- fa_fwd_paged with `scores` (NULL, or nothing in it set: fa_fwd_paged). Keys that no token of a block sees,
+ * such as those before its window, are mostly not read. Keys that are hidden from a row reach neither its O nor its LSE, except that,
+ * as in fa_fwd_paged, an infinity or a NaN in a value may. A capped score is off by up to 2^-22 softcap, which is
+ * why caps are bounded. The workspace has fa_fwd_paged_ex_workspace_bytes(...) bytes.
+ * Errors: as fa_fwd_paged, with a negative window, mask_words and mask_stride out of range among the sizes, the combinations
+ * above FA_ERR_UNSUPPORTED among what is supported, a softcap that is negative, no number or too large FA_ERR_BAD_SCALE behind the
+ * scale, and an alignment of 4 bytes of the arrays.
+ */
+fa_status_t fa_fwd_paged_ex(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const fa_paged_scores_t* scores,
+                            const void* Q, void* O, float* LSE, int Hq, const long long* strides, int max_q, int path,
+                            float scale, int causal, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of a fa_fwd_paged_ex call with these sizes, whatever its scores; as fa_fwd_paged_workspace_bytes. */
+size_t fa_fwd_paged_ex_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q,
+                                       int path);
+
 /* Static, human-readable name of a status code ("FA_OK", ...); "unknown status" otherwise. */
 const char* fa_status_str(fa_status_t s);
 

@@ -31,7 +31,8 @@ import math
 from typing import Optional
 
 from . import _lib
-from ._lib import (AppendStrides, PagedBatch, PagedCache, PagedStrides, Positions, RotateStrides,  # noqa: F401
+from ._lib import (AppendStrides, PagedBatch, PagedCache, PagedScores, PagedStrides, Positions, RotateStrides,  # noqa: F401
+                   FA_MAX_SOFTCAP,
                    FA_CACHE_BF16, FA_CACHE_E4M3, FA_PAGED_AUTO, FA_PAGED_FEW, FA_PAGED_MANY, FA_TREE_WORDS,
                    FA_ERR_BAD_SCALE, FA_ERR_BAD_SHAPE, FA_ERR_HIP, FA_ERR_NULL_POINTER,
                    FA_ERR_UNSUPPORTED, FA_ERR_WORKSPACE, FA_INSTANCE_HALVES, FA_INSTANCE_LONG, FA_INSTANCE_NONE,
@@ -45,7 +46,8 @@ __all__ = ["fa_fwd", "fa_fwd_ex", "fa_fwd_split", "fa_fwd_split_workspace_bytes"
            "fa_kv_append", "fa_fwd_paged", "fa_fwd_paged_workspace_bytes", "PagedCache", "PagedBatch", "AppendStrides",
            "PagedStrides", "FA_CACHE_BF16", "FA_CACHE_E4M3", "FA_PAGED_AUTO", "FA_PAGED_FEW",
            "FA_PAGED_MANY", "kv_append", "forward_paged", "fa_kv_append_at", "fa_rotate", "fa_tree_mask", "fa_kv_compact",
-           "fa_kv_copy", "Positions", "RotateStrides", "FA_TREE_WORDS", "rotate", "tree_mask", "kv_compact", "kv_copy"]
+           "fa_kv_copy", "Positions", "RotateStrides", "FA_TREE_WORDS", "rotate", "tree_mask", "kv_compact", "kv_copy",
+           "fa_fwd_paged_ex", "fa_fwd_paged_ex_workspace_bytes", "PagedScores", "FA_MAX_SOFTCAP"]
 
 
 class FaError(RuntimeError):
@@ -217,6 +219,20 @@ def fa_fwd_paged_workspace_bytes(B: int, T: int, max_keys: int, Hq: int, Hkv: in
                                  max_q: int, path: int = FA_PAGED_AUTO) -> int:
     """C ``fa_fwd_paged_workspace_bytes`` (``max_keys``: blocks of the table times page size)."""
     return int(_lib.load().fa_fwd_paged_workspace_bytes(B, T, max_keys, Hq, Hkv, d_qk, d_v, type, max_q, path))
+
+
+def fa_fwd_paged_ex(cache: PagedCache, batch: PagedBatch, scores: Optional[PagedScores], Q: int, O: int, LSE: Optional[int],
+                    Hq: int, strides: PagedStrides, max_q: int, path: int, scale: float, causal: bool,
+                    workspace: Optional[int], workspace_bytes: int, stream: int) -> int:
+    """C ``fa_fwd_paged_ex``: descriptions, raw device addresses and sizes; returns the status code."""
+    return int(_lib.load().fa_fwd_paged_ex(cache, batch, scores, Q, O, LSE, Hq, strides, max_q, path, float(scale),
+                                           int(bool(causal)), workspace, int(workspace_bytes), stream))
+
+
+def fa_fwd_paged_ex_workspace_bytes(B: int, T: int, max_keys: int, Hq: int, Hkv: int, d_qk: int, d_v: int, type: int,
+                                    max_q: int, path: int = FA_PAGED_AUTO) -> int:
+    """C ``fa_fwd_paged_ex_workspace_bytes`` (``max_keys``: blocks of the table times page size)."""
+    return int(_lib.load().fa_fwd_paged_ex_workspace_bytes(B, T, max_keys, Hq, Hkv, d_qk, d_v, type, max_q, path))
 
 
 # What a call costs on the host bounds the smallest problems (one head S256 d64: a 4.7 us kernel in a call
@@ -849,7 +865,8 @@ def kv_copy(k_cache, v_cache, src, dst, stream=None):
 
 def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Optional[int] = None, causal: bool = True,
                   scale: Optional[float] = None, k_scale=None, v_scale=None, return_lse: bool = False, out=None, lse=None,
-                  workspace=None, stream=None, path: Optional[str] = None):
+                  workspace=None, stream=None, path: Optional[str] = None, softcap: Optional[float] = None, slopes=None,
+                  window: Optional[int] = None, prefix_lens=None, tree_mask=None):
     """Attention of the new tokens q [T, Hq, d_qk] over a paged cache (see :func:`kv_append` for the cache and the
     batch, whose new tokens are in the cache already): returns O [T, Hq, d_v] (bf16) and, with ``return_lse``, LSE
     [T, Hq] (float32, natural log). Token i of the n new ones of sequence b sees the keys up to its position
@@ -858,7 +875,14 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
     longer ones; the results are right for any. Rows of tokens that belong to no
     sequence are left as they were, so a new tensor's hold anything.
 
-    ``scale`` defaults to 1/sqrt(d_qk). ``workspace`` is a CUDA tensor of ``fa_fwd_paged_workspace_bytes`` (default: from
+    Scores x = scale * q . k may be changed and keys hidden, for the token at position p and key j: ``softcap`` makes x softcap *
+    tanh(x / softcap) (up to 1024); ``slopes`` (float32 [Hq]) takes slopes[h] * abs(p - j) off; ``window`` hides keys with
+    abs(p - j) >= window; ``prefix_lens`` (int32 [B]) shows all tokens of a sequence its first keys, whatever window and causal masking
+    say; ``tree_mask`` (int32 [T, words], see :func:`tree_mask`) says which of their sequence's new tokens drafted ones see, beside
+    all cached keys (causal calls without slopes, window and prefix).
+
+    ``scale`` defaults to 1/sqrt(d_qk). ``workspace`` is a CUDA tensor of ``fa_fwd_paged_workspace_bytes`` (with any of the
+    options above ``fa_fwd_paged_ex_workspace_bytes``; default: from
     torch's allocator). The kernels are enqueued on ``stream`` (default: torch's current stream; new tensors belong to that
     stream); the call does not synchronise, and reads no array on the host: captured into a graph, it serves
     whatever lengths the arrays hold at a replay."""
@@ -881,11 +905,14 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
         if path not in ("few", "many"):
             raise ValueError(f'path must be "few", "many" or None, not {path!r}')
         way = FA_PAGED_FEW if path == "few" else FA_PAGED_MANY
+    scores = None
+    if not (softcap is None and slopes is None and window is None and prefix_lens is None and tree_mask is None):
+        scores = _scores(softcap, slopes, window, prefix_lens, tree_mask, T, hq, B, device)
     elsewhere = _elsewhere(stream, device)
     if elsewhere is not None:
         with elsewhere:
             return forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q, causal, scale, k_scale, v_scale,
-                                 return_lse, out, lse, workspace, path=path)
+                                 return_lse, out, lse, workspace, None, path, softcap, slopes, window, prefix_lens, tree_mask)
     if out is not None:
         ot, oh = _rows("out", out, (T, hq, dv), device, bf16, True)
     else:
@@ -901,7 +928,8 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
         lse = q.new_empty((T, hq), dtype=torch.float32)
     lib, ws = _lib.load(), None
     if workspace is None:
-        nbytes = lib.fa_fwd_paged_workspace_bytes(B, T, max_keys, hq, hkv, dqk, dv, type, max_q, way)
+        size = lib.fa_fwd_paged_workspace_bytes if scores is None else lib.fa_fwd_paged_ex_workspace_bytes
+        nbytes = size(B, T, max_keys, hq, hkv, dqk, dv, type, max_q, way)
         if nbytes > 0:
             workspace = q.new_empty(nbytes, dtype=torch.uint8)
             ws = workspace.data_ptr()
@@ -909,9 +937,48 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
         raise ValueError(f"workspace must be a contiguous tensor on cuda:{device}")
     else:
         nbytes, ws = workspace.numel() * workspace.element_size(), workspace.data_ptr()
-    st = lib.fa_fwd_paged(cache, batch, q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), hq,
-                          PagedStrides(qt, qh, ot, oh), max_q, way, scale, 1 if causal else 0, ws, nbytes,
-                          torch._C._cuda_getCurrentRawStream(device))
+    lsep, strides, stream = None if lse is None else lse.data_ptr(), PagedStrides(qt, qh, ot, oh), \
+        torch._C._cuda_getCurrentRawStream(device)
+    if scores is None:
+        st = lib.fa_fwd_paged(cache, batch, q.data_ptr(), out.data_ptr(), lsep, hq, strides, max_q, way, scale,
+                              1 if causal else 0, ws, nbytes, stream)
+    else:
+        st = lib.fa_fwd_paged_ex(cache, batch, scores, q.data_ptr(), out.data_ptr(), lsep, hq, strides, max_q, way, scale,
+                                 1 if causal else 0, ws, nbytes, stream)
     if st != FA_OK:
-        _raise("fa_fwd_paged", st)
+        _raise("fa_fwd_paged" if scores is None else "fa_fwd_paged_ex", st)
     return (out, lse) if return_lse else out
+
+
+def _scores(softcap, slopes, window, prefix_lens, tree_mask, T, hq, B, device):
+    """The C description of how scores are changed and keys hidden."""
+    import torch
+
+    s = PagedScores()
+    if softcap is not None:
+        s.softcap = softcap
+        if not 0 < softcap <= FA_MAX_SOFTCAP:
+            raise ValueError(f"softcap must be above 0 and at most {FA_MAX_SOFTCAP:g}, not {softcap}")
+    if window is not None:
+        if not 0 < window < 1 << 31:
+            raise ValueError(f"window must be at least 1 key, not {window}")
+        s.window = window
+    if slopes is not None:
+        if (not isinstance(slopes, torch.Tensor) or slopes.dtype != torch.float32 or slopes.shape != (hq,)
+                or not slopes.is_contiguous()):
+            raise ValueError(f"slopes must be a contiguous float32 tensor [{hq}]")
+        if slopes.get_device() != device:
+            raise ValueError(f"slopes must be on the cache's device cuda:{device}, not {slopes.device}")
+        s.slopes = slopes.data_ptr()
+    if prefix_lens is not None:
+        _int32("prefix_lens", prefix_lens, 1, device)
+        if prefix_lens.shape != (B,):
+            raise ValueError(f"prefix_lens must have shape {[B]}, not {list(prefix_lens.shape)}")
+        s.prefix_lens = prefix_lens.data_ptr()
+    if tree_mask is not None:
+        _int32("tree_mask", tree_mask, 2, device)
+        if tree_mask.shape[0] != T or not 1 <= tree_mask.shape[1] <= FA_TREE_WORDS:
+            raise ValueError(f"tree_mask must have shape [{T}, 1 to {FA_TREE_WORDS}], not {list(tree_mask.shape)}")
+        s.tree_mask, s.mask_words = tree_mask.data_ptr(), tree_mask.shape[1]
+        s.mask_stride = tree_mask.stride(0) if T > 1 else tree_mask.shape[1]
+    return s

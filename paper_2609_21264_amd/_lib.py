@@ -37,7 +37,8 @@ EXPORTED = ("fa_fwd", "fa_fwd_ex", "fa_fwd_split", "fa_fwd_split_workspace_bytes
             "fa_status_str", "fa_block_rows", "fa_fwd_rows", "fa_lbl_scores", "fa_lbl_softmax", "fa_lbl_pv", "fa_lbl_ld",
             "fa_lbl_workspace_bytes", "fa_fwd_unfused", "fa_fwd_decode", "fa_fwd_decode_parts",
             "fa_fwd_decode_noalloc", "fa_fwd_instance", "fa_kv_append", "fa_fwd_paged", "fa_fwd_paged_workspace_bytes",
-            "fa_kv_append_at", "fa_rotate", "fa_tree_mask", "fa_kv_compact", "fa_kv_copy")
+            "fa_kv_append_at", "fa_rotate", "fa_tree_mask", "fa_kv_compact", "fa_kv_copy",
+            "fa_fwd_paged_ex", "fa_fwd_paged_ex_workspace_bytes")
 
 # Values of fa_cache_type_t.
 FA_CACHE_BF16 = 0
@@ -71,6 +72,14 @@ class Positions(ctypes.Structure):
                 *((n, ctypes.c_longlong) for n in ("batch", "token", "axis")), ("n_axes", ctypes.c_int)]
 
 
+class PagedScores(ctypes.Structure):
+    """fa_paged_scores_t."""
+
+    _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int),
+                *((n, ctypes.c_void_p) for n in ("slopes", "prefix_lens", "tree_mask")), ("mask_stride", ctypes.c_longlong),
+                ("mask_words", ctypes.c_int)]
+
+
 #: Element strides of fa_kv_append, of fa_fwd_paged and of fa_rotate.
 AppendStrides = ctypes.c_longlong * 8
 PagedStrides = ctypes.c_longlong * 4
@@ -78,6 +87,9 @@ RotateStrides = ctypes.c_longlong * 6
 
 #: FA_TREE_WORDS of include/fa.h: most words of a row of a tree's mask.
 FA_TREE_WORDS = 64
+
+#: FA_MAX_SOFTCAP of include/fa.h: the largest cap of scores.
+FA_MAX_SOFTCAP = 1024.0
 
 _lib = None
 
@@ -148,5 +160,9 @@ def load() -> ctypes.CDLL:
     lib.fa_kv_compact.restype = i
     lib.fa_kv_copy.argtypes = [cache, vp, vp, i, vp]
     lib.fa_kv_copy.restype = i
+    lib.fa_fwd_paged_ex.argtypes = [cache, batch, ctypes.POINTER(PagedScores), vp, vp, vp, i, vp, i, i, f, i, vp, ctypes.c_size_t, vp]
+    lib.fa_fwd_paged_ex.restype = i
+    lib.fa_fwd_paged_ex_workspace_bytes.argtypes = [i] * 10
+    lib.fa_fwd_paged_ex_workspace_bytes.restype = ctypes.c_size_t
     _lib = lib
     return lib

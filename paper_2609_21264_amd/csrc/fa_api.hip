@@ -353,7 +353,7 @@ struct PagedPlan {
   int64_t lse, desc, many_o, many_lse, many_desc, bytes;  // 16-byte aligned offsets
 };
 PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, int d_v, int type, int max_q,
-                     int path) {
+                     int path, bool forms) {
   PagedPlan w{};
   const bool known = max_q > 0;
   if (!known) max_q = T > B ? T - B + 1 : 1;
@@ -374,7 +374,7 @@ PagedPlan paged_plan(int B, int T, int max_keys, int Hkv, int group, int d_qk, i
   w.few_cols = !w.many ? INT_MAX : w.few ? 32 : 0;
   const int64_t items32 = (rows / 32 + (B < T ? B : T)) * Hkv;
   w.col_blocks = w.usual <= 32 || w.many || (items32 <= 256 && (w.usual > kFewCols || max_keys <= kWholeKeys)) ? 1 : 2;
-  if (w.many) w.m = fa::paged_many(B, T, max_keys, Hkv, group, max_q, w.few_cols, d_qk, e4m3);
+  if (w.many) w.m = fa::paged_many(B, T, max_keys, Hkv, group, max_q, w.few_cols, d_qk, e4m3, forms);
   auto place = [&](int64_t n) {
     const int64_t at = w.bytes;
     w.bytes += (n + 15) / 16 * 16;
@@ -463,6 +463,116 @@ fa_status_t append(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch,
   p.inter = rot_dim > 0 && interleaved != 0;
   if (positions != nullptr) p.pos = positions_view(positions, n_pos);
   return fa::launch_append(p, cache->type == FA_CACHE_E4M3, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
+}
+
+// Whether a call changes scores or hides keys beyond causal masking. (A cap that is no number counts, so that it is refused.)
+bool any_forms(const fa_paged_scores_t* s) {
+  return s != nullptr && (s->softcap != 0.f || s->window != 0 || s->slopes != nullptr || s->prefix_lens != nullptr ||
+                          s->tree_mask != nullptr);
+}
+size_t workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q, int path, bool forms) {
+  if (B <= 0 || T <= 0 || max_keys < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_q < 0 || !dims_supported(d_qk, d_v) ||
+      (type != FA_CACHE_BF16 && type != FA_CACHE_E4M3) || path < FA_PAGED_AUTO || path > FA_PAGED_MANY)
+    return 0;
+  return static_cast<size_t>(paged_plan(B, T, max_keys, Hkv, Hq / Hkv, d_qk, d_v, type, max_q, path, forms).bytes);
+}
+
+// fa_fwd_paged, and with forms fa_fwd_paged_ex.
+fa_status_t attend(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const fa_paged_scores_t* scores, const void* Q,
+                   void* O, float* LSE, int Hq, const long long* strides, int max_q, int path, float scale, int causal,
+                   void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (cache == nullptr || batch == nullptr || strides == nullptr) return FA_ERR_NULL_POINTER;
+  fa_status_t st = check_paged_shape(cache, batch, Hq);
+  if (st != FA_OK) return st;
+  if (max_q < 0) return FA_ERR_BAD_SHAPE;
+  if (Hq > 0) {
+    // The kernel's line of work is counted in 32 bits.
+    const int64_t blocks = (static_cast<int64_t>(batch->T) * (Hq / cache->Hkv) / 32 + batch->B) * cache->Hkv;  // < 2^58
+    const int64_t tiles = static_cast<int64_t>(batch->max_blocks) * cache->page_size / 128 + 2;
+    if (blocks > INT_MAX / tiles) return FA_ERR_BAD_SHAPE;
+    if (path == FA_PAGED_MANY && !many_fits(batch->B, batch->T, cache->Hkv, Hq / cache->Hkv)) return FA_ERR_BAD_SHAPE;
+  }
+  const bool forms = any_forms(scores);
+  const bool tree = forms && scores->tree_mask != nullptr;
+  if (forms && (scores->window < 0 || (tree && (scores->mask_words < 1 || scores->mask_words > FA_TREE_WORDS ||
+                                                scores->mask_stride < scores->mask_words || scores->mask_stride > (1ll << 40)))))
+    return FA_ERR_BAD_SHAPE;
+  st = check_paged_support(cache);
+  if (st != FA_OK) return st;
+  if (tree && (causal == 0 || scores->window != 0 || scores->slopes != nullptr || scores->prefix_lens != nullptr))
+    return FA_ERR_UNSUPPORTED;
+  if (path < FA_PAGED_AUTO || path > FA_PAGED_MANY) return FA_ERR_UNSUPPORTED;
+  if (batch->T == 0 || batch->B == 0 || Hq == 0) return FA_OK;
+  if (!paged_pointers(cache, batch) || Q == nullptr || O == nullptr) return FA_ERR_NULL_POINTER;
+  if (!isfinite(scale)) return FA_ERR_BAD_SCALE;
+  const double c = static_cast<double>(scale) * 1.4426950408889634074;
+  if (fabs(c) > FLT_MAX) return FA_ERR_BAD_SCALE;
+  if (forms && !(scores->softcap >= 0.f && scores->softcap <= FA_MAX_SOFTCAP)) return FA_ERR_BAD_SCALE;
+  if (!paged_aligned(cache, batch) || !aligned(Q, 16) || !aligned(O, 16) || !aligned(LSE, 4) || !token_strides(strides, 4) ||
+      (forms && (!aligned(scores->slopes, 4) || !aligned(scores->prefix_lens, 4) || !aligned(scores->tree_mask, 4))))
+    return FA_ERR_UNSUPPORTED;
+  st = check_paged_strides(cache, false);
+  if (st != FA_OK) return st;
+  const PagedPlan w = paged_plan(batch->B, batch->T, batch->max_blocks * cache->page_size, cache->Hkv, Hq / cache->Hkv,
+                                 cache->d_qk, cache->d_v, cache->type, max_q, path, forms);
+  if (w.bytes > 0 && (workspace == nullptr || workspace_bytes < static_cast<size_t>(w.bytes))) return FA_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return FA_ERR_UNSUPPORTED;
+
+  fa::PagedParams p{};
+  paged_view(cache, batch, &p.c, &p.bt);
+  p.q = static_cast<const uint16_t*>(Q);
+  p.o = static_cast<uint16_t*>(O);
+  p.lse = LSE;
+  p.q_token = strides[0], p.q_head = strides[1], p.o_token = strides[2], p.o_head = strides[3];
+  p.hq = Hq;
+  p.group = Hq / cache->Hkv;
+  p.causal = causal != 0;
+  const float cmag = fabs(c) < FLT_MIN ? FLT_MIN : static_cast<float>(fabs(c));  // a masked score stays infinite
+  p.cs = c < 0 ? -cmag : cmag;
+  if (forms) {
+    if (scores->softcap > 0.f) {
+      const float a = scores->softcap * 1.44269504088896340736f, r = 2.f / scores->softcap;
+      p.f.cap_a = a < FLT_MIN ? FLT_MIN : a;
+      p.f.cap_r = r > FLT_MAX ? FLT_MAX : r;
+    }
+    p.f.slopes = scores->slopes;
+    p.f.prefix_lens = scores->prefix_lens;
+    p.f.mask = static_cast<const uint32_t*>(scores->tree_mask);
+    p.f.mask_stride = scores->mask_stride;
+    p.f.mask_words = scores->mask_words;
+    p.f.window = scores->window < kMaxPagedKeys ? scores->window : 0;  // no two keys are as far apart
+    p.f.causal = p.causal;
+  }
+  p.few_cols = w.few_cols;
+  p.many_work = w.many_work;
+  p.n_wg = w.n_wg;
+  p.part_cols = w.cols;
+  p.whole = w.whole;
+  p.many_wg = w.m.n_wg;
+  p.many_cols = w.m.cols;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  p.o_part = reinterpret_cast<float*>(ws);
+  p.lse_part = reinterpret_cast<float*>(ws + w.lse);
+  p.desc = reinterpret_cast<fa::PagedItem*>(ws + w.desc);
+  p.many_o = reinterpret_cast<float*>(ws + w.many_o);
+  p.many_lse = reinterpret_cast<float*>(ws + w.many_lse);
+  p.many_desc = reinterpret_cast<fa::PagedItem*>(ws + w.many_desc);
+  // A single item per sequence and head reads K and V once: they are then loaded past the caches.
+  const bool stream_kv = w.usual <= 32 * w.col_blocks;
+  // Beside the kernel for many rows the others are mostly single tokens.
+  const int64_t usual = w.many ? p.group : w.usual;
+  const int cols = usual < w.cols ? static_cast<int>(usual) : w.cols;
+  hipError_t e = hipSuccess;
+  const bool e4m3 = cache->type == FA_CACHE_E4M3;
+  if (w.many)
+    e = forms ? fa::launch_paged_many_forms(p, w.m, cache->d_qk, e4m3, stream) : fa::launch_paged_many(p, w.m, cache->d_qk, e4m3, stream);
+  if (e == hipSuccess && w.few)
+    e = forms ? fa::launch_paged_few_forms(p, cache->d_qk, e4m3, w.col_blocks, stream)
+              : fa::launch_paged_few(p, cache->d_qk, e4m3, w.col_blocks, stream_kv, stream);
+  const bool few_joins = w.few && !w.whole;
+  if (e == hipSuccess && (few_joins || w.m.split))
+    e = fa::launch_paged_join(p, cache->d_v, few_joins ? cols : 0, w.m.split ? w.m.cols : 0, stream);
+  return e == hipSuccess ? FA_OK : FA_ERR_HIP;
 }
 
 }  // namespace
@@ -588,80 +698,26 @@ fa_status_t fa_kv_copy(const fa_paged_cache_t* cache, const int* src, const int*
 
 size_t fa_fwd_paged_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q,
                                     int path) {
-  if (B <= 0 || T <= 0 || max_keys < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_q < 0 || !dims_supported(d_qk, d_v) ||
-      (type != FA_CACHE_BF16 && type != FA_CACHE_E4M3) || path < FA_PAGED_AUTO || path > FA_PAGED_MANY)
-    return 0;
-  return static_cast<size_t>(paged_plan(B, T, max_keys, Hkv, Hq / Hkv, d_qk, d_v, type, max_q, path).bytes);
+  return workspace_bytes(B, T, max_keys, Hq, Hkv, d_qk, d_v, type, max_q, path, false);
+}
+
+size_t fa_fwd_paged_ex_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv, int d_qk, int d_v, int type, int max_q,
+                                       int path) {
+  const size_t none = workspace_bytes(B, T, max_keys, Hq, Hkv, d_qk, d_v, type, max_q, path, false);
+  const size_t with = workspace_bytes(B, T, max_keys, Hq, Hkv, d_qk, d_v, type, max_q, path, true);
+  return none > with ? none : with;
 }
 
 fa_status_t fa_fwd_paged(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* Q, void* O, float* LSE,
                          int Hq, const long long* strides, int max_q, int path, float scale, int causal, void* workspace,
                          size_t workspace_bytes, hipStream_t stream) {
-  if (cache == nullptr || batch == nullptr || strides == nullptr) return FA_ERR_NULL_POINTER;
-  fa_status_t st = check_paged_shape(cache, batch, Hq);
-  if (st != FA_OK) return st;
-  if (max_q < 0) return FA_ERR_BAD_SHAPE;
-  if (Hq > 0) {
-    // The kernel's line of work is counted in 32 bits.
-    const int64_t blocks = (static_cast<int64_t>(batch->T) * (Hq / cache->Hkv) / 32 + batch->B) * cache->Hkv;  // < 2^58
-    const int64_t tiles = static_cast<int64_t>(batch->max_blocks) * cache->page_size / 128 + 2;
-    if (blocks > INT_MAX / tiles) return FA_ERR_BAD_SHAPE;
-    if (path == FA_PAGED_MANY && !many_fits(batch->B, batch->T, cache->Hkv, Hq / cache->Hkv)) return FA_ERR_BAD_SHAPE;
-  }
-  st = check_paged_support(cache);
-  if (st != FA_OK) return st;
-  if (path < FA_PAGED_AUTO || path > FA_PAGED_MANY) return FA_ERR_UNSUPPORTED;
-  if (batch->T == 0 || batch->B == 0 || Hq == 0) return FA_OK;
-  if (!paged_pointers(cache, batch) || Q == nullptr || O == nullptr) return FA_ERR_NULL_POINTER;
-  if (!isfinite(scale)) return FA_ERR_BAD_SCALE;
-  const double c = static_cast<double>(scale) * 1.4426950408889634074;
-  if (fabs(c) > FLT_MAX) return FA_ERR_BAD_SCALE;
-  if (!paged_aligned(cache, batch) || !aligned(Q, 16) || !aligned(O, 16) || !aligned(LSE, 4) || !token_strides(strides, 4))
-    return FA_ERR_UNSUPPORTED;
-  st = check_paged_strides(cache, false);
-  if (st != FA_OK) return st;
-  const PagedPlan w = paged_plan(batch->B, batch->T, batch->max_blocks * cache->page_size, cache->Hkv, Hq / cache->Hkv,
-                                 cache->d_qk, cache->d_v, cache->type, max_q, path);
-  if (w.bytes > 0 && (workspace == nullptr || workspace_bytes < static_cast<size_t>(w.bytes))) return FA_ERR_WORKSPACE;
-  if (!aligned(workspace, 16)) return FA_ERR_UNSUPPORTED;
+  return attend(cache, batch, nullptr, Q, O, LSE, Hq, strides, max_q, path, scale, causal, workspace, workspace_bytes, stream);
+}
 
-  fa::PagedParams p{};
-  paged_view(cache, batch, &p.c, &p.bt);
-  p.q = static_cast<const uint16_t*>(Q);
-  p.o = static_cast<uint16_t*>(O);
-  p.lse = LSE;
-  p.q_token = strides[0], p.q_head = strides[1], p.o_token = strides[2], p.o_head = strides[3];
-  p.hq = Hq;
-  p.group = Hq / cache->Hkv;
-  p.causal = causal != 0;
-  const float cmag = fabs(c) < FLT_MIN ? FLT_MIN : static_cast<float>(fabs(c));  // a masked score stays infinite
-  p.cs = c < 0 ? -cmag : cmag;
-  p.few_cols = w.few_cols;
-  p.many_work = w.many_work;
-  p.n_wg = w.n_wg;
-  p.part_cols = w.cols;
-  p.whole = w.whole;
-  p.many_wg = w.m.n_wg;
-  p.many_cols = w.m.cols;
-  unsigned char* ws = static_cast<unsigned char*>(workspace);
-  p.o_part = reinterpret_cast<float*>(ws);
-  p.lse_part = reinterpret_cast<float*>(ws + w.lse);
-  p.desc = reinterpret_cast<fa::PagedItem*>(ws + w.desc);
-  p.many_o = reinterpret_cast<float*>(ws + w.many_o);
-  p.many_lse = reinterpret_cast<float*>(ws + w.many_lse);
-  p.many_desc = reinterpret_cast<fa::PagedItem*>(ws + w.many_desc);
-  // A single item per sequence and head reads K and V once: they are then loaded past the caches.
-  const bool stream_kv = w.usual <= 32 * w.col_blocks;
-  // Beside the kernel for many rows the others are mostly single tokens.
-  const int64_t usual = w.many ? p.group : w.usual;
-  const int cols = usual < w.cols ? static_cast<int>(usual) : w.cols;
-  hipError_t e = hipSuccess;
-  if (w.many) e = fa::launch_paged_many(p, w.m, cache->d_qk, cache->type == FA_CACHE_E4M3, stream);
-  if (e == hipSuccess && w.few) e = fa::launch_paged_few(p, cache->d_qk, cache->type == FA_CACHE_E4M3, w.col_blocks, stream_kv, stream);
-  const bool few_joins = w.few && !w.whole;
-  if (e == hipSuccess && (few_joins || w.m.split))
-    e = fa::launch_paged_join(p, cache->d_v, few_joins ? cols : 0, w.m.split ? w.m.cols : 0, stream);
-  return e == hipSuccess ? FA_OK : FA_ERR_HIP;
+fa_status_t fa_fwd_paged_ex(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const fa_paged_scores_t* scores,
+                            const void* Q, void* O, float* LSE, int Hq, const long long* strides, int max_q, int path,
+                            float scale, int causal, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return attend(cache, batch, scores, Q, O, LSE, Hq, strides, max_q, path, scale, causal, workspace, workspace_bytes, stream);
 }
 
 fa_status_t fa_fwd_ex(const void* Q, const void* K, const void* V, void* O, float* LSE, int B, int Hq, int Hkv,

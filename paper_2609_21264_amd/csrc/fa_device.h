@@ -21,6 +21,7 @@ typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 constexpr int kNumXcd = 8;
 constexpr int kCusPerXcd = 32;
 constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // Row order of a 32-key block in the score product's A operand: A-row i holds key perm32(i).
 // With the 32x32 accumulator layout (register r of a lane in half h holds A-row

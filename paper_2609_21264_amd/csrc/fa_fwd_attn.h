@@ -8,6 +8,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fa_device.h"
 #include "fa_e4m3.h"
 #include "fa_fastdiv.h"
@@ -129,7 +131,7 @@ struct Ring {
 // K and V fragments read ahead from LDS (KPF, VPF), K and V ring slots in LDS (NKR, NVR), and the
 // parts each key tile is split into between the waves (KSPLIT).
 template <int DQK_, int DV_, int BN_, int NWAVES_, int QB_, bool CAUSAL_, bool SPLIT_, int OCC_, int KPF_, int VPF_,
-          int NKR_, int NVR_, int KSPLIT_ = 1, bool PAGED_ = false, bool E4M3_ = false>
+          int NKR_, int NVR_, int KSPLIT_ = 1, bool PAGED_ = false, bool E4M3_ = false, bool FORM_ = false>
 struct Cfg {
   static constexpr int DQK = DQK_, DV = DV_, BN = BN_, NWAVES = NWAVES_, QB = QB_;
   // KSPLIT = 2: the waves form two sets of NWAVES / 2 (RWAVES) that own the same query rows; set k
@@ -145,6 +147,9 @@ struct Cfg {
   // PAGED: the keys lie in pages (PagedKeys below), the columns of a wave are any rows of any of the group's heads,
   // and the last key each of them sees is in a register.
   static constexpr bool PAGED = PAGED_;
+  // FORM: scores may be capped or biased by distance, and keys hidden otherwise than by a last one (FormKeys, which the paged
+  // kernel defines).
+  static constexpr bool FORM = FORM_;
   // E4M3: K and V tiles are 8-bit. They stay so in LDS and are widened as fragments are read: K to bf16, V to fp16, with
   // P in fp16 too. The order of the dims in a score product follows the 16-byte reads of K: k-steps 2 m and 2 m + 1
   // take dims 32 m + 16 h + 0 .. 7 and + 8 .. 15 in lane half h.
@@ -215,7 +220,10 @@ struct PagedKeys<true, QB> {
 // O / l is invariant under the choice of reference, and l >= 1 since the reference is always a
 // score that has been seen.
 template <class C>
-struct Attn : PagedKeys<C::PAGED, C::QB> {
+struct FormKeys;
+struct NoForms {};
+template <class C>
+struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM, FormKeys<C>, NoForms> {
   static constexpr int DQK = C::DQK, DV = C::DV, BN = C::WBN, QB = C::QB;  // BN: this wave's keys of a tile
   static constexpr int KS = DQK / 16;  // k-steps of the score product
   static constexpr int KB = BN / 32;   // 32-key blocks per tile
@@ -353,6 +361,22 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
       for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kb][qb][r] * cs);
     return half_swap_max(m);
   }
+  // The same of mul * score, multiplied last.
+  __device__ __forceinline__ float row_max_times(const Scores& s, int qb, float mul) const {
+    float m = s[0][qb][0];
+    if (mul >= 0.f) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kb][qb][r]);
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m = fminf(m, s[kb][qb][r]);
+    }
+    return half_swap_max(m * mul);
+  }
 
   // Element schedule of the step: the NEL = 2 * NEP exponentials of a tile are spread
   // one by one over the NSL MFMA slots (element e in slot e * NSL / NEL), each as one fma and one
@@ -380,10 +404,10 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
     return true;
   }
 
-  // Element e of a tile: p = 2^(cs * s - m_ref).
-  __device__ __forceinline__ float exp_elem(int e, const Scores& cur, const float (&mref)[QB]) const {
+  // Element e of a tile: p = 2^(mul * s - m_ref), mul = cs (1 where the scores are final values).
+  __device__ __forceinline__ float exp_elem(int e, const Scores& cur, const float (&mref)[QB], float mul) const {
     const int u = e >> 1, qb = u % QB, rp = (u / QB) % 8, kb = u / (QB * 8);
-    float x = __builtin_amdgcn_exp2f(fmaf(cur[kb][qb][2 * rp + (e & 1)], cs, -mref[qb]));
+    float x = __builtin_amdgcn_exp2f(fmaf(cur[kb][qb][2 * rp + (e & 1)], mul, -mref[qb]));
     asm volatile("" : "+v"(x));
     return x;
   }
@@ -487,7 +511,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
     }
 #pragma unroll
     for (int u = 0; u < NEP; ++u) {
-      const float e0 = exp_elem(2 * u, cur, mref), e1 = exp_elem(2 * u + 1, cur, mref);
+      const float e0 = exp_elem(2 * u, cur, mref, cs), e1 = exp_elem(2 * u + 1, cur, mref, cs);
       pack_pair(u, e0, e1, pk, rs);
     }
   }
@@ -500,7 +524,33 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
   __device__ __forceinline__ void step(Scores& cur, Scores& nxt, Probs& pk_new, const Probs& pk_old,
                                        const unsigned char* sKn, const unsigned char* sVo, bool masked, int n0,
                                        Issue&& issue) {
-    if (masked) mask_tile(cur, n0);
+    float mul = cs, alpha[QB];
+    bool rescale = false;
+    if constexpr (C::FORM) {
+      // With forms the maximum is computed for every tile: rows may see their first key in any, and a bias makes maxima rise.
+      // The reference follows where some row's has risen over it by more than 2^3 (in log2); O and the sums, which
+      // hold the tiles before this one only after the step, follow at its end.
+      mul = this->values(cur, n0, masked, cs, h, *this);
+      float mt[QB];
+      bool up = false;
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        mt[qb] = row_max_times(cur, qb, mul);
+        up = up || mt[qb] > m_run[qb] + 8.f;
+        alpha[qb] = 1.f;
+      }
+      rescale = __builtin_amdgcn_ballot_w64(up) != 0;
+      if (rescale) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const float m_new = fmaxf(m_run[qb], mt[qb]);
+          alpha[qb] = __builtin_amdgcn_exp2f(m_run[qb] - (m_new == -INFINITY ? 0.f : m_new));
+          m_run[qb] = m_new;
+        }
+      }
+    } else {
+      if (masked) mask_tile(cur, n0);
+    }
     float mref[QB], rs[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
@@ -537,22 +587,37 @@ struct Attn : PagedKeys<C::PAGED, C::QB> {
           if (e & 1) pack_pair(e >> 1, ev[(e - 1) % 4], ev[e % 4], pk_new, rs);
       }
 #pragma unroll
-      for (int e = elem_begin(sl); e < elem_end(sl); ++e) ev[e % 4] = exp_elem(e, cur, mref);
+      for (int e = elem_begin(sl); e < elem_end(sl); ++e) ev[e % 4] = exp_elem(e, cur, mref, mul);
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
     for (int e = elem_begin(NSL - 1); e < elem_end(NSL - 1); ++e)
       if (e & 1) pack_pair(e >> 1, ev[(e - 1) % 4], ev[e % 4], pk_new, rs);
-    bool over = false;
+    if constexpr (C::FORM) {
+      if (rescale) {
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) over = over || !(rs[qb] <= C::OVERFLOW_SUM);
-    // Without pages that are not there a row that sees any key of its range sees the first, so it has a reference from
-    // tile 0 on; with them it takes one as soon as a tile has a key for it.
-    if constexpr (C::PAGED) {
+        for (int qb = 0; qb < QB; ++qb) {
+          l_run[qb] *= alpha[qb];
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) over = over || (this->holes && m_run[qb] == -INFINITY);
+          for (int db = 0; db < DB; ++db) {
+            agpr_fence<AG>(oacc[db][qb]);
+            oacc[db][qb] *= alpha[qb];
+            agpr_fence<AG>(oacc[db][qb]);
+          }
+        }
+      }
+    } else {
+      bool over = false;
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) over = over || !(rs[qb] <= C::OVERFLOW_SUM);
+      // Without pages that are not there a row that sees any key of its range sees the first, so it has a reference from
+      // tile 0 on; with them it takes one as soon as a tile has a key for it.
+      if constexpr (C::PAGED) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) over = over || (this->holes && m_run[qb] == -INFINITY);
+      }
+      if (__builtin_amdgcn_ballot_w64(over) != 0) rebase(pk_new, rs, n0, masked);
     }
-    if (__builtin_amdgcn_ballot_w64(over) != 0) rebase(pk_new, rs, n0, masked);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) l_run[qb] += rs[qb];
   }

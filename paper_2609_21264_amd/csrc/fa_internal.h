@@ -194,6 +194,18 @@ struct PagedItem {
   int pad[2];
 };
 
+// How scores are changed and keys hidden, beyond causal masking (fa_paged_scores_t).
+struct PagedForms {
+  float cap_a, cap_r;        // cap * log2(e), 2 / cap; 0: no cap
+  const float* slopes;       // [Hq] or nullptr
+  const int* prefix_lens;    // [n_seq] or nullptr
+  const uint32_t* mask;      // [n_tokens], rows mask_stride apart: the new tokens that a token sees; or nullptr
+  int64_t mask_stride;
+  int mask_words;
+  int window;                // 0: none; below 2^30
+  int causal;                // PagedParams::causal
+};
+
 struct PagedParams {
   PagedCache c;
   PagedBatch bt;
@@ -222,6 +234,7 @@ struct PagedParams {
   float* many_lse;       // fp32 [2 * many_wg][many_place_cols(many_cols)]
   PagedItem* many_desc;  // [many_wg]
   uint32_t m_group, sh_group;  // division by group, filled by the launchers
+  PagedForms f;            // used by the kernels with forms alone
 };
 
 // ---- rotation alone (fa_rotate_kernel.hip) --------------------------------------------------------
@@ -301,7 +314,11 @@ struct PagedMany {
   int cols, n_wg;
   int64_t blocks;
 };
-PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3);
+PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3,
+                     bool forms);
 hipError_t launch_paged_many(PagedParams p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream);
+// The same kernels with forms (fa_paged_forms_few_kernel.hip, fa_paged_forms_many_kernel.hip).
+hipError_t launch_paged_few_forms(PagedParams p, int d_qk, bool fp8, int col_blocks, hipStream_t stream);
+hipError_t launch_paged_many_forms(PagedParams p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream);
 
 }  // namespace fa

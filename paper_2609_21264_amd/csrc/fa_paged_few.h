@@ -45,8 +45,9 @@ constexpr int kItemCost = 1;  // fixed cost of an item in tiles
 constexpr int kMinUnits = 2;  // least work of a workgroup: one token over 1 023 keys 12.0 us with 2, 15.6 with 4
 constexpr float kRise = 8.f;  // how far (log2) a maximum may rise over its reference
 
-template <int DQK_, int DV_, bool FP8_, int QB_, bool STREAM_, int SLOTS_>
+template <int DQK_, int DV_, bool FP8_, int QB_, bool STREAM_, int SLOTS_, bool FORM_ = false>
 struct FewCfg {
+  static constexpr bool FORM = FORM_;                           // scores and masks by p.f
   static constexpr int QB = QB_, COLS = 32 * QB_;               // 32-column MFMA blocks per wave, columns of an item
   static constexpr bool STREAM = STREAM_;                       // K and V loaded past the caches
   static constexpr int DQK = DQK_, DV = DV_, NW = 4, SLOTS = SLOTS_;
@@ -77,13 +78,16 @@ __device__ __forceinline__ void load_q16(bf16x8& r, const void* ptr) {
 __device__ __forceinline__ void q_settled(bf16x8& r) { asm volatile("" : "+v"(r)); }
 
 // Units of a sequence on the line of work, and what they are made of. Where items are taken whole every item is one unit.
-template <int TILE, int COLS>
+template <int TILE, int COLS, bool FORM>
 struct SeqWork {
   int tiles, cost, n_cb;
   uint32_t units;  // below 2^31 by the host's check
   __device__ __forceinline__ SeqWork(const PagedSeq& s, const PagedParams& p, int few_cols) {
     const int64_t cols = (int64_t)s.n_q * p.group;
-    tiles = (s.kv + TILE - 1) / TILE;
+    if constexpr (FORM)
+      tiles = SeenTiles<TILE>(p.f, s, 0, s.n_q - 1).n;
+    else
+      tiles = (s.kv + TILE - 1) / TILE;
     cost = kItemCost + (p.whole ? 0 : tiles);
     n_cb = cols > few_cols ? 0 : (int)((cols + COLS - 1) / COLS);
     units = (uint32_t)n_cb * (uint32_t)p.c.hkv * (uint32_t)cost;
@@ -95,7 +99,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(C::NW * 64, C::NW * 64)))
 void fa_paged_few_kernel(PagedParams p) {
   constexpr int DQK = C::DQK, DV = C::DV, KS = C::KS, DB = C::DB, NW = C::NW, TILE = C::TILE, D = C::D;
   constexpr int QB = C::QB, COLS = C::COLS;
-  constexpr bool FP8 = C::FP8;
+  constexpr bool FP8 = C::FP8, FORM = C::FORM;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS_BYTES];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -105,14 +109,14 @@ void fa_paged_few_kernel(PagedParams p) {
   // The line's length, and the sequence that holds this workgroup's first unit (every wave for itself). The first 64
   // sequences stay in registers, one per lane.
   PagedSeq sl{};
-  if (lane < p.bt.n_seq) sl = load_seq_lane(p.bt, lane);
+  if (lane < p.bt.n_seq) sl = load_seq_lane<FORM>(p, lane);
   int few_cols = p.few_cols;
-  if (few_cols != INT32_MAX && big_work(p, sl, lane) < p.many_work) few_cols = INT32_MAX;  // all sequences run here
-  uint32_t mine = SeqWork<TILE, COLS>(sl, p, few_cols).units, incl = wave_scan(mine);
+  if (few_cols != INT32_MAX && big_work<FORM>(p, sl, lane) < p.many_work) few_cols = INT32_MAX;  // all sequences run here
+  uint32_t mine = SeqWork<TILE, COLS, FORM>(sl, p, few_cols).units, incl = wave_scan(mine);
   uint32_t sum = lane_of(incl, 63);
   if (p.bt.n_seq > 64) {
     uint32_t rest = 0;
-    for (int c = 64 + lane; c < p.bt.n_seq; c += 64) rest = add_sat(rest, SeqWork<TILE, COLS>(load_seq_lane(p.bt, c), p, few_cols).units);
+    for (int c = 64 + lane; c < p.bt.n_seq; c += 64) rest = add_sat(rest, SeqWork<TILE, COLS, FORM>(load_seq_lane<FORM>(p, c), p, few_cols).units);
     sum = add_sat(sum, wave_sum(rest));
   }
   const int total = uniform((int)min(sum, (uint32_t)INT32_MAX));
@@ -134,8 +138,8 @@ void fa_paged_few_kernel(PagedParams p) {
     b += 64;
     if (b >= p.bt.n_seq) return;  // not reached: r0 < total
     sl = PagedSeq{};
-    if (b + lane < p.bt.n_seq) sl = load_seq_lane(p.bt, b + lane);
-    mine = SeqWork<TILE, COLS>(sl, p, few_cols).units;
+    if (b + lane < p.bt.n_seq) sl = load_seq_lane<FORM>(p, b + lane);
+    mine = SeqWork<TILE, COLS, FORM>(sl, p, few_cols).units;
     incl = wave_scan(mine);
   }
 
@@ -164,15 +168,15 @@ void fa_paged_few_kernel(PagedParams p) {
   const int v_half = (lane & 1) * 8;
 
   int r = r0;
-  PagedSeq s{uniform(sl.q0), uniform(sl.q_end), uniform(sl.n_q), uniform(sl.kv)};
+  PagedSeq s{uniform(sl.q0), uniform(sl.q_end), uniform(sl.n_q), uniform(sl.kv), uniform(sl.pre)};
   b = uniform(b), start = uniform(start);
   while (r < r1) {
-    SeqWork<TILE, COLS> sw(s, p, few_cols);
+    SeqWork<TILE, COLS, FORM> sw(s, p, few_cols);
     while (sw.units == 0 || (uint32_t)(r - start) >= sw.units) {
       start += (int)sw.units;
       if (++b >= p.bt.n_seq) return;  // not reached: r < total
-      s = load_seq(p.bt, b);
-      sw = SeqWork<TILE, COLS>(s, p, few_cols);
+      s = load_seq<FORM>(p, b);
+      sw = SeqWork<TILE, COLS, FORM>(s, p, few_cols);
     }
     const int cost = sw.cost;
     const int item = uniform((int)((uint32_t)(r - start) / (uint32_t)cost)), item0 = start + item * cost;
@@ -197,12 +201,18 @@ void fa_paged_few_kernel(PagedParams p) {
     // Columns of this lane, one per 32-column block. Columns past the item's rows repeat the last and are never stored.
     const int cols = s.n_q * p.group, c0 = cb * COLS;
     int last_key[QB];
+    SeenRow row[QB];
+    float slope[QB];  // times log2(e)
     bf16x8 qf[QB][KS];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const int c = min(c0 + 32 * qb + i32, cols - 1);
       const int qi = (int)fast_div((uint32_t)c, p.m_group, p.sh_group), member = c - qi * p.group;
       last_key[qb] = p.causal ? s.kv - s.n_q + qi : s.kv - 1;
+      if constexpr (FORM) {
+        row[qb].init(p.f, s, qi);
+        slope[qb] = p.f.slopes != nullptr ? p.f.slopes[g * p.group + member] * kLog2e : 0.f;
+      }
       const uint16_t* qp = p.q + (int64_t)(s.q0 + qi) * p.q_token + (int64_t)(g * p.group + member) * p.q_head;
       // bf16: k-step ks holds dims 16 ks + 8 h .. + 7. e4m3: a lane reads 16 bytes of K at once, dims 32 m +
       // 16 h .. + 15, which serve k-steps 2 m and 2 m + 1; Q takes the same order.
@@ -212,8 +222,15 @@ void fa_paged_few_kernel(PagedParams p) {
     }
     // Keys visible to the block's last row; tiles behind them are left out.
     const int last_row = (int)fast_div((uint32_t)min(c0 + COLS - 1, cols - 1), p.m_group, p.sh_group);
-    const int k_end = p.causal ? max(0, s.kv - s.n_q + last_row + 1) : s.kv;
-    const int nt = max(0, min(t1, (k_end + TILE - 1) / TILE) - t0);
+    int k_end = p.causal ? max(0, s.kv - s.n_q + last_row + 1) : s.kv;
+    int nt = max(0, min(t1, (k_end + TILE - 1) / TILE) - t0);
+    // With forms: the sequence's tiles (those of all its rows), and what this block's rows see of them.
+    const SeenTiles<TILE> seen(p.f, s, 0, s.n_q - 1);
+    auto tile_of = [&](int t) { return FORM ? seen.tile(t) : t; };
+    if constexpr (FORM) {
+      k_end = SeenTiles<TILE>(p.f, s, 0, last_row).end;
+      nt = max(0, min(t1, seen.before((k_end + TILE - 1) / TILE)) - t0);
+    }
 
     const unsigned char* kbase = static_cast<const unsigned char*>(p.c.k) + (int64_t)g * p.c.k_head * C::E;
     const unsigned char* vbase = static_cast<const unsigned char*>(p.c.v) + (int64_t)g * p.c.v_head * C::E;
@@ -221,7 +238,7 @@ void fa_paged_few_kernel(PagedParams p) {
     const int smask = (1 << p.c.page_shift) - 1;
     // The pages of this wave's two halves of tile t (an index past the sequence's last page repeats that).
     auto page_of = [&](int t, int u) {
-      const int key = min(t * TILE + 32 * wave + 16 * u, s.kv - 1);
+      const int key = min(tile_of(t) * TILE + 32 * wave + 16 * u, s.kv - 1);
       return key < 0 ? -1 : scalar_load(table + (key >> p.c.page_shift));
     };
     // Buffer over the slots of a half that hold keys below k_end: none where the page is none of the cache's.
@@ -236,7 +253,7 @@ void fa_paged_few_kernel(PagedParams p) {
     };
     auto issue = [&](int t, int pg0, int pg1) {
       const uint32_t l = (uint32_t)uniform((int)(ring_lds + (uint32_t)((unsigned)t % C::SLOTS) * C::WSLOT));
-      const int key0 = t * TILE + 32 * wave;
+      const int key0 = tile_of(t) * TILE + 32 * wave;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const u32x4 rs = half_rsrc(kbase, p.c.k_page, p.c.k_slot, u ? pg1 : pg0, key0 + 16 * u);
@@ -256,7 +273,8 @@ void fa_paged_few_kernel(PagedParams p) {
       return (uint32_t)(pg0 >= 0 && pg0 < p.c.n_pages) | (uint32_t)(pg1 >= 0 && pg1 < p.c.n_pages) << 1;
     };
 
-    const float cs = p.cs * (FP8 && p.c.k_scale != nullptr ? scalar_load(p.c.k_scale + g) : 1.f);
+    const float ks = FP8 && p.c.k_scale != nullptr ? scalar_load(p.c.k_scale + g) : 1.f;
+    const float cs = p.cs * ks, cap_b = FORM ? cap_factor(p.f, cs) : 0.f;
     f32x16 oacc[DB][QB];
     float m_run[QB], l_run[QB];
 #pragma unroll
@@ -290,7 +308,7 @@ void fa_paged_few_kernel(PagedParams p) {
       compiler_fence();
       const unsigned char* sK = ring + ((unsigned)t % C::SLOTS) * C::WSLOT;
       const unsigned char* sV = sK + C::K_BYTES;
-      const int n0 = t * TILE + 32 * wave;
+      const int n0 = tile_of(t) * TILE + 32 * wave;
 
       // Scores: register r holds key n0 + 16 (r / 8) + 8 h + r % 8 of column i32 (of block qb).
       f32x16 sc[QB];
@@ -324,11 +342,33 @@ void fa_paged_few_kernel(PagedParams p) {
         const int lim = last_key[qb] - n0 - 8 * h;
         const int lim0 = there0 ? lim : -1, lim1 = there1 ? lim : -1;
         float mt = -INFINITY;
+        if constexpr (FORM) {
+          if (p.f.cap_a != 0.f) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float x = (16 * (e >> 3) + (e & 7)) > (e < 8 ? lim0 : lim1) ? -INFINITY : sc[qb][e] * cs;
-          sc[qb][e] = x;
-          mt = fmaxf(mt, x);
+            for (int e = 0; e < 16; ++e) sc[qb][e] = capped(sc[qb][e], p.f.cap_a, cap_b);
+          } else {
+            sc[qb] *= cs;
+          }
+          if (p.f.slopes != nullptr) {
+            const float far = (float)(row[qb].pos - n0 - 8 * h);  // from the lane's first key
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[qb][e] -= slope[qb] * fabsf(far - (float)(16 * (e >> 3) + (e & 7)));
+          }
+          const uint32_t held = (there0 ? 0xffffu : 0u) | (there1 ? 0xffff0000u : 0u);
+          const uint32_t v = (seen_bits(p.f, s, row[qb], n0) & held) >> (8 * h);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float x = (v >> (16 * (e >> 3) + (e & 7))) & 1u ? sc[qb][e] : -INFINITY;
+            sc[qb][e] = x;
+            mt = fmaxf(mt, x);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float x = (16 * (e >> 3) + (e & 7)) > (e < 8 ? lim0 : lim1) ? -INFINITY : sc[qb][e] * cs;
+            sc[qb][e] = x;
+            mt = fmaxf(mt, x);
+          }
         }
         mt = half_swap_max(mt);
         // The reference follows the maximum only where some column's has risen over it by more than 8 (P then stays
@@ -464,10 +504,10 @@ void fa_paged_few_kernel(PagedParams p) {
 
 // Instances by head dimensions, cache type and 32-column blocks; as many ring slots as leave two workgroups to a CU
 // where the waves' join fits in 80 KiB of LDS, else one.
-template <int DQK, int DV, bool FP8, int QB, bool STREAM>
+template <int DQK, int DV, bool FP8, int QB, bool STREAM, bool FORM = false>
 struct FewInstance {
   static constexpr int kSlots = FP8 && (QB == 2 || DQK == 64) ? 4 : 2;
-  using C = FewCfg<DQK, DV, FP8, QB, STREAM, kSlots>;
+  using C = FewCfg<DQK, DV, FP8, QB, STREAM, kSlots, FORM>;
   static constexpr int kWorkgroups = C::LDS_BYTES <= 81920 ? 512 : 256;
 };
 
@@ -476,6 +516,16 @@ hipError_t launch_few(PagedParams p, hipStream_t stream) {
   void* args[] = {&p};
   return hipLaunchKernel(reinterpret_cast<const void*>(&fa_paged_few_kernel<C>), dim3(p.n_wg), dim3(C::NW * 64), args, 0,
                          stream);
+}
+
+// What the launchers fill in.
+inline void few_constants(PagedParams& p) {
+  p.min_units = kMinUnits;
+  p.wg_log = 0;
+  while ((1 << p.wg_log) < p.n_wg) ++p.wg_log;
+  const FastDiv fg = make_fastdiv(p.group);
+  p.m_group = fg.m;
+  p.sh_group = fg.sh;
 }
 
 }  // namespace

@@ -8,12 +8,6 @@
 namespace fa {
 namespace {
 
-template <class C>
-hipError_t launch_many(PagedParams p, int64_t blocks, hipStream_t stream) {
-  void* args[] = {&p};
-  const dim3 grid((unsigned)(C::SPLIT ? p.many_wg : blocks * p.c.hkv));
-  return hipLaunchKernel(reinterpret_cast<const void*>(&fa_paged_fwd_kernel<C>), grid, dim3(C::NT), args, 0, stream);
-}
 // Where there is a short instance, the long one runs only grids that fill the chip (paged_many): it is never split.
 template <int DQK, int DV, bool E4M3, bool SHORT>
 hipError_t launch_many_split(const PagedParams& p, const PagedMany& m, hipStream_t stream) {
@@ -25,7 +19,8 @@ hipError_t launch_many_split(const PagedParams& p, const PagedMany& m, hipStream
 
 }  // namespace
 
-PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3) {
+PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3,
+                     bool forms) {
   PagedMany m{};
   const int64_t rows = (int64_t)n_tokens * group;
   int64_t seqs = rows / (few_cols + 1);
@@ -35,7 +30,8 @@ PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, 
   // 22.3 : 17.1 us, 2048 x 2048 (256 long blocks) 56.6 : 51.2, 4096 x 4096 (512) 133 : 143, 2048 x 8192 219 : 228; d = 64 16/16
   // 2048 x 2048 48.0 : 28.4, 4096 x 4096 87.1 : 55.8, 3 x 4096 x 4096 (768) 155 : 144.
   const int64_t fill = d_qk == 64 ? 1024 : 512;
-  m.is_short = !e4m3 && d_qk != 192 && ((int64_t)max_q * group <= 128 || (rows / 256 + seqs) * hkv < fill);
+  // With forms always: masks and changed scores are computed beside the matrix instructions of the other wave of a SIMD.
+  m.is_short = !e4m3 && d_qk != 192 && (forms || (int64_t)max_q * group <= 128 || (rows / 256 + seqs) * hkv < fill);
   m.cols = m.is_short ? 128 : 256;
   m.n_wg = m.is_short || (d_qk == 64 && !e4m3) ? 512 : 256;
   // The most blocks that the packed tokens can make: whole ones, and a last one for each sequence of this kernel.
@@ -51,12 +47,7 @@ PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, 
 }
 
 hipError_t launch_paged_many(PagedParams p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream) {
-  const FastDiv fg = make_fastdiv(p.group);
-  p.m_group = fg.m;
-  p.sh_group = fg.sh;
-  p.many_min_units = kBlockCost + 4;
-  p.many_log = 0;
-  while ((1 << p.many_log) < p.many_wg) ++p.many_log;
+  many_constants(p);
   if (e4m3) {
     if (d_qk == 64) return launch_many_split<64, 64, true, false>(p, m, stream);
     if (d_qk == 128) return launch_many_split<128, 128, true, false>(p, m, stream);

@@ -305,12 +305,7 @@ hipError_t launch_few_dims(PagedParams p, int d_qk, bool fp8, hipStream_t stream
 }
 
 hipError_t launch_paged_few(PagedParams p, int d_qk, bool fp8, int col_blocks, bool stream_kv, hipStream_t stream) {
-  p.min_units = kMinUnits;
-  p.wg_log = 0;
-  while ((1 << p.wg_log) < p.n_wg) ++p.wg_log;
-  const FastDiv fg = make_fastdiv(p.group);
-  p.m_group = fg.m;
-  p.sh_group = fg.sh;
+  few_constants(p);
   if (col_blocks == 1) return launch_few_dims<1, true>(p, d_qk, fp8, stream);
   return stream_kv ? launch_few_dims<2, true>(p, d_qk, fp8, stream) : launch_few_dims<2, false>(p, d_qk, fp8, stream);
 }

@@ -84,11 +84,127 @@ struct PagedLoader {
   }
 };
 
+// The kernel's parameters read anew from where they were passed: what few tiles need is not kept in scalar registers over the
+// loop, of which the step and the loads leave none.
+__device__ __forceinline__ const __attribute__((address_space(4))) PagedParams& fresh_params() {
+  auto p = (const __attribute__((address_space(4))) PagedParams*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *p;
+}
+template <bool FORM>
+__device__ __forceinline__ std::conditional_t<FORM, PagedParams, const PagedParams&> reread(const PagedParams& p) {
+  if constexpr (FORM) {
+    PagedParams q;
+    __builtin_memcpy(&q, (const void*)&fresh_params(), sizeof(q));
+    return q;
+  } else {
+    return p;
+  }
+}
+__device__ __forceinline__ PagedForms fresh_forms() {
+  const auto& f = fresh_params().f;
+  return PagedForms{f.cap_a, f.cap_r, f.slopes, f.prefix_lens, f.mask, f.mask_stride, f.mask_words, f.window, f.causal};
+}
+
+// The lane's number without a register that holds it meanwhile.
+__device__ __forceinline__ int lane_anew() {
+  uint32_t all = ~0u;
+  asm volatile("" : "+s"(all));
+  return (int)__builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0u));
+}
+
+// The state of a wave with forms. Scores are raw until values() makes them final (in units of log2, hidden keys -inf), which
+// it does where a tile hides keys from some row, or where scores are capped or biased; else the step multiplies them.
+template <class C>
+struct FormKeys {
+  static constexpr int BN = C::WBN, QB = C::QB, KB = BN / 32;
+  PagedSeq seq;
+  int row[QB];          // of the sequence's new tokens
+  float slope[QB];      // times log2(e)
+  int whole0, whole1;   // every row of the block sees the keys from whole0 to before whole1
+  bool final_always, last_first;
+  __device__ __forceinline__ void init_row(const PagedParams& p, int qb, int r, int head) {
+    row[qb] = r;
+    slope[qb] = p.f.slopes != nullptr ? p.f.slopes[head] * kLog2e : 0.f;
+  }
+  __device__ __forceinline__ void init_block(const PagedParams& p, const PagedSeq& s, int row0, int row1) {
+    SeenRow first, last;
+    first.init(p.f, s, row0);
+    last.init(p.f, s, row1);
+    whole0 = last.first, whole1 = first.last + 1;
+    seq = s;
+    final_always = p.f.cap_a != 0.f || p.f.slopes != nullptr;
+  }
+  // Whether the tile at key n0 hides a key from some row.
+  __device__ __forceinline__ bool hides(int n0) const {
+    return !((n0 >= whole0 && n0 + BN <= whole1) || n0 + BN <= seq.pre);
+  }
+  // Keys of the 32 from n0 on that the column sees, in pages that are there.
+  __device__ __forceinline__ uint32_t bits(const PagedForms& f, int qb, int n0, const PagedKeys<true, QB>& pages) const {
+    SeenRow r;
+    r.init(f, seq, row[qb]);
+    uint32_t v = seen_bits(f, seq, r, n0);
+    if (pages.holes) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {  // 16 keys lie in one page
+        const int key = n0 + 16 * u, page = key < seq.kv ? pages.page_of(key) : 0;
+        if (page < 0 || page >= pages.n_pages) v &= u == 0 ? 0xffff0000u : 0x0000ffffu;
+      }
+    }
+    return v;
+  }
+  // Makes a tile's scores final where they have to be; what the step multiplies them by. h: the half of the wave; g: head of K.
+  template <class Scores>
+  __device__ __forceinline__ float values(Scores& s, int n0, bool masked, float cs, int h, const PagedKeys<true, QB>& pages) const {
+    if (!masked && !final_always) return cs;
+    const PagedForms f = fresh_forms();
+    if (f.cap_a != 0.f) {
+      const float b = cap_factor(f, cs);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][qb][r] = capped(s[kb][qb][r], f.cap_a, b);
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) s[kb][qb] *= cs;
+    }
+    if (f.slopes != nullptr) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const float far = (float)(seq.kv - seq.n_q + row[qb] - n0 - 32 * kb - 8 * h);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][qb][r] -= slope[qb] * fabsf(far - (float)(16 * (r >> 3) + (r & 7)));
+        }
+    }
+    if (masked) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const uint32_t v = bits(f, qb, n0 + 32 * kb, pages) >> (8 * h);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)v, 16 * (r >> 3) + (r & 7), 1);
+            s[kb][qb][r] = __uint_as_float((__float_as_uint(s[kb][qb][r]) & m) | (0xff800000u & ~m));
+          }
+        }
+    }
+    return 1.f;
+  }
+};
+
 // A block's place: which keys its columns see.
-template <int BN, int BC>
+template <int BN, int BC, bool FORM>
 struct Block {
   int cols, c0, row0, row1;  // row-heads of the item, the block's first, its first and last row
   int kv_end, plain;         // keys visible to its last row; leading tiles that need no mask for any row
+  int pre, gap;              // with forms: its tiles (SeenTiles)
   __device__ __forceinline__ Block(const PagedSeq& s, int cb, const PagedParams& p) {
     cols = s.n_q * p.group;
     c0 = cb * BC;
@@ -96,28 +212,35 @@ struct Block {
     row1 = (int)fast_div((uint32_t)min(c0 + BC, cols) - 1u, p.m_group, p.sh_group);
     kv_end = p.causal ? max(0, s.kv - s.n_q + row1 + 1) : s.kv;
     plain = (p.causal ? max(0, s.kv - s.n_q + row0 + 1) : s.kv) / BN;
+    pre = gap = 0;
+    if constexpr (FORM) {
+      const SeenTiles<BN> seen(p.f, s, row0, row1);
+      kv_end = seen.end, pre = seen.pre, gap = seen.gap;
+    }
   }
-  __device__ __forceinline__ int tiles() const { return (kv_end + BN - 1) / BN; }
+  __device__ __forceinline__ int tiles() const { return (kv_end + BN - 1) / BN - (FORM ? gap : 0); }
 };
 template <int BC>
 __device__ __forceinline__ int n_blocks(const PagedSeq& s, const PagedParams& p) {
   const int64_t cols = (int64_t)s.n_q * p.group;
   return cols > p.few_cols ? (int)((cols + BC - 1) / BC) : 0;
 }
-template <int BN, int BC>
+template <int BN, int BC, bool FORM>
 __device__ __forceinline__ int head_units(const PagedSeq& s, int n_cb, const PagedParams& p, int lane) {
   uint32_t sum = 0;
-  for (int c = lane; c < n_cb; c += 64) sum += (uint32_t)(kBlockCost + Block<BN, BC>(s, c, p).tiles());
+  for (int c = lane; c < n_cb; c += 64) sum += (uint32_t)(kBlockCost + Block<BN, BC, FORM>(s, c, p).tiles());
   return (int)wave_sum(sum);
 }
 template <class C>
 __global__ __attribute__((amdgpu_flat_work_group_size(C::NT, C::NT), amdgpu_waves_per_eu(C::WPE, C::WPE)))
-void fa_paged_fwd_kernel(PagedParams p) {
+void fa_paged_fwd_kernel(PagedParams args) {
+  const PagedParams& p = args;
   using A = Attn<C>;
   constexpr int DQK = C::DQK, DV = C::DV, BN = C::BN, QB = C::QB;
   constexpr int BC = C::NWAVES * 32 * QB;  // row-heads per block
   constexpr int R = BN / C::NWAVES;        // keys that a wave brings of a tile
   constexpr int E = C::E;
+  constexpr bool FORM = C::FORM;
   static_assert(C::KSPLIT == 1 && C::KA - C::VA <= 1, "a V tile is loaded with its K tile or one step later");
   static_assert(!C::SPLIT || BN == kSplitTile, "the host counts the line's units");
 
@@ -143,16 +266,16 @@ void fa_paged_fwd_kernel(PagedParams p) {
   }
   // The first 64 sequences stay in registers, one per lane; those behind them are read again for each use.
   PagedSeq first{};
-  if (lane < p.bt.n_seq) first = load_seq_lane(p.bt, lane);
+  if (lane < p.bt.n_seq) first = load_seq_lane<FORM>(p, lane);
   auto seqs_from = [&](int c) {
     PagedSeq x{};
     if (c == 0)
       x = first;
     else if (c + lane < p.bt.n_seq)
-      x = load_seq_lane(p.bt, c + lane);
+      x = load_seq_lane<FORM>(p, c + lane);
     return x;
   };
-  if (p.few_cols != 0 && big_work(p, first, lane) < p.many_work) return;  // all sequences run in the kernel for few rows
+  if (p.few_cols != 0 && big_work<FORM>(p, first, lane) < p.many_work) return;  // all sequences run in the kernel for few rows
   if constexpr (C::SPLIT) {
     uint32_t sum = 0;
     int longest = 0;
@@ -163,8 +286,8 @@ void fa_paged_fwd_kernel(PagedParams p) {
         const PagedSeq x = seq_of_lane(sl, __builtin_ctzll(left));
         left &= left - 1;
         const int n = n_blocks<BC>(x, p);
-        sum = add_sat(sum, (uint32_t)min((int64_t)head_units<BN, BC>(x, n, p, lane) * p.c.hkv, (int64_t)UINT32_MAX));
-        longest = max(longest, kBlockCost + Block<BN, BC>(x, n - 1, p).tiles());
+        sum = add_sat(sum, (uint32_t)min((int64_t)head_units<BN, BC, FORM>(x, n, p, lane) * p.c.hkv, (int64_t)UINT32_MAX));
+        longest = max(longest, kBlockCost + Block<BN, BC, FORM>(x, n - 1, p).tiles());
       }
     }
     total = uniform((int)min(sum, (uint32_t)INT32_MAX));
@@ -193,7 +316,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
         left &= left - 1;
         s = seq_of_lane(sl, l);
         n_cb = n_blocks<BC>(s, p);
-        const int units = head_units<BN, BC>(s, n_cb, p, lane);
+        const int units = head_units<BN, BC, FORM>(s, n_cb, p, lane);
         if ((int64_t)r < start + (int64_t)units * p.c.hkv) {
           b = c + l;
           g = uniform((int)((uint32_t)(r - start) / (uint32_t)units));
@@ -206,7 +329,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
     }
     if (!found) return;  // not reached: r < total
     for (int c = 0; c < n_cb; c += 64) {
-      const uint32_t u = c + lane < n_cb ? (uint32_t)(kBlockCost + Block<BN, BC>(s, c + lane, p).tiles()) : 0u;
+      const uint32_t u = c + lane < n_cb ? (uint32_t)(kBlockCost + Block<BN, BC, FORM>(s, c + lane, p).tiles()) : 0u;
       const uint32_t incl = wave_scan(u);
       const uint64_t above = __builtin_amdgcn_ballot_w64(incl > (uint32_t)(r - start));
       if (above != 0) {
@@ -240,7 +363,8 @@ void fa_paged_fwd_kernel(PagedParams p) {
   }
 
   while (true) {
-    const Block<BN, BC> blk(s, cb, p);
+    decltype(auto) p = reread<FORM>(args);
+    const Block<BN, BC, FORM> blk(s, cb, p);
     const int tiles = blk.tiles();
     int t0 = 0, nt = tiles, n_parts = 1, first_wg = me;
     bool skip = false;
@@ -260,7 +384,10 @@ void fa_paged_fwd_kernel(PagedParams p) {
     if (!skip) {
       // What follows from the lane is computed for each block anew (and again for its output): kept over the loop,
       // the addresses would not fit in the registers beside the step.
-      if constexpr (C::SPLIT) asm volatile("" : "+v"(lane));
+      if constexpr (FORM)
+        lane = lane_anew();
+      else if constexpr (C::SPLIT)
+        asm volatile("" : "+v"(lane));
       st.i32 = lane & 31;
       st.h = lane >> 5;
       st.v_key = 8 * (lane >> 5) + ((lane & 15) >> (C::E4M3 ? 1 : 2));
@@ -268,7 +395,19 @@ void fa_paged_fwd_kernel(PagedParams p) {
                        : ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<DV>(st.v_key));
       st.v_half = (lane & 1) * 8;
       const int kb0 = t0 * BN, t1 = t0 + nt;
-      const int kv_lim = min(blk.kv_end, t1 * BN);  // keys loaded; behind it the tile loads read zeros
+      // Keys loaded; behind it the tile loads read zeros. (With forms tiles are not in order: see lim_of.)
+      const int kv_lim = FORM ? blk.kv_end : min(blk.kv_end, t1 * BN);
+      // First key of the j-th tile from t0 on. A bias by distance takes them from the last one on, so that the maximum comes
+      // early.
+      auto key_of = [&](int j) {
+        if constexpr (FORM) {
+          const int at = st.last_first ? max(tiles - 1 - t0 - j, 0) : t0 + j;
+          return (at < blk.pre ? at : at + blk.gap) * BN;
+        }
+        return kb0 + j * BN;
+      };
+      if constexpr (FORM) st.last_first = p.f.slopes != nullptr;
+      auto lim_of = [&](int j) { return FORM && j >= nt ? 0 : kv_lim; };
       st.sk = s.kv;
       st.table = p.bt.block_table + (int64_t)b * p.bt.table_stride;
       st.cs = p.cs;
@@ -286,6 +425,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
         const uint32_t c = (uint32_t)min(blk.c0 + wave * 32 * QB + qb * 32 + st.i32, blk.cols - 1);
         const int qi = (int)fast_div(c, p.m_group, p.sh_group), member = (int)c - qi * p.group;
         st.last_key[qb] = p.causal ? s.kv - s.n_q + qi : s.kv - 1;
+        if constexpr (FORM) st.init_row(p, qb, qi, g * p.group + member);
         const uint16_t* qp = p.q + (int64_t)(s.q0 + qi) * p.q_token + (int64_t)(g * p.group + member) * p.q_head;
 #pragma unroll
         for (int ks = 0; ks < A::KS; ++ks)
@@ -295,23 +435,41 @@ void fa_paged_fwd_kernel(PagedParams p) {
       // The pages of this wave's keys of tiles w0 .. w0 + 63, one per lane (behind the last key: the last one's).
       int entries = 0;
       auto window = [&](int w0) {
-        const int key = min((w0 + lane) * BN + wave * R, kv_lim - 1);
+        const int key = min((FORM ? key_of(min(w0 + lane - t0, nt - 1)) : (w0 + lane) * BN) + wave * R, kv_lim - 1);
         entries = key >= 0 ? st.table[key >> p.c.page_shift] : -1;
         asm volatile("" : "+v"(entries));  // waited for here, not at every use
       };
       // Whether a page of the range is not there. (The first 64 are read beside the window, so that both are waited for
       // once.)
       const int e0 = (kb0 >> p.c.page_shift) + lane, e1 = (kv_lim + smask) >> p.c.page_shift;
-      int page0 = 0;
-      if (e0 < e1) page0 = st.table[e0];
-      window(t0);
-      bool hole = e0 < e1 && (page0 < 0 || page0 >= p.c.n_pages);
-      for (int e = e0 + 64; e < e1; e += 64) {
-        const int page = st.table[e];
-        hole = hole || page < 0 || page >= p.c.n_pages;
+      bool hole = false;
+      auto look = [&](int from, int to) {
+        for (int e = from; e < to; e += 64) {
+          const int page = st.table[e];
+          hole = hole || page < 0 || page >= p.c.n_pages;
+        }
+      };
+      if constexpr (FORM) {  // the pages of all the block's tiles, those between prefix and window left out
+        window(t0);
+        const int pre_end = (blk.pre * BN + smask) >> p.c.page_shift;
+        look(lane, min(pre_end, e1));
+        if (blk.gap > 0) look(((blk.pre + blk.gap) * BN >> p.c.page_shift) + lane, e1);
+      } else {
+        int page0 = 0;
+        if (e0 < e1) page0 = st.table[e0];
+        window(t0);
+        hole = e0 < e1 && (page0 < 0 || page0 >= p.c.n_pages);
+        look(e0 + 64, e1);
       }
       st.holes = __builtin_amdgcn_ballot_w64(hole) != 0;
       int n_plain = st.holes ? 0 : min(max(blk.plain - t0, 0), nt);
+      if constexpr (FORM) st.init_block(p, s, blk.row0, blk.row1);
+      auto masked = [&](int j) {
+        if constexpr (FORM)
+          return st.holes || st.hides(key_of(j));
+        else
+          return j >= n_plain;
+      };
 
       const unsigned char* kh = static_cast<const unsigned char*>(p.c.k) + (int64_t)g * p.c.k_head * E;
       const unsigned char* vh = static_cast<const unsigned char*>(p.c.v) + (int64_t)g * p.c.v_head * E;
@@ -335,10 +493,10 @@ void fa_paged_fwd_kernel(PagedParams p) {
       int v_page = 0;
       auto aim_k = [&](int j) {
         const int page = __builtin_amdgcn_readlane(entries, j & 63);
-        gk = kload.rsrc(page, p.c.n_pages, kb0 + j * BN + wave * R, smask, kv_lim);
+        gk = kload.rsrc(page, p.c.n_pages, key_of(j) + wave * R, smask, lim_of(j));
         return page;
       };
-      auto aim_v = [&](int j, int page) { gv = vload.rsrc(page, p.c.n_pages, kb0 + j * BN + wave * R, smask, kv_lim); };
+      auto aim_v = [&](int j, int page) { gv = vload.rsrc(page, p.c.n_pages, key_of(j) + wave * R, smask, lim_of(j)); };
       // The prologue's groups j = -KA .. -1, as in the fused forward: K(j + KA) and V(j + VA), and in front of group 1 - KA
       // zeros in the slot of the V tile before the first, which step 0 multiplies by P = 0.
 #pragma unroll
@@ -376,9 +534,11 @@ void fa_paged_fwd_kernel(PagedParams p) {
         __builtin_amdgcn_s_barrier();
         compiler_fence();
         st.scores(sA, kslot(0));
-        if (n_plain == 0) st.mask_tile(sA, kb0);
+        if constexpr (!FORM) {
+          if (n_plain == 0) st.mask_tile(sA, kb0);
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) st.m_run[qb] = st.row_max(sA, qb);
+          for (int qb = 0; qb < QB; ++qb) st.m_run[qb] = st.row_max(sA, qb);
+        }
 #pragma unroll
         for (int kb = 0; kb < A::KB; ++kb)
 #pragma unroll
@@ -415,13 +575,13 @@ void fa_paged_fwd_kernel(PagedParams p) {
       int j = 0;
       for (; j + 1 < nt; j += 2) {
         sync_step(j);
-        st.step(sA, sB, pA, pB, kread(j + 1), j > 0 ? vread(j - 1) : vzero, j >= n_plain, kb0 + j * BN, issue);
+        st.step(sA, sB, pA, pB, kread(j + 1), j > 0 ? vread(j - 1) : vzero, masked(j), key_of(j), issue);
         sync_step(j + 1);
-        st.step(sB, sA, pB, pA, kread(j + 2), vread(j), j + 1 >= n_plain, kb0 + (j + 1) * BN, issue);
+        st.step(sB, sA, pB, pA, kread(j + 2), vread(j), masked(j + 1), key_of(j + 1), issue);
       }
       if (j < nt) {
         sync_step(j);
-        st.step(sA, sB, pA, pB, kread(j + 1), j > 0 ? vread(j - 1) : vzero, j >= n_plain, kb0 + j * BN, issue);
+        st.step(sA, sB, pA, pB, kread(j + 1), j > 0 ? vread(j - 1) : vzero, masked(j), key_of(j), issue);
       }
       if (nt > 0) {
         // P V of the last tile, on a selected copy of P (see the fused forward).
@@ -450,13 +610,17 @@ void fa_paged_fwd_kernel(PagedParams p) {
       for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
         for (int db = 0; db < A::DB; ++db) agpr_fence<A::AG>(st.oacc[db][qb]);
-      if constexpr (C::SPLIT) asm volatile("" : "+v"(lane));
+      decltype(auto) po = reread<FORM>(args);  // for the output
+      if constexpr (FORM)
+        lane = lane_anew();
+      else if constexpr (C::SPLIT)
+        asm volatile("" : "+v"(lane));
       st.i32 = lane & 31;
       st.h = lane >> 5;
       constexpr int WROWS = 32 * QB, RB = DV * 2;
       const int col0 = wave * WROWS;  // this wave's first column of the block
       float vs = 1.f;
-      if constexpr (C::E4M3) vs = p.c.v_scale != nullptr ? scalar_load(p.c.v_scale + g) : 1.f;
+      if constexpr (C::E4M3) vs = po.c.v_scale != nullptr ? scalar_load(po.c.v_scale + g) : 1.f;
       if (C::SPLIT && n_parts > 1) {
         // A part: O normalised by its own sum (fp32), and its LSE. Place 2 me: of a block that begins before.
         const int64_t place = (2 * (int64_t)me + (me == first_wg ? 1 : 0)) * many_place_cols(BC);
@@ -467,7 +631,7 @@ void fa_paged_fwd_kernel(PagedParams p) {
           const bool some = l_tot > 0.f;
           const int col = col0 + qb * 32 + st.i32;
           if (blk.c0 + col < blk.cols) {
-            float* orow = p.many_o + (place + col) * DV;
+            float* orow = po.many_o + (place + col) * DV;
 #pragma unroll
             for (int db = 0; db < A::DB; ++db)
 #pragma unroll
@@ -477,12 +641,12 @@ void fa_paged_fwd_kernel(PagedParams p) {
                 *reinterpret_cast<f32x4*>(orow + db * 32 + 8 * g4 + 4 * st.h) = some ? o : f32x4{0.f, 0.f, 0.f, 0.f};
               }
             if (st.h == 0)  // a sum that is no number stays one in the join
-              p.many_lse[place + col] =
+              po.many_lse[place + col] =
                   some ? (st.m_run[qb] - C::P_LOG2 + log2f(l_tot)) * kLn2 : isnan(l_tot) ? NAN : -INFINITY;
           }
         }
-        if (me == first_wg && tid == 0)
-          p.many_desc[blockIdx.x] = PagedItem{n_parts, s.q0, min(BC, blk.cols - blk.c0), blk.c0, g, me};
+        if (me == first_wg && (FORM ? wave == 0 && lane == 0 : tid == 0))
+          po.many_desc[blockIdx.x] = PagedItem{n_parts, s.q0, min(BC, blk.cols - blk.c0), blk.c0, g, me};
       } else {
         // O through LDS, so that each store instruction writes whole rows (layout: see the fused forward).
         unsigned char* stage = smem + wave * WROWS * RB;
@@ -502,9 +666,9 @@ void fa_paged_fwd_kernel(PagedParams p) {
               *reinterpret_cast<uint2*>(srow + (((4 * db + g4) << 4) ^ osw)) = some ? make_uint2(w0, w1) : make_uint2(0u, 0u);
             }
           const uint32_t c = (uint32_t)(blk.c0 + col0 + qb * 32 + st.i32);
-          if (p.lse != nullptr && st.h == 0 && (int)c < blk.cols) {
-            const int qi = (int)fast_div(c, p.m_group, p.sh_group);
-            p.lse[(int64_t)(s.q0 + qi) * p.hq + g * p.group + ((int)c - qi * p.group)] =
+          if (po.lse != nullptr && st.h == 0 && (int)c < blk.cols) {
+            const int qi = (int)fast_div(c, po.m_group, po.sh_group);
+            po.lse[(int64_t)(s.q0 + qi) * po.hq + g * po.group + ((int)c - qi * po.group)] =
                 some ? (st.m_run[qb] - C::P_LOG2 + log2f(l_tot)) * kLn2 : -INFINITY;
           }
         }
@@ -513,12 +677,12 @@ void fa_paged_fwd_kernel(PagedParams p) {
         // would take longer than the stores).
         constexpr int CPR = RB / 16, RPI = 64 / CPR, NIT = WROWS / RPI;
         const int ch = lane % CPR;
-        const int rows_on = (int)fast_div(RPI, p.m_group, p.sh_group), heads_on = RPI - rows_on * p.group;
-        const int64_t step = rows_on * p.o_token + heads_on * p.o_head, wrap = p.o_token - p.group * p.o_head;
+        const int rows_on = (int)fast_div(RPI, po.m_group, po.sh_group), heads_on = RPI - rows_on * po.group;
+        const int64_t step = rows_on * po.o_token + heads_on * po.o_head, wrap = po.o_token - po.group * po.o_head;
         int c = blk.c0 + col0 + lane / CPR;
-        const int qi = (int)fast_div((uint32_t)c, p.m_group, p.sh_group);
-        int member = c - qi * p.group;
-        uint16_t* dst = p.o + (int64_t)(s.q0 + qi) * p.o_token + (int64_t)(g * p.group + member) * p.o_head + ch * 8;
+        const int qi = (int)fast_div((uint32_t)c, po.m_group, po.sh_group);
+        int member = c - qi * po.group;
+        uint16_t* dst = po.o + (int64_t)(s.q0 + qi) * po.o_token + (int64_t)(g * po.group + member) * po.o_head + ch * 8;
         u32x4 ov[NIT];
 #pragma unroll
         for (int it = 0; it < NIT; ++it) {
@@ -537,8 +701,8 @@ void fa_paged_fwd_kernel(PagedParams p) {
           c += RPI;
           dst += step;
           member += heads_on;
-          const bool over = member >= p.group;
-          member -= over ? p.group : 0;
+          const bool over = member >= po.group;
+          member -= over ? po.group : 0;
           dst += over ? wrap : 0;
         }
       }
@@ -547,16 +711,17 @@ void fa_paged_fwd_kernel(PagedParams p) {
       break;
     } else {
       if (!split || r >= r1) break;
+      decltype(auto) pn = reread<FORM>(args);
       // The next block: of this head, of the next, of the next sequence with any.
       start += kBlockCost + tiles;
       if (++cb == n_cb) {
         cb = 0;
-        if (++g == p.c.hkv) {
+        if (++g == pn.c.hkv) {
           g = 0;
           do {
-            if (++b >= p.bt.n_seq) return;  // not reached: r < total
-            s = load_seq(p.bt, b);
-            n_cb = n_blocks<BC>(s, p);
+            if (++b >= pn.bt.n_seq) return;  // not reached: r < total
+            s = load_seq<FORM>(pn, b);
+            n_cb = n_blocks<BC>(s, pn);
           } while (n_cb == 0);
         }
       }
@@ -569,18 +734,34 @@ void fa_paged_fwd_kernel(PagedParams p) {
 // 64-key tiles at d = 64 over e4m3, whose 32-key tiles would be half a load per wave. Short: 32 columns per wave, two
 // workgroups per CU, where sequences have at most 128 row-heads or long blocks would not fill the chip (paged_many; bf16, d_qk 64
 // and 128: in 64-key tiles two waves per SIMD do not fit at d_qk = 192).
-template <int DQK, int DV, bool E4M3, bool SHORT, bool SPLIT>
+template <int DQK, int DV, bool E4M3, bool SHORT, bool SPLIT, bool FORM = false>
 struct PagedInstance {
-  using C = Cfg<DQK, DV, 64, 4, 2, true, SPLIT, 1, 2, 6, 2, 4, 1, true, E4M3>;
+  using C = Cfg<DQK, DV, 64, 4, 2, true, SPLIT, 1, 2, 6, 2, 4, 1, true, E4M3, FORM>;
 };
 template <bool SPLIT>
-struct PagedInstance<64, 64, false, false, SPLIT> {
+struct PagedInstance<64, 64, false, false, SPLIT, false> {
   using C = Cfg<64, 64, 32, 4, 2, true, SPLIT, 2, 2, 4, 2, 4, 1, true>;
 };
-template <int DQK, int DV, bool SPLIT>
-struct PagedInstance<DQK, DV, false, true, SPLIT> {
-  using C = Cfg<DQK, DV, 64, 4, 1, true, SPLIT, 2, DQK >= 128 ? 1 : 2, DQK >= 128 ? 2 : 6, 2, DQK >= 128 ? 3 : 4, 1, true>;
+template <int DQK, int DV, bool SPLIT, bool FORM>
+struct PagedInstance<DQK, DV, false, true, SPLIT, FORM> {
+  using C = Cfg<DQK, DV, 64, 4, 1, true, SPLIT, 2, DQK >= 128 ? 1 : 2, DQK >= 128 ? 2 : 6, 2, DQK >= 128 ? 3 : 4, 1, true, false, FORM>;
 };
+
+template <class C>
+hipError_t launch_many(PagedParams p, int64_t blocks, hipStream_t stream) {
+  void* args[] = {&p};
+  const dim3 grid((unsigned)(C::SPLIT ? p.many_wg : blocks * p.c.hkv));
+  return hipLaunchKernel(reinterpret_cast<const void*>(&fa_paged_fwd_kernel<C>), grid, dim3(C::NT), args, 0, stream);
+}
+// What the launchers fill in.
+inline void many_constants(PagedParams& p) {
+  const FastDiv fg = make_fastdiv(p.group);
+  p.m_group = fg.m;
+  p.sh_group = fg.sh;
+  p.many_min_units = kBlockCost + 4;
+  p.many_log = 0;
+  while ((1 << p.many_log) < p.many_wg) ++p.many_log;
+}
 
 }  // namespace
 }  // namespace fa

@@ -154,3 +154,80 @@ def test_oracle_visible():
     assert moves.visible(3, 3, prefix=2).tolist() == [[True, True, False], [True, True, False], [True] * 3]
     tree = np.array([[True, False], [False, True]])
     assert moves.visible(2, 4, tree=tree).tolist() == [[True, True, True, False], [True, True, False, True]]
+
+
+def test_oracle_attention():
+    """Against naive attention where nothing is set, and by hand for a cap, a bias and a tree."""
+    from oracle.paged import paged_attention as plain
+
+    rng = np.random.RandomState(1)
+    kc, vc = rng.randn(9, 2, 4, 6), rng.randn(9, 2, 4, 3)
+    table, lens, starts, q = np.array([[5, 1, 8], [0, 7, 2]]), [10, 7], [0, 3, 4], rng.randn(4, 4, 6)
+    for causal in (True, False):
+        o, lse = plain(q, kc, vc, table, lens, starts, 0.3, causal)
+        r = moves.paged_attention(q, kc, vc, table, lens, starts, 0.3, causal)
+        assert np.allclose(r.o, o, atol=1e-13) and np.allclose(r.lse, lse, atol=1e-13)
+    bits = moves.tree_bits(np.array([[1], [3], [5], [-2 ** 31]], dtype=np.int32))
+    assert bits.shape == (4, 32) and bits[:3, :3].tolist() == [[True, False, False], [True, True, False], [True, False, True]]
+    assert bits[3].tolist() == [False] * 31 + [True]
+    r = moves.paged_attention(q, kc, vc, table, lens, starts, 0.3, cap=0.8, tree=bits)
+    keys = np.concatenate([kc[p] for p in table[0]], axis=1)[:, [0, 1, 2, 3, 4, 5, 6, 7, 9]]  # token 2 sees 0 and 2
+    vals = np.concatenate([vc[p] for p in table[0]], axis=1)[:, [0, 1, 2, 3, 4, 5, 6, 7, 9]]
+    w = np.exp(0.8 * np.tanh(0.3 * keys[1] @ q[2, 3] / 0.8))
+    assert np.allclose(r.o[2, 3], (w / w.sum()) @ vals[1]) and np.allclose(r.lse[2, 3], np.log(w.sum()))
+    assert r.keys.tolist() == [8, 9, 9, 6] and np.isclose(r.lse[3, 0], np.log(np.exp(0.8 * np.tanh(
+        0.3 * np.concatenate([kc[p] for p in table[1]], axis=1)[0, :6] @ q[3, 0] / 0.8)).sum()))
+    r = moves.paged_attention(q, kc, vc, table, lens, starts, 0.0, slopes=[0.5] * 4, window=3, prefix=[1, 0])
+    w = np.exp(-0.5 * np.array([7, 2, 1, 0]))
+    assert np.isclose(r.lse[0, 2], np.log(w.sum()))
+
+
+def scores(**kw):
+    a = dict(softcap=0.0, window=0, slopes=None, prefix_lens=None, tree_mask=None, mask_stride=1, mask_words=1)
+    a.update(kw)
+    return fa.PagedScores(**a)
+
+
+def attend(sc, c=None, b=None, causal=True, scale=0.1, ws=P, nbytes=1 << 30, path=0):
+    return fa.fa_fwd_paged_ex(c or cache(), b or batch(), sc, P, P, P, 4, fa.PagedStrides(512, 128, 512, 128), 2, path, scale, causal,
+                              ws, nbytes, None)
+
+
+def test_scores_that_are_refused():
+    for kw in (dict(window=-1), dict(tree_mask=P, mask_words=0), dict(tree_mask=P, mask_words=65, mask_stride=65),
+               dict(tree_mask=P, mask_words=2, mask_stride=1), dict(tree_mask=P, mask_stride=(1 << 40) + 1)):
+        assert attend(scores(**kw)) == SHAPE, kw
+    for kw in (dict(tree_mask=P, window=3), dict(tree_mask=P, slopes=P), dict(tree_mask=P, prefix_lens=P), dict(tree_mask=P + 2),
+               dict(slopes=P + 1), dict(prefix_lens=P + 2)):
+        assert attend(scores(**kw)) == UNSUPPORTED, kw
+    assert attend(scores(tree_mask=P), causal=False) == UNSUPPORTED
+    for cap in (-1.0, float("nan"), float("inf"), 1025.0):
+        assert attend(scores(softcap=cap)) == fa.FA_ERR_BAD_SCALE, cap
+    # As fa_fwd_paged otherwise.
+    for sc in (None, scores(), scores(softcap=3.0), scores(tree_mask=P), scores(window=5)):
+        assert attend(sc, scale=float("inf")) == fa.FA_ERR_BAD_SCALE and attend(sc, path=3) == UNSUPPORTED
+        assert attend(sc, cache(K=None)) == NULL and attend(sc, cache(d_v=64)) == UNSUPPORTED
+        assert attend(sc, b=batch(T=0)) == fa.FA_OK
+        long = batch(max_blocks=256, table_stride=256)
+        need = fa.fa_fwd_paged_ex_workspace_bytes(3, 5, 4096, 4, 2, 128, 128, 0, 2)
+        assert need > 0 and attend(sc, b=long, nbytes=1024) == fa.FA_ERR_WORKSPACE and attend(sc, b=long, ws=None) == fa.FA_ERR_WORKSPACE
+    assert fa.fa_fwd_paged_ex_workspace_bytes(3, 5, 4096, 4, 2, 96, 128, 0, 2) == 0
+    assert ctypes.sizeof(fa.PagedScores) == 8 + 3 * 8 + 8 + 8
+
+
+def test_score_arguments_that_are_refused():
+    from paper_2609_21264_amd import _scores
+
+    for kw in (dict(softcap=0.0), dict(softcap=-2), dict(softcap=2000.0), dict(window=0), dict(window=-1), dict(window=1 << 31)):
+        a = dict(softcap=None, slopes=None, window=None, prefix_lens=None, tree_mask=None)
+        a.update(kw)
+        with pytest.raises(ValueError, match="softcap must be|window must be"):
+            _scores(*a.values(), 3, 4, 1, 0)
+    with pytest.raises(ValueError, match="slopes must be a contiguous"):
+        _scores(None, torch.zeros(3), None, None, None, 3, 4, 1, 0)
+    with pytest.raises(ValueError, match="slopes must be on"):
+        _scores(None, torch.zeros(4), None, None, None, 3, 4, 1, 0)
+    with pytest.raises(ValueError, match="1-d int32"):
+        _scores(None, None, None, torch.zeros(1), None, 3, 4, 1, 0)
+    with pytest.raises(ValueError, match="must be on the device"):
+        _scores(None, None, None, None, torch.zeros(3, 1, dtype=torch.int32), 3, 4, 1, 0)
