@@ -27,22 +27,30 @@ __device__ __forceinline__ u32x4 pack8(const F8& f) {
                pack_bf16x2(f.x[6], f.x[7])};
 }
 
-// A pair (x, y) becomes (x cos - y sin, y cos + x sin). Halves: the pairs are the elements of two chunks; else
+// A product that is rounded by itself: left to the compiler, which of two products that are added is rounded, and which
+// joins the sum exactly, differs from place to place.
+__device__ __forceinline__ float product(float a, float b) {
+  float x = a * b;
+  asm("" : "+v"(x));
+  return x;
+}
+
+// A pair (x, y) becomes (x cos - y sin, y cos + x sin), the products with the sine rounded first. Halves: the pairs are the elements of two chunks; else
 // neighbouring elements of one, by the first four angles.
 __device__ __forceinline__ void turn_halves(F8& x, F8& y, const F8& cs, const F8& sn) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float a = x.x[e], c = y.x[e];
-    x.x[e] = a * cs.x[e] - c * sn.x[e];
-    y.x[e] = c * cs.x[e] + a * sn.x[e];
+    x.x[e] = fmaf(a, cs.x[e], -product(c, sn.x[e]));
+    y.x[e] = fmaf(c, cs.x[e], product(a, sn.x[e]));
   }
 }
 __device__ __forceinline__ void turn_neighbours(F8& x, const F8& cs, const F8& sn) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float a = x.x[2 * e], c = x.x[2 * e + 1];
-    x.x[2 * e] = a * cs.x[e] - c * sn.x[e];
-    x.x[2 * e + 1] = c * cs.x[e] + a * sn.x[e];
+    x.x[2 * e] = fmaf(a, cs.x[e], -product(c, sn.x[e]));
+    x.x[2 * e + 1] = fmaf(c, cs.x[e], product(a, sn.x[e]));
   }
 }
 
