@@ -434,7 +434,7 @@ fa_status_t fa_kv_compact(const fa_paged_cache_t* cache, const fa_paged_batch_t*
  * the copies could leave. The scales of an e4m3 cache are per head and stay. Layers in one buffer count as heads, as above.
  * Enqueues one kernel. Errors: cache NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE); head dimensions, page size or type
  * not supported (FA_ERR_UNSUPPORTED); NULL buffers (FA_ERR_NULL_POINTER); alignment (FA_ERR_UNSUPPORTED); cache strides, or
- * n * ceil(Hkv * page_size * max(d_qk, d_v) * element bytes / 32768) >= 2^24 (FA_ERR_BAD_SHAPE). n == 0 returns FA_OK
+ * n * ceil(Hkv * page_size * max(d_qk, d_v) * element bytes / 4096) >= 2^24 (FA_ERR_BAD_SHAPE). n == 0 returns FA_OK
  * without a launch.
  */
 fa_status_t fa_kv_copy(const fa_paged_cache_t* cache, const int* src, const int* dst, int n, hipStream_t stream);

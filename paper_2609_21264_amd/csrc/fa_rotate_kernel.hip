@@ -13,6 +13,9 @@ namespace {
 // thread the same chunk of every head, so that the angles stay in registers and a pair is read, turned and
 // written by one thread (Y may be X). What bounds it: the bytes of X and Y.
 constexpr int kRotateThreads = 256;
+// Heads of a workgroup, fewer where that leaves too few workgroups: 2 x 9 999 tokens of 16 heads, d = 64, three axes, there and
+// back 34.6 us with 8 (4.7 TB/s read and written), 39.3 with all 16, 35.5 with 4, 38.3 with 2, 49.0 with one.
+constexpr int kRotateHeads = 8, kRotateWorkgroups = 512;
 
 template <bool AT>
 __global__ __launch_bounds__(kRotateThreads) void fa_rotate_kernel(RotateParams p) {
@@ -67,7 +70,8 @@ hipError_t launch_rotate(RotateParams p, hipStream_t stream) {
   p.n_blocks = p.batch * p.per;  // below 2^31: batch * s is
   const FastDiv f = make_fastdiv((uint32_t)p.per);
   p.m_per = f.m, p.sh_per = f.sh;
-  p.heads = p.h;
+  p.heads = p.h < kRotateHeads ? p.h : kRotateHeads;
+  while (p.heads > 1 && (int64_t)p.n_blocks * ((p.h + p.heads - 1) / p.heads) < kRotateWorkgroups) p.heads = (p.heads + 1) / 2;
   constexpr int kMost = 1 << 20;
   const dim3 grid((unsigned)(p.n_blocks < kMost ? p.n_blocks : kMost), (unsigned)((p.h + p.heads - 1) / p.heads));
   void* args[] = {&p};
