@@ -20,8 +20,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libfa.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 SOURCES = ["fa_api.hip", "fa_fwd_kernel.hip", "fa_lbl_kernel.hip", "fa_decode_kernel.hip", "fa_paged_kernel.hip",
-           "fa_paged_fwd_kernel.hip", "fa_paged_moves_kernel.hip", "fa_rotate_kernel.hip", "fa_paged_forms_few_kernel.hip",
-           "fa_paged_forms_many_kernel.hip"]
+           "fa_paged_fwd_kernel.hip", "fa_paged_moves_kernel.hip", "fa_rotate_kernel.hip", "fa_paged_forms_few_kernel.hip", "fa_paged_masked_kernel.hip",
+           "fa_paged_capped_kernel.hip", "fa_paged_biased_kernel.hip"]
 # Measurement-only microbenchmarks (measured ceilings), a library of their own.
 CEIL_LIB_PATH = os.path.join(PKG_DIR, "libfa_ceilings.so")
 CEIL_SOURCES = ["fa_ceilings.hip"]

@@ -564,8 +564,13 @@ fa_status_t attend(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch,
   const int cols = usual < w.cols ? static_cast<int>(usual) : w.cols;
   hipError_t e = hipSuccess;
   const bool e4m3 = cache->type == FA_CACHE_E4M3;
-  if (w.many)
-    e = forms ? fa::launch_paged_many_forms(p, w.m, cache->d_qk, e4m3, stream) : fa::launch_paged_many(p, w.m, cache->d_qk, e4m3, stream);
+  if (w.many) {
+    const auto launch = !forms                    ? fa::launch_paged_many
+                        : p.f.slopes != nullptr ? fa::launch_paged_many_biased
+                        : p.f.cap_a != 0.f      ? fa::launch_paged_many_capped
+                                                : fa::launch_paged_many_masked;
+    e = launch(p, w.m, cache->d_qk, e4m3, stream);
+  }
   if (e == hipSuccess && w.few)
     e = forms ? fa::launch_paged_few_forms(p, cache->d_qk, e4m3, w.col_blocks, stream)
               : fa::launch_paged_few(p, cache->d_qk, e4m3, w.col_blocks, stream_kv, stream);

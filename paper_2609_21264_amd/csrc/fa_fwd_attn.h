@@ -131,7 +131,7 @@ struct Ring {
 // K and V fragments read ahead from LDS (KPF, VPF), K and V ring slots in LDS (NKR, NVR), and the
 // parts each key tile is split into between the waves (KSPLIT).
 template <int DQK_, int DV_, int BN_, int NWAVES_, int QB_, bool CAUSAL_, bool SPLIT_, int OCC_, int KPF_, int VPF_,
-          int NKR_, int NVR_, int KSPLIT_ = 1, bool PAGED_ = false, bool E4M3_ = false, bool FORM_ = false>
+          int NKR_, int NVR_, int KSPLIT_ = 1, bool PAGED_ = false, bool E4M3_ = false, int FORM_ = 0>
 struct Cfg {
   static constexpr int DQK = DQK_, DV = DV_, BN = BN_, NWAVES = NWAVES_, QB = QB_;
   // KSPLIT = 2: the waves form two sets of NWAVES / 2 (RWAVES) that own the same query rows; set k
@@ -147,9 +147,10 @@ struct Cfg {
   // PAGED: the keys lie in pages (PagedKeys below), the columns of a wave are any rows of any of the group's heads,
   // and the last key each of them sees is in a register.
   static constexpr bool PAGED = PAGED_;
-  // FORM: scores may be capped or biased by distance, and keys hidden otherwise than by a last one (FormKeys, which the paged
-  // kernel defines).
-  static constexpr bool FORM = FORM_;
+  // FORM: keys may be hidden otherwise than by a last one (kMasked), and scores capped (kCapped) or biased by distance and
+  // perhaps capped (kBiased); by FormKeys, which the paged kernel defines.
+  static constexpr int kMasked = 1, kCapped = 2, kBiased = 3;
+  static constexpr int FORM = FORM_;
   // E4M3: K and V tiles are 8-bit. They stay so in LDS and are widened as fragments are read: K to bf16, V to fp16, with
   // P in fp16 too. The order of the dims in a score product follows the 16-byte reads of K: k-steps 2 m and 2 m + 1
   // take dims 32 m + 16 h + 0 .. 7 and + 8 .. 15 in lane half h.
@@ -223,7 +224,7 @@ template <class C>
 struct FormKeys;
 struct NoForms {};
 template <class C>
-struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM, FormKeys<C>, NoForms> {
+struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM != 0, FormKeys<C>, NoForms> {
   static constexpr int DQK = C::DQK, DV = C::DV, BN = C::WBN, QB = C::QB;  // BN: this wave's keys of a tile
   static constexpr int KS = DQK / 16;  // k-steps of the score product
   static constexpr int KB = BN / 32;   // 32-key blocks per tile
@@ -361,8 +362,8 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM, FormKeys<C
       for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kb][qb][r] * cs);
     return half_swap_max(m);
   }
-  // The same of mul * score, multiplied last.
-  __device__ __forceinline__ float row_max_times(const Scores& s, int qb, float mul) const {
+  // The same of mul * score + add (which the halves may have each for itself), multiplied last.
+  __device__ __forceinline__ float row_max_of(const Scores& s, int qb, float mul, float add) const {
     float m = s[0][qb][0];
     if (mul >= 0.f) {
 #pragma unroll
@@ -375,7 +376,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM, FormKeys<C
 #pragma unroll
         for (int r = 0; r < 16; ++r) m = fminf(m, s[kb][qb][r]);
     }
-    return half_swap_max(m * mul);
+    return half_swap_max(fmaf(m, mul, add));
   }
 
   // Element schedule of the step: the NEL = 2 * NEP exponentials of a tile are spread
@@ -404,7 +405,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM, FormKeys<C
     return true;
   }
 
-  // Element e of a tile: p = 2^(mul * s - m_ref), mul = cs (1 where the scores are final values).
+  // Element e of a tile: p = 2^(mul * s - m_ref), mul = cs without forms.
   __device__ __forceinline__ float exp_elem(int e, const Scores& cur, const float (&mref)[QB], float mul) const {
     const int u = e >> 1, qb = u % QB, rp = (u / QB) % 8, kb = u / (QB * 8);
     float x = __builtin_amdgcn_exp2f(fmaf(cur[kb][qb][2 * rp + (e & 1)], mul, -mref[qb]));
@@ -524,18 +525,18 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM, FormKeys<C
   __device__ __forceinline__ void step(Scores& cur, Scores& nxt, Probs& pk_new, const Probs& pk_old,
                                        const unsigned char* sKn, const unsigned char* sVo, bool masked, int n0,
                                        Issue&& issue) {
-    float mul = cs, alpha[QB];
+    float mul = cs, add[QB], alpha[QB];
     bool rescale = false;
-    if constexpr (C::FORM) {
+    if constexpr (C::FORM != 0) {
       // With forms the maximum is computed for every tile: rows may see their first key in any, and a bias makes maxima rise.
       // The reference follows where some row's has risen over it by more than 2^3 (in log2); O and the sums, which
       // hold the tiles before this one only after the step, follow at its end.
-      mul = this->values(cur, n0, masked, cs, h, *this);
+      mul = this->values(cur, add, n0, masked, cs, h, *this);
       float mt[QB];
       bool up = false;
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
-        mt[qb] = row_max_times(cur, qb, mul);
+        mt[qb] = row_max_of(cur, qb, mul, add[qb]);
         up = up || mt[qb] > m_run[qb] + 8.f;
         alpha[qb] = 1.f;
       }
@@ -555,6 +556,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM, FormKeys<C
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       mref[qb] = m_run[qb] == -INFINITY ? 0.f : m_run[qb] - C::P_LOG2;
+      if constexpr (C::FORM != 0) mref[qb] -= add[qb];
       rs[qb] = 0.f;
     }
     // V fragments first: the step's first MFMAs are P V's, so with one wave per SIMD every LDS read in
@@ -593,7 +595,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM, FormKeys<C
 #pragma unroll
     for (int e = elem_begin(NSL - 1); e < elem_end(NSL - 1); ++e)
       if (e & 1) pack_pair(e >> 1, ev[(e - 1) % 4], ev[e % 4], pk_new, rs);
-    if constexpr (C::FORM) {
+    if constexpr (C::FORM != 0) {
       if (rescale) {
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {

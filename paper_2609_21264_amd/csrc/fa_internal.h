@@ -316,9 +316,12 @@ struct PagedMany {
 };
 PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, int max_q, int few_cols, int d_qk, bool e4m3,
                      bool forms);
-hipError_t launch_paged_many(PagedParams p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream);
-// The same kernels with forms (fa_paged_forms_few_kernel.hip, fa_paged_forms_many_kernel.hip).
+hipError_t launch_paged_many(const PagedParams& p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream);
+// The same kernels with forms (fa_paged_forms_few_kernel.hip; fa_paged_masked_kernel.hip, fa_paged_capped_kernel.hip,
+// fa_paged_biased_kernel.hip: scores as they are, capped, or with slopes).
 hipError_t launch_paged_few_forms(PagedParams p, int d_qk, bool fp8, int col_blocks, hipStream_t stream);
-hipError_t launch_paged_many_forms(PagedParams p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream);
+hipError_t launch_paged_many_masked(const PagedParams& p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream);
+hipError_t launch_paged_many_capped(const PagedParams& p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream);
+hipError_t launch_paged_many_biased(const PagedParams& p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream);
 
 }  // namespace fa

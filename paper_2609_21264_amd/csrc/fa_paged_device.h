@@ -21,6 +21,7 @@ __device__ __forceinline__ float scalar_load(const float* p) {
 
 // A value that is the same for the whole wave, in a scalar register (some divisions and scans would leave it in a vector one).
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
 // One sequence: its new tokens are the packed ones [q0, q_end), the last of its kv keys.
 struct PagedSeq {

@@ -46,7 +46,8 @@ PagedMany paged_many(int n_seq, int n_tokens, int max_keys, int hkv, int group, 
   return m;
 }
 
-hipError_t launch_paged_many(PagedParams p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream) {
+hipError_t launch_paged_many(const PagedParams& args, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream) {
+  PagedParams p = args;
   many_constants(p);
   if (e4m3) {
     if (d_qk == 64) return launch_many_split<64, 64, true, false>(p, m, stream);

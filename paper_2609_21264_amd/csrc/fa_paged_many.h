@@ -113,27 +113,43 @@ __device__ __forceinline__ int lane_anew() {
   return (int)__builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0u));
 }
 
-// The state of a wave with forms. Scores are raw until values() makes them final (in units of log2, hidden keys -inf), which
-// it does where a tile hides keys from some row, or where scores are capped or biased; else the step multiplies them.
+// The state of a wave with forms. Before a step, values() turns a tile's raw scores s into what the step makes exponents of, mul * s
+// + add (in units of log2; hidden keys -inf), with as few operations per score as the form allows:
+//   masked   nothing: mul = cs
+//   capped   s = 1 / (1 + 2^(b s)): mul = -2 a, add = a (capped() in fa_paged_device.h)
+//   biased   in a tile before all rows' positions s += slope / cs * (key - the lane's first key), one operation, and add
+//            takes the distance of that key; else s -= slope / cs * |p - key|; capped too, or where cs is next to
+//            0, the final score
 template <class C>
 struct FormKeys {
   static constexpr int BN = C::WBN, QB = C::QB, KB = BN / 32;
   PagedSeq seq;
   int row[QB];          // of the sequence's new tokens
-  float slope[QB];      // times log2(e)
   int whole0, whole1;   // every row of the block sees the keys from whole0 to before whole1
-  bool final_always, last_first;
+  float cap_a, cap_b;   // capped; biased: cap_a 0 for none
+  float slope[QB];      // biased: times log2(e), over cs unless `final`
+  bool final;
+  int pos0;             // biased: position of the block's first row
   __device__ __forceinline__ void init_row(const PagedParams& p, int qb, int r, int head) {
     row[qb] = r;
-    slope[qb] = p.f.slopes != nullptr ? p.f.slopes[head] * kLog2e : 0.f;
+    if constexpr (C::FORM == C::kBiased) slope[qb] = p.f.slopes[head] * kLog2e;
   }
-  __device__ __forceinline__ void init_block(const PagedParams& p, const PagedSeq& s, int row0, int row1) {
+  __device__ __forceinline__ void init_block(const PagedParams& p, const PagedSeq& s, int row0, int row1, float cs) {
     SeenRow first, last;
     first.init(p.f, s, row0);
     last.init(p.f, s, row1);
     whole0 = last.first, whole1 = first.last + 1;
     seq = s;
-    final_always = p.f.cap_a != 0.f || p.f.slopes != nullptr;
+    if constexpr (C::FORM != C::kMasked) {
+      cap_a = p.f.cap_a;
+      cap_b = uniform(cap_factor(p.f, cs));
+    }
+    if constexpr (C::FORM == C::kBiased) {
+      pos0 = first.pos;
+      final = cap_a != 0.f || fabsf(cs) < 0x1p-60f;
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) slope[qb] = final ? slope[qb] : slope[qb] / cs;
+    }
   }
   // Whether the tile at key n0 hides a key from some row.
   __device__ __forceinline__ bool hides(int n0) const {
@@ -153,36 +169,53 @@ struct FormKeys {
     }
     return v;
   }
-  // Makes a tile's scores final where they have to be; what the step multiplies them by. h: the half of the wave; g: head of K.
+  static constexpr int key_of(int kb, int r) { return 32 * kb + 16 * (r >> 3) + (r & 7); }  // from the lane's first key on
+  // h: the half of the wave.
   template <class Scores>
-  __device__ __forceinline__ float values(Scores& s, int n0, bool masked, float cs, int h, const PagedKeys<true, QB>& pages) const {
-    if (!masked && !final_always) return cs;
-    const PagedForms f = fresh_forms();
-    if (f.cap_a != 0.f) {
-      const float b = cap_factor(f, cs);
+  __device__ __forceinline__ float values(Scores& s, float (&add)[QB], int n0, bool masked, float cs, int h,
+                                          const PagedKeys<true, QB>& pages) const {
+    float mul = cs;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) add[qb] = 0.f;
+    auto each = [&](auto f) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[kb][qb][r] = capped(s[kb][qb][r], f.cap_a, b);
-    } else {
+          for (int r = 0; r < 16; ++r) {
+            float x = f(s[kb][qb][r], qb, key_of(kb, r));
+            asm volatile("" : "+v"(x));  // in place: products for a branch not taken would move all scores
+            s[kb][qb][r] = x;
+          }
+    };
+    if (C::FORM == C::kCapped || (C::FORM == C::kBiased && cap_a != 0.f)) {
+      each([&](float x, int, int) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(cap_b * x)); });
+      mul = -2.f * cap_a;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) s[kb][qb] *= cs;
+      for (int qb = 0; qb < QB; ++qb) add[qb] = cap_a;
     }
-    if (f.slopes != nullptr) {
+    if constexpr (C::FORM == C::kBiased) {
+      float far[QB];  // the row's position less the lane's first key
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+      for (int qb = 0; qb < QB; ++qb) far[qb] = (float)(seq.kv - seq.n_q + row[qb] - n0 - 8 * h);
+      if (!final && n0 + BN <= pos0 + 1) {
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          const float far = (float)(seq.kv - seq.n_q + row[qb] - n0 - 32 * kb - 8 * h);
+        for (int qb = 0; qb < QB; ++qb) add[qb] = -(slope[qb] * far[qb]) * cs;
+        each([&](float x, int qb, int key) { return fmaf(slope[qb], (float)key, x); });
+      } else {
+        if (final) {
+          each([&](float x, int qb, int) { return fmaf(mul, x, add[qb]); });
+          mul = 1.f;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[kb][qb][r] -= slope[qb] * fabsf(far - (float)(16 * (r >> 3) + (r & 7)));
+          for (int qb = 0; qb < QB; ++qb) add[qb] = 0.f;
         }
+        each([&](float x, int qb, int key) { return fmaf(-slope[qb], fabsf(far[qb] - (float)key), x); });
+      }
     }
     if (masked) {
+      const PagedForms f = fresh_forms();
+      const uint32_t hidden = mul < 0.f ? 0x7f800000u : 0xff800000u;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -190,12 +223,15 @@ struct FormKeys {
           const uint32_t v = bits(f, qb, n0 + 32 * kb, pages) >> (8 * h);
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)v, 16 * (r >> 3) + (r & 7), 1);
-            s[kb][qb][r] = __uint_as_float((__float_as_uint(s[kb][qb][r]) & m) | (0xff800000u & ~m));
+            uint32_t m;  // (The builtin becomes an and, a compare and a select.)
+            asm("v_bfe_i32 %0, %1, %2, 1" : "=v"(m) : "v"(v), "i"(16 * (r >> 3) + (r & 7)));
+            float x = __uint_as_float((__float_as_uint(s[kb][qb][r]) & m) | (hidden & ~m));
+            asm volatile("" : "+v"(x));
+            s[kb][qb][r] = x;
           }
         }
     }
-    return 1.f;
+    return mul;
   }
 };
 
@@ -240,7 +276,7 @@ void fa_paged_fwd_kernel(PagedParams args) {
   constexpr int BC = C::NWAVES * 32 * QB;  // row-heads per block
   constexpr int R = BN / C::NWAVES;        // keys that a wave brings of a tile
   constexpr int E = C::E;
-  constexpr bool FORM = C::FORM;
+  constexpr bool FORM = C::FORM != 0;
   static_assert(C::KSPLIT == 1 && C::KA - C::VA <= 1, "a V tile is loaded with its K tile or one step later");
   static_assert(!C::SPLIT || BN == kSplitTile, "the host counts the line's units");
 
@@ -401,12 +437,11 @@ void fa_paged_fwd_kernel(PagedParams args) {
       // early.
       auto key_of = [&](int j) {
         if constexpr (FORM) {
-          const int at = st.last_first ? max(tiles - 1 - t0 - j, 0) : t0 + j;
+          const int at = C::FORM == C::kBiased ? max(tiles - 1 - t0 - j, 0) : t0 + j;
           return (at < blk.pre ? at : at + blk.gap) * BN;
         }
         return kb0 + j * BN;
       };
-      if constexpr (FORM) st.last_first = p.f.slopes != nullptr;
       auto lim_of = [&](int j) { return FORM && j >= nt ? 0 : kv_lim; };
       st.sk = s.kv;
       st.table = p.bt.block_table + (int64_t)b * p.bt.table_stride;
@@ -463,7 +498,7 @@ void fa_paged_fwd_kernel(PagedParams args) {
       }
       st.holes = __builtin_amdgcn_ballot_w64(hole) != 0;
       int n_plain = st.holes ? 0 : min(max(blk.plain - t0, 0), nt);
-      if constexpr (FORM) st.init_block(p, s, blk.row0, blk.row1);
+      if constexpr (FORM) st.init_block(p, s, blk.row0, blk.row1, st.cs);
       auto masked = [&](int j) {
         if constexpr (FORM)
           return st.holes || st.hides(key_of(j));
@@ -734,15 +769,15 @@ void fa_paged_fwd_kernel(PagedParams args) {
 // 64-key tiles at d = 64 over e4m3, whose 32-key tiles would be half a load per wave. Short: 32 columns per wave, two
 // workgroups per CU, where sequences have at most 128 row-heads or long blocks would not fill the chip (paged_many; bf16, d_qk 64
 // and 128: in 64-key tiles two waves per SIMD do not fit at d_qk = 192).
-template <int DQK, int DV, bool E4M3, bool SHORT, bool SPLIT, bool FORM = false>
+template <int DQK, int DV, bool E4M3, bool SHORT, bool SPLIT, int FORM = 0>
 struct PagedInstance {
   using C = Cfg<DQK, DV, 64, 4, 2, true, SPLIT, 1, 2, 6, 2, 4, 1, true, E4M3, FORM>;
 };
 template <bool SPLIT>
-struct PagedInstance<64, 64, false, false, SPLIT, false> {
+struct PagedInstance<64, 64, false, false, SPLIT, 0> {
   using C = Cfg<64, 64, 32, 4, 2, true, SPLIT, 2, 2, 4, 2, 4, 1, true>;
 };
-template <int DQK, int DV, bool SPLIT, bool FORM>
+template <int DQK, int DV, bool SPLIT, int FORM>
 struct PagedInstance<DQK, DV, false, true, SPLIT, FORM> {
   using C = Cfg<DQK, DV, 64, 4, 1, true, SPLIT, 2, DQK >= 128 ? 1 : 2, DQK >= 128 ? 2 : 6, 2, DQK >= 128 ? 3 : 4, 1, true, false, FORM>;
 };

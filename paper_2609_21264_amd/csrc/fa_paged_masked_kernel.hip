@@ -1,0 +1,10 @@
+// Attention of many new tokens per sequence over the paged cache with windows, prefixes and trees of drafted tokens.
+#include "fa_paged_forms_many.h"
+
+namespace fa {
+
+hipError_t launch_paged_many_masked(const PagedParams& p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream) {
+  return launch_form<1>(p, m, d_qk, e4m3, stream);
+}
+
+}  // namespace fa
