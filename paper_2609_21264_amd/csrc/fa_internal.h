@@ -265,7 +265,7 @@ struct TreeParams {
 hipError_t launch_tree_mask(TreeParams p, hipStream_t stream);
 
 // Sequences of one row of the grid (its second dimension; the third counts rows).
-constexpr int kMoveRows = 1 << 15;
+constexpr int kMoveRows = 65535;
 struct CompactParams {
   PagedCache c;
   PagedBatch bt;

@@ -241,11 +241,11 @@ void fa_paged_few_kernel(PagedParams p) {
       const int key = min(tile_of(t) * TILE + 32 * wave + 16 * u, s.kv - 1);
       return key < 0 ? -1 : scalar_load(table + (key >> p.c.page_shift));
     };
-    // Buffer over the slots of a half that hold keys below k_end: none where the page is none of the cache's.
-    auto half_rsrc = [&](const unsigned char* base, int64_t page_str, int64_t slot_str, int page, int key0) {
+    // Buffer over the slots of a half that hold keys below `lim`: none where the page is none of the cache's.
+    auto half_rsrc = [&](const unsigned char* base, int64_t page_str, int64_t slot_str, int page, int key0, int lim) {
       const bool ok = page >= 0 && page < p.c.n_pages;
       const int64_t at = ((int64_t)(ok ? page : 0) * page_str + (int64_t)(key0 & smask) * slot_str) * C::E;
-      const int rows = ok ? max(0, min(16, k_end - key0)) : 0;
+      const int rows = ok ? max(0, min(16, lim - key0)) : 0;
       const uint64_t a = reinterpret_cast<uint64_t>(base) + (uint64_t)at;
       return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
                    (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu)),
@@ -254,15 +254,16 @@ void fa_paged_few_kernel(PagedParams p) {
     auto issue = [&](int t, int pg0, int pg1) {
       const uint32_t l = (uint32_t)uniform((int)(ring_lds + (uint32_t)((unsigned)t % C::SLOTS) * C::WSLOT));
       const int key0 = tile_of(t) * TILE + 32 * wave;
+      const int lim = FORM && seen.gap > 0 && t < seen.pre ? min(s.pre, k_end) : k_end;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const u32x4 rs = half_rsrc(kbase, p.c.k_page, p.c.k_slot, u ? pg1 : pg0, key0 + 16 * u);
+        const u32x4 rs = half_rsrc(kbase, p.c.k_page, p.c.k_slot, u ? pg1 : pg0, key0 + 16 * u, lim);
 #pragma unroll
         for (int i = 0; i < C::KL; ++i) dma16_buffer<C::STREAM>(rs, koff[i], l + (u * C::KL + i) * 1024);
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const u32x4 rs = half_rsrc(vbase, p.c.v_page, p.c.v_slot, u ? pg1 : pg0, key0 + 16 * u);
+        const u32x4 rs = half_rsrc(vbase, p.c.v_page, p.c.v_slot, u ? pg1 : pg0, key0 + 16 * u, lim);
 #pragma unroll
         for (int i = 0; i < C::VL; ++i) dma16_buffer<C::STREAM>(rs, voff[i], l + C::K_BYTES + (u * C::VL + i) * 1024);
       }

@@ -117,9 +117,9 @@ __device__ __forceinline__ int lane_anew() {
 // + add (in units of log2; hidden keys -inf), with as few operations per score as the form allows:
 //   masked   nothing: mul = cs
 //   capped   s = 1 / (1 + 2^(b s)): mul = -2 a, add = a (capped() in fa_paged_device.h)
-//   biased   in a tile before all rows' positions s += slope / cs * (key - the lane's first key), one operation, and add
-//            takes the distance of that key; else s -= slope / cs * |p - key|; capped too, or where cs is next to
-//            0, the final score
+//   biased   in a tile before all rows' positions s -= slope / cs * (the lane's last key - key), one operation, and add
+//            takes the distance of that last key off (so that both are no more than the whole distance, and near keys lose
+//            nothing to far ones); else s -= slope / cs * |p - key|; capped too, or where cs is next to 0, the final score
 template <class C>
 struct FormKeys {
   static constexpr int BN = C::WBN, QB = C::QB, KB = BN / 32;
@@ -170,6 +170,7 @@ struct FormKeys {
     return v;
   }
   static constexpr int key_of(int kb, int r) { return 32 * kb + 16 * (r >> 3) + (r & 7); }  // from the lane's first key on
+  static constexpr int kLast = key_of(KB - 1, 15);
   // h: the half of the wave.
   template <class Scores>
   __device__ __forceinline__ float values(Scores& s, float (&add)[QB], int n0, bool masked, float cs, int h,
@@ -201,8 +202,8 @@ struct FormKeys {
       for (int qb = 0; qb < QB; ++qb) far[qb] = (float)(seq.kv - seq.n_q + row[qb] - n0 - 8 * h);
       if (!final && n0 + BN <= pos0 + 1) {
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) add[qb] = -(slope[qb] * far[qb]) * cs;
-        each([&](float x, int qb, int key) { return fmaf(slope[qb], (float)key, x); });
+        for (int qb = 0; qb < QB; ++qb) add[qb] = -(slope[qb] * (far[qb] - (float)kLast)) * cs;
+        each([&](float x, int qb, int key) { return fmaf(slope[qb], (float)(key - kLast), x); });
       } else {
         if (final) {
           each([&](float x, int qb, int) { return fmaf(mul, x, add[qb]); });
@@ -442,7 +443,10 @@ void fa_paged_fwd_kernel(PagedParams args) {
         }
         return kb0 + j * BN;
       };
-      auto lim_of = [&](int j) { return FORM && j >= nt ? 0 : kv_lim; };
+      auto lim_of = [&](int j) {
+        if (FORM && j >= nt) return 0;
+        return FORM && blk.gap > 0 && key_of(j) < blk.pre * BN ? s.pre : kv_lim;  // behind the prefix nothing is read
+      };
       st.sk = s.kv;
       st.table = p.bt.block_table + (int64_t)b * p.bt.table_stride;
       st.cs = p.cs;

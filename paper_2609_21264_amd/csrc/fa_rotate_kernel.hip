@@ -28,7 +28,8 @@ __global__ __launch_bounds__(kRotateThreads) void fa_rotate_kernel(RotateParams 
   const int ch = w.chunk(j);
   const int h0 = (int)blockIdx.y * p.heads, h1 = min(h0 + p.heads, p.h);
   for (int blk = (int)blockIdx.x; blk < p.n_blocks; blk += (int)gridDim.x) {
-    const int b = (int)fast_div((uint32_t)blk, p.m_per, p.sh_per), s = (blk - b * p.per) * lanes + row;
+    const int b = (int)fast_div((uint32_t)blk, p.m_per, p.sh_per);
+    const int64_t s = (int64_t)(blk - b * p.per) * lanes + row;
     if (s >= p.s) continue;
     F8 cs{}, sn{};
     if (turn) {
@@ -41,7 +42,7 @@ __global__ __launch_bounds__(kRotateThreads) void fa_rotate_kernel(RotateParams 
         if constexpr (AT)
           angles_at(cs, sn, i, p.pos, pos, table, p.rot, four);
         else
-          angles_of_row(cs, sn, i, table + (int64_t)s * p.rot, p.rot, four);
+          angles_of_row(cs, sn, i, table + s * p.rot, p.rot, four);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) sn.x[e] *= p.sign;

@@ -200,6 +200,53 @@ def test_steep_and_flat_scores(path):
 
 
 @pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("first", [255, 254, 191, 256])
+def test_steep_slopes_at_the_end_of_a_tile(path, first):
+    """The first row of a block stands on the last key of a tile, or about it: its own key, at distance 0, loses nothing to the
+    tile's far ones."""
+    for dims in DIMS:
+        bt = Batch([70, 1], [first + 70, first + 1], 4, 4, *dims, 16, seed=first)
+        kw = dict(slopes=torch.tensor([300.0, 40.0, 1.0, 0.01], device=DEV))
+        o, lse = bt.attend(scale=0.05, return_lse=True, path=path, **kw)
+        check(bt, o, lse, 0.05, what=str(dims), **kw)
+
+
+@pytest.mark.parametrize("path", ["few", "many"])
+def test_far_positions(path):
+    """A sequence of more than 2^24 keys (many of its pages are the same few): a window with slopes is that of its end alone."""
+    page, blocks = 1024, (1 << 14) + 3
+    g = torch.Generator().manual_seed(4)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    k, v = (torch.randn(8, 2, page, 64, generator=g).to(BF16).to(DEV) for _ in range(2))
+    q = torch.randn(40, 4, 64, generator=g).to(BF16).to(DEV)
+    table = (torch.arange(blocks, **i32) % 8)[None]
+    starts, out = torch.tensor([0, 40], **i32), []
+    for n, tab in ((blocks * page - 3, table), (3 * page - 3, table[:, blocks - 3:].contiguous())):
+        kw = dict(slopes=torch.tensor([0.5, 0.1, 0.02, 0.0], device=DEV), window=700)
+        a = fa.forward_paged(q, k, v, tab, torch.tensor([n], **i32), starts, max_q=40, return_lse=True, path=path, **kw)
+        b = fa.forward_paged(q, k, v, tab, torch.tensor([n], **i32), starts, max_q=40, return_lse=True, path=path, window=300, softcap=5.0)
+        out.append([*a, *b])
+    for x, y in zip(*out):  # cut over the chip in other places: P rounded and sums taken in another order, on both sides
+        x, y = f64(x), f64(y)
+        bar = 2.0 ** -19 * (1 + np.abs(y)) if x.ndim == 2 else 2 * (2.0 ** -8 + 2.0 ** -8 + 2.0 ** -17) * np.abs(f64(v)).max()
+        assert np.all(np.abs(x - y) <= bar)
+
+
+@pytest.mark.parametrize("path", ["few", "many"])
+def test_pages_behind_4_gib(path):
+    """The last pages of a cache of more than 2^32 bytes."""
+    bt = Batch([30, 40], [100, 70], 4, 2, 64, 64, 16, seed=12)
+    pages = (1 << 32) // (2 * 16 * 64 * 2) + 100
+    big = [torch.empty(pages, 2, 16, 64, dtype=BF16, device=DEV) for _ in range(2)]
+    for c, d in zip(big, (bt.d_k_cache, bt.d_v_cache)):
+        c[pages - bt.n_pages:] = d
+    table = torch.where(bt.d_table >= 0, bt.d_table + (pages - bt.n_pages), bt.d_table)
+    kw = dict(window=33, prefix_lens=torch.tensor([5, 9], dtype=torch.int32, device=DEV))
+    o, lse = fa.forward_paged(bt.d_q, *big, table, bt.d_kv_lens, bt.d_q_starts, max_q=40, scale=0.1, return_lse=True, path=path, **kw)
+    check(bt, o, lse, 0.1, **kw)
+
+
+@pytest.mark.parametrize("path", PATHS)
 def test_hidden_keys_do_not_reach_rows(path):
     """An infinity or a NaN in a hidden key reaches no row; one in a visible key makes that row's sum no number: O = 0, LSE =
     -inf."""
