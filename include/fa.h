@@ -394,8 +394,9 @@ fa_status_t fa_rotate(const void* X, void* Y, int B, int H, int S, int d, const 
                       const fa_positions_t* positions, const float* cos_sin, int n_pos, int rot_begin, int rot_dim,
                       int interleaved, int inverse, hipStream_t stream);
 
-/* Most 32-bit words of a row of a tree's mask (2048 drafted tokens). */
+/* Most 32-bit words of a row of a tree's mask (2048 drafted tokens), and most tokens of a tree of fa_tree_mask. */
 #define FA_TREE_WORDS 64
+#define FA_TREE_TOKENS 4096
 
 /*
  * fa_tree_mask -- mask and positions of trees of drafted tokens, as fa_fwd_paged_ex and fa_kv_append_at take them. The new tokens
@@ -404,8 +405,8 @@ fa_status_t fa_rotate(const void* X, void* Y, int B, int H, int S, int d, const 
  * parent is the last cached key. Bit j % 32 of word j / 32 of mask[t] is set where token j is token t itself or an ancestor (those
  * from 32 * words on have no bit); positions[t] = kv_lens[b] - n + its number of ancestors, for the n new ones.
  *   parents, mask, positions   int32 [T], 32-bit words [T] in rows mask_stride apart, int32 [T]
- * Rows of tokens that belong to no sequence are left as they were. Enqueues one kernel. Errors: sizes (FA_ERR_BAD_SHAPE: negative,
- * max_keys > 2^30, words outside [1, FA_TREE_WORDS], mask_stride < words), NULL arrays (FA_ERR_NULL_POINTER), alignment of 4 bytes
+ * Rows of tokens that belong to no sequence, or to one of more than FA_TREE_TOKENS new tokens, are left as they were. Enqueues one kernel.
+ * Errors: sizes (FA_ERR_BAD_SHAPE: negative, max_keys > 2^30, words outside [1, FA_TREE_WORDS], mask_stride < words), NULL arrays (FA_ERR_NULL_POINTER), alignment of 4 bytes
  * (FA_ERR_UNSUPPORTED). T == 0 or B == 0 returns FA_OK without a launch.
  */
 fa_status_t fa_tree_mask(const int* parents, const int* q_starts, const int* kv_lens, int B, int T, int max_keys, void* mask,

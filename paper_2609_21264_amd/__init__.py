@@ -740,7 +740,8 @@ def tree_mask(parents, q_starts, kv_lens, words: int = 1, max_keys: Optional[int
     sequence's new tokens, a smaller one than its own, or -1: it follows the cached keys. Returns (mask, positions): int32
     [T, ``words``], whose bit j % 32 of word j / 32 says whether the sequence's new token j is the token or one of its ancestors,
     for :func:`forward_paged`, and int32 [T], cached keys + ancestors, for :func:`kv_append`. ``words`` (up to 64) has to cover the
-    largest tree. Rows of tokens that belong to no sequence are left as they were, so new tensors' hold anything.
+    largest tree. Rows of tokens that belong to no sequence, or to one of more than 4096 new tokens, are left as they were, so
+    new tensors' hold anything.
 
     ``max_keys`` clamps ``kv_lens`` (default 2^30). The kernel is enqueued on ``stream`` (default: torch's current stream; new
     tensors belong to that stream); the call does not synchronise, and reads no array on the host."""

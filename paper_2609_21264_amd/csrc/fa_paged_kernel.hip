@@ -1,5 +1,5 @@
-// Paged key/value cache for gfx950: appending new tokens with their position rotation, and the attention
-// of few new tokens per sequence over the cache, split over its length and joined.
+// Paged key/value cache for gfx950: appending new tokens with their position rotation, the launches of the
+// attention of few new tokens per sequence (fa_paged_few.h), and the join of what either attention kernel splits.
 //
 // The cache holds keys and values in pages of `page_size` tokens; a block table names the pages of a
 // sequence in order. What a sequence holds (kv_lens), which of the packed tokens are its new ones
@@ -28,10 +28,11 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 //
 // One workgroup per packed token. A thread owns 16 bytes of a head, and with them the 16 bytes of their
 // partners where dim c turns with dim c + rot / 2, so that a pair is read, turned in fp32 and written by one
-// thread (Q may be rotated in place), and takes every kHeads-th head: the cos and sin of its dims stay in
+// thread (Q may be rotated in place), and takes every so many-th head: the cos and sin of its dims stay in
 // registers. What bounds it: the bytes of Q, K and V and the latency of the chain token -> sequence ->
 // page -> store, over which the loads of Q, K and V are in flight. 12 290 tokens of 32/8 heads, d = 128, bf16: 54 us in the
-// kernel, 5.7 TB/s read and written; 777 of 16/16 heads, d_qk = 192: 8 us; one token: 3.4 us.
+// kernel, 5.7 TB/s read and written; 777 of 16/16 heads, d_qk = 192: 8 us; one token: 3.4 us. By positions, 8 970 tokens of
+// 32/8 heads with three axes 50.8 us (4.3 TB/s), 26 tokens 5.0.
 
 // Sequence of packed token t: the last b with q_starts[b] <= t, by 64 probes at a time (one step up to 63
 // sequences, two up to 4 095). -1 if t comes before the first sequence; n_seq if behind the last.
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams 
   const bool held = page >= 0 && page < p.c.n_pages;
   const int64_t slot = pos & ((1 << p.c.page_shift) - 1);
 
-  // Q and K: thread (h0, j) takes task j of every kHeads-th head.
+  // Q and K: thread (h0, j) takes task j of every `lanes`-th head.
   const TurnTasks w(p.c.d_qk, p.rot, p.begin, p.inter);
   const int half = w.half, lanes = kAppendThreads / w.tasks;
   const int j = tid % w.tasks, h0 = tid / w.tasks;

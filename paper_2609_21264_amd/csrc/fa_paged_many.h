@@ -18,6 +18,13 @@
 // tokens 200-215 us by box (985-1 055 TFLOP/s; over an e4m3 cache 218, 969), a chunk of 1 024 over 9 000 keys, split, 140 (1 000) and its
 // part of the join; 32/32 heads, d_qk = 192, 512 tokens over 4 500 keys, split, 64 (700) and 13 for the join. Over contiguous keys the fused forward takes 1/1.03 to 1/1.06 of its time from 8 192 tokens
 // on, 1/1.10 at 2 048 (d = 128), 1/1.26 at 4 096 of 16/16 heads with d = 64.
+// With forms (FormKeys below): a tile's exact maximum is computed before its step, which takes the place of redoing tiles, so that
+// rows may see their first key anywhere and a bias may rise; tiles that all rows see whole are not masked; tiles between the
+// prefix and the block's first window are not visited; with slopes, tiles are taken from the last to the first, so that the
+// maximum comes early. Blocks of 128 row-heads, two waves on a SIMD, where there are such instances. 4 096 and 3 001
+// tokens, 32/8 heads, d = 128: masks 224 us where the plain kernel takes 209, caps 274, slopes 227, both 296; over e4m3 243, 319,
+// 272, 373 and 224; 16/16 heads, d_qk = 192: 144, 175, 160, 215 and 133; 32/32 heads, d = 64: 156, 196, 162, 246 and 138: what a cap
+// or a bias costs is VALU time (an exponential, a reciprocal and two operations more a score; one).
 // Internal; included by the kernel sources only.
 #pragma once
 

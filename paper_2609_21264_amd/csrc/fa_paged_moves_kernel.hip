@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "fa.h"
 #include "fa_fastdiv.h"
 #include "fa_paged_device.h"
 
@@ -13,38 +14,44 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ---- tree of drafted tokens ------------------------------------------------------------------------------
 //
-// A token sees itself and its ancestors: bit j of its row says so of the j-th new token of its sequence. A
-// workgroup per sequence, a thread per token, which walks up its parents (in LDS where they fit) and sets the bits of 64 tokens at
-// a time. A parent comes before its child, so a walk is never longer than the token's number; what is no such number
-// ends it (the root's -1 too). Bound by the chain of launch, lengths, parents and walk: a few us.
-constexpr int kTreeThreads = 256, kTreeLds = 2048;
+// A token sees itself and its ancestors: bit j of its row says so of the j-th new token of its sequence. A workgroup per
+// sequence, whose parents it keeps in LDS; a thread per token, which walks up its parents and, as their numbers only fall,
+// writes its row's words from the last to the first as it passes them. A parent comes before its child; what is no such number
+// (the root's -1 too) ends the walk. A chain of n tokens takes n / 2 steps a token, so a sequence of more than FA_TREE_TOKENS
+// tokens is left out, where a walk could go on for long. Bound by the chain of launch, lengths, parents and walk: 26 or 64 x 60
+// tokens 2.3 us.
+constexpr int kTreeThreads = 256;
 
 __global__ __launch_bounds__(kTreeThreads) void fa_tree_mask_kernel(TreeParams p) {
-  __shared__ int lds[kTreeLds];
+  __shared__ int parent[FA_TREE_TOKENS];
   for (int b = (int)blockIdx.x; b < p.bt.n_seq; b += (int)gridDim.x) {
     const PagedSeq s = load_seq(p.bt, b);
-    const bool staged = s.n_q <= kTreeLds;
-    const int* par = p.parents + s.q0;
-    if (staged) {
-      __syncthreads();  // the last sequence's walks are done
-      for (int i = threadIdx.x; i < s.n_q; i += kTreeThreads) lds[i] = par[i];
-      __syncthreads();
-    }
+    if (s.n_q > FA_TREE_TOKENS) continue;
+    __syncthreads();  // the last sequence's walks are done
+    for (int i = threadIdx.x; i < s.n_q; i += kTreeThreads) parent[i] = p.parents[s.q0 + i];
+    __syncthreads();
     for (int i = threadIdx.x; i < s.n_q; i += kTreeThreads) {
       uint32_t* row = p.mask + (int64_t)(s.q0 + i) * p.mask_stride;
-      int depth = 0;
-      for (int w = 0; w < p.words; w += 2) {
-        uint64_t bits = 0;
-        depth = -1;
-        for (int at = i; at >= 0;) {
-          ++depth;
-          if ((at >> 6) == (w >> 1)) bits |= uint64_t{1} << (at & 63);
-          const int up = staged ? lds[at] : par[at];
-          at = up < at ? up : -1;
+      int left = p.words, depth = -1;  // words from `left` on are written
+      uint32_t bits = 0;
+      auto down_to = [&](int w) {  // zeros in the words behind word w
+        for (; left > w + 1; --left) row[left - 1] = 0;
+      };
+      int word = i >> 5;
+      for (int at = i; at >= 0;) {
+        if ((at >> 5) != word) {
+          down_to(word);
+          if (word < p.words) row[word] = bits, left = word;
+          word = at >> 5, bits = 0;
         }
-        row[w] = (uint32_t)bits;
-        if (w + 1 < p.words) row[w + 1] = (uint32_t)(bits >> 32);
+        bits |= 1u << (at & 31);
+        ++depth;
+        const int up = parent[at];
+        at = up < at ? up : -1;
       }
+      down_to(word);
+      if (word < p.words) row[word] = bits, left = word;
+      down_to(-1);
       p.positions[s.q0 + i] = s.kv - s.n_q + depth;
     }
   }

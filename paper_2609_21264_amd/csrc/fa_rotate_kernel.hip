@@ -73,6 +73,7 @@ hipError_t launch_rotate(RotateParams p, hipStream_t stream) {
   p.m_per = f.m, p.sh_per = f.sh;
   p.heads = p.h < kRotateHeads ? p.h : kRotateHeads;
   while (p.heads > 1 && (int64_t)p.n_blocks * ((p.h + p.heads - 1) / p.heads) < kRotateWorkgroups) p.heads = (p.heads + 1) / 2;
+  if ((p.h - 1) / p.heads >= 65535) p.heads = (p.h - 1) / 65535 + 1;  // as many workgroups as the grid's second dimension holds
   constexpr int kMost = 1 << 20;
   const dim3 grid((unsigned)(p.n_blocks < kMost ? p.n_blocks : kMost), (unsigned)((p.h + p.heads - 1) / p.heads));
   void* args[] = {&p};

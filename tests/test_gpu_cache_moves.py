@@ -168,7 +168,8 @@ def tree_parents(n, seed, kind="random"):
 
 @pytest.mark.parametrize("sizes,words,kind", [([1], 1, "random"), ([26], 1, "random"), ([60, 0, 7, 64], 2, "random"), ([33] * 5, 2, "chain"),
                                               ([70], 2, "random"), ([64], 3, "chain"), ([2048], 64, "random"), ([2500, 3], 5, "chain"),
-                                              ([9] * 300, 1, "roots")], ids=str)
+                                              ([9] * 300, 1, "roots"), ([4096, 31], 64, "random"), ([4096], 2, "chain"),
+                                              ([97, 32, 31, 33, 64, 65], 4, "random")], ids=str)
 def test_tree_mask(sizes, words, kind):
     parents = [tree_parents(n, i, kind) for i, n in enumerate(sizes)]
     starts, lens = [2], []
@@ -193,6 +194,28 @@ def test_tree_mask(sizes, words, kind):
             want = [sum(1 << (j & 31) for j in path if j >> 5 == w) for w in range(words)]
             assert m[t].tolist() == want, (b, i)
             assert at[t] == lens[b] - n + len(path) - 1
+
+
+def test_tree_mask_of_too_long_a_sequence():
+    """Nothing is written for it, and the others have their rows."""
+    i32 = dict(dtype=torch.int32, device=DEV)
+    parents = torch.full((4097 + 3,), -1, **i32)
+    parents[4098:] = torch.tensor([0, 0])
+    mask, pos = torch.full((4100, 1), 9, **i32), torch.full((4100,), 9, **i32)
+    fa.tree_mask(parents, torch.tensor([0, 4097, 4100], **i32), torch.tensor([5000, 10], **i32), mask=mask, positions=pos)
+    assert bool((mask[:4097] == 9).all()) and bool((pos[:4097] == 9).all())
+    assert mask[4097:, 0].tolist() == [1, 3, 5] and pos[4097:].tolist() == [7, 8, 8]
+
+
+def test_rotate_many_heads():
+    """More heads than a dimension of the grid has workgroups for."""
+    g = torch.Generator().manual_seed(3)
+    x, table = torch.randn(2, 600001, 1, 8, generator=g).to(BF16), cos_sin_table(4, 8)
+    y = f64(fa.rotate(x.to(DEV), table.to(DEV), interleaved=True))
+    c, s = f64(table)[0, :4], f64(table)[0, 4:]
+    a, b = f64(x)[..., 0::2], f64(x)[..., 1::2]
+    near(y[..., 0::2], a * c - b * s, 10.0)
+    near(y[..., 1::2], b * c + a * s, 10.0)
 
 
 COMPACTS = [  # new, keys, kept, heads, dqk, dv, page, fp8, order
