@@ -531,6 +531,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM != 0, FormK
       // With forms the maximum is computed for every tile: rows may see their first key in any, and a bias makes maxima rise.
       // The reference follows where some row's has risen over it by more than 2^3 (in log2); O and the sums, which
       // hold the tiles before this one only after the step, follow at its end.
+      __builtin_amdgcn_s_setprio(0);
       mul = this->values(cur, add, n0, masked, cs, h, *this);
       float mt[QB];
       bool up = false;
@@ -552,6 +553,9 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM != 0, FormK
     } else {
       if (masked) mask_tile(cur, n0);
     }
+    // The SIMD's other wave may be at its values meanwhile: the matrix instructions' wave goes first (a prompt with slopes, d = 64
+    // 166 us -> 160, trees of 60 tokens 128 -> 125; capped prompts level).
+    if constexpr (C::FORM != 0) __builtin_amdgcn_s_setprio(1);
     float mref[QB], rs[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
