@@ -1,7 +1,7 @@
 /*
  * fa.h -- C ABI of the attention forward for AMD Instinct MI355X (gfx950): the fused kernel, its
  * split mode, the unfused layer-by-layer operators it is measured against, and a paged key/value cache: appending to
- * it and attention over it.
+ * it, attention over it (also with other masks and scores), drafted trees, and moves in it.
  *
  * Operation (the paper's scaled dot-product attention, Eq. (1), Sec. 2.1, replicated over heads):
  *
