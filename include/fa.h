@@ -404,7 +404,8 @@ fa_status_t fa_rotate(const void* X, void* Y, int B, int H, int S, int d, const 
  * parent is token parents[t] of the same sequence, one before it; anything else (-1) makes it a root, whose
  * parent is the last cached key. Bit j % 32 of word j / 32 of mask[t] is set where token j is token t itself or an ancestor (those
  * from 32 * words on have no bit); positions[t] = kv_lens[b] - n + its number of ancestors, for the n new ones.
- *   parents, mask, positions   int32 [T], 32-bit words [T] in rows mask_stride apart, int32 [T]
+ *   parents, mask, positions   int32 [T], 32-bit words [T] in rows mask_stride apart, int32 [T]; the outputs overlap neither each other
+ *               nor an input
  * Rows of tokens that belong to no sequence, or to one of more than FA_TREE_TOKENS new tokens, are left as they were. Enqueues one kernel.
  * Errors: sizes (FA_ERR_BAD_SHAPE: negative, max_keys > 2^30, words outside [1, FA_TREE_WORDS], mask_stride < words), NULL arrays (FA_ERR_NULL_POINTER), alignment of 4 bytes
  * (FA_ERR_UNSUPPORTED). T == 0 or B == 0 returns FA_OK without a launch.

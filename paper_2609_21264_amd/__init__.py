@@ -734,6 +734,21 @@ def _int32(name, t, dim, device):
         raise ValueError(f"the entries of {name} must lie one after the other")
 
 
+def _spans(t):
+    """Addresses of the first byte of a tensor of 4-byte elements and of that behind its last."""
+    n = t.numel() and 1 + sum((m - 1) * s for m, s in zip(t.shape, t.stride()))
+    return t.data_ptr(), t.data_ptr() + 4 * n
+
+
+def _apart_from(name, out, others):
+    """Refuses an output of 4-byte elements that shares memory with other tensors of such."""
+    a, z = _spans(out)
+    for other, t in others:
+        b, y = _spans(t)
+        if a < y and b < z:
+            raise ValueError(f"{name} must not overlap {other}")
+
+
 def tree_mask(parents, q_starts, kv_lens, words: int = 1, max_keys: Optional[int] = None, mask=None, positions=None, stream=None):
     """Mask and positions of trees of drafted tokens. ``parents`` int32 [T] (packed as in :func:`kv_append`, with its
     ``q_starts`` [B + 1] and ``kv_lens`` [B], which count the drafted tokens) holds the number of each token's parent among its
@@ -760,7 +775,8 @@ def tree_mask(parents, q_starts, kv_lens, words: int = 1, max_keys: Optional[int
     if elsewhere is not None:
         with elsewhere:
             return tree_mask(parents, q_starts, kv_lens, words, max_keys, mask, positions)
-    if mask is None:
+    new_mask = mask is None
+    if new_mask:
         mask = parents.new_empty((T, words))
     else:
         _int32("mask", mask, 2, device)
@@ -772,6 +788,9 @@ def tree_mask(parents, q_starts, kv_lens, words: int = 1, max_keys: Optional[int
         _int32("positions", positions, 1, device)
         if positions.shape != (T,):
             raise ValueError(f"positions must have shape {[T]}")
+        _apart_from("positions", positions, (("parents", parents), ("q_starts", q_starts), ("kv_lens", kv_lens), ("mask", mask)))
+    if not new_mask:
+        _apart_from("mask", mask, (("parents", parents), ("q_starts", q_starts), ("kv_lens", kv_lens)))
     st = _lib.load().fa_tree_mask(parents.data_ptr(), q_starts.data_ptr(), kv_lens.data_ptr(), B, T,
                                   1 << 30 if max_keys is None else int(max_keys), mask.data_ptr(), words,
                                   mask.stride(0) if T > 1 else words, positions.data_ptr(),
@@ -828,12 +847,8 @@ def kv_compact(k_cache, v_cache, block_table, kv_lens, q_starts, kept, n_kept, n
         _int32("new_lens", new_lens, 1, device)
         if new_lens.shape != (B,):
             raise ValueError(f"new_lens must have shape {[B]}")
-        at = new_lens.data_ptr()
-        for name, t in (("kv_lens", kv_lens), ("q_starts", q_starts), ("kept", kept), ("n_kept", n_kept),
-                        ("block_table", block_table)):
-            n = t.numel() and 1 + sum((m - 1) * s for m, s in zip(t.shape, t.stride()))
-            if at < t.data_ptr() + 4 * n and t.data_ptr() < at + 4 * B:
-                raise ValueError(f"new_lens must not overlap {name}")
+        _apart_from("new_lens", new_lens, (("kv_lens", kv_lens), ("q_starts", q_starts), ("kept", kept), ("n_kept", n_kept),
+                                           ("block_table", block_table)))
     st = _lib.load().fa_kv_compact(cache, batch, kept.data_ptr(), kept.stride(0) if B > 1 else 0, kept.shape[1],
                                    n_kept.data_ptr(), new_lens.data_ptr(), torch._C._cuda_getCurrentRawStream(device))
     if st != FA_OK:

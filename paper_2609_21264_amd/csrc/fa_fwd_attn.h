@@ -126,12 +126,16 @@ struct Ring {
   }
 };
 
+// Forms of an instance: keys may be hidden otherwise than by a last one, and scores be capped, or be biased by distance and perhaps
+// capped.
+constexpr int kFormNone = 0, kFormMasked = 1, kFormCapped = 2, kFormBiased = 3;
+
 // Compile-time configuration of one kernel instance: head dimensions, key-tile width, waves per
 // workgroup, 32-row query blocks per wave, causal masking, split mode, workgroups sharing a CU (OCC),
 // K and V fragments read ahead from LDS (KPF, VPF), K and V ring slots in LDS (NKR, NVR), and the
 // parts each key tile is split into between the waves (KSPLIT).
 template <int DQK_, int DV_, int BN_, int NWAVES_, int QB_, bool CAUSAL_, bool SPLIT_, int OCC_, int KPF_, int VPF_,
-          int NKR_, int NVR_, int KSPLIT_ = 1, bool PAGED_ = false, bool E4M3_ = false, int FORM_ = 0>
+          int NKR_, int NVR_, int KSPLIT_ = 1, bool PAGED_ = false, bool E4M3_ = false, int FORM_ = kFormNone>
 struct Cfg {
   static constexpr int DQK = DQK_, DV = DV_, BN = BN_, NWAVES = NWAVES_, QB = QB_;
   // KSPLIT = 2: the waves form two sets of NWAVES / 2 (RWAVES) that own the same query rows; set k
@@ -147,10 +151,7 @@ struct Cfg {
   // PAGED: the keys lie in pages (PagedKeys below), the columns of a wave are any rows of any of the group's heads,
   // and the last key each of them sees is in a register.
   static constexpr bool PAGED = PAGED_;
-  // FORM: keys may be hidden otherwise than by a last one (kMasked), and scores capped (kCapped) or biased by distance and
-  // perhaps capped (kBiased); by FormKeys, which the paged kernel defines.
-  static constexpr int kMasked = 1, kCapped = 2, kBiased = 3;
-  static constexpr int FORM = FORM_;
+  static constexpr int FORM = FORM_;  // by FormKeys, which the paged kernel defines
   // E4M3: K and V tiles are 8-bit. They stay so in LDS and are widened as fragments are read: K to bf16, V to fp16, with
   // P in fp16 too. The order of the dims in a score product follows the 16-byte reads of K: k-steps 2 m and 2 m + 1
   // take dims 32 m + 16 h + 0 .. 7 and + 8 .. 15 in lane half h.
@@ -224,7 +225,7 @@ template <class C>
 struct FormKeys;
 struct NoForms {};
 template <class C>
-struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM != 0, FormKeys<C>, NoForms> {
+struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM != kFormNone, FormKeys<C>, NoForms> {
   static constexpr int DQK = C::DQK, DV = C::DV, BN = C::WBN, QB = C::QB;  // BN: this wave's keys of a tile
   static constexpr int KS = DQK / 16;  // k-steps of the score product
   static constexpr int KB = BN / 32;   // 32-key blocks per tile
@@ -527,7 +528,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM != 0, FormK
                                        Issue&& issue) {
     float mul = cs, add[QB], alpha[QB];
     bool rescale = false;
-    if constexpr (C::FORM != 0) {
+    if constexpr (C::FORM != kFormNone) {
       // With forms the maximum is computed for every tile: rows may see their first key in any, and a bias makes maxima rise.
       // The reference follows where some row's has risen over it by more than 2^3 (in log2); O and the sums, which
       // hold the tiles before this one only after the step, follow at its end.
@@ -555,12 +556,12 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM != 0, FormK
     }
     // The SIMD's other wave may be at its values meanwhile: the matrix instructions' wave goes first (a prompt with slopes, d = 64
     // 166 us -> 160, trees of 60 tokens 128 -> 125; capped prompts level).
-    if constexpr (C::FORM != 0) __builtin_amdgcn_s_setprio(1);
+    if constexpr (C::FORM != kFormNone) __builtin_amdgcn_s_setprio(1);
     float mref[QB], rs[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       mref[qb] = m_run[qb] == -INFINITY ? 0.f : m_run[qb] - C::P_LOG2;
-      if constexpr (C::FORM != 0) mref[qb] -= add[qb];
+      if constexpr (C::FORM != kFormNone) mref[qb] -= add[qb];
       rs[qb] = 0.f;
     }
     // V fragments first: the step's first MFMAs are P V's, so with one wave per SIMD every LDS read in
@@ -599,7 +600,7 @@ struct Attn : PagedKeys<C::PAGED, C::QB>, std::conditional_t<C::FORM != 0, FormK
 #pragma unroll
     for (int e = elem_begin(NSL - 1); e < elem_end(NSL - 1); ++e)
       if (e & 1) pack_pair(e >> 1, ev[(e - 1) % 4], ev[e % 4], pk_new, rs);
-    if constexpr (C::FORM != 0) {
+    if constexpr (C::FORM != kFormNone) {
       if (rescale) {
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {

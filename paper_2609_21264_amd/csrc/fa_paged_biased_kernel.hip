@@ -4,7 +4,7 @@
 namespace fa {
 
 hipError_t launch_paged_many_biased(const PagedParams& p, const PagedMany& m, int d_qk, bool e4m3, hipStream_t stream) {
-  return launch_form<3>(p, m, d_qk, e4m3, stream);
+  return launch_form<kFormBiased>(p, m, d_qk, e4m3, stream);
 }
 
 }  // namespace fa

@@ -139,7 +139,7 @@ struct FormKeys {
   int pos0;             // biased: position of the block's first row
   __device__ __forceinline__ void init_row(const PagedParams& p, int qb, int r, int head) {
     row[qb] = r;
-    if constexpr (C::FORM == C::kBiased) slope[qb] = p.f.slopes[head] * kLog2e;
+    if constexpr (C::FORM == kFormBiased) slope[qb] = p.f.slopes[head] * kLog2e;
   }
   __device__ __forceinline__ void init_block(const PagedParams& p, const PagedSeq& s, int row0, int row1, float cs) {
     SeenRow first, last;
@@ -147,11 +147,11 @@ struct FormKeys {
     last.init(p.f, s, row1);
     whole0 = last.first, whole1 = first.last + 1;
     seq = s;
-    if constexpr (C::FORM != C::kMasked) {
+    if constexpr (C::FORM != kFormMasked) {
       cap_a = p.f.cap_a;
       cap_b = uniform(cap_factor(p.f, cs));
     }
-    if constexpr (C::FORM == C::kBiased) {
+    if constexpr (C::FORM == kFormBiased) {
       pos0 = first.pos;
       final = cap_a != 0.f || fabsf(cs) < 0x1p-60f;
 #pragma unroll
@@ -197,13 +197,13 @@ struct FormKeys {
             s[kb][qb][r] = x;
           }
     };
-    if (C::FORM == C::kCapped || (C::FORM == C::kBiased && cap_a != 0.f)) {
+    if (C::FORM == kFormCapped || (C::FORM == kFormBiased && cap_a != 0.f)) {
       each([&](float x, int, int) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(cap_b * x)); });
       mul = -2.f * cap_a;
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) add[qb] = cap_a;
     }
-    if constexpr (C::FORM == C::kBiased) {
+    if constexpr (C::FORM == kFormBiased) {
       float far[QB];  // the row's position less the lane's first key
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) far[qb] = (float)(seq.kv - seq.n_q + row[qb] - n0 - 8 * h);
@@ -284,7 +284,7 @@ void fa_paged_fwd_kernel(PagedParams args) {
   constexpr int BC = C::NWAVES * 32 * QB;  // row-heads per block
   constexpr int R = BN / C::NWAVES;        // keys that a wave brings of a tile
   constexpr int E = C::E;
-  constexpr bool FORM = C::FORM != 0;
+  constexpr bool FORM = C::FORM != kFormNone;
   static_assert(C::KSPLIT == 1 && C::KA - C::VA <= 1, "a V tile is loaded with its K tile or one step later");
   static_assert(!C::SPLIT || BN == kSplitTile, "the host counts the line's units");
 
@@ -445,7 +445,7 @@ void fa_paged_fwd_kernel(PagedParams args) {
       // early.
       auto key_of = [&](int j) {
         if constexpr (FORM) {
-          const int at = C::FORM == C::kBiased ? max(tiles - 1 - t0 - j, 0) : t0 + j;
+          const int at = C::FORM == kFormBiased ? max(tiles - 1 - t0 - j, 0) : t0 + j;
           return (at < blk.pre ? at : at + blk.gap) * BN;
         }
         return kb0 + j * BN;
@@ -781,17 +781,17 @@ void fa_paged_fwd_kernel(PagedParams args) {
 // workgroups per CU, where sequences have at most 128 row-heads or long blocks would not fill the chip (paged_many; bf16, d_qk 64
 // and 128: in 64-key tiles two waves per SIMD do not fit at d_qk = 192). With forms, which redo no tile, there are registers for a
 // second K fragment ahead at d = 128: prompts with masks 160.7 us -> 154.2, caps 253 -> 249, slopes 219 -> 211.
-template <int DQK, int DV, bool E4M3, bool SHORT, bool SPLIT, int FORM = 0>
+template <int DQK, int DV, bool E4M3, bool SHORT, bool SPLIT, int FORM = kFormNone>
 struct PagedInstance {
   using C = Cfg<DQK, DV, 64, 4, 2, true, SPLIT, 1, 2, 6, 2, 4, 1, true, E4M3, FORM>;
 };
 template <bool SPLIT>
-struct PagedInstance<64, 64, false, false, SPLIT, 0> {
+struct PagedInstance<64, 64, false, false, SPLIT, kFormNone> {
   using C = Cfg<64, 64, 32, 4, 2, true, SPLIT, 2, 2, 4, 2, 4, 1, true>;
 };
 template <int DQK, int DV, bool SPLIT, int FORM>
 struct PagedInstance<DQK, DV, false, true, SPLIT, FORM> {
-  using C = Cfg<DQK, DV, 64, 4, 1, true, SPLIT, 2, DQK >= 128 && FORM == 0 ? 1 : 2, DQK >= 128 ? 2 : 6, 2, DQK >= 128 ? 3 : 4, 1, true, false, FORM>;
+  using C = Cfg<DQK, DV, 64, 4, 1, true, SPLIT, 2, DQK >= 128 && FORM == kFormNone ? 1 : 2, DQK >= 128 ? 2 : 6, 2, DQK >= 128 ? 3 : 4, 1, true, false, FORM>;
 };
 
 template <class C>

@@ -207,6 +207,28 @@ def test_tree_mask_of_too_long_a_sequence():
     assert mask[4097:, 0].tolist() == [1, 3, 5] and pos[4097:].tolist() == [7, 8, 8]
 
 
+def test_outputs_that_overlap_are_refused():
+    i32 = dict(dtype=torch.int32, device=DEV)
+    buf = torch.zeros(64, **i32)
+    starts, lens = torch.tensor([0, 5], **i32), torch.tensor([9], **i32)
+    with pytest.raises(ValueError, match="positions must not overlap parents"):
+        fa.tree_mask(buf[:5], starts, lens, positions=buf[4:9])
+    with pytest.raises(ValueError, match="mask must not overlap parents"):
+        fa.tree_mask(buf[:5], starts, lens, mask=buf[:10:2, None])
+    with pytest.raises(ValueError, match="positions must not overlap mask"):
+        fa.tree_mask(buf[:5], starts, lens, mask=buf[10:15, None], positions=buf[12:17])
+    fa.tree_mask(buf[:5], starts, lens, mask=buf[10:15, None], positions=buf[15:20])
+    bt = Batch([3], [20], 2, 2, 64, 64, 16)
+    kept = torch.tensor([[0]], **i32)
+    with pytest.raises(ValueError, match="new_lens must not overlap kv_lens"):
+        fa.kv_compact(bt.d_k_cache, bt.d_v_cache, bt.d_table, bt.d_kv_lens, bt.d_q_starts, kept, kept[0], new_lens=bt.d_kv_lens)
+    x = torch.zeros(1, 4, 9, 64, dtype=BF16, device=DEV)
+    with pytest.raises(ValueError, match="x itself or lie before or behind"):
+        fa.rotate(x[:, :3], torch.zeros(9, 64, device=DEV), out=x[:, 1:])
+    with pytest.raises(ValueError, match="rows of out overlap"):
+        fa.rotate(x, torch.zeros(9, 64, device=DEV), out=torch.zeros(1, 1, 9, 64, dtype=BF16, device=DEV).expand(1, 4, 9, 64))
+
+
 def test_rotate_many_heads():
     """More heads than a dimension of the grid has workgroups for."""
     g = torch.Generator().manual_seed(3)
