@@ -723,15 +723,22 @@ def rotate(x, cos_sin, positions=None, pair_axes=None, rot_begin: int = 0, inter
 
 
 def _int32(name, t, dim, device):
-    """Checks a contiguous (in its last dimension) int32 tensor of `dim` dimensions on the device (None: on some GPU)."""
+    """Checks an int32 tensor of `dim` dimensions on the device (None: on some GPU) whose last dimension's entries lie one after
+    the other; its shape."""
     import torch
 
+    try:
+        shape, at = t.shape, t.get_device()
+        if (t.dtype == torch.int32 and len(shape) == dim and (at == device or device is None and at >= 0)
+                and (t.stride(-1) == 1 or shape[-1] <= 1)):
+            return shape
+    except (AttributeError, TypeError):
+        pass
     if not isinstance(t, torch.Tensor) or t.dim() != dim or t.dtype != torch.int32:
         raise ValueError(f"{name} must be a {dim}-d int32 torch tensor")
     if not t.is_cuda or (device is not None and t.get_device() != device):
         raise ValueError(f"{name} must be on {'a GPU' if device is None else f'the device cuda:{device}'}, not {t.device}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"the entries of {name} must lie one after the other")
+    raise ValueError(f"the entries of {name} must lie one after the other")
 
 
 def _spans(t):
@@ -762,12 +769,12 @@ def tree_mask(parents, q_starts, kv_lens, words: int = 1, max_keys: Optional[int
     tensors belong to that stream); the call does not synchronise, and reads no array on the host."""
     import torch
 
-    _int32("parents", parents, 1, None)
+    (T,) = _int32("parents", parents, 1, None)
     device = parents.get_device()
-    _int32("q_starts", q_starts, 1, device)
-    _int32("kv_lens", kv_lens, 1, device)
-    T, B, words = parents.shape[0], kv_lens.shape[0], int(words)
-    if q_starts.shape[0] != B + 1:
+    (starts,) = _int32("q_starts", q_starts, 1, device)
+    (B,) = _int32("kv_lens", kv_lens, 1, device)
+    words = int(words)
+    if starts != B + 1:
         raise ValueError(f"q_starts [B + 1] and kv_lens [B] do not agree: {list(q_starts.shape)}, {list(kv_lens.shape)}")
     if not 1 <= words <= FA_TREE_WORDS:
         raise ValueError(f"words must be 1 to {FA_TREE_WORDS}, not {words}")
@@ -779,14 +786,12 @@ def tree_mask(parents, q_starts, kv_lens, words: int = 1, max_keys: Optional[int
     if new_mask:
         mask = parents.new_empty((T, words))
     else:
-        _int32("mask", mask, 2, device)
-        if mask.shape != (T, words) or (T > 1 and mask.stride(0) < words):
+        if _int32("mask", mask, 2, device) != (T, words) or (T > 1 and mask.stride(0) < words):
             raise ValueError(f"mask must have shape {[T, words]}, its rows apart")
     if positions is None:
         positions = parents.new_empty(T)
     else:
-        _int32("positions", positions, 1, device)
-        if positions.shape != (T,):
+        if _int32("positions", positions, 1, device) != (T,):
             raise ValueError(f"positions must have shape {[T]}")
         _apart_from("positions", positions, (("parents", parents), ("q_starts", q_starts), ("kv_lens", kv_lens), ("mask", mask)))
     if not new_mask:
@@ -804,20 +809,29 @@ def _cache(k_cache, v_cache, device):
     """Checks a paged cache alone; its C description."""
     import torch
 
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        if not isinstance(t, torch.Tensor) or t.dim() != 4 or t.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
-            raise ValueError(f"{name} must be a 4-d torch tensor [pages, heads, page_size, d], bfloat16 or float8_e4m3fn")
-        if t.get_device() != device:
-            raise ValueError(f"{name} must be on the device cuda:{device}, not {t.device}")
-        if t.stride(3) != 1:
-            raise ValueError(f"the elements of a head of {name} must lie one after the other")
-    if k_cache.dtype != v_cache.dtype or k_cache.shape[:3] != v_cache.shape[:3]:
+    try:
+        (pages, hkv, page, dqk), (kp, kh, ks, kd) = k_cache.shape, k_cache.stride()
+        (vpages, vhkv, vpage, dv), (vp, vh, vs, vd) = v_cache.shape, v_cache.stride()
+        fp8 = k_cache.dtype == torch.float8_e4m3fn
+        ok = ((fp8 or k_cache.dtype == torch.bfloat16) and v_cache.dtype == k_cache.dtype and k_cache.get_device() == device
+              and v_cache.get_device() == device and kd == 1 and vd == 1 and (vpages, vhkv, vpage) == (pages, hkv, page))
+    except (AttributeError, TypeError, ValueError):
+        ok = False
+    if not ok:
+        for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+            if not isinstance(t, torch.Tensor) or t.dim() != 4 or t.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+                raise ValueError(f"{name} must be a 4-d torch tensor [pages, heads, page_size, d], bfloat16 or float8_e4m3fn")
+            if t.get_device() != device:
+                raise ValueError(f"{name} must be on the device cuda:{device}, not {t.device}")
+            if t.stride(3) != 1:
+                raise ValueError(f"the elements of a head of {name} must lie one after the other")
         raise ValueError("k_cache and v_cache must agree in type, pages, heads and page size")
-    (pages, hkv, page, dqk), dv = k_cache.shape, v_cache.shape[3]
-    (kp, kh, ks, _), (vp, vh, vs, _) = ([0 if n <= 1 and i < 2 else s for i, (s, n) in enumerate(zip(t.stride(), t.shape))]
-                                        for t in (k_cache, v_cache))
+    if pages <= 1:  # the stride of a dimension of one means nothing
+        kp = vp = 0
+    if hkv <= 1:
+        kh = vh = 0
     return PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), None, None, kp, kh, ks, vp, vh, vs, pages, page, hkv, dqk, dv,
-                      1 if k_cache.dtype == torch.float8_e4m3fn else 0)
+                      1 if fp8 else 0)
 
 
 def kv_compact(k_cache, v_cache, block_table, kv_lens, q_starts, kept, n_kept, new_lens=None, stream=None):
@@ -833,9 +847,8 @@ def kv_compact(k_cache, v_cache, block_table, kv_lens, q_starts, kept, n_kept, n
     import torch
 
     device, cache, batch, B, *_ = _paged(k_cache, v_cache, block_table, kv_lens, q_starts, None, None, 0, torch)
-    _int32("kept", kept, 2, device)
-    _int32("n_kept", n_kept, 1, device)
-    if kept.shape[0] != B or n_kept.shape[0] != B:
+    rows, most = _int32("kept", kept, 2, device)
+    if rows != B or _int32("n_kept", n_kept, 1, device) != (B,):
         raise ValueError(f"kept [B, m] and n_kept [B] do not agree with B = {B}: {list(kept.shape)}, {list(n_kept.shape)}")
     elsewhere = _elsewhere(stream, device)
     if elsewhere is not None:
@@ -844,12 +857,11 @@ def kv_compact(k_cache, v_cache, block_table, kv_lens, q_starts, kept, n_kept, n
     if new_lens is None:
         new_lens = kv_lens.new_empty(B)
     else:
-        _int32("new_lens", new_lens, 1, device)
-        if new_lens.shape != (B,):
+        if _int32("new_lens", new_lens, 1, device) != (B,):
             raise ValueError(f"new_lens must have shape {[B]}")
         _apart_from("new_lens", new_lens, (("kv_lens", kv_lens), ("q_starts", q_starts), ("kept", kept), ("n_kept", n_kept),
                                            ("block_table", block_table)))
-    st = _lib.load().fa_kv_compact(cache, batch, kept.data_ptr(), kept.stride(0) if B > 1 else 0, kept.shape[1],
+    st = _lib.load().fa_kv_compact(cache, batch, kept.data_ptr(), kept.stride(0) if B > 1 else 0, most,
                                    n_kept.data_ptr(), new_lens.data_ptr(), torch._C._cuda_getCurrentRawStream(device))
     if st != FA_OK:
         _raise("fa_kv_compact", st)
@@ -864,17 +876,16 @@ def kv_copy(k_cache, v_cache, src, dst, stream=None):
     synchronise, and reads no array on the host."""
     import torch
 
-    _int32("src", src, 1, None)
+    (n,) = _int32("src", src, 1, None)
     device = src.get_device()
-    _int32("dst", dst, 1, device)
-    if src.shape != dst.shape:
+    if _int32("dst", dst, 1, device) != (n,):
         raise ValueError(f"src and dst must have as many pages: {list(src.shape)}, {list(dst.shape)}")
     cache = _cache(k_cache, v_cache, device)
     elsewhere = _elsewhere(stream, device)
     if elsewhere is not None:
         with elsewhere:
             return kv_copy(k_cache, v_cache, src, dst)
-    st = _lib.load().fa_kv_copy(cache, src.data_ptr(), dst.data_ptr(), src.shape[0], torch._C._cuda_getCurrentRawStream(device))
+    st = _lib.load().fa_kv_copy(cache, src.data_ptr(), dst.data_ptr(), n, torch._C._cuda_getCurrentRawStream(device))
     if st != FA_OK:
         _raise("fa_kv_copy", st)
 
@@ -970,31 +981,30 @@ def _scores(softcap, slopes, window, prefix_lens, tree_mask, T, hq, B, device):
     """The C description of how scores are changed and keys hidden."""
     import torch
 
-    s = PagedScores()
+    cap = wide = words = stride = 0
+    sp = pp = mp = None
     if softcap is not None:
-        s.softcap = softcap
         if not 0 < softcap <= FA_MAX_SOFTCAP:
             raise ValueError(f"softcap must be above 0 and at most {FA_MAX_SOFTCAP:g}, not {softcap}")
+        cap = softcap
     if window is not None:
         if not 0 < window < 1 << 31:
             raise ValueError(f"window must be at least 1 key, not {window}")
-        s.window = window
+        wide = window
     if slopes is not None:
         if (not isinstance(slopes, torch.Tensor) or slopes.dtype != torch.float32 or slopes.shape != (hq,)
                 or not slopes.is_contiguous()):
             raise ValueError(f"slopes must be a contiguous float32 tensor [{hq}]")
         if slopes.get_device() != device:
             raise ValueError(f"slopes must be on the cache's device cuda:{device}, not {slopes.device}")
-        s.slopes = slopes.data_ptr()
+        sp = slopes.data_ptr()
     if prefix_lens is not None:
-        _int32("prefix_lens", prefix_lens, 1, device)
-        if prefix_lens.shape != (B,):
+        if _int32("prefix_lens", prefix_lens, 1, device) != (B,):
             raise ValueError(f"prefix_lens must have shape {[B]}, not {list(prefix_lens.shape)}")
-        s.prefix_lens = prefix_lens.data_ptr()
+        pp = prefix_lens.data_ptr()
     if tree_mask is not None:
-        _int32("tree_mask", tree_mask, 2, device)
-        if tree_mask.shape[0] != T or not 1 <= tree_mask.shape[1] <= FA_TREE_WORDS:
+        rows, words = _int32("tree_mask", tree_mask, 2, device)
+        if rows != T or not 1 <= words <= FA_TREE_WORDS:
             raise ValueError(f"tree_mask must have shape [{T}, 1 to {FA_TREE_WORDS}], not {list(tree_mask.shape)}")
-        s.tree_mask, s.mask_words = tree_mask.data_ptr(), tree_mask.shape[1]
-        s.mask_stride = tree_mask.stride(0) if T > 1 else tree_mask.shape[1]
-    return s
+        mp, stride = tree_mask.data_ptr(), tree_mask.stride(0) if T > 1 else words
+    return PagedScores(cap, wide, sp, pp, mp, stride, words)
