@@ -627,13 +627,13 @@ def _positions(positions, pair_axes, tokens, rot, device):
     import torch
 
     n = len(tokens)
-    if (not isinstance(positions, torch.Tensor) or positions.dtype != torch.int32 or positions.dim() not in (n, n + 1)
-            or positions.shape[:n] != tokens):
+    if (not isinstance(positions, torch.Tensor) or positions.dtype != torch.int32 or (shape := positions.shape)[:n] != tokens
+            or len(shape) > n + 1):
         raise ValueError(f"positions must be an int32 tensor of shape {list(tokens)} or {list(tokens)} + [axes]")
     if positions.get_device() != device:
         raise ValueError(f"positions must be on the device cuda:{device}, not {positions.device}")
     strides = positions.stride()
-    axes, axis = (positions.shape[n], strides[n]) if positions.dim() > n else (1, 0)
+    axes, axis = (shape[n], strides[n]) if len(shape) > n else (1, 0)
     where = None
     if pair_axes is not None:
         if (not isinstance(pair_axes, torch.Tensor) or pair_axes.dtype != torch.uint8 or pair_axes.shape != (rot // 2,)
@@ -657,6 +657,17 @@ def _apart(shape, strides):
     return True
 
 
+def _rotate_strides(name, strides, B, H, S, d):
+    """Strides of batches, heads and tokens of a [B, H, S, d] or [S, H, d] tensor, 0 for a dimension of one."""
+    if len(strides) == 4:
+        b, h, s, e = strides
+    else:
+        b, (s, h, e) = 0, strides
+    if e != 1 and d > 1:
+        raise ValueError(f"the elements of a head of {name} must lie one after the other")
+    return (b if B > 1 else 0, h if H > 1 else 0, s if S > 1 else 0)
+
+
 def rotate(x, cos_sin, positions=None, pair_axes=None, rot_begin: int = 0, interleaved: bool = False, inverse: bool = False,
            out=None, stream=None):
     """The position rotation of :func:`kv_append` for queries or keys x [B, H, S, d] or [T, H, d] (bf16, any strides of
@@ -674,28 +685,23 @@ def rotate(x, cos_sin, positions=None, pair_axes=None, rot_begin: int = 0, inter
         raise ValueError("x must be a bfloat16 torch tensor [B, H, S, d] or [T, H, d]")
     if not x.is_cuda:
         raise ValueError("x must be on a GPU")
-    device = x.get_device()
-
-    def strides(name, t):
-        if t.stride(-1) != 1 and t.shape[-1] > 1:
-            raise ValueError(f"the elements of a head of {name} must lie one after the other")
-        st = [s if n > 1 else 0 for s, n in zip(t.stride(), t.shape)]
-        return st[:3] if t.dim() == 4 else [0, st[1], st[0]]
-
-    if x.dim() == 4:
-        B, H, S, d = x.shape
+    device, shape = x.get_device(), x.shape
+    if len(shape) == 4:
+        B, H, S, d = shape
         tokens = (B, S)
     else:
-        B, (S, H, d) = 1, x.shape
+        B, (S, H, d) = 1, shape
         tokens = (S,)
+    xs = _rotate_strides("x", x.stride(), B, H, S, d)
     if (not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2 or cos_sin.dtype != torch.float32
             or not cos_sin.is_contiguous()):
         raise ValueError("cos_sin must be a contiguous float32 tensor [positions, rotated dims]")
     if cos_sin.get_device() != device:
         raise ValueError(f"cos_sin must be on x's device {x.device}, not {cos_sin.device}")
+    n_pos, rot = cos_sin.shape
     at = None
     if positions is not None:
-        at = _positions(positions, pair_axes, tokens, cos_sin.shape[1], device)
+        at = _positions(positions, pair_axes, tokens, rot, device)
     elif pair_axes is not None:
         raise ValueError("pair_axes goes with positions")
     elsewhere = _elsewhere(stream, device)
@@ -703,20 +709,24 @@ def rotate(x, cos_sin, positions=None, pair_axes=None, rot_begin: int = 0, inter
         with elsewhere:
             return rotate(x, cos_sin, positions, pair_axes, rot_begin, interleaved, inverse, out)
     if out is None:
-        out = x.new_empty(x.shape)
-    elif out is not x:
-        if not isinstance(out, torch.Tensor) or out.shape != x.shape or out.dtype != x.dtype or out.get_device() != device:
-            raise ValueError(f"out must be a bfloat16 tensor {list(x.shape)} on {x.device}")
-        n = x.numel() and 1 + sum((m - 1) * s for m, s in zip(x.shape, x.stride()))
-        m = out.numel() and 1 + sum((m - 1) * s for m, s in zip(out.shape, out.stride()))
-        x0, o0 = x.data_ptr(), out.data_ptr()
-        if x0 < o0 + 2 * m and o0 < x0 + 2 * n and (x0, strides("x", x)) != (o0, strides("out", out)):
-            raise ValueError("out must be x itself or lie before or behind it in memory")
-    if not _apart(out.shape, out.stride()):
-        raise ValueError("rows of out overlap")
-    st = _lib.load().fa_rotate(x.data_ptr(), out.data_ptr(), B, H, S, d, RotateStrides(*strides("x", x), *strides("out", out)),
-                               at, cos_sin.data_ptr(), cos_sin.shape[0], int(rot_begin), cos_sin.shape[1],
-                               1 if interleaved else 0, 1 if inverse else 0, torch._C._cuda_getCurrentRawStream(device))
+        out = x.new_empty(shape)
+        ys = (H * S * d, S * d, d) if len(shape) == 4 else (0, d, H * d)
+    else:
+        if out is not x and (not isinstance(out, torch.Tensor) or out.shape != shape or out.dtype != x.dtype
+                             or out.get_device() != device):
+            raise ValueError(f"out must be a bfloat16 tensor {list(shape)} on {x.device}")
+        ys = xs if out is x else _rotate_strides("out", out.stride(), B, H, S, d)
+        if out is not x and x.numel() > 0:
+            # Bytes from the first element to behind the last, of x and of out.
+            x0, o0 = x.data_ptr(), out.data_ptr()
+            x1, o1 = (a + 2 * ((B - 1) * b + (H - 1) * h + (S - 1) * s + d) for a, (b, h, s) in ((x0, xs), (o0, ys)))
+            if x0 < o1 and o0 < x1 and (x0, xs) != (o0, ys):
+                raise ValueError("out must be x itself or lie before or behind it in memory")
+        if not _apart((B, H, S, d), (*ys, 1)):
+            raise ValueError("rows of out overlap")
+    st = _lib.load().fa_rotate(x.data_ptr(), out.data_ptr(), B, H, S, d, RotateStrides(*xs, *ys), at, cos_sin.data_ptr(), n_pos,
+                               int(rot_begin), rot, 1 if interleaved else 0, 1 if inverse else 0,
+                               torch._C._cuda_getCurrentRawStream(device))
     if st != FA_OK:
         _raise("fa_rotate", st)
     return out
