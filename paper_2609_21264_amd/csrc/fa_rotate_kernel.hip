@@ -27,9 +27,10 @@ __global__ __launch_bounds__(kRotateThreads) void fa_rotate_kernel(RotateParams 
   if (!turn && p.in_place) return;
   const int ch = w.chunk(j);
   const int h0 = (int)blockIdx.y * p.heads, h1 = min(h0 + p.heads, p.h);
-  for (int blk = (int)blockIdx.x; blk < p.n_blocks; blk += (int)gridDim.x) {
-    const int b = (int)fast_div((uint32_t)blk, p.m_per, p.sh_per);
-    const int64_t s = (int64_t)(blk - b * p.per) * lanes + row;
+  // Unsigned: a step past the last block may lead behind 2^31.
+  for (uint32_t blk = blockIdx.x; blk < (uint32_t)p.n_blocks; blk += gridDim.x) {
+    const int b = (int)fast_div(blk, p.m_per, p.sh_per);
+    const int64_t s = (int64_t)((int)blk - b * p.per) * lanes + row;
     if (s >= p.s) continue;
     F8 cs{}, sn{};
     if (turn) {
