@@ -24,8 +24,9 @@ constexpr int kTreeThreads = 256;
 
 __global__ __launch_bounds__(kTreeThreads) void fa_tree_mask_kernel(TreeParams p) {
   __shared__ int parent[FA_TREE_TOKENS];
-  for (int b = (int)blockIdx.x; b < p.bt.n_seq; b += (int)gridDim.x) {
-    const PagedSeq s = load_seq(p.bt, b);
+  // Unsigned: a step past the last sequence may lead behind 2^31.
+  for (uint32_t b = blockIdx.x; b < (uint32_t)p.bt.n_seq; b += gridDim.x) {
+    const PagedSeq s = load_seq(p.bt, (int)b);
     if (s.n_q > FA_TREE_TOKENS) continue;
     __syncthreads();  // the last sequence's walks are done
     for (int i = threadIdx.x; i < s.n_q; i += kTreeThreads) parent[i] = p.parents[s.q0 + i];
