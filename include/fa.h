@@ -424,7 +424,8 @@ fa_status_t fa_tree_mask(const int* parents, const int* q_starts, const int* kv_
  *   kv_lens_out     int32 [B], apart from all inputs
  * Nothing moves to or from a page that is not there. A cache whose layers lie in one buffer, [n_pages][layers][Hkv] .., closes up in
  * one call with layers * Hkv heads. Enqueues one kernel. Errors: as fa_kv_append's of cache and batch, in that order (sizes
- * also: max_kept or kept_stride < 0, Hkv >= 2^25). B == 0 returns FA_OK without a launch.
+ * also: max_kept or kept_stride < 0, Hkv >= 2^25; behind what is supported: B * ceil(Hkv * (d_qk + d_v) * element bytes /
+ * 4096) >= 2^24). B == 0 returns FA_OK without a launch.
  */
 fa_status_t fa_kv_compact(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const int* kept, long long kept_stride,
                           int max_kept, const int* n_kept, int* kv_lens_out, hipStream_t stream);

@@ -664,6 +664,9 @@ fa_status_t fa_kv_compact(const fa_paged_cache_t* cache, const fa_paged_batch_t*
   if (max_kept < 0 || kept_stride < 0 || kept_stride > (1ll << 40) || cache->Hkv > INT_MAX / 64) return FA_ERR_BAD_SHAPE;
   st = check_paged_support(cache);
   if (st != FA_OK) return st;
+  // Workgroups of all sequences, as many as of a copy at most: the kernel's number of a sequence stays far below 2^31.
+  const int elem = cache->type == FA_CACHE_E4M3 ? 1 : 2;
+  if (fa::kv_compact_blocks(cache->Hkv, cache->d_qk, cache->d_v, elem) * batch->B >= 1 << 24) return FA_ERR_BAD_SHAPE;
   if (batch->B == 0) return FA_OK;
   if (!paged_pointers(cache, batch) || (max_kept > 0 && kept == nullptr) || n_kept == nullptr || kv_lens_out == nullptr)
     return FA_ERR_NULL_POINTER;
@@ -674,7 +677,7 @@ fa_status_t fa_kv_compact(const fa_paged_cache_t* cache, const fa_paged_batch_t*
   paged_view(cache, batch, &p.c, &p.bt);
   p.bt.n_tokens = INT_MAX;
   p.kept = kept, p.n_kept = n_kept, p.kept_stride = kept_stride, p.max_kept = max_kept;
-  p.elem = cache->type == FA_CACHE_E4M3 ? 1 : 2;
+  p.elem = elem;
   p.lens_out = kv_lens_out;
   return fa::launch_kv_compact(p, stream) == hipSuccess ? FA_OK : FA_ERR_HIP;
 }

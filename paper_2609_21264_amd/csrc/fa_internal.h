@@ -276,6 +276,8 @@ struct CompactParams {
   int* lens_out;          // [n_seq]
   uint32_t k_chunks, v_chunks, m_k, sh_k, m_v, sh_v;  // filled by launch_kv_compact: 16-byte chunks of a row
 };
+// Workgroups of a sequence, one at least.
+int64_t kv_compact_blocks(int hkv, int d_qk, int d_v, int elem);
 hipError_t launch_kv_compact(CompactParams p, hipStream_t stream);
 
 // K or V of a page as heads of rows of `run` 16-byte chunks; strides in bytes.

@@ -159,13 +159,17 @@ hipError_t launch_tree_mask(TreeParams p, hipStream_t stream) {
                          dim3(kTreeThreads), args, 0, stream);
 }
 
+int64_t kv_compact_blocks(int hkv, int d_qk, int d_v, int elem) {
+  const int64_t chunks = (int64_t)hkv * ((d_qk + d_v) * elem / 16);  // of 16 bytes; below 2^31 by the host's check
+  return chunks == 0 ? 1 : (chunks + kMoveThreads - 1) / kMoveThreads;
+}
+
 hipError_t launch_kv_compact(CompactParams p, hipStream_t stream) {
   p.k_chunks = (uint32_t)(p.c.d_qk * p.elem / 16), p.v_chunks = (uint32_t)(p.c.d_v * p.elem / 16);
   const FastDiv k = make_fastdiv(p.k_chunks), v = make_fastdiv(p.v_chunks);
   p.m_k = k.m, p.sh_k = k.sh, p.m_v = v.m, p.sh_v = v.sh;
-  const int64_t chunks = (int64_t)p.c.hkv * (p.k_chunks + p.v_chunks);  // below 2^31 by the host's check
-  const int n = p.bt.n_seq;
-  const dim3 grid((unsigned)(chunks == 0 ? 1 : (chunks + kMoveThreads - 1) / kMoveThreads), (unsigned)(n < kMoveRows ? n : kMoveRows),
+  const int n = p.bt.n_seq;  // below 2^24, with the grid's first dimension
+  const dim3 grid((unsigned)kv_compact_blocks(p.c.hkv, p.c.d_qk, p.c.d_v, p.elem), (unsigned)(n < kMoveRows ? n : kMoveRows),
                   (unsigned)((n + kMoveRows - 1) / kMoveRows));
   void* args[] = {&p};
   return hipLaunchKernel(reinterpret_cast<const void*>(&fa_kv_compact_kernel), grid, dim3(kMoveThreads), args, 0, stream);

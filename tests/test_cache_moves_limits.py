@@ -1,0 +1,17 @@
+"""Counts at the borders of what the moves around the paged cache launch, on the host (no GPU needed)."""
+
+import pytest
+
+import paper_2609_21264_amd as fa
+from test_cache_moves_host import NULL, SHAPE, batch, cache, compact
+
+
+@pytest.mark.parametrize("Hkv,blocks", [(1, 1), (8, 1), (9, 2), (4096, 512)])
+def test_compact_of_more_workgroups_than_a_copy(Hkv, blocks):
+    """A workgroup moves 256 chunks of 16 bytes of a sequence's tokens, a token's K and V in d = 128, bf16 being 32 a head:
+    fewer than 2^24 workgroups in all, as in a copy of pages. Behind 2^31 the kernel's number of a sequence would wrap."""
+    c = cache(Hkv=Hkv, k_page=Hkv * 16 * 128, v_page=Hkv * 16 * 128)
+    most = (2 ** 24 - 1) // blocks
+    assert compact(c, batch(B=most), n_kept=None) == NULL  # sizes are right
+    for B in (most + 1, 2 ** 30, 2 ** 31 - 32768, 2 ** 31 - 65, 2 ** 31 - 2):
+        assert compact(c, batch(B=B), n_kept=None) == SHAPE, B
