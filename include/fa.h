@@ -342,7 +342,7 @@ typedef struct {
  * or V. Enqueues one kernel.
  *
  * Errors, in this order: cache, batch, strides or cos_sin description NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE: negative
- * (table_stride too), Hkv <= 0 with T > 0, Hq not a multiple of Hkv, max_blocks * page_size > 2^30, T * Hq >= 2^31, n_pos too small, the rotated dims
+ * (table_stride too), Hkv <= 0 with T > 0, Hq not a multiple of Hkv, max_blocks * page_size > 2^30, T * Hq >= 2^31, B > 2^31 - 65, n_pos too small, the rotated dims
  * outside [0, d_qk)); head dimensions, page size, type or rotation not supported (FA_ERR_UNSUPPORTED); a NULL buffer that
  * has elements (FA_ERR_NULL_POINTER); alignment (FA_ERR_UNSUPPORTED: 16 bytes for buffers and strides, 4 for the int
  * and scale arrays); cache strides negative, too large, or letting two elements of the cache overlap (FA_ERR_BAD_SHAPE).

@@ -239,7 +239,8 @@ fa_status_t check_paged_shape(const fa_paged_cache_t* c, const fa_paged_batch_t*
   if ((bt->T > 0 || Hq > 0) && (c->Hkv <= 0 || Hq % c->Hkv != 0)) return FA_ERR_BAD_SHAPE;
   if (bt->table_stride < 0 || static_cast<int64_t>(bt->max_blocks) * c->page_size > kMaxPagedKeys) return FA_ERR_BAD_SHAPE;
   const int64_t heads = Hq > c->Hkv ? Hq : c->Hkv;
-  if (static_cast<int64_t>(bt->T) * heads > INT_MAX || bt->B == INT_MAX) return FA_ERR_BAD_SHAPE;
+  // (The kernels count the B + 1 starts 64 at a time.)
+  if (static_cast<int64_t>(bt->T) * heads > INT_MAX || bt->B > INT_MAX - 64) return FA_ERR_BAD_SHAPE;
   return FA_OK;
 }
 fa_status_t check_paged_support(const fa_paged_cache_t* c) {

@@ -3,7 +3,8 @@
 import pytest
 
 import paper_2609_21264_amd as fa
-from test_cache_moves_host import NULL, SHAPE, batch, cache, compact
+from test_cache_moves_host import NULL, SHAPE, append_at, batch, cache, compact
+from test_paged_host import append
 
 
 @pytest.mark.parametrize("Hkv,blocks", [(1, 1), (8, 1), (9, 2), (4096, 512)])
@@ -15,3 +16,11 @@ def test_compact_of_more_workgroups_than_a_copy(Hkv, blocks):
     assert compact(c, batch(B=most), n_kept=None) == NULL  # sizes are right
     for B in (most + 1, 2 ** 30, 2 ** 31 - 32768, 2 ** 31 - 65, 2 ** 31 - 2):
         assert compact(c, batch(B=B), n_kept=None) == SHAPE, B
+
+
+@pytest.mark.parametrize("call", [append, append_at])
+def test_append_to_as_many_sequences_as_32_bits_count(call):
+    """The search for a token's sequence rounds the number of starts, B + 1, up to a multiple of 64."""
+    assert call(b=batch(B=2 ** 31 - 65), K=None) == NULL  # sizes are right
+    for B in (2 ** 31 - 64, 2 ** 31 - 63, 2 ** 31 - 2, 2 ** 31 - 1):
+        assert call(b=batch(B=B), K=None) == SHAPE, B
