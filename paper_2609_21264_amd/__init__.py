@@ -766,13 +766,15 @@ def _apart_from(name, out, others):
             raise ValueError(f"{name} must not overlap {other}")
 
 
-def tree_mask(parents, q_starts, kv_lens, words: int = 1, max_keys: Optional[int] = None, mask=None, positions=None, stream=None):
+def tree_mask(parents, q_starts, kv_lens, words: Optional[int] = None, max_keys: Optional[int] = None, mask=None, positions=None,
+              stream=None):
     """Mask and positions of trees of drafted tokens. ``parents`` int32 [T] (packed as in :func:`kv_append`, with its
     ``q_starts`` [B + 1] and ``kv_lens`` [B], which count the drafted tokens) holds the number of each token's parent among its
     sequence's new tokens, a smaller one than its own, or -1: it follows the cached keys. Returns (mask, positions): int32
     [T, ``words``], whose bit j % 32 of word j / 32 says whether the sequence's new token j is the token or one of its ancestors,
     for :func:`forward_paged`, and int32 [T], cached keys + ancestors, for :func:`kv_append`. ``words`` (up to 64) has to cover the
-    largest tree. Rows of tokens that belong to no sequence, or to one of more than 4096 new tokens, are left as they were, so
+    largest tree: tokens from 32 * ``words`` on have no bit, not even their own. The default, that of ``mask`` where one is given,
+    covers any tree of the T tokens (2048 at most); a program that knows its largest tree saves memory by naming it. Rows of tokens that belong to no sequence, or to one of more than 4096 new tokens, are left as they were, so
     new tensors' hold anything.
 
     ``max_keys`` clamps ``kv_lens`` (default 2^30). The kernel is enqueued on ``stream`` (default: torch's current stream; new
@@ -783,7 +785,12 @@ def tree_mask(parents, q_starts, kv_lens, words: int = 1, max_keys: Optional[int
     device = parents.get_device()
     (starts,) = _int32("q_starts", q_starts, 1, device)
     (B,) = _int32("kv_lens", kv_lens, 1, device)
-    words = int(words)
+    if words is not None:
+        words = int(words)
+    elif mask is not None:
+        words = _int32("mask", mask, 2, device)[1]
+    else:
+        words = min(max((T + 31) // 32, 1), FA_TREE_WORDS)
     if starts != B + 1:
         raise ValueError(f"q_starts [B + 1] and kv_lens [B] do not agree: {list(q_starts.shape)}, {list(kv_lens.shape)}")
     if not 1 <= words <= FA_TREE_WORDS:
