@@ -33,7 +33,7 @@ from typing import Optional
 from . import _lib
 from ._lib import (AppendStrides, PagedBatch, PagedCache, PagedScores, PagedStrides, Positions, RotateStrides,  # noqa: F401
                    FA_MAX_SOFTCAP,
-                   FA_CACHE_BF16, FA_CACHE_E4M3, FA_PAGED_AUTO, FA_PAGED_FEW, FA_PAGED_MANY, FA_TREE_WORDS,
+                   FA_CACHE_BF16, FA_CACHE_E4M3, FA_PAGED_AUTO, FA_PAGED_FEW, FA_PAGED_MANY, FA_TREE_TOKENS, FA_TREE_WORDS,
                    FA_ERR_BAD_SCALE, FA_ERR_BAD_SHAPE, FA_ERR_HIP, FA_ERR_NULL_POINTER,
                    FA_ERR_UNSUPPORTED, FA_ERR_WORKSPACE, FA_INSTANCE_HALVES, FA_INSTANCE_LONG, FA_INSTANCE_NONE,
                    FA_INSTANCE_QUARTERS, FA_INSTANCE_SHORT, FA_INSTANCE_SHORT_WIDE, FA_NOALLOC_SCRATCH_BYTES, FA_OK,
@@ -46,8 +46,8 @@ __all__ = ["fa_fwd", "fa_fwd_ex", "fa_fwd_split", "fa_fwd_split_workspace_bytes"
            "fa_kv_append", "fa_fwd_paged", "fa_fwd_paged_workspace_bytes", "PagedCache", "PagedBatch", "AppendStrides",
            "PagedStrides", "FA_CACHE_BF16", "FA_CACHE_E4M3", "FA_PAGED_AUTO", "FA_PAGED_FEW",
            "FA_PAGED_MANY", "kv_append", "forward_paged", "fa_kv_append_at", "fa_rotate", "fa_tree_mask", "fa_kv_compact",
-           "fa_kv_copy", "Positions", "RotateStrides", "FA_TREE_WORDS", "rotate", "tree_mask", "kv_compact", "kv_copy",
-           "fa_fwd_paged_ex", "fa_fwd_paged_ex_workspace_bytes", "PagedScores", "FA_MAX_SOFTCAP"]
+           "fa_kv_copy", "Positions", "RotateStrides", "FA_TREE_TOKENS", "FA_TREE_WORDS", "rotate", "tree_mask", "kv_compact",
+           "kv_copy", "fa_fwd_paged_ex", "fa_fwd_paged_ex_workspace_bytes", "PagedScores", "FA_MAX_SOFTCAP"]
 
 
 class FaError(RuntimeError):
@@ -774,8 +774,9 @@ def tree_mask(parents, q_starts, kv_lens, words: Optional[int] = None, max_keys:
     [T, ``words``], whose bit j % 32 of word j / 32 says whether the sequence's new token j is the token or one of its ancestors,
     for :func:`forward_paged`, and int32 [T], cached keys + ancestors, for :func:`kv_append`. ``words`` (up to 64) has to cover the
     largest tree: tokens from 32 * ``words`` on have no bit, not even their own. The default, that of ``mask`` where one is given,
-    covers any tree of the T tokens (2048 at most); a program that knows its largest tree saves memory by naming it. Rows of tokens that belong to no sequence, or to one of more than 4096 new tokens, are left as they were, so
-    new tensors' hold anything.
+    covers any tree of the T tokens (2048 at most); a program that knows its largest tree saves memory by naming it. Rows of
+    tokens that belong to no sequence are left as they were, so new tensors' hold anything; those of a sequence of more than 4096
+    new tokens too, but in new tensors they are zeros: such tokens see the cached keys alone.
 
     ``max_keys`` clamps ``kv_lens`` (default 2^30). The kernel is enqueued on ``stream`` (default: torch's current stream; new
     tensors belong to that stream); the call does not synchronise, and reads no array on the host."""
@@ -800,13 +801,14 @@ def tree_mask(parents, q_starts, kv_lens, words: Optional[int] = None, max_keys:
         with elsewhere:
             return tree_mask(parents, q_starts, kv_lens, words, max_keys, mask, positions)
     new_mask = mask is None
+    new = parents.new_empty if T <= FA_TREE_TOKENS else parents.new_zeros
     if new_mask:
-        mask = parents.new_empty((T, words))
+        mask = new((T, words))
     else:
         if _int32("mask", mask, 2, device) != (T, words) or (T > 1 and mask.stride(0) < words):
             raise ValueError(f"mask must have shape {[T, words]}, its rows apart")
     if positions is None:
-        positions = parents.new_empty(T)
+        positions = new(T)
     else:
         if _int32("positions", positions, 1, device) != (T,):
             raise ValueError(f"positions must have shape {[T]}")

@@ -88,6 +88,9 @@ RotateStrides = ctypes.c_longlong * 6
 #: FA_TREE_WORDS of include/fa.h: most words of a row of a tree's mask.
 FA_TREE_WORDS = 64
 
+#: FA_TREE_TOKENS of include/fa.h: most tokens of a tree of fa_tree_mask.
+FA_TREE_TOKENS = 4096
+
 #: FA_MAX_SOFTCAP of include/fa.h: the largest cap of scores.
 FA_MAX_SOFTCAP = 1024.0
 

@@ -38,3 +38,17 @@ def test_attention_of_a_tree_of_more_than_32_tokens_by_default(path):
     o, lse = bt.attend(scale=0.1, return_lse=True, tree_mask=mask, path=path)
     check(bt, o, lse, 0.1, tree_mask=mask)
     assert moves.tree_bits(mask.cpu().numpy())[range(60), range(60)].all()
+
+
+def test_new_rows_of_a_tree_that_is_too_long():
+    """A sequence of 4 097 new tokens has rows of zeros in new tensors, also where memory held something; those that
+    belong to others are right."""
+    parents = torch.full((4100,), -1, **I32)
+    parents[4098:] = torch.tensor([0, 0], **I32)
+    for _ in range(2):
+        mask, positions = fa.tree_mask(parents, torch.tensor([0, 4097, 4100], **I32), torch.tensor([5000, 10], **I32))
+        assert mask.shape == (4100, 64) and not bool(mask[:4097].any()) and not bool(positions[:4097].any())
+        assert mask[4097:, 0].tolist() == [1, 3, 5] and not bool(mask[:, 1:].any()) and positions[4097:].tolist() == [7, 8, 8]
+        held = mask.fill_(-1), positions.fill_(-1)
+        torch.cuda.synchronize()
+        del mask, positions, held
