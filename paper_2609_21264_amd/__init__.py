@@ -27,6 +27,7 @@ kernel. The functions below marshal arguments and translate status codes, nothin
 from __future__ import annotations
 
 import contextlib
+import ctypes
 import math
 from typing import Optional
 
@@ -1003,7 +1004,7 @@ def _scores(softcap, slopes, window, prefix_lens, tree_mask, T, hq, B, device):
     cap = wide = words = stride = 0
     sp = pp = mp = None
     if softcap is not None:
-        if not 0 < softcap <= FA_MAX_SOFTCAP:
+        if not (0 < softcap <= FA_MAX_SOFTCAP and ctypes.c_float(softcap).value > 0):  # 0 would be no cap
             raise ValueError(f"softcap must be above 0 and at most {FA_MAX_SOFTCAP:g}, not {softcap}")
         cap = softcap
     if window is not None:

@@ -24,3 +24,13 @@ def test_append_to_as_many_sequences_as_32_bits_count(call):
     assert call(b=batch(B=2 ** 31 - 65), K=None) == NULL  # sizes are right
     for B in (2 ** 31 - 64, 2 ** 31 - 63, 2 ** 31 - 2, 2 ** 31 - 1):
         assert call(b=batch(B=B), K=None) == SHAPE, B
+
+
+def test_a_softcap_that_float32_does_not_hold():
+    """What rounds to 0 would be no cap at all; what float32 holds, down to its smallest number, is one."""
+    none = None, None, None, None, 1, 4, 1, 0
+    for cap in (1e-46, 1e-50, 5e-324):
+        with pytest.raises(ValueError, match="softcap must be above 0"):
+            fa._scores(cap, *none)
+    for cap in (1e-45, 1e-30, 1, 1024.0):
+        assert fa._scores(cap, *none).softcap > 0
