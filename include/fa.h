@@ -495,7 +495,7 @@ size_t fa_fwd_paged_workspace_bytes(int B, int T, int max_keys, int Hq, int Hkv,
  * How fa_fwd_paged_ex changes scores and hides keys. For the token at position p (its place among its sequence's kv_lens[b] keys)
  * and key j, with x = scale * q . k:
  *   softcap      > 0: x becomes softcap * tanh(x / softcap), up to FA_MAX_SOFTCAP; 0: none
- *   slopes       float32 [Hq] or NULL: then slopes[h] * |p - j| is taken off
+ *   slopes       float32 [Hq] or NULL: then slopes[h] * |p - j| is taken off (a slope beyond +-2^96 / log2(e), 5e28, counts as that)
  *   window       > 0: key j is hidden where |p - j| >= window (the token itself counts); 0: none
  *   prefix_lens  int32 [B] or NULL: keys j < prefix_lens[b] (clamped to [0, kv_lens[b]]) are visible to all tokens of the
  *                sequence, whatever window and causal masking say: a bidirectional prefix, or first tokens kept beside a window

@@ -923,9 +923,9 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
     sequence are left as they were, so a new tensor's hold anything.
 
     Scores x = scale * q . k may be changed and keys hidden, for the token at position p and key j: ``softcap`` makes x softcap *
-    tanh(x / softcap) (up to 1024); ``slopes`` (float32 [Hq]) takes slopes[h] * abs(p - j) off; ``window`` hides keys with
-    abs(p - j) >= window; ``prefix_lens`` (int32 [B]) shows all tokens of a sequence its first keys, whatever window and causal masking
-    say; ``tree_mask`` (int32 [T, words], see :func:`tree_mask`) says which of their sequence's new tokens drafted ones see, beside
+    tanh(x / softcap) (up to 1024); ``slopes`` (float32 [Hq]) takes slopes[h] * abs(p - j) off (slopes beyond +-5e28 count as that);
+    ``window`` hides keys with abs(p - j) >= window; ``prefix_lens`` (int32 [B]) shows all tokens of a sequence its first keys, whatever
+    window and causal masking say; ``tree_mask`` (int32 [T, words], see :func:`tree_mask`) says which of their sequence's new tokens drafted ones see, beside
     all cached keys (causal calls without slopes, window and prefix).
 
     ``scale`` defaults to 1/sqrt(d_qk). ``workspace`` is a CUDA tensor of ``fa_fwd_paged_workspace_bytes`` (with any of the

@@ -163,6 +163,13 @@ __device__ __forceinline__ uint32_t seen_bits(const PagedForms& f, const PagedSe
   return v;
 }
 
+// A bias by distance in units of log2. Beyond 2^96 it stays at that, so that it times a distance below 2^31 is finite: 0 times an
+// infinity would be no number.
+__device__ __forceinline__ float bounded_slope(float s) {
+  constexpr float kMost = 0x1p96f;
+  return s > kMost ? kMost : s < -kMost ? -kMost : s;
+}
+
 // A score in units of log2: cap * tanh(x / cap) = cap (1 - 2 / (1 + e^(2 x / cap))). Its error of 2^-23 cap log2(e), mostly of the
 // last sum, is why caps end at 1024, where it moves a probability by less than its rounding to fp16 does.
 // a: cap_a; b: cap_factor() of what takes raw scores to units of log2.

@@ -217,7 +217,7 @@ void fa_paged_few_kernel(PagedParams p) {
       last_key[qb] = p.causal ? s.kv - s.n_q + qi : s.kv - 1;
       if constexpr (FORM) {
         row[qb].init(p.f, s, qi);
-        slope[qb] = p.f.slopes != nullptr ? p.f.slopes[g * p.group + member] * kLog2e : 0.f;
+        slope[qb] = p.f.slopes != nullptr ? bounded_slope(p.f.slopes[g * p.group + member] * kLog2e) : 0.f;
       }
       const uint16_t* qp = p.q + (int64_t)(s.q0 + qi) * p.q_token + (int64_t)(g * p.group + member) * p.q_head;
       // bf16: k-step ks holds dims 16 ks + 8 h .. + 7. e4m3: a lane reads 16 bytes of K at once, dims 32 m +

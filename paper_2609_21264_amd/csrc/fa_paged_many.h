@@ -126,7 +126,9 @@ __device__ __forceinline__ int lane_anew() {
 //   capped   s = 1 / (1 + 2^(b s)): mul = -2 a, add = a (capped() in fa_paged_device.h)
 //   biased   in a tile before all rows' positions s -= slope / cs * (the lane's last key - key), one operation, and add
 //            takes the distance of that last key off (so that both are no more than the whole distance, and near keys lose
-//            nothing to far ones); else s -= slope / cs * |p - key|; capped too, or where cs is next to 0, the final score
+//            nothing to far ones); else s -= slope / cs * |p - key|; the final score where it
+//            is capped too, where cs is next to 0, and where a bias may reach 2^20: maximum, reference and exponents are
+//            rounded apart, by up to 2^-22 of them, and of the final score alone they are the same
 template <class C>
 struct FormKeys {
   static constexpr int BN = C::WBN, QB = C::QB, KB = BN / 32;
@@ -139,7 +141,7 @@ struct FormKeys {
   int pos0;             // biased: position of the block's first row
   __device__ __forceinline__ void init_row(const PagedParams& p, int qb, int r, int head) {
     row[qb] = r;
-    if constexpr (C::FORM == kFormBiased) slope[qb] = p.f.slopes[head] * kLog2e;
+    if constexpr (C::FORM == kFormBiased) slope[qb] = bounded_slope(p.f.slopes[head] * kLog2e);
   }
   __device__ __forceinline__ void init_block(const PagedParams& p, const PagedSeq& s, int row0, int row1, float cs) {
     SeenRow first, last;
@@ -153,7 +155,10 @@ struct FormKeys {
     }
     if constexpr (C::FORM == kFormBiased) {
       pos0 = first.pos;
-      final = cap_a != 0.f || fabsf(cs) < 0x1p-60f;
+      bool steep = false;
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) steep = steep || fabsf(slope[qb]) * (float)max(s.kv, s.n_q) >= 0x1p20f;
+      final = cap_a != 0.f || fabsf(cs) < 0x1p-60f || __builtin_amdgcn_ballot_w64(steep) != 0;
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) slope[qb] = final ? slope[qb] : slope[qb] / cs;
     }
