@@ -30,9 +30,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // partners where dim c turns with dim c + rot / 2, so that a pair is read, turned in fp32 and written by one
 // thread (Q may be rotated in place), and takes every so many-th head: the cos and sin of its dims stay in
 // registers. What bounds it: the bytes of Q, K and V and the latency of the chain token -> sequence ->
-// page -> store, over which the loads of Q, K and V are in flight. 12 290 tokens of 32/8 heads, d = 128, bf16: 54 us in the
-// kernel, 5.7 TB/s read and written; 777 of 16/16 heads, d_qk = 192: 8 us; one token: 3.4 us. By positions, 8 970 tokens of
-// 32/8 heads with three axes 50.8 us (4.3 TB/s), 26 tokens 5.0.
+// page -> load -> store. 12 290 tokens of 32/8 heads, d = 128, bf16: 53 us in the kernel, 5.8 TB/s read and written; 777 of 16/16
+// heads, d_qk = 192: 8 us; one token: 3.4 us. By positions, 8 970 tokens of 32/8 heads with three axes 46 us (4.8 TB/s), 26
+// tokens 5.
 
 // Sequence of packed token t: the last b with q_starts[b] <= t, by 64 probes at a time (one step up to 63
 // sequences, two up to 4 095). -1 if t comes before the first sequence; n_seq if behind the last.
@@ -93,16 +93,11 @@ __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams 
     const int ch = w.chunk(j);
     const bool pair = turn && !p.inter;
     const int heads = p.hq + (held ? p.c.hkv : 0);
-    // By positions, a chain of three loads leads to the angles: the words of the first head are loaded before it, those of the
-    // next ones ahead (8 970 tokens of 32/8 heads, three axes 50.8 us against 53.1; with angles by place 53.4 against 52.6).
-    u32x4 wx{}, wy{};
-    auto load = [&](int h) {
-      const uint16_t* src =
-          (h < p.hq ? p.q + t * p.q_token + h * p.q_head : p.k + t * p.k_token + (h - p.hq) * p.k_head) + 8 * ch;
-      wx = *reinterpret_cast<const u32x4*>(src);
-      if (pair) wy = *reinterpret_cast<const u32x4*>(src + 8 * half);
-    };
-    if (AT && h0 < heads) load(h0);
+    // (Pointers and strides in registers of their own: of a choice between fields of p the compiler makes a load from the chosen
+    // one's address, and then loads no argument before its use: one token 4.2 us against 3.4, 777 tokens 9.5 against 8.6.)
+    const uint16_t* const q = p.q + t * p.q_token + 8 * ch;
+    const uint16_t* const k = p.k + t * p.k_token + 8 * ch;
+    const int64_t q_head = p.q_head, k_head = p.k_head;
     F8 cs{}, sn{};
     if (turn) {
       // Half-split: cos and sin of 8 pairs; neighbouring pairs: of the chunk's 4.
@@ -119,13 +114,19 @@ __global__ __launch_bounds__(kAppendThreads) void fa_append_kernel(AppendParams 
     for (int h = h0; h < heads; h += lanes) {
       const bool is_q = h < p.hq;
       const int g = h - p.hq;
-      if constexpr (!AT) load(h);
-      F8 x = unpack8(wx), y = unpack8(wy);
-      if (AT && h + lanes < heads) load(h + lanes);
-      if (pair)
+      const uint16_t* src = is_q ? q + h * q_head : k + g * k_head;
+      // Both words of a pair are loaded before either is used (threads that copy load theirs twice, from L1: a branch would wait
+      // in between): 12 290 tokens 51.8 us against 53.2, 8 970 by three axes 45.7 against 50.7; loaded a head ahead 53.0 and 47.1.
+      const u32x4 wx = *reinterpret_cast<const u32x4*>(src);
+      u32x4 wy;
+      if (!p.inter) wy = *reinterpret_cast<const u32x4*>(src + (pair ? 8 * half : 0));
+      F8 x = unpack8(wx), y;
+      if (pair) {
+        y = unpack8(wy);
         turn_halves(x, y, cs, sn);
-      else if (turn)
+      } else if (turn) {
         turn_neighbours(x, cs, sn);
+      }
       if (is_q) {
         uint16_t* dst = p.q_out + t * p.qo_token + h * p.qo_head + 8 * ch;
         *reinterpret_cast<u32x4*>(dst) = pack8(x);
