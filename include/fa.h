@@ -341,12 +341,12 @@ typedef struct {
  * written for it. Neither inputs nor Q_out may overlap the cache, nor Q_out K
  * or V. Enqueues one kernel.
  *
- * Errors, in this order: cache, batch, strides or cos_sin description NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE: negative
- * (table_stride too), Hkv <= 0 with T > 0, Hq not a multiple of Hkv, max_blocks * page_size > 2^30, T * Hq >= 2^31, B > 2^31 - 65, n_pos too small, the rotated dims
- * outside [0, d_qk)); head dimensions, page size, type or rotation not supported (FA_ERR_UNSUPPORTED); a NULL buffer that
- * has elements (FA_ERR_NULL_POINTER); alignment (FA_ERR_UNSUPPORTED: 16 bytes for buffers and strides, 4 for the int
- * and scale arrays); cache strides negative, too large, or letting two elements of the cache overlap (FA_ERR_BAD_SHAPE).
- * T == 0 or B == 0 returns FA_OK without a launch.
+ * Errors, in this order: cache, batch, strides or cos_sin description NULL (FA_ERR_NULL_POINTER); sizes (FA_ERR_BAD_SHAPE:
+ * negative (table_stride too), Hkv <= 0 with T > 0, Hq not a multiple of Hkv, max_blocks * page_size > 2^30, T * Hq >= 2^31,
+ * B > 2^31 - 65, n_pos too small, the rotated dims outside [0, d_qk)); head dimensions, page size, type or rotation not supported
+ * (FA_ERR_UNSUPPORTED); a NULL buffer that has elements (FA_ERR_NULL_POINTER); alignment (FA_ERR_UNSUPPORTED: 16 bytes for
+ * buffers and strides, 4 for the int and scale arrays); cache strides negative, too large, or letting two elements of the cache
+ * overlap (FA_ERR_BAD_SHAPE). T == 0 or B == 0 returns FA_OK without a launch.
  */
 fa_status_t fa_kv_append(const fa_paged_cache_t* cache, const fa_paged_batch_t* batch, const void* K, const void* V,
                          const void* Q, void* Q_out, int Hq, const long long* strides, const float* cos_sin, int n_pos,
@@ -406,9 +406,10 @@ fa_status_t fa_rotate(const void* X, void* Y, int B, int H, int S, int d, const 
  * from 32 * words on have no bit); positions[t] = kv_lens[b] - n + its number of ancestors, for the n new ones.
  *   parents, mask, positions   int32 [T], 32-bit words [T] in rows mask_stride apart, int32 [T]; the outputs overlap neither each other
  *               nor an input
- * Rows of tokens that belong to no sequence, or to one of more than FA_TREE_TOKENS new tokens, are left as they were. Enqueues one kernel.
- * Errors: sizes (FA_ERR_BAD_SHAPE: negative, max_keys > 2^30, words outside [1, FA_TREE_WORDS], mask_stride < words), NULL arrays (FA_ERR_NULL_POINTER), alignment of 4 bytes
- * (FA_ERR_UNSUPPORTED). T == 0 or B == 0 returns FA_OK without a launch.
+ * Rows of tokens that belong to no sequence, or to one of more than FA_TREE_TOKENS new tokens, are left as they were. Enqueues
+ * one kernel.
+ * Errors: sizes (FA_ERR_BAD_SHAPE: negative, max_keys > 2^30, words outside [1, FA_TREE_WORDS], mask_stride < words), NULL
+ * arrays (FA_ERR_NULL_POINTER), alignment of 4 bytes (FA_ERR_UNSUPPORTED). T == 0 or B == 0 returns FA_OK without a launch.
  */
 fa_status_t fa_tree_mask(const int* parents, const int* q_starts, const int* kv_lens, int B, int T, int max_keys, void* mask,
                          int words, long long mask_stride, int* positions, hipStream_t stream);

@@ -674,7 +674,8 @@ def rotate(x, cos_sin, positions=None, pair_axes=None, rot_begin: int = 0, inter
     """The position rotation of :func:`kv_append` for queries or keys x [B, H, S, d] or [T, H, d] (bf16, any strides of
     whole rows) that are in no cache, as :func:`forward` takes them: dims ``rot_begin`` to ``rot_begin + rot_dim - 1`` turn by the
     angles of ``cos_sin`` float32 [positions, rot_dim], the others are copied. ``inverse`` turns back; the
-    gradient with respect to x is that of the output's gradient.
+    gradient with respect to x is that of the output's gradient (to be called by the program: like all calls here, this one records
+    nothing for autograd).
 
     ``positions`` int32 [B, S] or [B, S, axes] ([T] or [T, axes]; any strides, so one row may be expanded over the batch) with
     ``pair_axes`` as in :func:`kv_append`; default: token s stands at s. Returns ``out`` (x itself, or apart from it in
@@ -922,11 +923,11 @@ def forward_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q: Op
     longer ones; the results are right for any. Rows of tokens that belong to no
     sequence are left as they were, so a new tensor's hold anything.
 
-    Scores x = scale * q . k may be changed and keys hidden, for the token at position p and key j: ``softcap`` makes x softcap *
-    tanh(x / softcap) (up to 1024); ``slopes`` (float32 [Hq]) takes slopes[h] * abs(p - j) off (slopes beyond +-5e28 count as that);
-    ``window`` hides keys with abs(p - j) >= window; ``prefix_lens`` (int32 [B]) shows all tokens of a sequence its first keys, whatever
-    window and causal masking say; ``tree_mask`` (int32 [T, words], see :func:`tree_mask`) says which of their sequence's new tokens drafted ones see, beside
-    all cached keys (causal calls without slopes, window and prefix).
+    Scores x = scale * q . k may be changed and keys hidden, for the token at position p and key j: ``softcap`` makes x softcap
+    * tanh(x / softcap) (up to 1024); ``slopes`` (float32 [Hq]) takes slopes[h] * abs(p - j) off (slopes beyond +-5e28 count as
+    that); ``window`` hides keys with abs(p - j) >= window; ``prefix_lens`` (int32 [B]) shows all tokens of a sequence its first
+    keys, whatever window and causal masking say; ``tree_mask`` (int32 [T, words], see :func:`tree_mask`) says which of their
+    sequence's new tokens drafted ones see, beside all cached keys (causal calls without slopes, window and prefix).
 
     ``scale`` defaults to 1/sqrt(d_qk). ``workspace`` is a CUDA tensor of ``fa_fwd_paged_workspace_bytes`` (with any of the
     options above ``fa_fwd_paged_ex_workspace_bytes``; default: from

@@ -329,6 +329,13 @@ bool token_strides(const long long* s, int n) {
 //    what runs): d = 64 16/16 16 x 100 x 100 9.4 : 15.0, 700 x 700 15.8 : 20.8, 4 x 128 x 2000 26.5 : 35.0; d_qk = 192 16/16
 //    1024 x 1024 32.0 : 43.3, 4 x 128 x 2000 44.7 : 61.5; e4m3 32/8 d = 128 4 x 128 x 2000 45.4 : 68.6; e4m3 14/2 d = 64
 //    4 x 400 x 400 13.8 : 19.9, 4 x 512 x 512 14.3 : 21.2. A caller who knows better names the path.
+//    With forms the thresholds are these too. Few against many, us, another box (masks; caps; slopes): d = 128 32/8 512 x 512
+//    17.9 : 20.3; 19.2 : 24.5; 19.8 : 22.3, 4 x 200 x 200 24.7 : 17.1; 25.4 : 19.0; 26.3 : 18.8, 700 x 700 42.7 : 23.5; 44.7 :
+//    28.9; 46.3 : 26.3, 4 x 128 x 2000 50.5 : 47.3; 54.5 : 61.0; 56.1 : 53.7, 300 x 4000 63.8 : 47.3; 68.1 : 52.1; 71.2 : 48.9;
+//    d = 64 16/16 300 x 4000 36.2 : 29.8; 37.5 : 37.2; 37.3 : 34.1; trees of 8 x 60 over 4 000 keys (9.5 K) 93.5 : 71.1, 16 x
+//    26 90.9 : 86.7. Where most off (the better kernel : what runs): caps at d_qk = 192 16/16 1024 x 1024 36.5 : 70.8, e4m3 4 x
+//    128 x 2000 55.9 : 123, d = 128 4 x 128 x 2000 54.5 : 64.9; trees of 2 x 60 over 4 000 keys (2.4 K) 38.2 : 56.5, of 4 x
+//    60 over 2 000 (2.7 K) 40.0 : 55.0.
 //  * Items of 64 where sequences have more than 32 row-heads, so that K and V are read half as often (8 x 35 row-heads x 3 001
 //    keys 13.4 us against 15.7), except where items of 32 are no more than the CUs and the keys few, or read several
 //    times anyway (40 tokens x 40 keys of one sequence, 32/8 heads: 7.2 us in items of 32, 9.6 of 64; 16 of 128 x 128

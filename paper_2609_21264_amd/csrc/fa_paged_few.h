@@ -43,9 +43,9 @@ namespace {
 
 //
 // With forms (p.f): what a column sees of a tile is a word of 32 bits, scores are capped and biased before it is applied, and
-// tiles between the prefix and the first row's window are no part of an item. Still bound by K and V: 32 tokens over 8 000 to 700
-// keys with capped scores 77 us (5.8 TB/s), without 78; 48 tokens over 60 001 and 9 000 e4m3 keys with a window of 4 096 77 (5.2), without
-// one 526.
+// tiles between the prefix and the first row's window are no part of an item. Still bound by K and V: 32 tokens over 8 000 to
+// 700 keys with capped scores 77 us (5.8 TB/s), with slopes 79, without 77, over e4m3 48 with either (4.7); 48 tokens over
+// 60 001 and 9 000 e4m3 keys with a window of 4 096 77 (5.2), without one 526.
 
 constexpr int kItemCost = 1;  // fixed cost of an item in tiles
 constexpr int kMinUnits = 2;  // least work of a workgroup: one token over 1 023 keys 12.0 us with 2, 15.6 with 4

@@ -15,16 +15,18 @@
 //    workgroups share evenly, and parts of a block that several share are joined as those of the kernel for few
 //    rows are; else a workgroup takes one block here too.
 // What bounds it: MFMA and the softmax between them, as in the fused forward. 32/8 heads, d = 128, prompts of 4 096 and 3 001
-// tokens 200-215 us by box (985-1 055 TFLOP/s; over an e4m3 cache 218, 969), a chunk of 1 024 over 9 000 keys, split, 140 (1 000) and its
-// part of the join; 32/32 heads, d_qk = 192, 512 tokens over 4 500 keys, split, 64 (700) and 13 for the join. Over contiguous keys the fused forward takes 1/1.03 to 1/1.06 of its time from 8 192 tokens
-// on, 1/1.10 at 2 048 (d = 128), 1/1.26 at 4 096 of 16/16 heads with d = 64.
+// tokens 200-215 us by box (985-1 055 TFLOP/s; over an e4m3 cache 218, 969), a chunk of 1 024 over 9 000 keys, split, 140
+// (1 000) and its part of the join; 32/32 heads, d_qk = 192, 512 tokens over 4 500 keys, split, 64 (700) and 13 for the join. Over
+// contiguous keys the fused forward takes 1/1.03 to 1/1.06 of its time from 8 192 tokens on, 1/1.10 at 2 048 (d = 128), 1/1.26
+// at 4 096 of 16/16 heads with d = 64.
 // With forms (FormKeys below): a tile's exact maximum is computed before its step, which takes the place of redoing tiles, so that
 // rows may see their first key anywhere and a bias may rise; tiles that all rows see whole are not masked; tiles between the
 // prefix and the block's first window are not visited; with slopes, tiles are taken from the last to the first, so that the
 // maximum comes early. Blocks of 128 row-heads, two waves on a SIMD, where there are such instances. 4 096 and 3 001
-// tokens, 32/8 heads, d = 128: masks 224 us where the plain kernel takes 209, caps 274, slopes 227, both 296; over e4m3 243, 319,
-// 272, 373 and 224; 16/16 heads, d_qk = 192: 144, 175, 160, 215 and 133; 32/32 heads, d = 64: 156, 196, 162, 246 and 138: what a cap
-// or a bias costs is VALU time (an exponential, a reciprocal and two operations more a score; one).
+// tokens, us, plain : masks : caps : slopes : both: 32/8 heads, d = 128 204 : 215 : 265 : 230 : 289, over e4m3 217 : 242 : 368 : 273 : 376;
+// 16/16 heads, d_qk = 192 132 : 145 : 204 : 165 : 221; 32/32 heads, d = 64 135 : 148 : 202 : 162 : 231. What a cap or a bias costs is
+// VALU time (an exponential, a reciprocal and two operations more a score; one), beside which only another wave of the SIMD
+// computes: most with one wave (e4m3, d_qk = 192).
 // Internal; included by the kernel sources only.
 #pragma once
 
@@ -44,11 +46,15 @@ namespace {
 constexpr int kBlockCost = 4;  // fixed cost of a block in tiles
 constexpr int kSplitTile = 64;  // keys of a tile where blocks are split
 // Splitting costs a second block's start, writing and reading the parts and the join, 20-40 us in all, so it pays where the
-// longest block has 32 units more than an even share, and 1.9 times as many. Measured, a block per workgroup against
-// split, 128-row-head blocks, one box: d = 128 32/8 heads 1024 x 1024 26 us against 42, 256 x 4096 (8 times the share) 73 : 42,
-// 512 x 4096 (4 times) 74 : 56, 3 x 512 x 4096 (1.4) 112 : 123, 1024 x 8192 (2.0) 148 : 145; d = 64 16/16 2048 x 2048 (26 units
-// more) 28 : 36, 256 x 4096 47 : 28, 3 x 1024 x 8192 (1.3) 145 : 135; blocks of 256, d = 128: 2048 x 2048 57 : 79, 1024 x 8192
-// (2.0) 176 : 137, 3 x 512 x 4096 101 : 119.
+// longest block has 32 units more than an even share, and 1.9 times as many. Measured, a block per workgroup against split,
+// 128-row-head blocks, one box: d = 128 32/8 heads 1024 x 1024 26 us against 42, 256 x 4096 (8 times the share) 73 : 42, 512 x
+// 4096 (4 times) 74 : 56, 3 x 512 x 4096 (1.4) 112 : 123, 1024 x 8192 (2.0) 148 : 145; d = 64 16/16 2048 x 2048 (26 units more)
+// 28 : 36, 256 x 4096 47 : 28, 3 x 1024 x 8192 (1.3) 145 : 135; blocks of 256, d = 128: 2048 x 2048 57 : 79, 1024 x 8192 (2.0)
+// 176 : 137, 3 x 512 x 4096 101 : 119. The rule is the same with forms, whose tiles cost more, so that splitting pays a little
+// earlier (another box; caps): d = 128 32/8 256 x 4096 102 : 46, 512 x 4096 103 : 64, 1024 x 1024 36 : 37, 3 x 512 x 4096 144 :
+// 149, 1024 x 8192 192 : 180 (masks 152 : 150, slopes 168 : 156), trees of 60 of 16 sequences over 9 000 to 1 200 keys 183 :
+// 122, over e4m3 268 : 115; e4m3 1024 x 8192 366 : 223; d_qk = 192 32/32 512 x 4500 223 : 99. Off at d = 64 16/16, where it
+// does not split: 2048 x 2048 47 : 36, 3 x 1024 x 8192 229 : 189.
 constexpr int kSplitUnits = 32;
 
 // This wave's share of the loads of one K or V tile: BN / NWAVES rows of CH 16-byte chunks, all in one page; E bytes per
@@ -785,7 +791,8 @@ void fa_paged_fwd_kernel(PagedParams args) {
 // 64-key tiles at d = 64 over e4m3, whose 32-key tiles would be half a load per wave. Short: 32 columns per wave, two
 // workgroups per CU, where sequences have at most 128 row-heads or long blocks would not fill the chip (paged_many; bf16, d_qk 64
 // and 128: in 64-key tiles two waves per SIMD do not fit at d_qk = 192). With forms, which redo no tile, there are registers for a
-// second K fragment ahead at d = 128: prompts with masks 160.7 us -> 154.2, caps 253 -> 249, slopes 219 -> 211.
+// second K fragment ahead at d = 128: with it and the step's priority, prompts of 4 096 and 3 001 tokens with masks 221 us -> 212, caps
+// 279 -> 262, slopes 233 -> 227.
 template <int DQK, int DV, bool E4M3, bool SHORT, bool SPLIT, int FORM = kFormNone>
 struct PagedInstance {
   using C = Cfg<DQK, DV, 64, 4, 2, true, SPLIT, 1, 2, 6, 2, 4, 1, true, E4M3, FORM>;

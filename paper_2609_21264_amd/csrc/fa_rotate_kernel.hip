@@ -14,7 +14,7 @@ namespace {
 // written by one thread (Y may be X). What bounds it: the bytes of X and Y.
 constexpr int kRotateThreads = 256;
 // Heads of a workgroup, fewer where that leaves too few workgroups: 2 x 9 999 tokens of 16 heads, d = 64, three axes, there and
-// back 34.6 us with 8 (4.7 TB/s read and written), 39.3 with all 16, 35.5 with 4, 38.3 with 2, 49.0 with one.
+// back 34.6 us with 8 (4.7 TB/s read and written; 36.2 on a slower box), 39.3 with all 16, 35.5 with 4, 38.3 with 2, 49.0 with one.
 constexpr int kRotateHeads = 8, kRotateWorkgroups = 512;
 
 template <bool AT>

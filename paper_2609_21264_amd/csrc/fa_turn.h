@@ -35,8 +35,8 @@ __device__ __forceinline__ float product(float a, float b) {
   return x;
 }
 
-// A pair (x, y) becomes (x cos - y sin, y cos + x sin), the products with the sine rounded first. Halves: the pairs are the elements of two chunks; else
-// neighbouring elements of one, by the first four angles.
+// A pair (x, y) becomes (x cos - y sin, y cos + x sin), the products with the sine rounded first. Halves: the pairs are the
+// elements of two chunks; else neighbouring elements of one, by the first four angles.
 __device__ __forceinline__ void turn_halves(F8& x, F8& y, const F8& cs, const F8& sn) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
