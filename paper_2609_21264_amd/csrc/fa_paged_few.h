@@ -206,18 +206,19 @@ void fa_paged_few_kernel(PagedParams p) {
 
     // Columns of this lane, one per 32-column block. Columns past the item's rows repeat the last and are never stored.
     const int cols = s.n_q * p.group, c0 = cb * COLS;
-    int last_key[QB];
-    SeenRow row[QB];
-    float slope[QB];  // times log2(e)
+    int last_key[QB];  // without forms
+    SeenRow row[QB];   // with them
+    float slope[QB];   // times log2(e)
     bf16x8 qf[QB][KS];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const int c = min(c0 + 32 * qb + i32, cols - 1);
       const int qi = (int)fast_div((uint32_t)c, p.m_group, p.sh_group), member = c - qi * p.group;
-      last_key[qb] = p.causal ? s.kv - s.n_q + qi : s.kv - 1;
       if constexpr (FORM) {
         row[qb].init(p.f, s, qi);
         slope[qb] = p.f.slopes != nullptr ? bounded_slope(p.f.slopes[g * p.group + member] * kLog2e) : 0.f;
+      } else {
+        last_key[qb] = p.causal ? s.kv - s.n_q + qi : s.kv - 1;
       }
       const uint16_t* qp = p.q + (int64_t)(s.q0 + qi) * p.q_token + (int64_t)(g * p.group + member) * p.q_head;
       // bf16: k-step ks holds dims 16 ks + 8 h .. + 7. e4m3: a lane reads 16 bytes of K at once, dims 32 m +
@@ -346,8 +347,6 @@ void fa_paged_few_kernel(PagedParams p) {
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
         // Mask keys past the column's last visible key and those of halves without a page.
-        const int lim = last_key[qb] - n0 - 8 * h;
-        const int lim0 = there0 ? lim : -1, lim1 = there1 ? lim : -1;
         float mt = -INFINITY;
         if constexpr (FORM) {
           if (p.f.cap_a != 0.f) {
@@ -370,6 +369,8 @@ void fa_paged_few_kernel(PagedParams p) {
             mt = fmaxf(mt, x);
           }
         } else {
+          const int lim = last_key[qb] - n0 - 8 * h;
+          const int lim0 = there0 ? lim : -1, lim1 = there1 ? lim : -1;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float x = (16 * (e >> 3) + (e & 7)) > (e < 8 ? lim0 : lim1) ? -INFINITY : sc[qb][e] * cs;

@@ -258,19 +258,21 @@ struct FormKeys {
 template <int BN, int BC, bool FORM>
 struct Block {
   int cols, c0, row0, row1;  // row-heads of the item, the block's first, its first and last row
-  int kv_end, plain;         // keys visible to its last row; leading tiles that need no mask for any row
+  int kv_end;                // keys visible to its last row
+  int plain;                 // without forms: leading tiles that need no mask for any row
   int pre, gap;              // with forms: its tiles (SeenTiles)
   __device__ __forceinline__ Block(const PagedSeq& s, int cb, const PagedParams& p) {
     cols = s.n_q * p.group;
     c0 = cb * BC;
     row0 = (int)fast_div((uint32_t)c0, p.m_group, p.sh_group);
     row1 = (int)fast_div((uint32_t)min(c0 + BC, cols) - 1u, p.m_group, p.sh_group);
-    kv_end = p.causal ? max(0, s.kv - s.n_q + row1 + 1) : s.kv;
-    plain = (p.causal ? max(0, s.kv - s.n_q + row0 + 1) : s.kv) / BN;
-    pre = gap = 0;
+    plain = pre = gap = 0;
     if constexpr (FORM) {
       const SeenTiles<BN> seen(p.f, s, row0, row1);
       kv_end = seen.end, pre = seen.pre, gap = seen.gap;
+    } else {
+      kv_end = p.causal ? max(0, s.kv - s.n_q + row1 + 1) : s.kv;
+      plain = (p.causal ? max(0, s.kv - s.n_q + row0 + 1) : s.kv) / BN;
     }
   }
   __device__ __forceinline__ int tiles() const { return (kv_end + BN - 1) / BN - (FORM ? gap : 0); }
@@ -519,7 +521,7 @@ void fa_paged_fwd_kernel(PagedParams args) {
         look(e0 + 64, e1);
       }
       st.holes = __builtin_amdgcn_ballot_w64(hole) != 0;
-      int n_plain = st.holes ? 0 : min(max(blk.plain - t0, 0), nt);
+      const int n_plain = FORM || st.holes ? 0 : min(max(blk.plain - t0, 0), nt);
       if constexpr (FORM) st.init_block(p, s, blk.row0, blk.row1, st.cs);
       auto masked = [&](int j) {
         if constexpr (FORM)
