@@ -52,3 +52,22 @@ def test_new_rows_of_a_tree_that_is_too_long():
         held = mask.fill_(-1), positions.fill_(-1)
         torch.cuda.synchronize()
         del mask, positions, held
+
+
+def test_new_rows_of_a_tree_that_is_too_long_captured():
+    """The zeros are part of the captured call: every replay writes them again."""
+    parents = torch.full((4100,), -1, **I32)
+    starts, lens = torch.tensor([0, 4097, 4100], **I32), torch.tensor([5000, 10], **I32)
+    fa.tree_mask(parents, starts, lens)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mask, positions = fa.tree_mask(parents, starts, lens)
+    for turn in range(4):
+        mask.fill_(-1)
+        positions.fill_(-1)
+        parents[4098:] = torch.tensor([turn - 1, 1 if turn > 1 else -1], **I32)
+        graph.replay()
+        want, at = fa.tree_mask(parents, starts, lens)
+        assert torch.equal(mask, want) and torch.equal(positions, at)
+        assert not bool(mask[:4097].any()) and not bool(positions[:4097].any()) and bool(mask[4097:, 0].all())
